@@ -354,6 +354,76 @@ int moei_cache_last_step(moei_cache* c, float* h_gate_w, float* h_best_sim,
 int moei_cache_last_heads(moei_cache* c, int32_t* h_pf_head, int32_t cap_pf, int32_t* h_n_pf_head,
                           int32_t* h_ev_head, int32_t cap_ev, int32_t* h_n_ev_head, void* stream);
 
+/* ------------------------------------------------------------------ KV cache and attention of a decode step
+ * The attention half of a layer: appending a token's rotated key and its value to a paged cache, and attention of one new token per
+ * sequence over it, over all of its tokens or over pages that a bound of their logits selects.
+ * The caller owns the pages of every layer (moei_kv_pages) and the page tables; a moei_kv holds the shapes, the scratch that its calls
+ * reuse (partial sums of split sequences, scores of pages) and error flags.  One moei_kv serves all layers of a model; as
+ * for the other objects, calls that name it must be ordered by the caller, replays of captured calls among them.  Calls allocate nothing and wait
+ * for nothing; they can be captured.  The current device must be the one that the moei_kv was created on (MOEI_ESTATE). */
+#define MOEI_KVDTYPE_FP8 2  /* e4m3, with a scale for each key/value head; queries, outputs and page summaries are bf16 then */
+
+typedef struct moei_kv moei_kv;
+
+typedef struct moei_kv_desc {
+    int32_t n_q_heads, n_kv_heads;  /* query heads (<= 1024), a multiple of the key/value heads; query head h reads key/value head h / (n_q_heads / n_kv_heads) */
+    int32_t k_dim, v_dim;           /* widths of a key (and query) head and of a value head: multiples of 16, <= 256 */
+    int32_t page_size;              /* tokens of a page: 16, 32, 64, 128 or 256 */
+    int32_t dtype;                  /* of the pages: MOEI_WDTYPE_FP32, MOEI_WDTYPE_BF16 (queries, new keys and values, outputs and summaries alike) or MOEI_KVDTYPE_FP8 */
+    int32_t max_batch;              /* sequences of a call, <= 4096 */
+    int32_t max_pages;              /* pages of a sequence (width of the page table) */
+    int32_t max_sel;                /* largest n_sel of kv_attend_blocks, 0: it is not called (no scratch for it) */
+} moei_kv_desc;
+
+/* The pages of one layer, device memory at multiples of 16 bytes: K [n_pages][n_kv_heads][page_size][k_dim], V likewise with v_dim. */
+typedef struct moei_kv_pages {
+    void *d_k, *d_v;
+    int64_t k_stride, v_stride;           /* elements between pages, 0: dense */
+    int32_t n_pages;
+    const float *d_k_scale, *d_v_scale;   /* [n_kv_heads], 8-bit pages: value = code * scale, scales > 0; else NULL */
+    void *d_k_min, *d_k_max;              /* [n_pages][n_kv_heads][k_dim] smallest and largest key values (codes) of a page, or both NULL */
+} moei_kv_pages;
+
+int moei_kv_create(const moei_kv_desc* desc, moei_kv** out);
+/* The caller has waited for every call that names it. */
+int moei_kv_destroy(moei_kv* kv);
+/* Error flags raised since the last call (bit 0: a page id outside the pool, bit 1: a length or position outside the page table, or a
+ * sequence number outside the batch).  Synchronises `stream`. */
+int moei_kv_error_flags(moei_kv* kv, int32_t* h_flags, void* stream);
+
+/* Appends T tokens: d_q[T][n_q_heads][k_dim], d_k[T][n_kv_heads][k_dim], d_v[T][n_kv_heads][v_dim], *_stride elements between tokens (0: dense).
+ * Token t has position d_pos[t] in sequence d_seq[t] (d_seq NULL: sequence t, T <= B); a negative position is no token, and nothing of it
+ * is read or written.  The first rot_dim elements of every query and key head are rotated by the angles position * d_inv_freq[i],
+ * 0 <= i < rot_dim / 2, formed in 64 bits: elements i and i + rot_dim / 2 (interleaved: 2i and 2i + 1) are turned as a pair in fp32.
+ * Rotated queries go to d_q_out[T][n_q_heads][k_dim] (dense; d_q itself if that is dense), keys and values into row position % page_size
+ * of page d_table[sequence][position / page_size] (d_table [B][table_width] int32), rounded once; 8-bit pages hold value / scale, limited to +-448.
+ * A token whose position lies outside the table or whose page outside the pool is left out, its query too, and raises an error flag.
+ * With summaries: when the last row of a page is appended, d_k_min and d_k_max of that page are formed from all of its rows as they are stored
+ * then (values that are no numbers are passed over).  A token's place must not be another token's of the same call. */
+int kv_append(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, int32_t table_width, int32_t B,
+              const int32_t* d_seq, const int32_t* d_pos, int32_t T,
+              const void* d_q, int64_t q_stride, const void* d_k, int64_t k_stride, const void* d_v, int64_t v_stride,
+              const float* d_inv_freq, int32_t rot_dim, int32_t interleaved, void* d_q_out, void* stream);
+
+/* Attention of one token per sequence: for every sequence b and query head h,
+ *   d_out[b][h] = sum_j softmax_j(scale * q.k_j) v_j  over its tokens j with d_len[b] - window <= j < d_len[b]  (window 0: all of them),
+ * d_lse[b][h] (fp32, may be NULL) = the natural logarithm of the softmax's denominator.  d_q[B][n_q_heads][k_dim] with q_stride elements
+ * between sequences (0: dense; multiples of 16 bytes), d_out[B][n_q_heads][v_dim].  Sums are fp32 and bit-reproducible run to run for the same
+ * batch.  A sequence without tokens gets zeros and -inf.  Rows behind a sequence's last token may hold anything.  A page id outside the pool
+ * counts as a page that is masked, a length outside [0, table_width * page_size] as the nearest one inside; both raise an error flag.
+ * scale must be positive. */
+int kv_attend(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, int32_t table_width, const int32_t* d_len, int32_t B,
+              const void* d_q, int64_t q_stride, float scale, int32_t window, void* d_out, float* d_lse, void* stream);
+
+/* kv_attend over at most n_sel pages of a sequence for each key/value head: its first keep_first and last keep_last (>= 1) pages, and of the
+ * others those with the largest score  max over the head's queries of sum_d max(q_d k_min_d, q_d k_max_d),  which no logit of the page exceeds
+ * (formed in 64 bits; equal scores go to the lower page; one that is no number comes last).  A sequence of at most n_sel pages is attended to whole.
+ * d_blocks[B][n_kv_heads][n_sel] int32 (may be NULL): the pages' numbers within their sequence, ascending, -1 behind the last.
+ * The pages between the kept ones need their summaries. */
+int kv_attend_blocks(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, int32_t table_width, const int32_t* d_len, int32_t B,
+                     const void* d_q, int64_t q_stride, float scale, int32_t n_sel, int32_t keep_first, int32_t keep_last,
+                     void* d_out, float* d_lse, int32_t* d_blocks, void* stream);
+
 /* ------------------------------------------------------------------ kernel timing (diagnostic)
  * While enabled, every kernel launch of the library carries a start and a stop HIP event
  * that the runtime stamps with the kernel's own begin and end on its stream (at most

@@ -18,9 +18,11 @@ __all__ = [
     "moe_route_topk", "eam_update", "eamc_match", "eamc_match_topm", "expert_priority", "expert_ffn_gemv",
     "expert_ffn_gemv_static",
     "moe_decode_layer", "moe_prefill_layer", "expert_ffn_grouped", "WDTYPE_FP32", "WDTYPE_BF16", "EXPORTS", "expert_pack", "profile_enable", "profile_disable", "profile_read", "profile_samples",
+    "Kv", "KvDesc", "KvPages", "kv_append", "kv_attend", "kv_attend_blocks", "KVDTYPE_FP8",
 ]
 
 WDTYPE_FP32, WDTYPE_BF16 = 0, 1
+KVDTYPE_FP8 = 2
 _HERE = os.path.dirname(os.path.abspath(__file__))
 
 EXPORTS = [
@@ -32,6 +34,7 @@ EXPORTS = [
     "moe_decode_layer", "moei_cache_last_step", "moei_cache_last_heads", "moei_cache_join", "moei_cache_sync",
     "moei_cache_set_match_count", "moei_cache_last_matches",
     "moe_prefill_layer", "moei_cache_set_policy", "moei_cache_prefetch", "moei_cache_set_prefetch", "moei_cache_last_prefetch",
+    "moei_kv_create", "moei_kv_destroy", "moei_kv_error_flags", "kv_append", "kv_attend", "kv_attend_blocks",
     "moei_profile_enable", "moei_profile_disable", "moei_profile_kernels", "moei_profile_kernel_name",
     "moei_profile_read", "moei_profile_samples",
 ]
@@ -75,6 +78,10 @@ def lib() -> C.CDLL:
         for name in EXPORTS[2:]:
             getattr(L, name).restype = C.c_int
         L.moei_profile_kernel_name.restype = C.c_char_p
+        P, i32, i64, f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_float
+        L.kv_append.argtypes = [P, P, P, i32, i32, P, P, i32, P, i64, P, i64, P, i64, P, i32, i32, P, P]
+        L.kv_attend.argtypes = [P, P, P, i32, P, i32, P, i64, f32, i32, P, P, P]
+        L.kv_attend_blocks.argtypes = [P, P, P, i32, P, i32, P, i64, f32, i32, i32, i32, P, P, P, P]
         _lib = L
     return _lib
 
@@ -443,6 +450,149 @@ def moe_decode_layer(cache: Cache, eamc: Eamc, eam: torch.Tensor, layer: int, ro
     _check(lib().moe_decode_layer(cache.h, eamc.h, _p(eam), layer, _p(router_w), _p(router_bias), _p(x), _p(y),
                                   _p(idx), C.byref(best), C.byref(n_miss), _stream(stream)))
     return idx, best.value, n_miss.value
+
+
+# -------------------------------------------------------------------- KV cache and attention
+class KvDesc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_q_heads", "n_kv_heads", "k_dim", "v_dim", "page_size", "dtype",
+                                         "max_batch", "max_pages", "max_sel")]
+
+
+class _KvPages(C.Structure):
+    _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p), ("k_stride", C.c_int64), ("v_stride", C.c_int64),
+                ("n_pages", C.c_int32), ("d_k_scale", C.c_void_p), ("d_v_scale", C.c_void_p),
+                ("d_k_min", C.c_void_p), ("d_k_max", C.c_void_p)]
+
+
+class Kv:
+    """Owner of a moei_kv handle: shapes, scratch and error flags of a paged KV cache (the pages are the caller's)."""
+
+    DTYPES = {"fp32": WDTYPE_FP32, "bf16": WDTYPE_BF16, "fp8": KVDTYPE_FP8}
+    _PAGE = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp8": torch.float8_e4m3fn}
+
+    def __init__(self, n_q_heads: int, n_kv_heads: int, k_dim: int, v_dim: int, page_size: int, dtype: str = "bf16",
+                 max_batch: int = 64, max_pages: int = 4096, max_sel: int | None = None):
+        max_sel = min(256, max_pages) if max_sel is None else max_sel
+        self.desc = KvDesc(n_q_heads, n_kv_heads, k_dim, v_dim, page_size, self.DTYPES[dtype], max_batch, max_pages, max_sel)
+        self.max_batch, self.max_pages = max_batch, max_pages
+        self.h = C.c_void_p(0)
+        _check(lib().moei_kv_create(C.byref(self.desc), C.byref(self.h)))
+        self.device = torch.device("cuda", torch.cuda.current_device())
+        self.page_dtype = self._PAGE[dtype]
+        self.dtype = torch.float32 if dtype == "fp32" else torch.bfloat16  # of queries, new keys and values, outputs, summaries
+        self.k_page = (n_kv_heads, page_size, k_dim)
+        self.v_page = (n_kv_heads, page_size, v_dim)
+        self.heads = (n_q_heads, k_dim)
+        self.out_heads = (n_q_heads, v_dim)
+
+    def error_flags(self, stream=None) -> int:
+        f = C.c_int32(0)
+        _check(lib().moei_kv_error_flags(self.h, C.byref(f), _stream(stream)))
+        return f.value
+
+    def close(self) -> None:
+        if self.h:
+            lib().moei_kv_destroy(self.h)
+            self.h = C.c_void_p(0)
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def _pages(kv: Kv, t: torch.Tensor, shape: tuple) -> int:
+    """Checks a pool of pages (each page dense) and returns the elements between pages."""
+    assert t.device == kv.device and t.dtype == kv.page_dtype and tuple(t.shape[1:]) == shape, (t.device, t.dtype, t.shape, shape)
+    assert t[:1].is_contiguous(), "a page must be dense"
+    return t.stride(0) if t.shape[0] > 1 else 0
+
+
+class KvPages:
+    """One layer's pages: k [n_pages][Hkv][page][k_dim], v likewise with v_dim (pages may lie apart: any stride between them);
+    8-bit pages with k_scale, v_scale [Hkv] fp32; k_min, k_max [n_pages][Hkv][k_dim] for kv_attend_blocks."""
+
+    def __init__(self, kv: Kv, k: torch.Tensor, v: torch.Tensor, k_min: torch.Tensor | None = None, k_max: torch.Tensor | None = None,
+                 k_scale: torch.Tensor | None = None, v_scale: torch.Tensor | None = None):
+        ks, vs = _pages(kv, k, kv.k_page), _pages(kv, v, kv.v_page)
+        n = k.shape[0]
+        assert v.shape[0] == n
+        for t in (k_scale, v_scale):
+            assert t is None or (t.numel() == kv.k_page[0] and t.device == kv.device and _dev(t, torch.float32) is t)
+        for t in (k_min, k_max):
+            assert t is None or (tuple(t.shape) == (n, kv.k_page[0], kv.k_page[2]) and t.device == kv.device and _dev(t, kv.dtype) is t)
+        self._keep = (k, v, k_min, k_max, k_scale, v_scale)
+        ptr = [None if t is None else t.data_ptr() for t in self._keep]
+        self.c = _KvPages(ptr[0], ptr[1], ks, vs, n, ptr[4], ptr[5], ptr[2], ptr[3])
+        self.ref = C.addressof(self.c)
+
+
+def _rows(kv: Kv, t: torch.Tensor, n: int, heads: tuple) -> int:
+    """Checks [n][heads][width] with dense tokens and returns the elements between tokens."""
+    assert t.device == kv.device and t.dtype == kv.dtype and tuple(t.shape) == (n, *heads), (t.device, t.dtype, t.shape, (n, *heads))
+    s = t.stride()
+    assert n == 0 or ((s[2] == 1 or heads[1] == 1) and (s[1] == heads[1] or heads[0] == 1)), "a token's heads must be dense"
+    return s[0] if n > 1 else 0
+
+
+def _ints(kv: Kv, t: torch.Tensor) -> int:
+    assert t.device == kv.device and t.dtype == torch.int32 and t.is_contiguous(), (t.device, t.dtype)
+    return t.data_ptr()
+
+
+def kv_append(kv: Kv, pages: KvPages, table: torch.Tensor, pos: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+              inv_freq: torch.Tensor | None, seq: torch.Tensor | None = None, interleaved: bool = False,
+              q_out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """q [T][Hq][k_dim], k [T][Hkv][k_dim], v [T][Hkv][v_dim] of the tokens at pos [T] of sequences seq [T] (None: token t is of
+    sequence t) -> rotated queries; keys and values go into the pages that table [B][width] names.  inv_freq [rot_dim / 2] fp32."""
+    T = pos.numel()
+    B, width = table.shape
+    if q_out is None:
+        q_out = torch.empty((T, *kv.heads), dtype=kv.dtype, device=kv.device)
+    assert q_out.is_contiguous() and q_out.dtype == kv.dtype and q_out.numel() == T * kv.heads[0] * kv.heads[1] and q_out.device == kv.device
+    assert inv_freq is None or (inv_freq.device == kv.device and _dev(inv_freq, torch.float32) is inv_freq)
+    assert seq is None or seq.numel() == T
+    _check(lib().kv_append(kv.h, pages.ref, _ints(kv, table), width, B, None if seq is None else _ints(kv, seq), _ints(kv, pos), T,
+                           q.data_ptr(), _rows(kv, q, T, kv.heads), k.data_ptr(), _rows(kv, k, T, (kv.k_page[0], kv.k_page[2])),
+                           v.data_ptr(), _rows(kv, v, T, (kv.v_page[0], kv.v_page[2])),
+                           None if inv_freq is None else inv_freq.data_ptr(), 0 if inv_freq is None else 2 * inv_freq.numel(),
+                           interleaved, q_out.data_ptr(), _stream(stream)))
+    return q_out
+
+
+def _attend_outputs(kv: Kv, B: int, table, lens, out, want_lse):
+    assert table.shape[0] == B and lens.numel() == B
+    if out is None:
+        out = torch.empty((B, *kv.out_heads), dtype=kv.dtype, device=kv.device)
+    assert out.is_contiguous() and out.dtype == kv.dtype and out.numel() == B * kv.out_heads[0] * kv.out_heads[1] and out.device == kv.device
+    return out, torch.empty((B, kv.heads[0]), dtype=torch.float32, device=kv.device) if want_lse else None
+
+
+def kv_attend(kv: Kv, pages: KvPages, table: torch.Tensor, lens: torch.Tensor, q: torch.Tensor, scale: float, window: int = 0,
+              out: torch.Tensor | None = None, want_lse: bool = False, stream=None):
+    """q [B][Hq][k_dim] (any stride between sequences) over the first lens [B] tokens of each sequence, or the last `window` of them
+    -> out [B][Hq][v_dim], or (out, lse [B][Hq] fp32) with want_lse."""
+    B = q.shape[0]
+    out, lse = _attend_outputs(kv, B, table, lens, out, want_lse)
+    _check(lib().kv_attend(kv.h, pages.ref, _ints(kv, table), table.shape[1], _ints(kv, lens), B, q.data_ptr(), _rows(kv, q, B, kv.heads),
+                           scale, window, out.data_ptr(), lse.data_ptr() if want_lse else None, _stream(stream)))
+    return (out, lse) if want_lse else out
+
+
+def kv_attend_blocks(kv: Kv, pages: KvPages, table: torch.Tensor, lens: torch.Tensor, q: torch.Tensor, scale: float, n_sel: int,
+                     keep_first: int = 1, keep_last: int = 1, out: torch.Tensor | None = None, want_lse: bool = False,
+                     want_blocks: bool = False, stream=None):
+    """kv_attend over at most n_sel pages a sequence and key/value head: the first keep_first, the last keep_last and those whose
+    logits have the highest bounds.  Returns out, or a tuple with lse [B][Hq] and blocks [B][Hkv][n_sel] int32 as wanted."""
+    B = q.shape[0]
+    out, lse = _attend_outputs(kv, B, table, lens, out, want_lse)
+    blocks = torch.empty((B, kv.k_page[0], max(n_sel, 0)), dtype=torch.int32, device=kv.device) if want_blocks else None
+    _check(lib().kv_attend_blocks(kv.h, pages.ref, _ints(kv, table), table.shape[1], _ints(kv, lens), B, q.data_ptr(),
+                                  _rows(kv, q, B, kv.heads), scale, n_sel, keep_first, keep_last, out.data_ptr(),
+                                  lse.data_ptr() if want_lse else None, blocks.data_ptr() if want_blocks else None, _stream(stream)))
+    got = (out,) + ((lse,) if want_lse else ()) + ((blocks,) if want_blocks else ())
+    return got if len(got) > 1 else out
 
 
 # -------------------------------------------------------------------- kernel timing

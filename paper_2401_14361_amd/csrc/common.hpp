@@ -59,6 +59,12 @@ enum KernelId {
     K_PF_DOWN,
     K_PF_REDUCE,
     K_FFN_GROUPED_MM,
+    K_KV_APPEND,
+    K_KV_SUMMARY,
+    K_KV_ATTEND,
+    K_KV_JOIN,
+    K_KV_SCORE,
+    K_KV_SELECT,
     K_COUNT
 };
 extern bool g_prof_on;

@@ -1,0 +1,458 @@
+// The paged KV cache of a decode step: its handle, appending tokens, and the entry points.
+#include <math.h>
+
+#include <new>
+
+#include "kv.hpp"
+
+namespace moei {
+
+namespace {
+
+constexpr int kAppThreads = 256;
+constexpr float kFp8Max = 448.f;
+
+struct KvAppendArgs {
+    const void *q, *k, *v;
+    long long q_stride, k_row, v_row;  // elements between tokens
+    void* q_out;                       // [T][Hq][k_dim]
+    const float* inv_freq;             // [rot / 2]
+    const int32_t *seq, *pos;          // seq null: token t belongs to sequence t
+    const int32_t* table;
+    int T, B, width, page_shift, n_pages;
+    int n_q, n_kv, k_dim, v_dim, rot, interleaved;
+    void *k_pages, *v_pages;
+    long long k_stride, v_stride;
+    const float *k_scale, *v_scale;
+    void *k_min, *k_max;
+    int32_t* flags;
+};
+
+// ------------------------------------------------------------------------------------------------ element access
+// W elements at p as fp32 and back; p is aligned to them.
+template <typename IO, int W>
+__device__ __forceinline__ void get(const IO* p, float* f) {
+    if constexpr (sizeof(IO) == 4 && W == 4) {
+        const float4 v = *reinterpret_cast<const float4*>(p);
+        f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
+    } else if constexpr (sizeof(IO) == 2 && W == 8) {
+        const uint4 v = *reinterpret_cast<const uint4*>(p);
+        f[0] = bf16_lo(v.x); f[1] = bf16_hi(v.x); f[2] = bf16_lo(v.y); f[3] = bf16_hi(v.y);
+        f[4] = bf16_lo(v.z); f[5] = bf16_hi(v.z); f[6] = bf16_lo(v.w); f[7] = bf16_hi(v.w);
+    } else if constexpr (sizeof(IO) == 4) {
+        static_assert(W == 1);
+        f[0] = *p;
+    } else {
+        static_assert(W == 1);
+        f[0] = bf16_one(*p);
+    }
+}
+template <typename IO, int W>
+__device__ __forceinline__ void put(IO* p, const float* f) {
+    if constexpr (sizeof(IO) == 4 && W == 4) *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
+    else if constexpr (sizeof(IO) == 2 && W == 8)
+        *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
+    else if constexpr (sizeof(IO) == 4) *p = f[0];
+    else *p = (uint16_t)pack_bf16(f[0], 0.f);
+}
+// 8-bit values: divided by the head's scale, limited to the largest that the type has (what is no number stays none), rounded to nearest even
+__device__ __forceinline__ float for_fp8(float x, float scale) {
+    const float y = x / scale;
+    return y > kFp8Max ? kFp8Max : y < -kFp8Max ? -kFp8Max : y;
+}
+template <int W>
+__device__ __forceinline__ void put8(uint8_t* p, const float* f, float scale) {
+    if constexpr (W == 8) {
+        int a = 0, b = 0;
+        a = __builtin_amdgcn_cvt_pk_fp8_f32(for_fp8(f[0], scale), for_fp8(f[1], scale), a, false);
+        a = __builtin_amdgcn_cvt_pk_fp8_f32(for_fp8(f[2], scale), for_fp8(f[3], scale), a, true);
+        b = __builtin_amdgcn_cvt_pk_fp8_f32(for_fp8(f[4], scale), for_fp8(f[5], scale), b, false);
+        b = __builtin_amdgcn_cvt_pk_fp8_f32(for_fp8(f[6], scale), for_fp8(f[7], scale), b, true);
+        *reinterpret_cast<uint2*>(p) = make_uint2((unsigned)a, (unsigned)b);
+    } else {
+        *p = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(for_fp8(f[0], scale), 0.f, 0, false);
+    }
+}
+
+// cos and sin of position times frequency.  The product and its reduction to a turn are formed in 64 bits: at position 10^5 the fp32 product
+// would be off by up to 2^-8.
+__device__ __forceinline__ float2 turn(int pos, float freq) {
+    const double turns = (double)pos * (double)freq * 0.15915494309189535;  // 1 / (2 pi)
+    float2 cs;
+    sincospif((float)(2.0 * (turns - rint(turns))), &cs.y, &cs.x);
+    return cs;
+}
+
+// A workgroup takes a share of one token's heads: the turns of all pairs first, in LDS, then units of W pairs (of rotated heads), W plain
+// elements of keys and queries behind them, W elements of values.
+template <typename IO, typename PG, int W>
+__global__ void __launch_bounds__(kAppThreads) kv_append_kernel(KvAppendArgs a) {
+    __shared__ float2 s_turn[kKvMaxDim / 2];
+    const int t = blockIdx.x;
+    const int pos = a.pos[t];
+    if (pos < 0) return;  // a place of the batch without a token
+    const int seq = a.seq ? a.seq[t] : t;
+    const int at = pos >> a.page_shift;
+    bool ok = seq >= 0 && seq < a.B && at < a.width;
+    if (!ok) {
+        if (threadIdx.x == 0 && blockIdx.y == 0) atomicOr(a.flags, kKvBadLength);
+        return;
+    }
+    const int page = a.table[(long long)seq * a.width + at];
+    if (page < 0 || page >= a.n_pages) {
+        if (threadIdx.x == 0 && blockIdx.y == 0) atomicOr(a.flags, kKvBadPage);
+        return;
+    }
+    const int half = a.rot / 2;
+    for (int i = threadIdx.x; i < half; i += kAppThreads) s_turn[i] = turn(pos, a.inv_freq[i]);
+    __syncthreads();
+    const int row = pos & ((1 << a.page_shift) - 1);
+    const int turned = half / W, plain = (a.k_dim - a.rot) / W, of_head = turned + plain, of_v = a.v_dim / W;
+    const int n_rot = (a.n_q + a.n_kv) * of_head, n = n_rot + a.n_kv * of_v;
+    for (int i = blockIdx.y * kAppThreads + threadIdx.x; i < n; i += gridDim.y * kAppThreads) {
+        if (i >= n_rot) {
+            const int h = (i - n_rot) / of_v, d = (i - n_rot - h * of_v) * W;
+            float f[W];
+            get<IO, W>(static_cast<const IO*>(a.v) + t * a.v_row + h * a.v_dim + d, f);
+            PG* to = static_cast<PG*>(a.v_pages) + page * a.v_stride + (((long long)h << a.page_shift) + row) * a.v_dim + d;
+            if constexpr (sizeof(PG) == 1) put8<W>(to, f, a.v_scale[h]);
+            else put<PG, W>(to, f);
+            continue;
+        }
+        const int head = i / of_head, u = i - head * of_head;
+        const bool is_q = head < a.n_q;
+        const int h = is_q ? head : head - a.n_q;
+        const IO* src = is_q ? static_cast<const IO*>(a.q) + t * a.q_stride + h * a.k_dim : static_cast<const IO*>(a.k) + t * a.k_row + h * a.k_dim;
+        IO* q_to = static_cast<IO*>(a.q_out) + ((long long)t * a.n_q + h) * a.k_dim;
+        PG* k_to = static_cast<PG*>(a.k_pages) + page * a.k_stride + (((long long)h << a.page_shift) + row) * a.k_dim;
+        auto store = [&](int d, const float* f) {
+            if (is_q) put<IO, W>(q_to + d, f);
+            else if constexpr (sizeof(PG) == 1) put8<W>(k_to + d, f, a.k_scale[h]);
+            else put<PG, W>(k_to + d, f);
+        };
+        if (u >= turned) {
+            const int d = a.rot + (u - turned) * W;
+            float f[W];
+            get<IO, W>(src + d, f);
+            store(d, f);
+            continue;
+        }
+        // W pairs: elements i and i + half, or 2 i and 2 i + 1
+        const int d1 = a.interleaved ? 2 * u * W : u * W, d2 = a.interleaved ? d1 + W : d1 + half;
+        float x[2 * W], y[2 * W];
+        get<IO, W>(src + d1, x);
+        get<IO, W>(src + d2, x + W);
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            const float2 cs = s_turn[u * W + j];
+            const float x1 = a.interleaved ? x[2 * j] : x[j], x2 = a.interleaved ? x[2 * j + 1] : x[W + j];
+            const float y1 = __builtin_fmaf(x1, cs.x, -(x2 * cs.y)), y2 = __builtin_fmaf(x2, cs.x, x1 * cs.y);
+            if (a.interleaved) { y[2 * j] = y1; y[2 * j + 1] = y2; }
+            else { y[j] = y1; y[W + j] = y2; }
+        }
+        store(d1, y);
+        store(d2, y + W);
+    }
+}
+
+// Smallest and largest value of every key dimension of the pages that a call has completed.  A workgroup looks at kEndTokens tokens for one
+// head; runs of a sequence complete a page in every page_size tokens.
+constexpr int kEndTokens = 16;
+template <typename IO, typename PG>
+__global__ void __launch_bounds__(kAppThreads) kv_summary_kernel(KvAppendArgs a) {
+    __shared__ float s_lo[kAppThreads], s_hi[kAppThreads];
+    const int h = blockIdx.y;
+    const int size = 1 << a.page_shift;
+    for (int t = blockIdx.x * kEndTokens; t < min(a.T, (int)(blockIdx.x + 1) * kEndTokens); ++t) {
+        const int pos = a.pos[t];
+        if (pos < 0 || (pos & (size - 1)) != size - 1) continue;
+        const int seq = a.seq ? a.seq[t] : t, at = pos >> a.page_shift;
+        if (seq < 0 || seq >= a.B || at >= a.width) continue;
+        const int page = a.table[(long long)seq * a.width + at];
+        if (page < 0 || page >= a.n_pages) continue;
+        const PG* src = static_cast<const PG*>(a.k_pages) + page * a.k_stride + ((long long)h << a.page_shift) * a.k_dim;
+        // threads: k_dim columns (up to 256), rows shared among the rest
+        const int groups = kAppThreads / a.k_dim > 0 ? kAppThreads / a.k_dim : 1;
+        const int d = threadIdx.x % a.k_dim, g = threadIdx.x / a.k_dim;
+        float lo = INFINITY, hi = -INFINITY;
+        if (g < groups)
+            for (int r = g; r < size; r += groups) {
+                const PG raw = src[(long long)r * a.k_dim + d];
+                float x;
+                if constexpr (sizeof(PG) == 1) x = __builtin_amdgcn_cvt_f32_fp8((int)raw, 0);
+                else if constexpr (sizeof(PG) == 2) x = bf16_one(raw);
+                else x = raw;
+                lo = fminf(lo, x);
+                hi = fmaxf(hi, x);
+            }
+        s_lo[threadIdx.x] = lo;
+        s_hi[threadIdx.x] = hi;
+        __syncthreads();
+        if (g == 0) {
+            for (int j = 1; j < groups; ++j) {
+                lo = fminf(lo, s_lo[j * a.k_dim + d]);
+                hi = fmaxf(hi, s_hi[j * a.k_dim + d]);
+            }
+            const long long to = ((long long)page * a.n_kv + h) * a.k_dim + d;
+            put<IO, 1>(static_cast<IO*>(a.k_min) + to, &lo);
+            put<IO, 1>(static_cast<IO*>(a.k_max) + to, &hi);
+        }
+        __syncthreads();
+    }
+}
+
+template <typename IO, typename PG>
+void launch_append(const KvAppendArgs& a, bool wide, int parts, hipStream_t s) {
+    constexpr int W = 16 / sizeof(IO);
+    launch(K_KV_APPEND, wide ? kv_append_kernel<IO, PG, W> : kv_append_kernel<IO, PG, 1>, dim3((unsigned)a.T, (unsigned)parts), dim3(kAppThreads), 0, s, a);
+    if (a.k_min)
+        launch(K_KV_SUMMARY, kv_summary_kernel<IO, PG>, dim3((unsigned)((a.T + kEndTokens - 1) / kEndTokens), (unsigned)a.n_kv), dim3(kAppThreads), 0, s, a);
+}
+
+int log2_of(int v) { return 31 - __builtin_clz((unsigned)v); }
+
+// What every call on a handle has in common.
+int check_call(const char* who, const moei_kv* kv, const moei_kv_pages* p, const int32_t* d_table, int32_t width) {
+    MOEI_REQUIRE(kv && p && d_table, "%s: null pointer", who);
+    MOEI_REQUIRE(p->d_k && p->d_v, "%s: null pages", who);
+    MOEI_REQUIRE(p->n_pages >= 1, "%s: n_pages = %d must be positive", who, p->n_pages);
+    MOEI_REQUIRE(width >= 1 && width <= kv->d.max_pages, "%s: table of %d pages a sequence, outside [1, max_pages = %d]", who, width, kv->d.max_pages);
+    const long long eb = kv_page_bytes(kv->d.dtype), dense_k = (long long)kv->d.n_kv_heads * kv->d.page_size * kv->d.k_dim;
+    const long long dense_v = (long long)kv->d.n_kv_heads * kv->d.page_size * kv->d.v_dim;
+    MOEI_REQUIRE((p->k_stride == 0 || p->k_stride >= dense_k) && (p->v_stride == 0 || p->v_stride >= dense_v),
+                 "%s: page strides %lld, %lld are shorter than a page (%lld, %lld)", who, (long long)p->k_stride, (long long)p->v_stride, dense_k, dense_v);
+    MOEI_REQUIRE((uintptr_t)p->d_k % 16 == 0 && (uintptr_t)p->d_v % 16 == 0 && p->k_stride * eb % 16 == 0 && p->v_stride * eb % 16 == 0,
+                 "%s: pages must begin at multiples of 16 bytes", who);
+    MOEI_REQUIRE(kv->d.dtype != MOEI_KVDTYPE_FP8 || (p->d_k_scale && p->d_v_scale), "%s: 8-bit pages need d_k_scale and d_v_scale", who);
+    MOEI_REQUIRE(!p->d_k_min == !p->d_k_max, "%s: d_k_min and d_k_max go together", who);
+    MOEI_REQUIRE((uintptr_t)p->d_k_min % 16 == 0 && (uintptr_t)p->d_k_max % 16 == 0, "%s: d_k_min and d_k_max must begin at multiples of 16 bytes", who);
+    int dev = -1;
+    MOEI_HIP(hipGetDevice(&dev));
+    if (dev != kv->device) MOEI_FAIL(MOEI_ESTATE, "%s: the handle belongs to device %d, the current one is %d", who, kv->device, dev);
+    return MOEI_OK;
+}
+
+void strides_of(const moei_kv* kv, const moei_kv_pages* p, long long* k, long long* v) {
+    const long long rows = (long long)kv->d.n_kv_heads * kv->d.page_size;
+    *k = p->k_stride ? p->k_stride : rows * kv->d.k_dim;
+    *v = p->v_stride ? p->v_stride : rows * kv->d.v_dim;
+}
+
+int fill_attend(const char* who, const moei_kv* kv, const moei_kv_pages* p, const int32_t* d_table, int32_t width, const int32_t* d_len,
+                int32_t B, const void* d_q, int64_t q_stride, float scale, void* d_out, float* d_lse, KvAttendArgs* a) {
+    const moei_kv_desc& d = kv->d;
+    MOEI_REQUIRE(d_len && d_q && d_out, "%s: null pointer", who);
+    MOEI_REQUIRE(scale > 0.f && scale < INFINITY, "%s: scale must be positive and finite", who);
+    const int io = kv_io_bytes(d.dtype);
+    const long long dense = (long long)d.n_q_heads * d.k_dim;
+    MOEI_REQUIRE(q_stride == 0 || (q_stride >= dense && q_stride * io % 16 == 0), "%s: q_stride = %lld is shorter than a token (%lld) or no multiple of 16 bytes",
+                 who, (long long)q_stride, dense);
+    MOEI_REQUIRE((uintptr_t)d_q % 16 == 0 && (uintptr_t)d_out % 16 == 0, "%s: d_q and d_out must begin at multiples of 16 bytes", who);
+    *a = KvAttendArgs{};
+    a->q = d_q;
+    a->q_stride = q_stride ? q_stride : dense;
+    a->out = d_out;
+    a->lse = d_lse;
+    a->k = static_cast<const unsigned char*>(p->d_k);
+    a->v = static_cast<const unsigned char*>(p->d_v);
+    strides_of(kv, p, &a->k_stride, &a->v_stride);
+    if (d.dtype == MOEI_KVDTYPE_FP8) {
+        a->k_scale = p->d_k_scale;
+        a->v_scale = p->d_v_scale;
+    }
+    a->table = d_table;
+    a->lens = d_len;
+    a->B = B;
+    a->n_kv = d.n_kv_heads;
+    a->group = d.n_q_heads / d.n_kv_heads;
+    a->blocks_of_heads = (a->group + kKvHeads - 1) / kKvHeads;
+    a->k_dim = d.k_dim;
+    a->v_dim = d.v_dim;
+    a->width = width;
+    a->page_shift = log2_of(d.page_size);
+    a->n_pages = p->n_pages;
+    a->scale2 = scale * 1.4426950408889634f;
+    a->part = kv->d_part;
+    a->stat = kv->d_stat;
+    a->n_target = kv->n_target;
+    a->min_chunk = 64;
+    a->flags = kv->d_flags;
+    return MOEI_OK;
+}
+
+}  // namespace
+
+}  // namespace moei
+
+using namespace moei;
+
+extern "C" int moei_kv_destroy(moei_kv* kv) {
+    if (!kv) return MOEI_OK;
+    int dev = -1;
+    const bool other = hipGetDevice(&dev) == hipSuccess && dev != kv->device && hipSetDevice(kv->device) == hipSuccess;
+    for (void* p : {(void*)kv->d_part, (void*)kv->d_stat, (void*)kv->d_keys, (void*)kv->d_list, (void*)kv->d_flags})
+        if (p) (void)hipFree(p);
+    if (other) (void)hipSetDevice(dev);
+    delete kv;
+    return MOEI_OK;
+}
+
+extern "C" int moei_kv_create(const moei_kv_desc* desc, moei_kv** out) {
+    MOEI_REQUIRE(desc && out, "moei_kv_create: null pointer");
+    *out = nullptr;
+    const moei_kv_desc& d = *desc;
+    MOEI_REQUIRE(d.n_kv_heads >= 1 && d.n_q_heads >= d.n_kv_heads && d.n_q_heads % d.n_kv_heads == 0 && d.n_q_heads <= 1024,
+                 "moei_kv_create: %d query heads are not a multiple of %d key/value heads, or more than 1024", d.n_q_heads, d.n_kv_heads);
+    MOEI_REQUIRE(d.k_dim >= 16 && d.k_dim <= kKvMaxDim && d.k_dim % 16 == 0 && d.v_dim >= 16 && d.v_dim <= kKvMaxDim && d.v_dim % 16 == 0,
+                 "moei_kv_create: head widths %d, %d must be multiples of 16 up to %d", d.k_dim, d.v_dim, kKvMaxDim);
+    MOEI_REQUIRE(d.page_size >= 16 && d.page_size <= kKvMaxPage && (d.page_size & (d.page_size - 1)) == 0,
+                 "moei_kv_create: page_size = %d must be 16, 32, 64, 128 or 256", d.page_size);
+    MOEI_REQUIRE(d.dtype == MOEI_WDTYPE_FP32 || d.dtype == MOEI_WDTYPE_BF16 || d.dtype == MOEI_KVDTYPE_FP8, "moei_kv_create: unknown dtype %d", d.dtype);
+    MOEI_REQUIRE(d.max_batch >= 1 && d.max_batch <= kKvMaxBatch, "moei_kv_create: max_batch = %d outside [1, %d]", d.max_batch, kKvMaxBatch);
+    MOEI_REQUIRE(d.max_pages >= 1 && (long long)d.max_pages * d.page_size <= (1ll << 30), "moei_kv_create: max_pages = %d must be positive, and hold 2^30 tokens at most", d.max_pages);
+    MOEI_REQUIRE(d.max_sel >= 0 && d.max_sel <= d.max_pages, "moei_kv_create: max_sel = %d outside [0, max_pages = %d]", d.max_sel, d.max_pages);
+    moei_kv* kv = new (std::nothrow) moei_kv;
+    if (!kv) MOEI_FAIL(MOEI_ENOMEM, "moei_kv_create: out of host memory");
+    kv->d = d;
+    hipError_t e = hipGetDevice(&kv->device);
+    if (e == hipSuccess) e = hipDeviceGetAttribute(&kv->cus, hipDeviceAttributeMultiprocessorCount, kv->device);
+    if (e != hipSuccess) {
+        delete kv;
+        MOEI_FAIL(MOEI_EHIP, "moei_kv_create: no device: %s", hipGetErrorString(e));
+    }
+    const int group = d.n_q_heads / d.n_kv_heads;
+    kv->rows = group < kKvHeads ? group : kKvHeads;
+    kv->n_target = 2 * kv->cus;
+    const size_t rows = (size_t)2 * kv->n_target * kv->rows, sel = d.max_sel ? (size_t)d.max_batch * d.n_kv_heads : 0;
+    auto room = [&](auto*& p, size_t n) { return n == 0 || (e = hipMalloc(reinterpret_cast<void**>(&p), n * sizeof(*p))) == hipSuccess; };
+    if (!room(kv->d_part, rows * d.v_dim) || !room(kv->d_stat, rows * 2) || !room(kv->d_keys, sel * d.max_pages) ||
+        !room(kv->d_list, sel * d.max_sel) || !room(kv->d_flags, 1) || (e = hipMemset(kv->d_flags, 0, 4)) != hipSuccess ||
+        (e = hipDeviceSynchronize()) != hipSuccess) {
+        (void)hipGetLastError();
+        moei_kv_destroy(kv);
+        MOEI_FAIL(e == hipErrorOutOfMemory ? MOEI_ENOMEM : MOEI_EHIP, "moei_kv_create: %s", hipGetErrorString(e));
+    }
+    *out = kv;
+    return MOEI_OK;
+}
+
+extern "C" int moei_kv_error_flags(moei_kv* kv, int32_t* h_flags, void* stream) {
+    MOEI_REQUIRE(kv && h_flags, "moei_kv_error_flags: null pointer");
+    hipStream_t s = as_stream(stream);
+    int32_t flags = 0;
+    MOEI_HIP(hipMemcpyAsync(&flags, kv->d_flags, 4, hipMemcpyDeviceToHost, s));
+    MOEI_HIP(hipStreamSynchronize(s));
+    if (flags) {
+        const int32_t none = 0;
+        MOEI_HIP(hipMemcpyAsync(kv->d_flags, &none, 4, hipMemcpyHostToDevice, s));
+        MOEI_HIP(hipStreamSynchronize(s));
+    }
+    *h_flags = flags;
+    return MOEI_OK;
+}
+
+extern "C" int kv_append(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, int32_t table_width, int32_t B,
+                         const int32_t* d_seq, const int32_t* d_pos, int32_t T,
+                         const void* d_q, int64_t q_stride, const void* d_k, int64_t k_stride, const void* d_v, int64_t v_stride,
+                         const float* d_inv_freq, int32_t rot_dim, int32_t interleaved, void* d_q_out, void* stream) {
+    const char* who = "kv_append";
+    MOEI_REQUIRE(T >= 0 && B >= 0, "%s: T = %d or B = %d is negative", who, T, B);
+    if (T == 0) return MOEI_OK;
+    const int rc = check_call(who, kv, pages, d_table, table_width);
+    if (rc) return rc;
+    const moei_kv_desc& d = kv->d;
+    MOEI_REQUIRE(d_pos && d_q && d_k && d_v && d_q_out, "%s: null pointer", who);
+    MOEI_REQUIRE(B >= 1 && B <= d.max_batch, "%s: B = %d outside [1, max_batch = %d]", who, B, d.max_batch);
+    MOEI_REQUIRE(d_seq || T <= B, "%s: %d tokens of %d sequences need d_seq", who, T, B);
+    MOEI_REQUIRE(T <= (1 << 24), "%s: T = %d exceeds 2^24", who, T);
+    MOEI_REQUIRE(rot_dim >= 0 && rot_dim <= d.k_dim && rot_dim % 2 == 0, "%s: rot_dim = %d must be even and at most k_dim = %d", who, rot_dim, d.k_dim);
+    MOEI_REQUIRE(rot_dim == 0 || d_inv_freq, "%s: null d_inv_freq", who);
+    const long long nq = (long long)d.n_q_heads * d.k_dim, nk = (long long)d.n_kv_heads * d.k_dim, nv = (long long)d.n_kv_heads * d.v_dim;
+    MOEI_REQUIRE((q_stride == 0 || q_stride >= nq) && (k_stride == 0 || k_stride >= nk) && (v_stride == 0 || v_stride >= nv),
+                 "%s: strides %lld, %lld, %lld are shorter than a token (%lld, %lld, %lld)", who, (long long)q_stride, (long long)k_stride, (long long)v_stride, nq, nk, nv);
+    const int io = kv_io_bytes(d.dtype);
+    MOEI_REQUIRE((uintptr_t)d_q % io == 0 && (uintptr_t)d_k % io == 0 && (uintptr_t)d_v % io == 0 && (uintptr_t)d_q_out % io == 0, "%s: elements are not aligned", who);
+    KvAppendArgs a{};
+    a.q = d_q; a.k = d_k; a.v = d_v;
+    a.q_stride = q_stride ? q_stride : nq;
+    a.k_row = k_stride ? k_stride : nk;
+    a.v_row = v_stride ? v_stride : nv;
+    a.q_out = d_q_out;
+    a.inv_freq = d_inv_freq;
+    a.seq = d_seq; a.pos = d_pos; a.table = d_table;
+    a.T = T; a.B = B; a.width = table_width;
+    a.page_shift = log2_of(d.page_size);
+    a.n_pages = pages->n_pages;
+    a.n_q = d.n_q_heads; a.n_kv = d.n_kv_heads; a.k_dim = d.k_dim; a.v_dim = d.v_dim;
+    a.rot = rot_dim; a.interleaved = interleaved != 0;
+    a.k_pages = pages->d_k; a.v_pages = pages->d_v;
+    strides_of(kv, pages, &a.k_stride, &a.v_stride);
+    a.k_scale = pages->d_k_scale; a.v_scale = pages->d_v_scale;
+    a.k_min = pages->d_k_min; a.k_max = pages->d_k_max;
+    a.flags = kv->d_flags;
+    // Sixteen bytes at a time where every vector of elements begins at a multiple of 16 bytes and a vector of pairs fits the rotated part.
+    const int W = 16 / io;
+    auto even = [&](const void* p, long long stride) { return (uintptr_t)p % 16 == 0 && stride % W == 0; };
+    const bool wide = rot_dim / 2 % W == 0 && even(d_q, a.q_stride) && even(d_k, a.k_row) && even(d_v, a.v_row) && even(d_q_out, 0);
+    const int w = wide ? W : 1;
+    const int units = (d.n_q_heads + d.n_kv_heads) * (rot_dim / 2 / w + (d.k_dim - rot_dim) / w) + d.n_kv_heads * (d.v_dim / w);
+    int parts = (units + kAppThreads - 1) / kAppThreads;  // few tokens: a thread a unit
+    const int enough = (8 * kv->cus + T - 1) / T;
+    if (parts > enough) parts = enough;
+    hipStream_t s = as_stream(stream);
+    if (d.dtype == MOEI_WDTYPE_FP32) launch_append<float, float>(a, wide, parts, s);
+    else if (d.dtype == MOEI_WDTYPE_BF16) launch_append<uint16_t, uint16_t>(a, wide, parts, s);
+    else launch_append<uint16_t, uint8_t>(a, wide, parts, s);
+    MOEI_LAUNCH_CHECK();
+    return MOEI_OK;
+}
+
+extern "C" int kv_attend(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, int32_t table_width, const int32_t* d_len,
+                         int32_t B, const void* d_q, int64_t q_stride, float scale, int32_t window, void* d_out, float* d_lse, void* stream) {
+    MOEI_REQUIRE(B >= 0, "kv_attend: B = %d is negative", B);
+    if (B == 0) return MOEI_OK;
+    int rc = check_call("kv_attend", kv, pages, d_table, table_width);
+    if (rc) return rc;
+    MOEI_REQUIRE(B <= kv->d.max_batch, "kv_attend: B = %d exceeds max_batch = %d", B, kv->d.max_batch);
+    MOEI_REQUIRE(window >= 0, "kv_attend: window = %d is negative", window);
+    KvAttendArgs a;
+    rc = fill_attend("kv_attend", kv, pages, d_table, table_width, d_len, B, d_q, q_stride, scale, d_out, d_lse, &a);
+    if (rc) return rc;
+    a.window = window;
+    return launch_kv_attend(*kv, a, as_stream(stream));
+}
+
+extern "C" int kv_attend_blocks(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, int32_t table_width, const int32_t* d_len,
+                                int32_t B, const void* d_q, int64_t q_stride, float scale, int32_t n_sel, int32_t keep_first,
+                                int32_t keep_last, void* d_out, float* d_lse, int32_t* d_blocks, void* stream) {
+    const char* who = "kv_attend_blocks";
+    MOEI_REQUIRE(B >= 0, "%s: B = %d is negative", who, B);
+    if (B == 0) return MOEI_OK;
+    int rc = check_call(who, kv, pages, d_table, table_width);
+    if (rc) return rc;
+    MOEI_REQUIRE(B <= kv->d.max_batch, "%s: B = %d exceeds max_batch = %d", who, B, kv->d.max_batch);
+    MOEI_REQUIRE(pages->d_k_min, "%s: the pages have no d_k_min and d_k_max", who);
+    MOEI_REQUIRE(n_sel >= 1 && n_sel <= kv->d.max_sel, "%s: n_sel = %d outside [1, max_sel = %d]", who, n_sel, kv->d.max_sel);
+    MOEI_REQUIRE(keep_first >= 0 && keep_last >= 1 && (long long)keep_first + keep_last <= n_sel,
+                 "%s: keep_first = %d and keep_last = %d (one at least) must fit n_sel = %d", who, keep_first, keep_last, n_sel);
+    KvAttendArgs a;
+    rc = fill_attend(who, kv, pages, d_table, table_width, d_len, B, d_q, q_stride, scale, d_out, d_lse, &a);
+    if (rc) return rc;
+    KvBlocksArgs c{};
+    c.q = d_q;
+    c.q_stride = a.q_stride;
+    c.k_min = pages->d_k_min; c.k_max = pages->d_k_max;
+    c.table = d_table;
+    c.lens = d_len;
+    c.B = B; c.n_kv = a.n_kv; c.group = a.group; c.k_dim = a.k_dim;
+    c.width = table_width; c.page_shift = a.page_shift; c.n_pages = a.n_pages;
+    c.n_sel = n_sel; c.keep_first = keep_first; c.keep_last = keep_last;
+    c.keys = kv->d_keys;
+    c.list = d_blocks ? d_blocks : kv->d_list;
+    c.flags = kv->d_flags;
+    rc = launch_kv_blocks(*kv, c, as_stream(stream));
+    if (rc) return rc;
+    a.list = c.list;
+    a.n_sel = n_sel;
+    return launch_kv_attend(*kv, a, as_stream(stream));
+}

@@ -1,0 +1,597 @@
+// Attention of one new token per sequence over a paged KV cache.
+//
+// out[b][h] = sum_j softmax_j(scale q.k_j) v_j over the sequence's tokens, in one pass over keys and values with the running
+// maximum and sum of the softmax.  Bound by the bytes of the pages: up to sixteen query heads of a group share a pass, and on the matrix
+// cores their products take a tenth of the time that the bytes need.
+#include <math.h>
+
+#include "kv.hpp"
+#include "lds_limit.hpp"
+
+namespace moei {
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kWaves = 4;  // of a workgroup; each has a state of its own and every fourth tile
+constexpr int kRows = 16;  // keys of a subtile: the rows of a matrix instruction; a page holds whole ones
+
+// ------------------------------------------------------------------------------------------------ the plan
+// The tokens of all (sequence, key/value head, block of heads) are cut into chunks of equal length, a workgroup each: about n_target
+// of them, whatever the lengths, and one at least for every item.  Nobody but the device knows the lengths, so every
+// workgroup works the plan out for itself.
+struct Span {
+    int begin, end, start;  // tokens [begin, end) of the (listed) sequence; chunks are counted from `start`, a whole subtile
+};
+
+__device__ __forceinline__ Span span_of(const KvAttendArgs& a, int b, bool& bad) {
+    int len = ((kv_const_ints)(uintptr_t)a.lens)[b];
+    const long long room = (long long)a.width << a.page_shift;
+    bad = len < 0 || len > room;
+    len = len < 0 ? 0 : len > room ? (int)room : len;
+    Span s{0, len, 0};
+    if (a.list) {
+        const int nb = (len + (1 << a.page_shift) - 1) >> a.page_shift;
+        if (nb > a.n_sel) s.end = len - ((nb - a.n_sel) << a.page_shift);  // the last page, whole or not, is always listed
+    } else if (a.window > 0 && len > a.window) {
+        s.begin = len - a.window;
+        s.start = s.begin & ~(kRows - 1);
+    }
+    return s;
+}
+
+__device__ __forceinline__ int span_tokens(const KvAttendArgs& a, int b) {  // per lane
+    int len = a.lens[b];
+    const long long room = (long long)a.width << a.page_shift;
+    len = len < 0 ? 0 : len > room ? (int)room : len;
+    if (a.list) {
+        const int nb = (len + (1 << a.page_shift) - 1) >> a.page_shift;
+        return nb > a.n_sel ? len - ((nb - a.n_sel) << a.page_shift) : len;
+    }
+    return a.window > 0 && len > a.window ? len - ((len - a.window) & ~(kRows - 1)) : len;
+}
+
+struct Plan {
+    int chunk;  // tokens
+    int b;      // the sequence that `want` falls into, -1: none
+    int first;  // its first chunk's number
+    int parts;  // chunks of one of its items
+    int slot;   // number of its first partial result
+};
+
+// inclusive sum over the lanes
+__device__ __forceinline__ int lane_scan(int v, int lane) {
+#pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) {
+        const int up = __shfl_up(v, off, kWave);
+        if (lane >= off) v += up;
+    }
+    return v;
+}
+
+// by_chunk: `want` is a chunk's number, else a sequence's.
+template <bool by_chunk>
+__device__ __forceinline__ Plan make_plan(const KvAttendArgs& a, int want, int lane) {
+    const int items = a.n_kv * a.blocks_of_heads;
+    unsigned long long total = 0;
+    for (int b0 = 0; b0 < a.B; b0 += kWave) total += wave_sum_u64(b0 + lane < a.B ? (unsigned long long)span_tokens(a, b0 + lane) : 0ull);
+    const unsigned long long even = min((total * items + a.n_target - 1) / a.n_target, 1ull << 30);
+    Plan p;
+    p.chunk = __builtin_amdgcn_readfirstlane((max((int)even, a.min_chunk) + kWaves * kRows - 1) & -(kWaves * kRows));
+    p.b = -1;
+    p.first = p.parts = p.slot = 0;
+    int first = 0, slot = 0;
+    for (int b0 = 0; b0 < a.B; b0 += kWave) {
+        const int b = b0 + lane;
+        const int n = b < a.B ? span_tokens(a, b) : 0;
+        const int parts = b < a.B ? max(1, (int)(((unsigned)n + (unsigned)p.chunk - 1) / (unsigned)p.chunk)) : 0;
+        const int mine = parts * items, mine_slots = parts > 1 ? mine : 0;
+        const int upto = lane_scan(mine, lane), upto_slots = lane_scan(mine_slots, lane);
+        const bool here = b < a.B && (by_chunk ? want >= first + upto - mine && want < first + upto : b == want);
+        const unsigned long long who = __ballot(here);
+        if (who) {
+            const int l = __builtin_ctzll(who);
+            p.b = b0 + l;
+            p.first = first + __builtin_amdgcn_readlane(upto - mine, l);
+            p.parts = __builtin_amdgcn_readlane(parts, l);
+            p.slot = slot + __builtin_amdgcn_readlane(upto_slots - mine_slots, l);
+            break;
+        }
+        first += __builtin_amdgcn_readlane(upto, kWave - 1);
+        slot += __builtin_amdgcn_readlane(upto_slots, kWave - 1);
+    }
+    return p;
+}
+
+// ------------------------------------------------------------------------------------------------ types
+struct Bf16 {
+    static constexpr int kBytes = 2, kSub = 1;  // bytes of an element; subtiles of a tile
+    typedef uint16_t io;
+};
+struct Fp8 {
+    static constexpr int kBytes = 1, kSub = 2;  // (the transposing read gives eight keys of 8 bits)
+    typedef uint16_t io;
+};
+struct Fp32 {
+    static constexpr int kBytes = 4, kSub = 1;
+    typedef float io;
+};
+
+// Which 16-byte piece of a row lies at which place of its LDS row: place = piece ^ key(row), so that the rows that are read together lie
+// in different banks.
+constexpr int key_bits(int pieces) { return pieces % 8 ? 3 : 7; }  // (rows have a multiple of four pieces)
+__device__ __forceinline__ int k_key(int row, int pieces) { return row & key_bits(pieces); }
+template <typename T>
+__device__ __forceinline__ int v_key(int row, int pieces) {
+    if (T::kBytes == 4) return row & 4;                                        // rows 4 apart, four pieces of each
+    if (T::kBytes == 2) return (row & 3) << 1;                                 // four rows, two pieces of each
+    return ((row & 3) | ((row >> 4) & 1) << 2) & key_bits(pieces);             // eight rows, one piece of each
+}
+
+// maximum and sum over the four lanes that hold a query head's values (l, l ^ 16, l ^ 32, l ^ 48)
+__device__ __forceinline__ float quad_max(float v) {
+    const unsigned u = __float_as_uint(v);
+    auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const unsigned w = __float_as_uint(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+    auto t = __builtin_amdgcn_permlane16_swap(w, w, false, false);
+    return fmaxf(__uint_as_float(t[0]), __uint_as_float(t[1]));
+}
+__device__ __forceinline__ float quad_sum(float v) {
+    const unsigned u = __float_as_uint(v);
+    auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+    const unsigned w = __float_as_uint(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+    auto t = __builtin_amdgcn_permlane16_swap(w, w, false, false);
+    return __uint_as_float(t[0]) + __uint_as_float(t[1]);
+}
+
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ u32x4 lds_16(uint32_t at) { return *(const __attribute__((address_space(3))) u32x4*)(uintptr_t)at; }
+
+// eight 8-bit values as bf16, exactly
+__device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    bf16x2 v[4] = {__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true),
+                   __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true)};
+    bf16x8 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        r[2 * i] = v[i][0];
+        r[2 * i + 1] = v[i][1];
+    }
+    return r;
+}
+
+// ------------------------------------------------------------------------------------------------ one chunk
+template <typename T, int KC, int VC, int NS>
+struct Shape {
+    static constexpr int kTile = T::kSub * kRows;                       // keys
+    static constexpr int kPiecesK = KC * T::kBytes / 16, kPiecesV = VC * T::kBytes / 16;  // 16-byte pieces of a row
+    static constexpr int kLoadsK = kTile * kPiecesK / kWave, kLoadsV = kTile * kPiecesV / kWave;  // instructions that bring a tile
+    static constexpr int kTileK = kTile * KC * T::kBytes, kTileV = kTile * VC * T::kBytes;        // bytes
+    static constexpr int kStage = kTileK + kTileV;
+    static constexpr int kRing = kStage * NS;
+    static constexpr int kOutRow = VC + 4;  // floats of a row of the workgroup's sums in LDS: rows begin in different banks
+    static constexpr int kMerge = kWaves * kKvHeads * (kOutRow + 2) * 4;
+    static constexpr int kLds = kWaves * kRing > kMerge ? kWaves * kRing : kMerge;
+    static_assert(kTile * kPiecesK % kWave == 0 && kTile * kPiecesV % kWave == 0, "whole instructions");
+};
+
+// Waits for the loads that `rest` (uniform, below NS) whole stages of PER loads and EXTRA others were issued behind.
+template <int NS, int PER, int EXTRA>
+__device__ __forceinline__ void wait_stage(int rest) {
+    if constexpr (NS > 1) {
+        if (rest == NS - 1) return wait_vm_fence<(NS - 1) * PER + EXTRA>();
+        return wait_stage<NS - 1, PER, EXTRA>(rest);
+    }
+    wait_vm_fence<EXTRA>();
+}
+
+template <typename T, int KC, int VC, int NS>
+__global__ void __launch_bounds__(kWaves * kWave) kv_attend_kernel(KvAttendArgs a) {
+    using S = Shape<T, KC, VC, NS>;
+    typedef typename T::io io;
+    constexpr int kUnits = KC * T::kBytes / 64;  // of 64 bytes of a key: a 16-byte piece for each of the four lane groups
+    constexpr int kOut = VC / 16;                // tiles of sixteen output columns
+    extern __shared__ __align__(16) unsigned char smem[];
+    const int lane = threadIdx.x & (kWave - 1);
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int col = lane & 15, grp = lane >> 4;
+
+    const Plan p = make_plan<true>(a, blockIdx.x, lane);
+    if (p.b < 0) return;
+    bool bad_len;
+    const Span sp = span_of(a, p.b, bad_len);
+    const int items = a.n_kv * a.blocks_of_heads;
+    const int local = blockIdx.x - p.first;
+    const int part = local / items, item = local - part * items;
+    const int hk = item / a.blocks_of_heads, h0 = (item - hk * a.blocks_of_heads) * kKvHeads;
+    const int heads = min(kKvHeads, a.group - h0);
+    const int c0 = sp.start + part * p.chunk, c1 = min(c0 + p.chunk, sp.end);
+    if (bad_len && local == 0 && threadIdx.x == 0) atomicOr(a.flags, kKvBadLength);
+
+    // the queries, as the second operand of the products: lane (col, grp) holds piece grp of every unit of head col
+    constexpr int kQ = T::kBytes == 1 ? 2 * kUnits : kUnits;  // 16-byte pieces
+    uint4 q[kQ];
+    {
+        const io* src = static_cast<const io*>(a.q) + (long long)p.b * a.q_stride + (long long)(hk * a.group + h0 + col) * a.k_dim;
+#pragma unroll
+        for (int u = 0; u < kQ; ++u) {
+            const int d = T::kBytes == 1 ? (u >> 1) * 64 + grp * 16 + (u & 1) * 8 : T::kBytes == 2 ? u * 32 + grp * 8 : u * 16 + grp * 4;
+            q[u] = make_uint4(0u, 0u, 0u, 0u);
+            if (col < heads && d < a.k_dim) q[u] = *reinterpret_cast<const uint4*>(src + d);
+        }
+    }
+
+    // where a lane's pieces of a tile come from, behind the subtile's first byte
+    uint32_t off_k[S::kLoadsK / T::kSub], off_v[S::kLoadsV];
+#pragma unroll
+    for (int i = 0; i < S::kLoadsK / T::kSub; ++i) {
+        const int n = i * kWave + lane, row = n / S::kPiecesK, at = n % S::kPiecesK;
+        const int piece = at ^ k_key(row, S::kPiecesK);
+        off_k[i] = row * a.k_dim * T::kBytes + (piece * 16 < a.k_dim * T::kBytes ? piece * 16 : 0);  // (past the row: any valid piece, the query is zero there)
+    }
+#pragma unroll
+    for (int i = 0; i < S::kLoadsV; ++i) {
+        const int n = i * kWave + lane, row = n / S::kPiecesV, at = n % S::kPiecesV;
+        const int piece = at ^ v_key<T>(row, S::kPiecesV);
+        off_v[i] = (row % kRows) * a.v_dim * T::kBytes + (piece * 16 < a.v_dim * T::kBytes ? piece * 16 : 0);
+    }
+
+    const uint32_t ring = lds_address(smem) + wv * S::kRing;
+    const int n_tiles = c1 > c0 ? (c1 - c0 + S::kTile - 1) / S::kTile : 0;
+    const int mine = n_tiles > wv ? (n_tiles - wv + kWaves - 1) / kWaves : 0;
+    const kv_const_ints table = (kv_const_ints)(uintptr_t)(a.table + (long long)p.b * a.width);
+    const kv_const_ints list = (kv_const_ints)(uintptr_t)(a.list ? a.list + ((long long)p.b * a.n_kv + hk) * a.n_sel : nullptr);
+    const long long head_k = (long long)hk * a.k_dim << a.page_shift, head_v = (long long)hk * a.v_dim << a.page_shift;
+    const int in_page = (1 << a.page_shift) - 1;
+
+    // the page of a tile's subtile, -1: none
+    auto page_of = [&](int k, int st) -> int {
+        const int tok = c0 + (wv + k * kWaves) * S::kTile + st * kRows;
+        if (tok >= c1) return -1;
+        int at = tok >> a.page_shift;
+        if (a.list) {
+            at = list[at];
+            if (at < 0 || at >= a.width) return -1;
+        }
+        const int pg = table[at];
+        return pg;
+    };
+    int next[T::kSub];
+    unsigned gone = 0;  // a bit per stage and subtile: its page is none of the pool's
+    const unsigned char *src_k[T::kSub], *src_v[T::kSub];
+    auto look_up = [&](int k) {
+#pragma unroll
+        for (int st = 0; st < T::kSub; ++st) next[st] = k < mine ? page_of(k, st) : -1;
+    };
+    auto place = [&](int k, int stage) {
+#pragma unroll
+        for (int st = 0; st < T::kSub; ++st) {
+            const int tok = c0 + (wv + k * kWaves) * S::kTile + st * kRows;
+            int pg = next[st];
+            const bool ok = pg >= 0 && pg < a.n_pages;
+            const unsigned bit = 1u << (stage * T::kSub + st);
+            gone = ok ? gone & ~bit : gone | bit;
+            pg = ok ? pg : 0;
+            const long long row = tok & in_page;
+            src_k[st] = a.k + ((long long)pg * a.k_stride + head_k + row * a.k_dim) * T::kBytes;
+            src_v[st] = a.v + ((long long)pg * a.v_stride + head_v + row * a.v_dim) * T::kBytes;
+            if (!ok && tok < c1) {
+                if (lane == 0) atomicOr(a.flags, kKvBadPage);
+                wait_vm_fence<0>();  // the waits below count loads, which need not stay in order with an atomic
+            }
+        }
+    };
+    auto bring_k = [&](int stage) {
+        const uint32_t to = ring + stage * S::kStage;
+#pragma unroll
+        for (int i = 0; i < S::kLoadsK; ++i)
+            load16_once_to_lds_at(src_k[i / (S::kLoadsK / T::kSub)], off_k[i % (S::kLoadsK / T::kSub)], to + i * (kWave * 16));
+    };
+    auto bring_v = [&](int stage) {
+        const uint32_t to = ring + stage * S::kStage + S::kTileK;
+#pragma unroll
+        for (int i = 0; i < S::kLoadsV; ++i) {
+            load16_once_to_lds_at(src_v[i / (S::kLoadsV / T::kSub)], off_v[i], to + i * (kWave * 16));
+        }
+    };
+
+    float top = -INFINITY, sum = 0.f;  // of head col: the running maximum (of what exp2 takes) and this lane's share of the sum
+    f32x4 acc[kOut];
+#pragma unroll
+    for (int t = 0; t < kOut; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const float scale2 = a.k_scale ? a.scale2 * a.k_scale[hk] : a.scale2;
+
+    look_up(0);
+    for (int k = 0; k < NS && k < mine; ++k) {
+        place(k, k);
+        look_up(k + 1);
+        bring_k(k);
+        bring_v(k);
+    }
+    int stage = 0;
+    for (int k = 0; k < mine; ++k) {
+        const int rest = min(mine - 1 - k, NS - 1);  // stages under way behind this one
+        const bool more = k + NS < mine;
+        const uint32_t at_k = ring + stage * S::kStage, at_v = at_k + S::kTileK;
+        const int t0 = c0 + (wv + k * kWaves) * S::kTile;
+        const unsigned lost = (gone >> (stage * T::kSub)) & ((1u << T::kSub) - 1);
+        const bool edge = t0 < sp.begin || t0 + S::kTile > c1 || lost;
+
+        wait_stage<NS, S::kLoadsK + S::kLoadsV, S::kLoadsV>(rest);
+        f32x4 s[T::kSub];
+#pragma unroll
+        for (int st = 0; st < T::kSub; ++st) {
+            s[st] = f32x4{0.f, 0.f, 0.f, 0.f};
+            const uint32_t row = at_k + (st * kRows + col) * (KC * T::kBytes);
+#pragma unroll
+            for (int u = 0; u < kUnits; ++u) {
+                const u32x4 kk = lds_16(row + (((4 * u + grp) ^ k_key(col, S::kPiecesK)) << 4));
+                if constexpr (T::kBytes == 2) {
+                    s[st] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kk), __builtin_bit_cast(bf16x8, q[u]), s[st], 0, 0, 0);
+                } else if constexpr (T::kBytes == 1) {
+                    s[st] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(kk.x, kk.y), __builtin_bit_cast(bf16x8, q[2 * u]), s[st], 0, 0, 0);
+                    s[st] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(kk.z, kk.w), __builtin_bit_cast(bf16x8, q[2 * u + 1]), s[st], 0, 0, 0);
+                } else {
+                    const f32x4 x = __builtin_bit_cast(f32x4, kk), y = __builtin_bit_cast(f32x4, q[u]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) s[st] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], s[st], 0, 0, 0);
+                }
+            }
+        }
+        if (more) {
+            wait_lds_fence();
+            place(k + NS, stage);
+            look_up(k + NS + 1);
+            bring_k(stage);
+        }
+
+        // lane (col, grp) holds the logits of head col with keys 4 grp + r of every subtile
+        if (edge) {
+#pragma unroll
+            for (int st = 0; st < T::kSub; ++st)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int tok = t0 + st * kRows + 4 * grp + r;
+                    if (tok < sp.begin || tok >= c1 || (lost >> st & 1)) s[st][r] = -INFINITY;
+                }
+        }
+        float best = s[0][0];
+#pragma unroll
+        for (int st = 0; st < T::kSub; ++st)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) best = fmaxf(best, s[st][r]);
+        best = quad_max(best) * scale2;
+        if (__ballot(best > top)) {
+            const float higher = fmaxf(top, best);
+            const float fade = higher == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top - higher);
+            top = higher;
+            sum *= fade;
+#pragma unroll
+            for (int t = 0; t < kOut; ++t) acc[t] *= fade;
+        }
+        const float from = top == -INFINITY ? 0.f : top;
+        f32x4 e[T::kSub];
+#pragma unroll
+        for (int st = 0; st < T::kSub; ++st)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                e[st][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[st][r], scale2, -from));
+                sum += e[st][r];
+            }
+
+        if (more) wait_vm_fence<(NS - 1) * (S::kLoadsK + S::kLoadsV) + S::kLoadsK>();
+        else wait_stage<NS, S::kLoadsK + S::kLoadsV, 0>(rest);
+        if (edge) {  // what lies in rows that are not the sequence's may be anything, and 0 times it not 0
+#pragma unroll
+            for (int i = 0; i < S::kLoadsV; ++i) {
+                const int row = (i * kWave + lane) / S::kPiecesV, tok = t0 + row;
+                if (tok < sp.begin || tok >= c1 || (lost >> (row / kRows) & 1))
+                    *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(at_v + (i * kWave + lane) * 16) = u32x4{0u, 0u, 0u, 0u};
+            }
+            wait_lds_fence();
+        }
+        // The weights go to the products as they lie: a lane's keys are the summation indices of its group.  As bf16 they are split in two,
+        // the value and what rounding took from it: the matrix cores have the time, and the sums are as exact as the logits.
+        if constexpr (T::kBytes == 2) {
+            const uint2 hi = make_uint2(pack_bf16(e[0][0], e[0][1]), pack_bf16(e[0][2], e[0][3]));
+            const uint2 lo = make_uint2(pack_bf16(e[0][0] - bf16_lo(hi.x), e[0][1] - bf16_hi(hi.x)), pack_bf16(e[0][2] - bf16_lo(hi.y), e[0][3] - bf16_hi(hi.y)));
+            const uint32_t row = at_v + (4 * grp + (col >> 2)) * (VC * 2) + ((col & 1) << 3);
+            const int key = v_key<T>(4 * grp + (col >> 2), S::kPiecesV);
+#pragma unroll
+            for (int t = 0; t < kOut; ++t) {
+                const s16x4 vt = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (__attribute__((address_space(3))) s16x4*)(uintptr_t)(row + (((2 * t + ((col >> 1) & 1)) ^ key) << 4)));
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vt, __builtin_bit_cast(s16x4, hi), acc[t], 0, 0, 0);
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vt, __builtin_bit_cast(s16x4, lo), acc[t], 0, 0, 0);
+            }
+        } else if constexpr (T::kBytes == 1) {
+            uint4 hi, lo;
+            hi.x = pack_bf16(e[0][0], e[0][1]); hi.y = pack_bf16(e[0][2], e[0][3]);
+            hi.z = pack_bf16(e[1][0], e[1][1]); hi.w = pack_bf16(e[1][2], e[1][3]);
+            lo.x = pack_bf16(e[0][0] - bf16_lo(hi.x), e[0][1] - bf16_hi(hi.x)); lo.y = pack_bf16(e[0][2] - bf16_lo(hi.y), e[0][3] - bf16_hi(hi.y));
+            lo.z = pack_bf16(e[1][0] - bf16_lo(hi.z), e[1][1] - bf16_hi(hi.z)); lo.w = pack_bf16(e[1][2] - bf16_lo(hi.w), e[1][3] - bf16_hi(hi.w));
+            // eight rows of sixteen 8-bit columns, lanes 2r and 2r + 1 name row r's: the keys of the lane group in both subtiles
+            const int r8 = col >> 1, vrow = (r8 >> 2) * kRows + 4 * grp + (r8 & 3);
+            const uint32_t row = at_v + vrow * VC + ((col & 1) << 3);
+            const int key = v_key<T>(vrow, S::kPiecesV);
+#pragma unroll
+            for (int t = 0; t < kOut; ++t) {
+                const i32x2 vt = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                    (__attribute__((address_space(3))) i32x2*)(uintptr_t)(row + ((t ^ key) << 4)));
+                const bf16x8 w = widen8(vt[0], vt[1]);
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(bf16x8, hi), acc[t], 0, 0, 0);
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(bf16x8, lo), acc[t], 0, 0, 0);
+            }
+        } else {
+#pragma unroll
+            for (int t = 0; t < kOut; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int vrow = 4 * grp + r, piece = 4 * t + (col >> 2);
+                    const float x = *(const __attribute__((address_space(3))) float*)(uintptr_t)(
+                        at_v + vrow * (VC * 4) + ((piece ^ v_key<T>(vrow, S::kPiecesV)) << 4) + ((col & 3) << 2));
+                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, e[0][r], acc[t], 0, 0, 0);
+                }
+        }
+        if (more) {
+            wait_lds_fence();
+            bring_v(stage);
+        }
+        stage = stage + 1 == NS ? 0 : stage + 1;
+    }
+    sum = quad_sum(sum);
+
+    // the wavefronts' sums, joined in LDS
+    __syncthreads();  // the rings are read
+    float* out = reinterpret_cast<float*>(smem);                              // [kWaves][kKvHeads][kOutRow]
+    float* stat = out + kWaves * kKvHeads * S::kOutRow;                        // [kWaves][kKvHeads][2]
+    if (col < heads) {
+#pragma unroll
+        for (int t = 0; t < kOut; ++t)
+            *reinterpret_cast<f32x4*>(out + (wv * kKvHeads + col) * S::kOutRow + t * 16 + grp * 4) = acc[t];
+        if (grp == 0) {
+            stat[(wv * kKvHeads + col) * 2] = top;
+            stat[(wv * kKvHeads + col) * 2 + 1] = sum;
+        }
+    }
+    __syncthreads();
+    const long long head0 = (long long)p.b * a.n_kv * a.group + hk * a.group + h0;
+    const int quads = a.v_dim / 4;
+    const long long slot = p.slot + local;
+    const int rows = min(kKvHeads, a.group);
+    const float v_scale = a.v_scale ? a.v_scale[hk] : 1.f;
+    for (int n = threadIdx.x; n < heads * quads; n += kWaves * kWave) {
+        const int h = n / quads, d = (n - h * quads) * 4;
+        float m = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) m = fmaxf(m, stat[(w * kKvHeads + h) * 2]);
+        float l = 0.f;
+        f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float mw = stat[(w * kKvHeads + h) * 2];
+            const float f = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - m);
+            l = __builtin_fmaf(f, stat[(w * kKvHeads + h) * 2 + 1], l);
+            const f32x4 x = *reinterpret_cast<const f32x4*>(out + (w * kKvHeads + h) * S::kOutRow + d);
+            if (mw != -INFINITY)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] = __builtin_fmaf(f, x[i], o[i]);
+        }
+        if (p.parts > 1) {
+            *reinterpret_cast<f32x4*>(a.part + (slot * rows + h) * a.v_dim + d) = o;
+            if (d == 0) {
+                a.stat[(slot * rows + h) * 2] = m;
+                a.stat[(slot * rows + h) * 2 + 1] = l;
+            }
+        } else {
+            const float div = m == -INFINITY ? 0.f : v_scale / l;
+            if constexpr (sizeof(io) == 2)
+                *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + (head0 + h) * a.v_dim + d) =
+                    make_uint2(pack_bf16(o[0] * div, o[1] * div), pack_bf16(o[2] * div, o[3] * div));
+            else
+                *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + (head0 + h) * a.v_dim + d) = o * div;
+            if (d == 0 && a.lse) a.lse[head0 + h] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ the chunks of an item joined
+// A workgroup a query head; its wavefronts take the chunks in turn, a lane up to four output columns.
+template <typename io>
+__global__ void __launch_bounds__(kWaves * kWave) kv_join_kernel(KvAttendArgs a) {
+    const int lane = threadIdx.x & (kWave - 1);
+    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+    const int n_q = a.n_kv * a.group;
+    const int b = blockIdx.x / n_q, hq = blockIdx.x - b * n_q;
+    const Plan p = make_plan<false>(a, b, lane);
+    if (p.parts < 2) return;
+    const int items = a.n_kv * a.blocks_of_heads, rows = min(kKvHeads, a.group);
+    const int hk = hq / a.group, in_group = hq - hk * a.group;
+    const int item = hk * a.blocks_of_heads + in_group / kKvHeads, row = in_group % kKvHeads;
+    auto at = [&](int part) -> long long { return ((long long)p.slot + (long long)part * items + item) * rows + row; };
+    float m = -INFINITY;
+    for (int i = lane; i < p.parts; i += kWave) m = fmaxf(m, a.stat[at(i) * 2]);
+    m = wave_max(m);
+    const int d = lane * 4;
+    float l = 0.f;
+    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = wv; i < p.parts; i += kWaves) {
+        const float mi = a.stat[at(i) * 2];
+        const float f = mi == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mi - m);
+        l = __builtin_fmaf(f, a.stat[at(i) * 2 + 1], l);
+        if (d < a.v_dim && mi != -INFINITY) {
+            const f32x4 x = *reinterpret_cast<const f32x4*>(a.part + at(i) * a.v_dim + d);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] = __builtin_fmaf(f, x[j], o[j]);
+        }
+    }
+    __shared__ f32x4 s_o[kWaves][kWave];
+    __shared__ float s_l[kWaves];
+    s_o[wv][lane] = o;
+    if (lane == 0) s_l[wv] = l;
+    __syncthreads();
+    if (wv) return;
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) {
+        o += s_o[w][lane];
+        l += s_l[w];
+    }
+    const float div = m == -INFINITY ? 0.f : (a.v_scale ? a.v_scale[hk] : 1.f) / l;
+    const long long head = (long long)b * n_q + hq;
+    if (d < a.v_dim) {
+        if constexpr (sizeof(io) == 2)
+            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + head * a.v_dim + d) = make_uint2(pack_bf16(o[0] * div, o[1] * div), pack_bf16(o[2] * div, o[3] * div));
+        else
+            *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + head * a.v_dim + d) = o * div;
+    }
+    if (lane == 0 && a.lse) a.lse[head] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+}
+
+LdsLimits<64> g_limits;
+
+template <typename T, int KC, int VC>
+int launch_shape(const KvAttendArgs& a, hipStream_t s) {
+    constexpr int NS = Shape<T, KC, VC, 2>::kLds <= 160 * 1024 ? 2 : 1;
+    using S = Shape<T, KC, VC, NS>;
+    static_assert(S::kLds <= 160 * 1024, "the rings fit a compute unit");
+    const auto kernel = kv_attend_kernel<T, KC, VC, NS>;
+    if (S::kLds > 64 * 1024) {
+        const int rc = g_limits.at_least(reinterpret_cast<const void*>(kernel), S::kLds, [&]() -> int {
+            MOEI_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds));
+            return MOEI_OK;
+        });
+        if (rc) return rc;
+    }
+    const int items = a.n_kv * a.blocks_of_heads;
+    launch(K_KV_ATTEND, kernel, dim3((unsigned)(a.B * items + a.n_target)), dim3(kWaves * kWave), S::kLds, s, a);
+    MOEI_LAUNCH_CHECK();
+    launch(K_KV_JOIN, kv_join_kernel<typename T::io>, dim3((unsigned)(a.B * a.n_kv * a.group)), dim3(kWaves * kWave), 0, s, a);
+    MOEI_LAUNCH_CHECK();
+    return MOEI_OK;
+}
+
+// Heads are padded in LDS to the next of four widths; the classes are the pairs in use, others round both widths up.
+template <typename T>
+int launch_type(const KvAttendArgs& a, hipStream_t s) {
+    if (a.k_dim <= 64 && a.v_dim <= 64) return launch_shape<T, 64, 64>(a, s);
+    if (a.k_dim <= 128 && a.v_dim <= 128) return launch_shape<T, 128, 128>(a, s);
+    if (a.k_dim <= 192 && a.v_dim <= 128) return launch_shape<T, 192, 128>(a, s);
+    return launch_shape<T, 256, 256>(a, s);
+}
+
+}  // namespace
+
+int launch_kv_attend(const moei_kv& kv, const KvAttendArgs& a, hipStream_t s) {
+    switch (kv.d.dtype) {
+        case MOEI_WDTYPE_FP32: return launch_type<Fp32>(a, s);
+        case MOEI_WDTYPE_BF16: return launch_type<Bf16>(a, s);
+        default: return launch_type<Fp8>(a, s);
+    }
+}
+
+}  // namespace moei

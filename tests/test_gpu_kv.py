@@ -1,0 +1,706 @@
+"""The paged KV cache against its definitions in 64 bits (oracle/kv_oracle.py), through the Python entry points.
+
+Tolerances.  e = 2^-24.  A rotated element: the reduced angle is off by pi e (it is at most half a turn, rounded to fp32 once), sine and cosine
+by 2 e and the three operations by 3 e together, of |x1| + |x2|: 2^-20 of that bounds all of it.  Outputs and stored values are then rounded:
+half a step of their type.  A logit is a sum of k_dim products in fp32: off by at most (k_dim + 4) e of sum |q_d k_d|; a weight by that and by
+2^-21 for exp2 and its argument; bf16 products take weights in two parts, whose rest is below 2^-16; a sum of n weighted values is off
+by n e of the largest value.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv_oracle as O
+
+pytestmark = pytest.mark.gpu
+
+E = 2.0 ** -24
+HALF = {"fp32": 2.0 ** -24, "bf16": 2.0 ** -8, "fp8": 2.0 ** -4}     # half a step relative to the value
+LEAST = {"fp32": 0.0, "bf16": 0.0, "fp8": 2.0 ** -10}                # half the step below the smallest normal value
+
+
+@pytest.fixture(scope="module")
+def m():
+    import paper_2401_14361_amd as mod
+    mod.lib()
+    return mod
+
+
+def host(t):
+    return t.detach().to(torch.float64).cpu().numpy()
+
+
+def bits(t):
+    return t.detach().contiguous().view(torch.uint8).cpu().numpy().copy()
+
+
+class Case:
+    """A handle with pages of random values, a random page table and what the oracle needs of them."""
+
+    def __init__(self, m, dtype, Hq, Hkv, Dk, Dv, page, lens, seed=0, spare=3, summaries=False, gap=0, width=None, nan_tail=True, max_sel=None):
+        g = torch.Generator(device="cuda")
+        g.manual_seed(seed)
+        self.m, self.dtype, self.page = m, dtype, page
+        self.lens = list(lens)
+        B = len(self.lens)
+        per = [-(-max(n, 0) // page) for n in self.lens]
+        self.width = width or max(max(per), 1)
+        self.n_pages = sum(per) + spare
+        self.kv = m.Kv(Hq, Hkv, Dk, Dv, page, dtype, max_batch=max(B, 1), max_pages=max(self.width, 1), max_sel=max_sel)
+        order = torch.randperm(self.n_pages, generator=g, device="cuda").to(torch.int32)
+        table = torch.full((B, self.width), 2 ** 30, dtype=torch.int32, device="cuda")  # entries behind the last page are never used
+        at = 0
+        for b, n in enumerate(per):
+            table[b, :n] = order[at:at + n]
+            at += n
+        self.table = table
+        self.spare = order[at:]
+        dt, io = self.kv.page_dtype, self.kv.dtype
+
+        def pool(shape):
+            x = torch.randn((self.n_pages, *shape), generator=g, device="cuda")
+            if gap:
+                room = torch.full((self.n_pages, int(np.prod(shape)) + gap), float("nan"), device="cuda").to(dt)
+                view = room[:, :int(np.prod(shape))].view(self.n_pages, *shape)
+                view.copy_((x * (8 if dtype == "fp8" else 1)).to(dt))
+                return view
+            return (x * (8 if dtype == "fp8" else 1)).to(dt)
+
+        self.k, self.v = pool((Hkv, page, Dk)), pool((Hkv, page, Dv))
+        if nan_tail:  # rows behind the last token and pages that nobody has: anything may lie there
+            for t in (self.k, self.v):
+                for b, n in enumerate(self.lens):
+                    if n > 0 and n % page:
+                        t[int(table[b, per[b] - 1]), :, n % page:] = float("nan")
+                for s in self.spare.tolist():
+                    t[s] = float("nan")
+        self.ks = self.vs = None
+        if dtype == "fp8":
+            self.ks = 0.1 + 0.1 * torch.rand(Hkv, generator=g, device="cuda")
+            self.vs = 0.1 + 0.1 * torch.rand(Hkv, generator=g, device="cuda")
+        self.lo = self.hi = None
+        if summaries:
+            self.lo, self.hi = self.k.to(io).amin(2), self.k.to(io).amax(2)
+        self.pages = m.KvPages(self.kv, self.k, self.v, k_min=self.lo, k_max=self.hi, k_scale=self.ks, v_scale=self.vs)
+        self.q = (torch.randn((B, Hq, Dk), generator=g, device="cuda") * 1.5).to(io)
+        self.len_t = torch.tensor(self.lens, dtype=torch.int32, device="cuda")
+        self.scale = Dk ** -0.5
+
+    def oracle(self, window=0, chosen=None, lens=None, table=None):
+        scales = {} if self.ks is None else dict(k_scale=host(self.ks), v_scale=host(self.vs))
+        return O.attend(host(self.q), host(self.k), host(self.v), (self.table if table is None else table).cpu().numpy(), lens or self.lens,
+                        self.scale, window=window, chosen=chosen, **scales)
+
+    def bound(self, ref, n):
+        """(of outputs, of logarithms)"""
+        q, k, v = host(self.q), np.nan_to_num(host(self.k)), np.nan_to_num(host(self.v))
+        if self.ks is not None:
+            k, v = k * host(self.ks)[None, :, None, None], v * host(self.vs)[None, :, None, None]
+        big = np.abs(q).max() * np.abs(k).sum(-1).max() * self.scale
+        dz = (q.shape[2] + 4) * E * big + 2.0 ** -21
+        split = 0.0 if self.dtype == "fp32" else 2.0 ** -16
+        io = "fp32" if self.dtype == "fp32" else "bf16"
+        return (2 * dz + split + (n + 8) * E) * np.abs(v).max() + HALF[io] * np.abs(ref), dz + (n + 8) * E + 2.0 ** -22 * 40
+
+    def check(self, out, lse, ref, ref_lse):
+        n = max(max(self.lens), 1)
+        tol, tol_l = self.bound(ref, n)
+        got, got_l = host(out), host(lse)
+        assert np.isfinite(got).all()
+        assert (np.abs(got - ref) <= tol).all(), (np.abs(got - ref) / tol).max()
+        empty = np.isneginf(ref_lse)
+        assert (np.isneginf(got_l) == empty).all()
+        assert (np.abs(got_l - ref_lse)[~empty] <= tol_l).all(), np.abs(got_l - ref_lse)[~empty].max()
+
+
+# ------------------------------------------------------------------------------------------------ attention
+ATTEND = [
+    # dtype, Hq, Hkv, Dk, Dv, page, lens
+    ("bf16", 1, 1, 64, 64, 16, [1]),
+    ("bf16", 4, 1, 128, 128, 16, [1, 15, 16, 17]),
+    ("bf16", 8, 2, 128, 128, 64, [0, 63, 64, 65, 700]),
+    ("bf16", 6, 2, 80, 96, 32, [33, 0, 129]),
+    ("bf16", 16, 1, 192, 128, 16, [300, 5]),
+    ("bf16", 40, 2, 64, 64, 32, [257, 31]),          # twenty query heads a group: two passes
+    ("bf16", 2, 2, 256, 256, 128, [129, 1000]),
+    ("bf16", 3, 3, 16, 16, 16, [50, 2]),
+    ("fp8", 8, 1, 128, 128, 16, [1, 31, 32, 33, 500]),
+    ("fp8", 4, 4, 64, 64, 32, [100, 0, 17]),
+    ("fp8", 6, 2, 192, 128, 64, [65, 640]),
+    ("fp8", 2, 1, 256, 256, 16, [77]),
+    ("fp8", 17, 1, 80, 48, 16, [49, 48]),
+    ("fp32", 4, 2, 64, 64, 16, [0, 1, 40, 333]),
+    ("fp32", 3, 1, 128, 112, 32, [65, 200]),
+    ("fp32", 2, 2, 192, 128, 16, [31]),
+    ("fp32", 5, 1, 256, 240, 64, [130, 64]),
+]
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,Dk,Dv,page,lens", ATTEND)
+def test_attend(m, dtype, Hq, Hkv, Dk, Dv, page, lens):
+    c = Case(m, dtype, Hq, Hkv, Dk, Dv, page, lens, seed=len(lens) + Dk)
+    out, lse = m.kv_attend(c.kv, c.pages, c.table, c.len_t, c.q, c.scale, want_lse=True)
+    c.check(out, lse, *c.oracle())
+    again = m.kv_attend(c.kv, c.pages, c.table, c.len_t, c.q, c.scale)
+    assert (bits(again) == bits(out)).all()
+    assert c.kv.error_flags() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8", "fp32"])
+@pytest.mark.parametrize("window", [1, 16, 17, 100, 5000])
+def test_attend_to_a_window(m, dtype, window):
+    c = Case(m, dtype, 4, 2, 64, 64, 16, [0, 1, 16, 17, 100, 101, 730], seed=window)
+    for b, n in enumerate(c.lens):  # tokens before the window may have been given up: their rows hold anything
+        for j in range(max(0, n - window)):
+            c.k[int(c.table[b, j // 16]), :, j % 16] = float("nan")
+            c.v[int(c.table[b, j // 16]), :, j % 16] = float("nan")
+    out, lse = m.kv_attend(c.kv, c.pages, c.table, c.len_t, c.q, c.scale, window=window, want_lse=True)
+    c.check(out, lse, *c.oracle(window=window))
+
+
+@pytest.mark.parametrize("B", [1, 63, 64, 65, 130, 300])
+def test_attend_batches_of_any_size(m, B):
+    rng = np.random.default_rng(B)
+    lens = rng.integers(0, 120, B).tolist()
+    lens[B // 2] = 900
+    c = Case(m, "bf16", 4, 2, 64, 64, 16, lens, seed=B)
+    out, lse = m.kv_attend(c.kv, c.pages, c.table, c.len_t, c.q, c.scale, want_lse=True)
+    c.check(out, lse, *c.oracle())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8", "fp32"])
+def test_attend_splits_a_long_sequence(m, dtype):
+    # one head pair over 40,000 tokens: hundreds of workgroups share an item, a short one beside it stays whole
+    c = Case(m, dtype, 2, 1, 64, 64, 64, [40001, 70], seed=4)
+    out, lse = m.kv_attend(c.kv, c.pages, c.table, c.len_t, c.q, c.scale, want_lse=True)
+    c.check(out, lse, *c.oracle())
+    for _ in range(3):
+        assert (bits(m.kv_attend(c.kv, c.pages, c.table, c.len_t, c.q, c.scale)) == bits(out)).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8", "fp32"])
+def test_attend_pages_that_lie_apart_and_packed_queries(m, dtype):
+    c = Case(m, dtype, 4, 2, 64, 128, 32, [100, 31, 64], seed=9, gap=64)
+    packed = torch.full((3, 4 * 64 + 96), float("nan"), dtype=c.kv.dtype, device="cuda")
+    packed[:, 32:32 + 256] = c.q.reshape(3, -1)
+    q = packed[:, 32:32 + 256].view(3, 4, 64)
+    out, lse = m.kv_attend(c.kv, c.pages, c.table, c.len_t, q, c.scale, want_lse=True)
+    c.check(out, lse, *c.oracle())
+
+
+def test_attend_masks_bad_pages_and_lengths(m):
+    c = Case(m, "bf16", 4, 2, 64, 64, 16, [100, 60, 80], seed=1)
+    c.table[0, 2], c.table[0, 5], c.table[2, 0] = -1, c.n_pages, 2 ** 31 - 1
+    out, lse = m.kv_attend(c.kv, c.pages, c.table, c.len_t, c.q, c.scale, want_lse=True)
+    c.check(out, lse, *c.oracle())
+    assert c.kv.error_flags() == 1 and c.kv.error_flags() == 0
+    c.table[1] = -5  # nothing left of a sequence
+    out, lse = m.kv_attend(c.kv, c.pages, c.table, c.len_t, c.q, c.scale, want_lse=True)
+    c.check(out, lse, *c.oracle())
+    assert (host(out)[1] == 0).all()
+    assert c.kv.error_flags() == 1
+    d = Case(m, "bf16", 4, 2, 64, 64, 16, [112, 112, 112], seed=2)
+    out, lse = m.kv_attend(d.kv, d.pages, d.table, torch.tensor([-7, 113, 2 ** 31 - 1], dtype=torch.int32, device="cuda"), d.q, d.scale, want_lse=True)
+    d.check(out, lse, *d.oracle(lens=[0, 112, 112]))
+    assert d.kv.error_flags() == 2
+
+
+def test_attend_extreme_logits(m):
+    # logits of +-10^4 and equal ones: weights of exactly one key, and of all alike
+    c = Case(m, "fp32", 2, 1, 64, 64, 16, [200], seed=3)
+    c.q *= 1000.0
+    out, lse = m.kv_attend(c.kv, c.pages, c.table, c.len_t, c.q, c.scale, want_lse=True)
+    c.check(out, lse, *c.oracle())
+    c.q.zero_()
+    out, lse = m.kv_attend(c.kv, c.pages, c.table, c.len_t, c.q, c.scale, want_lse=True)
+    c.check(out, lse, *c.oracle())
+    # a +inf key makes the softmax undefined, a -inf one leaves it without that token
+    c.q.fill_(1.0)
+    c.k[int(c.table[0, 3]), 0, 5, 7] = float("-inf")
+    out, lse = m.kv_attend(c.kv, c.pages, c.table, c.len_t, c.q, c.scale, want_lse=True)
+    ref, ref_l = c.oracle()
+    assert np.isfinite(host(out)).all() and np.abs(host(out) - ref).max() <= 1e-4 and np.abs(host(lse) - ref_l).max() <= 1e-4
+
+
+def test_attend_offsets_beyond_32_bits(m):
+    # a pool of 2.6 * 10^9 elements; the sequence's pages lie at its end
+    Hkv, page, D, n_pages = 8, 64, 128, 40000
+    kv = m.Kv(8, Hkv, D, D, page, "bf16", max_batch=1, max_pages=4)
+    k = torch.empty((n_pages, Hkv, page, D), dtype=torch.bfloat16, device="cuda")
+    v = torch.empty((n_pages, Hkv, page, D), dtype=torch.bfloat16, device="cuda")
+    g = torch.Generator(device="cuda")
+    g.manual_seed(5)
+    ids = [n_pages - 1, n_pages - 3, 2, n_pages - 2]
+    for i in ids:
+        k[i] = torch.randn((Hkv, page, D), generator=g, device="cuda").bfloat16()
+        v[i] = torch.randn((Hkv, page, D), generator=g, device="cuda").bfloat16()
+    table = torch.tensor([ids], dtype=torch.int32, device="cuda")
+    q = torch.randn((1, 8, D), generator=g, device="cuda").bfloat16()
+    pages = m.KvPages(kv, k, v)
+    new_k, new_v = torch.randn((1, Hkv, D), generator=g, device="cuda").bfloat16(), torch.randn((1, Hkv, D), generator=g, device="cuda").bfloat16()
+    m.kv_append(kv, pages, table, torch.tensor([249], dtype=torch.int32, device="cuda"), q, new_k, new_v, None)
+    assert (k[ids[3], :, 249 - 192] == new_k[0]).all() and (v[ids[3], :, 249 - 192] == new_v[0]).all()
+    out = m.kv_attend(kv, pages, table, torch.tensor([250], dtype=torch.int32, device="cuda"), q, D ** -0.5)
+    keys, vals = k[ids].transpose(0, 1).reshape(Hkv, 256, D)[:, :250].double(), v[ids].transpose(0, 1).reshape(Hkv, 256, D)[:, :250].double()
+    p = torch.softmax((keys @ q[0].double()[:, :, None])[..., 0] * D ** -0.5, -1)
+    ref = (p[:, None] @ vals)[:, 0]
+    tol = (2 * ((D + 4) * E * 60 + 2.0 ** -21) + 2.0 ** -16 + 260 * E) * float(vals.abs().max()) + HALF["bf16"] * ref.abs()
+    assert ((out[0].double() - ref).abs() <= tol).all()
+    assert kv.error_flags() == 0
+
+
+# ------------------------------------------------------------------------------------------------ appending
+def _append_inputs(c, T, seed, layout="dense"):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    Hq, Dk = c.kv.heads
+    Hkv, Dv = c.kv.v_page[0], c.kv.v_page[2]
+    sizes = [Hq * Dk, Hkv * Dk, Hkv * Dv]
+    x = (torch.randn((T, sum(sizes) + 5), generator=g, device="cuda") * 2).to(c.kv.dtype)
+    if layout == "dense":
+        return [x[:, a:a + n].contiguous().view(T, -1, d) for a, n, d in ((0, sizes[0], Dk), (sizes[0], sizes[1], Dk), (sizes[0] + sizes[1], sizes[2], Dv))]
+    first = {"packed": 0, "odd": 3}[layout]
+    x = x[:, first:] if layout == "odd" else x[:, :sum(sizes)].contiguous()
+    return [x[:, a:a + n].unflatten(1, (-1, d)) for a, n, d in ((0, sizes[0], Dk), (sizes[0], sizes[1], Dk), (sizes[0] + sizes[1], sizes[2], Dv))]
+
+
+def _check_append(c, q, k, v, q_out, q_before, k_before, v_before, seq, pos, inv_freq, interleaved):
+    """Everything that the call may write, and that it has written nothing else."""
+    place = O.places(c.table.cpu().numpy().tolist(), seq, pos, c.page, c.n_pages)
+    io = "fp32" if c.dtype == "fp32" else "bf16"
+    freq = host(inv_freq) if inv_freq is not None else np.zeros(0)
+    P = [max(p, 0) for p in pos]
+    rot = 2 * len(freq)
+
+    def slack(x):  # 2^-20 of |x1| + |x2|, for rotated elements
+        a = np.abs(x)
+        s = np.zeros_like(a)
+        if interleaved:
+            s[..., 0:rot:2] = s[..., 1:rot:2] = a[..., 0:rot:2] + a[..., 1:rot:2]
+        else:
+            s[..., :rot // 2] = s[..., rot // 2:rot] = a[..., :rot // 2] + a[..., rot // 2:rot]
+        return 2.0 ** -20 * s
+
+    qr, kr, vr = O.rotate(host(q), P, freq, interleaved), O.rotate(host(k), P, freq, interleaved), host(v)
+    qs, ks = slack(host(q)), slack(host(k))
+    got_q, before_q = host(q_out), host(q_before)
+    want_k, want_v = host(k_before), host(v_before)
+    tol_k, tol_v = np.zeros_like(want_k), np.zeros_like(want_v)
+    for t, at in enumerate(place):
+        if at is None:
+            assert (bits(q_out[t]) == bits(q_before[t])).all()
+            continue
+        assert (np.abs(got_q[t] - qr[t]) <= HALF[io] * np.abs(qr[t]) + 2 * qs[t]).all()
+        a, b, sa = kr[t], vr[t], ks[t]
+        if c.dtype == "fp8":
+            a, b, sa = a / host(c.ks)[:, None], b / host(c.vs)[:, None], sa / host(c.ks)[:, None]
+            a, b = np.clip(a, -448, 448), np.clip(b, -448, 448)
+        want_k[at[0], :, at[1]], want_v[at[0], :, at[1]] = a, b
+        tol_k[at[0], :, at[1]] = HALF[c.dtype] * np.abs(a) + LEAST[c.dtype] + 2 * sa + 4 * E * np.abs(a)
+        tol_v[at[0], :, at[1]] = 0.0 if c.dtype != "fp8" else HALF["fp8"] * np.abs(b) + LEAST["fp8"] + 4 * E * np.abs(b)
+    for got, want, tol in ((host(c.k), want_k, tol_k), (host(c.v), want_v, tol_v)):
+        same = (got == want) | (np.isnan(got) & np.isnan(want))
+        assert (same | (np.abs(got - want) <= tol)).all()
+    return place
+
+
+def _freq(rot, base=10000.0):
+    return (base ** (-torch.arange(rot // 2, dtype=torch.float64) * 2 / max(rot, 1))).float().cuda()
+
+
+APPEND = [
+    # dtype, Hq, Hkv, Dk, Dv, page, rot, interleaved, layout
+    ("bf16", 4, 2, 128, 128, 16, 128, False, "dense"),
+    ("bf16", 4, 2, 128, 128, 16, 128, True, "packed"),
+    ("bf16", 3, 1, 80, 96, 32, 40, False, "dense"),       # pairs 20 apart: element by element
+    ("bf16", 6, 3, 192, 128, 64, 64, True, "odd"),
+    ("bf16", 2, 2, 64, 64, 16, 0, False, "dense"),        # nothing is rotated
+    ("bf16", 5, 5, 16, 32, 16, 2, False, "packed"),
+    ("fp8", 8, 2, 128, 128, 32, 128, False, "dense"),
+    ("fp8", 3, 1, 80, 48, 16, 40, True, "odd"),
+    ("fp8", 4, 4, 256, 256, 16, 128, False, "packed"),
+    ("fp32", 4, 2, 64, 64, 16, 64, False, "dense"),
+    ("fp32", 2, 1, 192, 128, 16, 64, True, "packed"),
+    ("fp32", 3, 1, 48, 64, 128, 6, False, "odd"),
+]
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,Dk,Dv,page,rot,interleaved,layout", APPEND)
+def test_append_a_token_to_each_sequence(m, dtype, Hq, Hkv, Dk, Dv, page, rot, interleaved, layout):
+    pos = [0, page - 1, -1, 2 * page, 3 * page - 1, 2 * page + 5, 3 * page - 1, 7]
+    c = Case(m, dtype, Hq, Hkv, Dk, Dv, page, [max(p, 0) + 1 for p in pos], seed=rot + page, summaries=True, nan_tail=False)
+    q, k, v = _append_inputs(c, len(pos), seed=page, layout=layout)
+    before = [t.clone() for t in (c.k, c.v, c.lo, c.hi)]
+    q_out = torch.full((len(pos), Hq, Dk), 7.0, dtype=c.kv.dtype, device="cuda")
+    q_before = q_out.clone()
+    freq = _freq(rot) if rot else None
+    got = m.kv_append(c.kv, c.pages, c.table, torch.tensor(pos, dtype=torch.int32, device="cuda"), q, k, v, freq, interleaved=interleaved, q_out=q_out)
+    assert got is q_out
+    place = _check_append(c, q, k, v, q_out, q_before, before[0], before[1], range(len(pos)), pos, freq, interleaved)
+    full = [at[0] for at in place if at is not None and at[1] == page - 1]
+    assert len(full) == 3
+    lo, hi = before[2], before[3]
+    for i in full:
+        lo[i], hi[i] = c.k[i].to(c.kv.dtype).amin(1), c.k[i].to(c.kv.dtype).amax(1)
+    assert (bits(c.lo) == bits(lo)).all() and (bits(c.hi) == bits(hi)).all()
+    assert c.kv.error_flags() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8", "fp32"])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_append_prompts(m, dtype, in_place):
+    # three prompts in one call, behind what their sequences hold, in a mixed order; a page is filled by tokens of this call alone, another
+    # one by the rest of an earlier call's
+    page, starts, counts = 16, [0, 21, 1000], [75, 11, 40]
+    rng = np.random.default_rng(3)
+    tokens = [(b, starts[b] + i) for b in range(3) for i in range(counts[b])]
+    rng.shuffle(tokens)
+    seq, pos = [t[0] for t in tokens], [t[1] for t in tokens]
+    c = Case(m, dtype, 4, 2, 64, 96, page, [a + n for a, n in zip(starts, counts)], seed=8, summaries=True, nan_tail=False)
+    q, k, v = _append_inputs(c, len(tokens), seed=2)
+    before = [t.clone() for t in (c.k, c.v, c.lo, c.hi, q)]
+    q_out = q if in_place else torch.zeros_like(q)
+    q_in = before[4]
+    m.kv_append(c.kv, c.pages, c.table, torch.tensor(pos, dtype=torch.int32, device="cuda"), q, k, v, _freq(64),
+                seq=torch.tensor(seq, dtype=torch.int32, device="cuda"), q_out=q_out)
+    place = _check_append(c, q_in, k, v, q_out, q_out, before[0], before[1], seq, pos, _freq(64), False)
+    lo, hi = before[2], before[3]
+    for i in {at[0] for at in place if at[1] == page - 1}:
+        lo[i], hi[i] = c.k[i].to(c.kv.dtype).amin(1), c.k[i].to(c.kv.dtype).amax(1)
+    assert (bits(c.lo) == bits(lo)).all() and (bits(c.hi) == bits(hi)).all()
+
+
+def test_append_far_positions(m):
+    # angles of 10^6 radians: the product of position and frequency does not fit fp32
+    c = Case(m, "fp32", 2, 1, 64, 64, 256, [1], seed=0, width=4096, nan_tail=False)
+    for pos in (2 ** 20 - 1, 999_999, 131_071, 16_777 * 3):
+        c.table[0, pos // 256] = 0
+        q, k, v = _append_inputs(c, 1, seed=pos)
+        before = c.k.clone(), c.v.clone()
+        q_out = m.kv_append(c.kv, c.pages, c.table, torch.tensor([pos], dtype=torch.int32, device="cuda"), q, k, v, _freq(64))
+        _check_append(c, q, k, v, q_out, q_out, *before, [0], [pos], _freq(64), False)
+
+
+def test_append_leaves_out_tokens_without_a_place(m):
+    c = Case(m, "bf16", 4, 2, 64, 64, 16, [32, 32, 32], seed=6, summaries=True, nan_tail=False)
+    c.table[1, 0], c.table[2, 1] = -1, c.n_pages
+    seq, pos = [0, 0, 1, 2, 3, -1, 2], [5, 32, 7, 31, 1, 1, 2 ** 31 - 1]
+    q, k, v = _append_inputs(c, len(seq), seed=6)
+    before = [bits(t) for t in (c.k, c.v, c.lo, c.hi)]
+    kb, vb = c.k.clone(), c.v.clone()
+    q_out = torch.full_like(q, 3.0)
+    m.kv_append(c.kv, c.pages, c.table, torch.tensor(pos, dtype=torch.int32, device="cuda"), q, k, v, _freq(64),
+                seq=torch.tensor(seq, dtype=torch.int32, device="cuda"), q_out=q_out)
+    _check_append(c, q, k, v, q_out, torch.full_like(q, 3.0), kb, vb, seq, pos, _freq(64), False)
+    assert (bits(c.lo) == before[2]).all() and (bits(c.hi) == before[3]).all()
+    assert c.kv.error_flags() == 3
+
+
+def test_append_limits_8_bit_values(m):
+    c = Case(m, "fp8", 1, 1, 16, 16, 16, [16], seed=1, nan_tail=False)
+    c.ks.fill_(0.5)
+    c.vs.fill_(0.25)
+    q, k, v = _append_inputs(c, 1, seed=1)
+    k[0, 0, :4] = torch.tensor([1e6, -1e6, float("nan"), 0.0])
+    v[0, 0, :4] = torch.tensor([448 * 0.25, float("inf"), float("-inf"), 1e-9])
+    m.kv_append(c.kv, c.pages, c.table, torch.tensor([3], dtype=torch.int32, device="cuda"), q, k, v, None)
+    at = int(c.table[0, 0])
+    kk, vv = host(c.k[at, 0, 3])[:4], host(c.v[at, 0, 3])[:4]
+    assert kk[0] == 448 and kk[1] == -448 and np.isnan(kk[2]) and kk[3] == 0
+    assert vv.tolist() == [448.0, 448.0, -448.0, 0.0]
+
+
+# ------------------------------------------------------------------------------------------------ chosen pages
+def _choice(c, n_sel, first, last):
+    q, lo, hi = host(c.q), host(c.lo), host(c.hi)
+    G = c.kv.heads[0] // c.kv.k_page[0]
+    got = []
+    for b, n in enumerate(c.lens):
+        nb = -(-n // c.page)
+        at = c.table[b, :nb].cpu().numpy()
+        got.append([O.choose(q[b, h * G:(h + 1) * G], lo[at, h], hi[at, h], nb, n_sel, first, last) for h in range(c.kv.k_page[0])])
+    return got
+
+
+def _check_blocks(c, n_sel, first, last):
+    out, lse, blocks = c.m.kv_attend_blocks(c.kv, c.pages, c.table, c.len_t, c.q, c.scale, n_sel, keep_first=first, keep_last=last, want_lse=True, want_blocks=True)
+    chosen = _choice(c, n_sel, first, last)
+    want = np.full((len(c.lens), c.kv.k_page[0], n_sel), -1)
+    for b, heads in enumerate(chosen):
+        for h, pages in enumerate(heads):
+            want[b, h, :len(pages)] = pages
+    assert (blocks.cpu().numpy() == want).all()
+    c.check(out, lse, *c.oracle(chosen=chosen))
+    only = c.m.kv_attend_blocks(c.kv, c.pages, c.table, c.len_t, c.q, c.scale, n_sel, keep_first=first, keep_last=last)
+    assert (bits(only) == bits(out)).all()
+    assert c.kv.error_flags() == 0
+
+
+BLOCKS = [
+    # dtype, Hq, Hkv, Dk, Dv, page, lens, n_sel, first, last
+    ("bf16", 8, 2, 128, 128, 16, [1, 0, 160, 161, 1000, 3111], 10, 1, 1),
+    ("bf16", 4, 4, 64, 64, 32, [999, 64], 5, 0, 1),
+    ("bf16", 12, 1, 80, 80, 16, [600, 599, 40], 7, 2, 4),
+    ("bf16", 24, 1, 256, 128, 16, [400], 6, 1, 2),         # two passes of query heads
+    ("bf16", 10, 2, 128, 64, 16, [1300], 3, 1, 2),         # nothing is left to choose
+    ("bf16", 6, 2, 64, 64, 16, [2000], 1, 0, 1),
+    ("fp8", 8, 1, 128, 128, 16, [2000, 17, 1111], 20, 1, 1),
+    ("fp8", 4, 2, 64, 64, 32, [777], 4, 0, 2),
+    ("fp32", 4, 2, 64, 64, 16, [500, 499, 3], 9, 1, 1),
+    ("fp32", 3, 1, 192, 128, 16, [300], 8, 0, 1),
+    ("fp32", 5, 1, 256, 64, 64, [2000], 8, 0, 1),
+]
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,Dk,Dv,page,lens,n_sel,first,last", BLOCKS)
+def test_attend_blocks(m, dtype, Hq, Hkv, Dk, Dv, page, lens, n_sel, first, last):
+    # (a page that is not full has the summary of garbage; it is the last one, which needs none)
+    c = Case(m, dtype, Hq, Hkv, Dk, Dv, page, lens, seed=n_sel, summaries=True, max_sel=min(32, max(1, -(-max(lens) // page))))
+    _check_blocks(c, min(n_sel, c.kv.desc.max_sel), first, last)
+
+
+@pytest.mark.parametrize("n_sel", [3, 200, 1500, 3000])
+def test_attend_blocks_of_many_pages(m, n_sel):
+    c = Case(m, "bf16", 4, 1, 64, 64, 16, [16 * 3100 - 5], seed=n_sel, summaries=True, max_sel=3000)
+    _check_blocks(c, n_sel, 1, 1)
+
+
+def test_attend_blocks_equal_and_undefined_scores(m):
+    # all pages alike but a few: ties go to the lower page; a score that is no number comes last, also among ties
+    c = Case(m, "bf16", 4, 1, 64, 64, 16, [16 * 2000], seed=1, summaries=True, max_sel=64)
+    at = c.table[0].long()
+    c.lo[at], c.hi[at] = -1.0, 1.0
+    c.hi[at[[1500, 77]]] = 2.0
+    c.lo[at[3], 0, 5] = float("nan")
+    c.hi[at[3], 0, 5] = float("nan")
+    _check_blocks(c, 40, 1, 2)
+    c.lo[at], c.hi[at] = 0.0, -0.0   # scores of both zeros are equal
+    c.lo[at[::2]], c.hi[at[::2]] = -0.0, 0.0
+    _check_blocks(c, 33, 0, 1)
+
+
+def test_attend_blocks_passes_over_pages_outside_the_pool(m):
+    c = Case(m, "bf16", 4, 2, 64, 64, 16, [640], seed=3, summaries=True, max_sel=16)
+    c.table[0, 5] = -3
+    out, lse, blocks = m.kv_attend_blocks(c.kv, c.pages, c.table, c.len_t, c.q, c.scale, 8, want_lse=True, want_blocks=True)
+    assert np.isfinite(host(out)).all() and 5 not in blocks.cpu().numpy()
+    assert c.kv.error_flags() == 1
+    c.check(out, lse, *c.oracle(chosen=[[h.tolist() for h in blocks.cpu().numpy()[0]]]))
+
+
+# ------------------------------------------------------------------------------------------------ as a program uses them
+def test_decode_steps_from_an_empty_cache(m):
+    """Prompts, then tokens one by one: what the cache holds and answers is the attention over all tokens so far."""
+    Hq, Hkv, D, page, B = 8, 2, 64, 16, 3
+    prompts, steps = [37, 1, 16], 20
+    c = Case(m, "bf16", Hq, Hkv, D, D, page, [n + steps for n in prompts], seed=11, summaries=True, nan_tail=True, max_sel=4)
+    for t in (c.k, c.v):
+        t.fill_(float("nan"))
+    c.lo.fill_(float("nan"))
+    c.hi.fill_(float("nan"))
+    freq = _freq(D)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    hist = [[] for _ in range(B)]
+
+    def feed(seq, pos):
+        T = len(pos)
+        q, k, v = (torch.randn((T, h, D), generator=g, device="cuda").bfloat16() for h in (Hq, Hkv, Hkv))
+        out = m.kv_append(c.kv, c.pages, c.table, torch.tensor(pos, dtype=torch.int32, device="cuda"), q, k, v, freq,
+                          seq=None if seq is None else torch.tensor(seq, dtype=torch.int32, device="cuda"))
+        kr, vr = O.rotate(host(k), pos, host(freq), False), host(v)
+        for t, s in enumerate(seq if seq is not None else range(B)):
+            hist[s].append((kr[t], vr[t]))
+        return out, O.rotate(host(q), pos, host(freq), False)
+
+    feed([b for b in range(B) for _ in range(prompts[b])], [i for b in range(B) for i in range(prompts[b])])
+    for step in range(steps):
+        q, q_exact = feed(None, [n + step for n in prompts])
+        lens = torch.tensor([n + step + 1 for n in prompts], dtype=torch.int32, device="cuda")
+        out = host(m.kv_attend(c.kv, c.pages, c.table, lens, q, D ** -0.5))
+        few = host(m.kv_attend_blocks(c.kv, c.pages, c.table, lens, q, D ** -0.5, 4))
+        for b in range(B):
+            K, V = np.stack([x[0] for x in hist[b]]), np.stack([x[1] for x in hist[b]])
+            for h in range(Hq):
+                z = K[:, h // 4] @ q_exact[b, h] * D ** -0.5
+                p = np.exp(z - z.max())
+                ref = p @ V[:, h // 4] / p.sum()
+                # queries and keys are rounded to bf16: a logit is off by 2 * 2^-8 of sum |q k| / 8 <= |q| |k| / 8, the output by twice that
+                dz = 2.0 ** -7 * 1.01 * np.linalg.norm(q_exact[b, h]) * np.linalg.norm(K[:, h // 4], axis=1).max() * D ** -0.5
+                tol = (2 * dz + 1e-4) * np.abs(V).max() + HALF["bf16"] * np.abs(ref)
+                assert (np.abs(out[b, h] - ref) <= tol).all()
+            if lens[b] <= 4 * page:
+                assert (few[b] == out[b]).all()
+    assert c.kv.error_flags() == 0
+
+
+def test_calls_in_captured_graphs_and_on_other_streams(m):
+    """Two graphs that share a handle, replayed in turn with eager calls between them, on streams that are not the current one."""
+    c = Case(m, "bf16", 8, 2, 128, 128, 16, [9000, 40, 0], seed=2, summaries=True, max_sel=16, nan_tail=False)
+    T, freq = 3, _freq(128)
+    pos = torch.tensor([8999, 39, -1], dtype=torch.int32, device="cuda")
+    xs = [_append_inputs(c, T, seed=s) for s in range(4)]
+    q, k, v = (t.clone() for t in xs[0])
+    q_out, out_a, out_b = torch.zeros_like(q), torch.zeros_like(q), torch.zeros_like(q)
+
+    def step_a():
+        m.kv_append(c.kv, c.pages, c.table, pos, q, k, v, freq, q_out=q_out)
+        m.kv_attend(c.kv, c.pages, c.table, c.len_t, q_out, c.scale, out=out_a)
+
+    def step_b():
+        m.kv_attend_blocks(c.kv, c.pages, c.table, c.len_t, q_out, c.scale, 12, out=out_b)
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step_a(), step_b()
+    torch.cuda.synchronize()
+    graphs = []
+    for step in (step_a, step_b):
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            step()
+        graphs.append(gr)
+    for x in xs + xs[:2]:
+        for t, s in zip((q, k, v), x):
+            t.copy_(s)
+        with torch.cuda.stream(side):
+            side.wait_stream(torch.cuda.default_stream())
+            for gr in graphs:
+                gr.replay()
+        side.synchronize()
+        got = [t.clone() for t in (q_out, out_a, out_b, c.k, c.v, c.lo)]
+        for t in (q_out, out_a, out_b):
+            t.zero_()
+        step_a(), step_b()
+        torch.cuda.synchronize()
+        for a, b in zip(got, (q_out, out_a, out_b, c.k, c.v, c.lo)):
+            assert (bits(a) == bits(b)).all()
+    assert c.kv.error_flags() == 0
+
+
+def test_a_decoder_layer(m):
+    """Both halves of a layer step: projections, appending, attention, then the router, the cached experts and the match."""
+    import moei_inputs as mi
+    from moei_inputs.plumbing import EPS, dev, pack_bank, pinned, rel_max_err, split_expert
+    from oracle import moei_oracle as MO
+    cfg = mi.get_config("C1")
+    L, Eh, H = cfg.L, cfg.E, cfg.H
+    Tr, _, _ = mi.eamc_traces(cfg, threads=1)
+    req = mi.make_request(cfg, 0)
+    bank = mi.expert_bank(cfg, L * Eh, threads=2)
+    desc = m.ModelDesc.from_config(cfg)
+    eamc = m.Eamc(desc, cfg.N)
+    eamc.load(Tr)
+    cache = m.Cache(desc, cfg.S, pinned(pack_bank(m, cfg, bank)))
+    cache.reset(cfg.S)
+    Hq, Hkv, D, page = 4, 2, 64, 16
+    c = Case(m, "fp32", Hq, Hkv, D, D, page, [40], seed=5)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    Wqkv = torch.randn((H, (Hq + 2 * Hkv) * D), generator=g, device="cuda") * H ** -0.5
+    Wo = torch.randn((Hq * D, H), generator=g, device="cuda") * (Hq * D) ** -0.5
+    x = dev(req.x[0, 0]).float()
+    qkv = (x @ Wqkv).view(1, -1)
+    q, k, v = (t.unflatten(1, (-1, D)) for t in qkv.split([Hq * D, Hkv * D, Hkv * D], 1))
+    kb, vb = c.k.clone(), c.v.clone()
+    q_out = m.kv_append(c.kv, c.pages, c.table, torch.tensor([39], dtype=torch.int32, device="cuda"), q, k, v, _freq(D))
+    _check_append(c, q, k, v, q_out, q_out, kb, vb, [0], [39], _freq(D), False)
+    c.q = q_out
+    out, lse = m.kv_attend(c.kv, c.pages, c.table, c.len_t, q_out, c.scale, want_lse=True)
+    c.check(out, lse, *c.oracle())
+    h = (x + (out.view(1, -1) @ Wo)[0]).contiguous()
+    d_eam, W = dev(req.prefill_eam.astype(np.int32)), mi.router_weights(cfg, 0)
+    y = torch.empty(H, dtype=torch.float32, device="cuda")
+    idx, best, _ = m.moe_decode_layer(cache, eamc, d_eam, 0, dev(W), dev(req.bias[0]), h, y)
+    ref = MO.decode_layer(Tr, req.prefill_eam.astype(np.int64).copy(), MO.ExpertCache(L, Eh, cfg.S), 0, W, req.bias[0], h.cpu().numpy(),
+                          lambda f: split_expert(cfg, bank[f]), lambda _l: [], cfg.k, bool(cfg.renorm), EPS)
+    assert idx.tolist() == ref["idx"].tolist() and best == ref["best"]
+    assert rel_max_err(y.cpu().numpy(), ref["y"]) <= 2e-4
+    cache.close()
+
+
+# ------------------------------------------------------------------------------------------------ refusals (no kernel runs)
+def test_refusals(m):
+    c = Case(m, "bf16", 4, 2, 64, 64, 16, [40, 20], seed=0, summaries=True, max_sel=3)
+    f8 = Case(m, "fp8", 4, 2, 64, 64, 16, [40], seed=0)
+    L, h = m.lib(), c.kv.h
+    P = lambda t: t.data_ptr()  # noqa: E731
+    out = torch.empty_like(c.q)
+
+    def refused(rc, text, code=-1):
+        assert rc == code and text in L.moei_last_error().decode(), (rc, L.moei_last_error())
+
+    def attend(kv=h, pages=c.pages.ref, table=P(c.table), width=c.width, lens=P(c.len_t), B=2, q=P(c.q), stride=0, scale=0.125, window=0, o=P(out)):
+        return L.kv_attend(kv, pages, table, width, lens, B, q, stride, scale, window, o, None, None)
+
+    assert attend() == 0 and attend(B=0) == 0
+    refused(attend(kv=None), "null")
+    refused(attend(table=None), "null")
+    refused(attend(lens=None), "null")
+    refused(attend(q=None), "null")
+    refused(attend(B=-1), "negative")
+    refused(attend(B=3), "max_batch")
+    refused(attend(width=0), "table of 0")
+    refused(attend(width=c.kv.max_pages + 1), "max_pages")
+    refused(attend(stride=255), "q_stride")
+    refused(attend(stride=260), "q_stride")
+    refused(attend(q=P(c.q) + 2), "16 bytes")
+    refused(attend(window=-1), "window")
+    for s in (0.0, -1.0, float("inf"), float("nan")):
+        refused(attend(scale=s), "scale")
+    C = type(c.pages.c)
+
+    def pages(**kw):
+        p = C.from_buffer_copy(c.pages.c)
+        for n, x in kw.items():
+            setattr(p, n, x)
+        return p
+
+    import ctypes
+    for kw, text in ((dict(d_k=0), "null pages"), (dict(n_pages=0), "n_pages"), (dict(k_stride=2047), "strides"), (dict(d_v=P(c.v) + 8), "16 bytes"),
+                     (dict(v_stride=2050), "16 bytes"), (dict(d_k_min=0), "go together")):
+        p = pages(**kw)
+        refused(attend(pages=ctypes.addressof(p)), text)
+    p = type(f8.pages.c).from_buffer_copy(f8.pages.c)
+    p.d_k_scale = 0
+    refused(L.kv_attend(f8.kv.h, ctypes.addressof(p), P(f8.table), f8.width, P(f8.len_t), 1, P(f8.q), 0, 0.125, 0, P(out), None, None), "d_k_scale")
+
+    def blocks(pages=c.pages.ref, n_sel=3, first=1, last=1):
+        return L.kv_attend_blocks(h, pages, P(c.table), c.width, P(c.len_t), 2, P(c.q), 0, 0.125, n_sel, first, last, P(out), None, None, None)
+
+    assert blocks() == 0
+    refused(blocks(n_sel=0), "n_sel")
+    refused(blocks(n_sel=4), "max_sel")
+    refused(blocks(last=0), "keep_last")
+    refused(blocks(first=-1), "keep_first")
+    refused(blocks(first=2, last=2), "must fit")
+    p = pages(d_k_min=0, d_k_max=0)
+    refused(blocks(pages=ctypes.addressof(p)), "no d_k_min")
+    q, k, v = _append_inputs(c, 2, seed=0)
+    pos, freq, qo = torch.tensor([-1, -1], dtype=torch.int32, device="cuda"), _freq(64), torch.empty_like(q)
+
+    def append(T=2, B=2, seq=None, pos=P(pos), q=P(q), qs=0, ks=0, vs=0, freq=P(freq), rot=64, qo=P(qo)):
+        return L.kv_append(h, c.pages.ref, P(c.table), c.width, B, seq, pos, T, q, qs, P(k), ks, P(v), vs, freq, rot, 0, qo, None)
+
+    assert append() == 0 and append(T=0) == 0
+    refused(append(T=-1), "negative")
+    refused(append(T=3), "need d_seq")
+    refused(append(B=3), "max_batch")
+    refused(append(pos=None), "null")
+    refused(append(qo=None), "null")
+    refused(append(freq=None), "d_inv_freq")
+    refused(append(rot=65), "rot_dim")
+    refused(append(rot=66), "rot_dim")
+    refused(append(rot=-2), "rot_dim")
+    refused(append(qs=100), "strides")
+    refused(append(ks=100), "strides")
+    refused(append(vs=100), "strides")
+    refused(append(q=P(q) + 1), "aligned")
+    torch.cuda.synchronize()
+    assert c.kv.error_flags() == 0
+    with pytest.raises(AssertionError):
+        m.kv_attend(c.kv, c.pages, c.table, c.len_t, c.q.transpose(1, 2).contiguous().transpose(1, 2), 0.125)
+    with pytest.raises(AssertionError):
+        m.KvPages(c.kv, c.k.transpose(1, 2), c.v)
+    with pytest.raises(AssertionError):
+        m.kv_attend(c.kv, c.pages, c.table.long(), c.len_t, c.q, 0.125)
