@@ -62,7 +62,6 @@ enum KernelId {
     K_KV_APPEND,
     K_KV_SUMMARY,
     K_KV_ATTEND,
-    K_KV_JOIN,
     K_KV_SCORE,
     K_KV_SELECT,
     K_COUNT

@@ -274,8 +274,7 @@ int fill_attend(const char* who, const moei_kv* kv, const moei_kv_pages* p, cons
     a->scale2 = scale * 1.4426950408889634f;
     a->part = kv->d_part;
     a->stat = kv->d_stat;
-    a->n_target = kv->n_target;
-    a->min_chunk = 64;
+    a->arrived = kv->d_arrived;
     a->flags = kv->d_flags;
     return MOEI_OK;
 }
@@ -290,7 +289,7 @@ extern "C" int moei_kv_destroy(moei_kv* kv) {
     if (!kv) return MOEI_OK;
     int dev = -1;
     const bool other = hipGetDevice(&dev) == hipSuccess && dev != kv->device && hipSetDevice(kv->device) == hipSuccess;
-    for (void* p : {(void*)kv->d_part, (void*)kv->d_stat, (void*)kv->d_keys, (void*)kv->d_list, (void*)kv->d_flags})
+    for (void* p : {(void*)kv->d_part, (void*)kv->d_stat, (void*)kv->d_arrived, (void*)kv->d_keys, (void*)kv->d_list, (void*)kv->d_flags})
         if (p) (void)hipFree(p);
     if (other) (void)hipSetDevice(dev);
     delete kv;
@@ -322,11 +321,11 @@ extern "C" int moei_kv_create(const moei_kv_desc* desc, moei_kv** out) {
     }
     const int group = d.n_q_heads / d.n_kv_heads;
     kv->rows = group < kKvHeads ? group : kKvHeads;
-    kv->n_target = 2 * kv->cus;
-    const size_t rows = (size_t)2 * kv->n_target * kv->rows, sel = d.max_sel ? (size_t)d.max_batch * d.n_kv_heads : 0;
+    const size_t groups = (size_t)kKvResident * kv->cus, rows = 2 * groups * kv->rows, sel = d.max_sel ? (size_t)d.max_batch * d.n_kv_heads : 0;
     auto room = [&](auto*& p, size_t n) { return n == 0 || (e = hipMalloc(reinterpret_cast<void**>(&p), n * sizeof(*p))) == hipSuccess; };
-    if (!room(kv->d_part, rows * d.v_dim) || !room(kv->d_stat, rows * 2) || !room(kv->d_keys, sel * d.max_pages) ||
+    if (!room(kv->d_part, rows * d.v_dim) || !room(kv->d_stat, rows * 2) || !room(kv->d_arrived, groups) || !room(kv->d_keys, sel * d.max_pages) ||
         !room(kv->d_list, sel * d.max_sel) || !room(kv->d_flags, 1) || (e = hipMemset(kv->d_flags, 0, 4)) != hipSuccess ||
+        (e = hipMemset(kv->d_arrived, 0, groups * sizeof(unsigned))) != hipSuccess ||
         (e = hipDeviceSynchronize()) != hipSuccess) {
         (void)hipGetLastError();
         moei_kv_destroy(kv);

@@ -9,6 +9,7 @@ constexpr int kKvHeads = 16;     // query heads of a group that share one pass o
 constexpr int kKvMaxDim = 256;   // widest head
 constexpr int kKvMaxPage = 256;  // tokens of the largest page
 constexpr int kKvMaxBatch = 4096;
+constexpr int kKvResident = 4;   // workgroups of the attention that a compute unit holds, at most
 
 // error flag bits (moei_kv_error_flags)
 constexpr int kKvBadPage = 1, kKvBadLength = 2;
@@ -36,9 +37,9 @@ struct KvAttendArgs {
     const int32_t* list;     // [B][n_kv][n_sel] pages to attend to, ascending; null: all
     int n_sel;
     float scale2;            // softmax scale times log2(e)
-    float* part;             // [2 * n_target][rows][v_dim] sums of chunks, not yet divided
-    float* stat;             // [2 * n_target][rows][2] their maximum and sum
-    int n_target, min_chunk; // chunks that the plan aims at; tokens of the smallest
+    float* part;             // [workgroups][2][rows][v_dim] sums of parts of an item, not yet divided
+    float* stat;             // [workgroups][2][rows][2] their maximum and sum
+    unsigned* arrived;       // [workgroups] parts that are there, of the item that begins in a workgroup's stretch; zero between launches
     int32_t* flags;
 };
 
@@ -61,10 +62,10 @@ struct moei_kv {
     moei_kv_desc d{};
     int device = 0;
     int cus = 0;
-    int rows = 0;      // query heads of a partial result
-    int n_target = 0;  // chunks that the plan aims at; as many partial results again have room
+    int rows = 0;  // query heads of a partial result
     float* d_part = nullptr;
     float* d_stat = nullptr;
+    unsigned* d_arrived = nullptr;
     unsigned long long* d_keys = nullptr;
     int32_t* d_list = nullptr;
     int32_t* d_flags = nullptr;

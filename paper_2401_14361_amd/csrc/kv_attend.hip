@@ -21,17 +21,16 @@ constexpr int kWaves = 4;  // of a workgroup; each has a state of its own and ev
 constexpr int kRows = 16;  // keys of a subtile: the rows of a matrix instruction; a page holds whole ones
 
 // ------------------------------------------------------------------------------------------------ the plan
-// The tokens of all (sequence, key/value head, block of heads) are cut into chunks of equal length, a workgroup each: about n_target
-// of them, whatever the lengths, and one at least for every item.  Nobody but the device knows the lengths, so every
-// workgroup works the plan out for itself.
+// An item is a (sequence, key/value head, block of query heads); its tokens are units of a tile for each wavefront.  All units stand in a
+// line, sequence by sequence and item by item, and every workgroup takes an equal stretch of it: it ends with the others whatever the
+// lengths are, and works through the items that begin or end inside its stretch one by one.  Nobody but the device knows the
+// lengths, so every workgroup works out for itself where its stretch begins.
 struct Span {
-    int begin, end, start;  // tokens [begin, end) of the (listed) sequence; chunks are counted from `start`, a whole subtile
+    int begin, end, start;  // tokens [begin, end) of the (listed) sequence; units are counted from `start`, a whole subtile
 };
 
-__device__ __forceinline__ Span span_of(const KvAttendArgs& a, int b, bool& bad) {
-    int len = ((kv_const_ints)(uintptr_t)a.lens)[b];
+__device__ __forceinline__ Span span_of(const KvAttendArgs& a, int len) {
     const long long room = (long long)a.width << a.page_shift;
-    bad = len < 0 || len > room;
     len = len < 0 ? 0 : len > room ? (int)room : len;
     Span s{0, len, 0};
     if (a.list) {
@@ -43,68 +42,61 @@ __device__ __forceinline__ Span span_of(const KvAttendArgs& a, int b, bool& bad)
     }
     return s;
 }
-
-__device__ __forceinline__ int span_tokens(const KvAttendArgs& a, int b) {  // per lane
-    int len = a.lens[b];
-    const long long room = (long long)a.width << a.page_shift;
-    len = len < 0 ? 0 : len > room ? (int)room : len;
-    if (a.list) {
-        const int nb = (len + (1 << a.page_shift) - 1) >> a.page_shift;
-        return nb > a.n_sel ? len - ((nb - a.n_sel) << a.page_shift) : len;
-    }
-    return a.window > 0 && len > a.window ? len - ((len - a.window) & ~(kRows - 1)) : len;
-}
-
-struct Plan {
-    int chunk;  // tokens
-    int b;      // the sequence that `want` falls into, -1: none
-    int first;  // its first chunk's number
-    int parts;  // chunks of one of its items
-    int slot;   // number of its first partial result
-};
+template <int kUnit>
+__device__ __forceinline__ int units_of(const Span& s) { return max(1, (s.end - s.start + kUnit - 1) / kUnit); }  // (an empty one has its zeros to write)
 
 // inclusive sum over the lanes
-__device__ __forceinline__ int lane_scan(int v, int lane) {
-#pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
-        const int up = __shfl_up(v, off, kWave);
-        if (lane >= off) v += up;
-    }
+__device__ __forceinline__ unsigned lane_scan(unsigned v) {
+#define MOEI_DPP_ADD(ctrl, rows) v += (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, rows, 0xF, false)
+    MOEI_DPP_ADD(0x111, 0xF);  // row_shr 1, 2, 4, 8: inside rows of sixteen lanes
+    MOEI_DPP_ADD(0x112, 0xF);
+    MOEI_DPP_ADD(0x114, 0xF);
+    MOEI_DPP_ADD(0x118, 0xF);
+    MOEI_DPP_ADD(0x142, 0xA);  // the rows before
+    MOEI_DPP_ADD(0x143, 0xC);
+#undef MOEI_DPP_ADD
     return v;
 }
 
-// by_chunk: `want` is a chunk's number, else a sequence's.
-template <bool by_chunk>
-__device__ __forceinline__ Plan make_plan(const KvAttendArgs& a, int want, int lane) {
-    const int items = a.n_kv * a.blocks_of_heads;
-    unsigned long long total = 0;
-    for (int b0 = 0; b0 < a.B; b0 += kWave) total += wave_sum_u64(b0 + lane < a.B ? (unsigned long long)span_tokens(a, b0 + lane) : 0ull);
-    const unsigned long long even = min((total * items + a.n_target - 1) / a.n_target, 1ull << 30);
-    Plan p;
-    p.chunk = __builtin_amdgcn_readfirstlane((max((int)even, a.min_chunk) + kWaves * kRows - 1) & -(kWaves * kRows));
-    p.b = -1;
-    p.first = p.parts = p.slot = 0;
-    int first = 0, slot = 0;
+struct Stretch {
+    unsigned per;         // units of a workgroup
+    unsigned first, end;  // this one's, in the line
+    int b;                // the sequence in which it begins
+    unsigned base;        // and its first unit in the line
+};
+
+template <int kUnit>
+__device__ __forceinline__ Stretch my_stretch(const KvAttendArgs& a, int lane) {
+    const unsigned items = a.n_kv * a.blocks_of_heads;
+    unsigned total = 0, upto = 0, mine = 0;
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
-        const int b = b0 + lane;
-        const int n = b < a.B ? span_tokens(a, b) : 0;
-        const int parts = b < a.B ? max(1, (int)(((unsigned)n + (unsigned)p.chunk - 1) / (unsigned)p.chunk)) : 0;
-        const int mine = parts * items, mine_slots = parts > 1 ? mine : 0;
-        const int upto = lane_scan(mine, lane), upto_slots = lane_scan(mine_slots, lane);
-        const bool here = b < a.B && (by_chunk ? want >= first + upto - mine && want < first + upto : b == want);
-        const unsigned long long who = __ballot(here);
+        mine = b0 + lane < a.B ? units_of<kUnit>(span_of(a, a.lens[b0 + lane])) * items : 0u;
+        upto = total + lane_scan(mine);
+        total = __builtin_amdgcn_readlane(upto, kWave - 1);
+    }
+    Stretch s;
+    s.per = (total + gridDim.x - 1) / gridDim.x;
+    s.first = blockIdx.x * s.per;
+    s.end = min(s.first + s.per, total);
+    s.b = -1;
+    s.base = 0;
+    if (s.first >= s.end) return s;
+    unsigned before = 0;
+    for (int b0 = 0; b0 < a.B; b0 += kWave) {
+        if (a.B > kWave) {
+            mine = b0 + lane < a.B ? units_of<kUnit>(span_of(a, a.lens[b0 + lane])) * items : 0u;
+            upto = before + lane_scan(mine);
+            before = __builtin_amdgcn_readlane(upto, kWave - 1);
+        }
+        const unsigned long long who = __ballot(upto > s.first && upto - mine <= s.first);
         if (who) {
             const int l = __builtin_ctzll(who);
-            p.b = b0 + l;
-            p.first = first + __builtin_amdgcn_readlane(upto - mine, l);
-            p.parts = __builtin_amdgcn_readlane(parts, l);
-            p.slot = slot + __builtin_amdgcn_readlane(upto_slots - mine_slots, l);
+            s.b = b0 + l;
+            s.base = __builtin_amdgcn_readlane(upto - mine, l);
             break;
         }
-        first += __builtin_amdgcn_readlane(upto, kWave - 1);
-        slot += __builtin_amdgcn_readlane(upto_slots, kWave - 1);
     }
-    return p;
+    return s;
 }
 
 // ------------------------------------------------------------------------------------------------ types
@@ -165,10 +157,48 @@ __device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi) {
     return r;
 }
 
-// ------------------------------------------------------------------------------------------------ one chunk
+// Sums of a head's weighted values and of its weights, relative to exponents of m.
+struct Sums {
+    float m, l;
+    f32x4 o;
+    __device__ __forceinline__ void raise(float to) {
+        if (m == to) return;  // (of nothing: m is -inf, and l and o are zero)
+        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - to);
+        m = to;
+        l *= f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] *= f;
+    }
+    __device__ __forceinline__ void add(float pm, float pl, f32x4 po) {  // pm <= m
+        if (pm == -INFINITY) return;
+        const float f = __builtin_amdgcn_exp2f(pm - m);
+        l = __builtin_fmaf(f, pl, l);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[i] = __builtin_fmaf(f, po[i], o[i]);
+    }
+};
+__device__ __forceinline__ void store_past(unsigned long long* p, float x, float y) {
+    __hip_atomic_store(p, (unsigned long long)__float_as_uint(y) << 32 | __float_as_uint(x), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+__device__ __forceinline__ float2 load_past(const unsigned long long* p) {
+    const unsigned long long v = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    return make_float2(__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32)));
+}
+template <typename io>
+__device__ __forceinline__ void write_out(const KvAttendArgs& a, long long head, int d, int hk, const Sums& r) {
+    const float f = r.m == -INFINITY ? 0.f : (a.v_scale ? a.v_scale[hk] : 1.f) / r.l;
+    if constexpr (sizeof(io) == 2)
+        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + head * a.v_dim + d) = make_uint2(pack_bf16(r.o[0] * f, r.o[1] * f), pack_bf16(r.o[2] * f, r.o[3] * f));
+    else
+        *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + head * a.v_dim + d) = r.o * f;
+    if (d == 0 && a.lse) a.lse[head] = r.m == -INFINITY ? -INFINITY : (r.m + log2f(r.l)) * 0.69314718055994531f;
+}
+
+// ------------------------------------------------------------------------------------------------ a stretch of units
 template <typename T, int KC, int VC, int NS>
 struct Shape {
     static constexpr int kTile = T::kSub * kRows;                       // keys
+    static constexpr int kUnit = kWaves * kTile;
     static constexpr int kPiecesK = KC * T::kBytes / 16, kPiecesV = VC * T::kBytes / 16;  // 16-byte pieces of a row
     static constexpr int kLoadsK = kTile * kPiecesK / kWave, kLoadsV = kTile * kPiecesV / kWave;  // instructions that bring a tile
     static constexpr int kTileK = kTile * KC * T::kBytes, kTileV = kTile * VC * T::kBytes;        // bytes
@@ -177,6 +207,7 @@ struct Shape {
     static constexpr int kOutRow = VC + 4;  // floats of a row of the workgroup's sums in LDS: rows begin in different banks
     static constexpr int kMerge = kWaves * kKvHeads * (kOutRow + 2) * 4;
     static constexpr int kLds = kWaves * kRing > kMerge ? kWaves * kRing : kMerge;
+    static constexpr int kResident = kLds <= 40 * 1024 ? 4 : kLds <= 80 * 1024 ? 2 : 1;  // workgroups of a compute unit
     static_assert(kTile * kPiecesK % kWave == 0 && kTile * kPiecesV % kWave == 0, "whole instructions");
 };
 
@@ -191,7 +222,7 @@ __device__ __forceinline__ void wait_stage(int rest) {
 }
 
 template <typename T, int KC, int VC, int NS>
-__global__ void __launch_bounds__(kWaves * kWave) kv_attend_kernel(KvAttendArgs a) {
+__global__ void __launch_bounds__(kWaves * kWave, (Shape<T, KC, VC, NS>::kResident)) kv_attend_kernel(KvAttendArgs a) {
     using S = Shape<T, KC, VC, NS>;
     typedef typename T::io io;
     constexpr int kUnits = KC * T::kBytes / 64;  // of 64 bytes of a key: a 16-byte piece for each of the four lane groups
@@ -201,30 +232,9 @@ __global__ void __launch_bounds__(kWaves * kWave) kv_attend_kernel(KvAttendArgs 
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int col = lane & 15, grp = lane >> 4;
 
-    const Plan p = make_plan<true>(a, blockIdx.x, lane);
-    if (p.b < 0) return;
-    bool bad_len;
-    const Span sp = span_of(a, p.b, bad_len);
-    const int items = a.n_kv * a.blocks_of_heads;
-    const int local = blockIdx.x - p.first;
-    const int part = local / items, item = local - part * items;
-    const int hk = item / a.blocks_of_heads, h0 = (item - hk * a.blocks_of_heads) * kKvHeads;
-    const int heads = min(kKvHeads, a.group - h0);
-    const int c0 = sp.start + part * p.chunk, c1 = min(c0 + p.chunk, sp.end);
-    if (bad_len && local == 0 && threadIdx.x == 0) atomicOr(a.flags, kKvBadLength);
-
-    // the queries, as the second operand of the products: lane (col, grp) holds piece grp of every unit of head col
-    constexpr int kQ = T::kBytes == 1 ? 2 * kUnits : kUnits;  // 16-byte pieces
-    uint4 q[kQ];
-    {
-        const io* src = static_cast<const io*>(a.q) + (long long)p.b * a.q_stride + (long long)(hk * a.group + h0 + col) * a.k_dim;
-#pragma unroll
-        for (int u = 0; u < kQ; ++u) {
-            const int d = T::kBytes == 1 ? (u >> 1) * 64 + grp * 16 + (u & 1) * 8 : T::kBytes == 2 ? u * 32 + grp * 8 : u * 16 + grp * 4;
-            q[u] = make_uint4(0u, 0u, 0u, 0u);
-            if (col < heads && d < a.k_dim) q[u] = *reinterpret_cast<const uint4*>(src + d);
-        }
-    }
+    const Stretch mine_of = my_stretch<S::kUnit>(a, lane);
+    if (mine_of.b < 0) return;
+    const unsigned items = a.n_kv * a.blocks_of_heads;
 
     // where a lane's pieces of a tile come from, behind the subtile's first byte
     uint32_t off_k[S::kLoadsK / T::kSub], off_v[S::kLoadsV];
@@ -241,11 +251,39 @@ __global__ void __launch_bounds__(kWaves * kWave) kv_attend_kernel(KvAttendArgs 
         off_v[i] = (row % kRows) * a.v_dim * T::kBytes + (piece * 16 < a.v_dim * T::kBytes ? piece * 16 : 0);
     }
 
+    int b = mine_of.b;
+    unsigned base = mine_of.base;  // of the sequence, in the line
+    unsigned at_unit = mine_of.first;
+    do {
+    const int len = ((kv_const_ints)(uintptr_t)a.lens)[b];
+    const Span sp = span_of(a, len);
+    const unsigned units = units_of<S::kUnit>(sp);
+    const unsigned item = (at_unit - base) / units, u0 = at_unit - base - item * units;
+    const unsigned u1 = min(units, u0 + (mine_of.end - at_unit));
+    const unsigned item_first = base + item * units;  // the item's first unit in the line
+    const int hk = item / a.blocks_of_heads, h0 = (item - hk * a.blocks_of_heads) * kKvHeads;
+    const int heads = min(kKvHeads, a.group - h0);
+    const int c0 = sp.start + u0 * S::kUnit, c1 = min(sp.start + (int)u1 * S::kUnit, sp.end);
+    if (item == 0 && u0 == 0 && threadIdx.x == 0 && (len < 0 || len > (long long)a.width << a.page_shift)) atomicOr(a.flags, kKvBadLength);
+
+    // the queries, as the second operand of the products: lane (col, grp) holds piece grp of every unit of head col
+    constexpr int kQ = T::kBytes == 1 ? 2 * kUnits : kUnits;  // 16-byte pieces
+    uint4 q[kQ];
+    {
+        const io* src = static_cast<const io*>(a.q) + (long long)b * a.q_stride + (long long)(hk * a.group + h0 + col) * a.k_dim;
+#pragma unroll
+        for (int u = 0; u < kQ; ++u) {
+            const int d = T::kBytes == 1 ? (u >> 1) * 64 + grp * 16 + (u & 1) * 8 : T::kBytes == 2 ? u * 32 + grp * 8 : u * 16 + grp * 4;
+            q[u] = make_uint4(0u, 0u, 0u, 0u);
+            if (col < heads && d < a.k_dim) q[u] = *reinterpret_cast<const uint4*>(src + d);
+        }
+    }
+
     const uint32_t ring = lds_address(smem) + wv * S::kRing;
     const int n_tiles = c1 > c0 ? (c1 - c0 + S::kTile - 1) / S::kTile : 0;
     const int mine = n_tiles > wv ? (n_tiles - wv + kWaves - 1) / kWaves : 0;
-    const kv_const_ints table = (kv_const_ints)(uintptr_t)(a.table + (long long)p.b * a.width);
-    const kv_const_ints list = (kv_const_ints)(uintptr_t)(a.list ? a.list + ((long long)p.b * a.n_kv + hk) * a.n_sel : nullptr);
+    const kv_const_ints table = (kv_const_ints)(uintptr_t)(a.table + (long long)b * a.width);
+    const kv_const_ints list = (kv_const_ints)(uintptr_t)(a.list ? a.list + ((long long)b * a.n_kv + hk) * a.n_sel : nullptr);
     const long long head_k = (long long)hk * a.k_dim << a.page_shift, head_v = (long long)hk * a.v_dim << a.page_shift;
     const int in_page = (1 << a.page_shift) - 1;
 
@@ -460,102 +498,105 @@ __global__ void __launch_bounds__(kWaves * kWave) kv_attend_kernel(KvAttendArgs 
         }
     }
     __syncthreads();
-    const long long head0 = (long long)p.b * a.n_kv * a.group + hk * a.group + h0;
-    const int quads = a.v_dim / 4;
-    const long long slot = p.slot + local;
+    const long long head0 = (long long)b * a.n_kv * a.group + hk * a.group + h0;
+    const int quads = a.v_dim / 4, cols = heads * quads;
+    const bool whole = u0 == 0 && u1 == units;
     const int rows = min(kKvHeads, a.group);
-    const float v_scale = a.v_scale ? a.v_scale[hk] : 1.f;
-    for (int n = threadIdx.x; n < heads * quads; n += kWaves * kWave) {
+    const unsigned w0 = item_first / mine_of.per;  // the workgroup in whose stretch the item begins
+    // A workgroup leaves two partial results at most: of an item that began before its stretch and of one that ends behind it.
+    auto slot_of = [&](unsigned w) -> long long { return (2ll * w + (w == w0 ? 1 : 0)) * rows; };
+    for (int n = threadIdx.x; n < cols; n += kWaves * kWave) {
         const int h = n / quads, d = (n - h * quads) * 4;
-        float m = -INFINITY;
+        Sums r{-INFINITY, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) m = fmaxf(m, stat[(w * kKvHeads + h) * 2]);
-        float l = 0.f;
-        f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int w = 0; w < kWaves; ++w) r.m = fmaxf(r.m, stat[(w * kKvHeads + h) * 2]);
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const float mw = stat[(w * kKvHeads + h) * 2];
-            const float f = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - m);
-            l = __builtin_fmaf(f, stat[(w * kKvHeads + h) * 2 + 1], l);
-            const f32x4 x = *reinterpret_cast<const f32x4*>(out + (w * kKvHeads + h) * S::kOutRow + d);
-            if (mw != -INFINITY)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[i] = __builtin_fmaf(f, x[i], o[i]);
+        for (int w = 0; w < kWaves; ++w)
+            r.add(stat[(w * kKvHeads + h) * 2], stat[(w * kKvHeads + h) * 2 + 1], *reinterpret_cast<const f32x4*>(out + (w * kKvHeads + h) * S::kOutRow + d));
+        if (whole) {
+            write_out<io>(a, head0 + h, d, hk, r);
+        } else {  // past the caches: another workgroup, on another die, may read it before this launch ends
+            const long long row = slot_of(blockIdx.x) + h;
+            unsigned long long* to = reinterpret_cast<unsigned long long*>(a.part + row * a.v_dim + d);
+            store_past(to, r.o[0], r.o[1]);
+            store_past(to + 1, r.o[2], r.o[3]);
+            if (d == 0) store_past(reinterpret_cast<unsigned long long*>(a.stat) + row, r.m, r.l);
         }
-        if (p.parts > 1) {
-            *reinterpret_cast<f32x4*>(a.part + (slot * rows + h) * a.v_dim + d) = o;
-            if (d == 0) {
-                a.stat[(slot * rows + h) * 2] = m;
-                a.stat[(slot * rows + h) * 2 + 1] = l;
+    }
+    if (!whole) {
+        int* last = reinterpret_cast<int*>(smem + 8192);  // behind what the join below uses
+        const unsigned w1 = (item_first + units - 1) / mine_of.per, parts = w1 - w0 + 1;
+        wait_vm_fence<0>();  // the partial result has arrived before it is counted
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            const unsigned n = __hip_atomic_fetch_add(&a.arrived[w0], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            *last = n == parts - 1;
+            if (*last) __hip_atomic_store(&a.arrived[w0], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // for the next launch
+        }
+        __syncthreads();
+        if (*last) {  // the last of the item's workgroups joins the parts, in their order in the line
+            const int lanes = cols < kWaves * kWave ? cols : kWaves * kWave, groups = kWaves * kWave / lanes;
+            float* sh = reinterpret_cast<float*>(smem);  // [groups][lanes][6]
+            for (int c = 0; c < cols; c += lanes) {
+                const int g = threadIdx.x / lanes, i = threadIdx.x - g * lanes, n = c + i;
+                Sums r{-INFINITY, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
+                const int h = n / quads, d = (n - h * quads) * 4;
+                const bool here = g < groups && n < cols;
+                if (here) {
+                    constexpr int kAhead = 8;
+                    for (unsigned p0 = g; p0 < parts; p0 += kAhead * groups) {
+                        float2 ps[kAhead], lo[kAhead], hi[kAhead];
+                        float m = r.m;
+#pragma unroll
+                        for (int j = 0; j < kAhead; ++j) {
+                            const unsigned p = min(p0 + j * groups, parts - 1);
+                            const long long row = slot_of(w0 + p) + h;
+                            const unsigned long long* from = reinterpret_cast<const unsigned long long*>(a.part + row * a.v_dim + d);
+                            ps[j] = load_past(reinterpret_cast<const unsigned long long*>(a.stat) + row);
+                            lo[j] = load_past(from);
+                            hi[j] = load_past(from + 1);
+                        }
+#pragma unroll
+                        for (int j = 0; j < kAhead; ++j)
+                            if (p0 + j * groups < parts) m = fmaxf(m, ps[j].x);
+                        r.raise(m);
+#pragma unroll
+                        for (int j = 0; j < kAhead; ++j)
+                            if (p0 + j * groups < parts) r.add(ps[j].x, ps[j].y, f32x4{lo[j].x, lo[j].y, hi[j].x, hi[j].y});
+                    }
+                }
+                if (groups > 1) {
+                    float* mine = sh + threadIdx.x * 6;
+                    if (here) {
+                        mine[0] = r.m; mine[1] = r.l;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) mine[2 + j] = r.o[j];
+                    }
+                    __syncthreads();
+                    if (here && g == 0)
+                        for (int k = 1; k < groups; ++k) {
+                            const float* x = sh + (k * lanes + i) * 6;
+                            r.raise(fmaxf(r.m, x[0]));
+                            r.add(x[0], x[1], f32x4{x[2], x[3], x[4], x[5]});
+                        }
+                }
+                if (here && g == 0) write_out<io>(a, head0 + h, d, hk, r);
             }
-        } else {
-            const float div = m == -INFINITY ? 0.f : v_scale / l;
-            if constexpr (sizeof(io) == 2)
-                *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + (head0 + h) * a.v_dim + d) =
-                    make_uint2(pack_bf16(o[0] * div, o[1] * div), pack_bf16(o[2] * div, o[3] * div));
-            else
-                *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + (head0 + h) * a.v_dim + d) = o * div;
-            if (d == 0 && a.lse) a.lse[head0 + h] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
         }
     }
-}
-
-// ------------------------------------------------------------------------------------------------ the chunks of an item joined
-// A workgroup a query head; its wavefronts take the chunks in turn, a lane up to four output columns.
-template <typename io>
-__global__ void __launch_bounds__(kWaves * kWave) kv_join_kernel(KvAttendArgs a) {
-    const int lane = threadIdx.x & (kWave - 1);
-    const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    const int n_q = a.n_kv * a.group;
-    const int b = blockIdx.x / n_q, hq = blockIdx.x - b * n_q;
-    const Plan p = make_plan<false>(a, b, lane);
-    if (p.parts < 2) return;
-    const int items = a.n_kv * a.blocks_of_heads, rows = min(kKvHeads, a.group);
-    const int hk = hq / a.group, in_group = hq - hk * a.group;
-    const int item = hk * a.blocks_of_heads + in_group / kKvHeads, row = in_group % kKvHeads;
-    auto at = [&](int part) -> long long { return ((long long)p.slot + (long long)part * items + item) * rows + row; };
-    float m = -INFINITY;
-    for (int i = lane; i < p.parts; i += kWave) m = fmaxf(m, a.stat[at(i) * 2]);
-    m = wave_max(m);
-    const int d = lane * 4;
-    float l = 0.f;
-    f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int i = wv; i < p.parts; i += kWaves) {
-        const float mi = a.stat[at(i) * 2];
-        const float f = mi == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mi - m);
-        l = __builtin_fmaf(f, a.stat[at(i) * 2 + 1], l);
-        if (d < a.v_dim && mi != -INFINITY) {
-            const f32x4 x = *reinterpret_cast<const f32x4*>(a.part + at(i) * a.v_dim + d);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) o[j] = __builtin_fmaf(f, x[j], o[j]);
-        }
+    at_unit = item_first + u1;
+    if (item + 1 == items && u1 == units) {
+        base += items * units;
+        ++b;
     }
-    __shared__ f32x4 s_o[kWaves][kWave];
-    __shared__ float s_l[kWaves];
-    s_o[wv][lane] = o;
-    if (lane == 0) s_l[wv] = l;
-    __syncthreads();
-    if (wv) return;
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) {
-        o += s_o[w][lane];
-        l += s_l[w];
-    }
-    const float div = m == -INFINITY ? 0.f : (a.v_scale ? a.v_scale[hk] : 1.f) / l;
-    const long long head = (long long)b * n_q + hq;
-    if (d < a.v_dim) {
-        if constexpr (sizeof(io) == 2)
-            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + head * a.v_dim + d) = make_uint2(pack_bf16(o[0] * div, o[1] * div), pack_bf16(o[2] * div, o[3] * div));
-        else
-            *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + head * a.v_dim + d) = o * div;
-    }
-    if (lane == 0 && a.lse) a.lse[head] = m == -INFINITY ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+    if (at_unit < mine_of.end) __syncthreads();  // what the joins read in LDS is the next item's ring
+    } while (at_unit < mine_of.end);
 }
 
 LdsLimits<64> g_limits;
 
 template <typename T, int KC, int VC>
-int launch_shape(const KvAttendArgs& a, hipStream_t s) {
+int launch_shape(const KvAttendArgs& a, int cus, hipStream_t s) {
     constexpr int NS = Shape<T, KC, VC, 2>::kLds <= 160 * 1024 ? 2 : 1;
     using S = Shape<T, KC, VC, NS>;
     static_assert(S::kLds <= 160 * 1024, "the rings fit a compute unit");
@@ -567,30 +608,30 @@ int launch_shape(const KvAttendArgs& a, hipStream_t s) {
         });
         if (rc) return rc;
     }
-    const int items = a.n_kv * a.blocks_of_heads;
-    launch(K_KV_ATTEND, kernel, dim3((unsigned)(a.B * items + a.n_target)), dim3(kWaves * kWave), S::kLds, s, a);
-    MOEI_LAUNCH_CHECK();
-    launch(K_KV_JOIN, kv_join_kernel<typename T::io>, dim3((unsigned)(a.B * a.n_kv * a.group)), dim3(kWaves * kWave), 0, s, a);
+    const long long units = ((long long)a.width << a.page_shift) / S::kUnit + 1, line = units * a.B * a.n_kv * a.blocks_of_heads;
+    if (line > 0x7fffffffll) MOEI_FAIL(MOEI_ECAPACITY, "kv_attend: %d sequences of up to %lld tokens are more than one call takes", a.B, (long long)a.width << a.page_shift);
+    const int grid = cus * S::kResident;
+    launch(K_KV_ATTEND, kernel, dim3((unsigned)(line < grid ? line : grid)), dim3(kWaves * kWave), S::kLds, s, a);
     MOEI_LAUNCH_CHECK();
     return MOEI_OK;
 }
 
 // Heads are padded in LDS to the next of four widths; the classes are the pairs in use, others round both widths up.
 template <typename T>
-int launch_type(const KvAttendArgs& a, hipStream_t s) {
-    if (a.k_dim <= 64 && a.v_dim <= 64) return launch_shape<T, 64, 64>(a, s);
-    if (a.k_dim <= 128 && a.v_dim <= 128) return launch_shape<T, 128, 128>(a, s);
-    if (a.k_dim <= 192 && a.v_dim <= 128) return launch_shape<T, 192, 128>(a, s);
-    return launch_shape<T, 256, 256>(a, s);
+int launch_type(const KvAttendArgs& a, int cus, hipStream_t s) {
+    if (a.k_dim <= 64 && a.v_dim <= 64) return launch_shape<T, 64, 64>(a, cus, s);
+    if (a.k_dim <= 128 && a.v_dim <= 128) return launch_shape<T, 128, 128>(a, cus, s);
+    if (a.k_dim <= 192 && a.v_dim <= 128) return launch_shape<T, 192, 128>(a, cus, s);
+    return launch_shape<T, 256, 256>(a, cus, s);
 }
 
 }  // namespace
 
 int launch_kv_attend(const moei_kv& kv, const KvAttendArgs& a, hipStream_t s) {
     switch (kv.d.dtype) {
-        case MOEI_WDTYPE_FP32: return launch_type<Fp32>(a, s);
-        case MOEI_WDTYPE_BF16: return launch_type<Bf16>(a, s);
-        default: return launch_type<Fp8>(a, s);
+        case MOEI_WDTYPE_FP32: return launch_type<Fp32>(a, kv.cus, s);
+        case MOEI_WDTYPE_BF16: return launch_type<Bf16>(a, kv.cus, s);
+        default: return launch_type<Fp8>(a, kv.cus, s);
     }
 }
 
