@@ -477,7 +477,8 @@ class Kv:
         self.max_batch, self.max_pages = max_batch, max_pages
         self.h = C.c_void_p(0)
         _check(lib().moei_kv_create(C.byref(self.desc), C.byref(self.h)))
-        self.device = torch.device("cuda", torch.cuda.current_device())
+        self.index = torch.cuda.current_device()
+        self.device = torch.device("cuda", self.index)
         self.page_dtype = self._PAGE[dtype]
         self.dtype = torch.float32 if dtype == "fp32" else torch.bfloat16  # of queries, new keys and values, outputs, summaries
         self.k_page = (n_kv_heads, page_size, k_dim)
@@ -528,6 +529,11 @@ class KvPages:
         self.ref = C.addressof(self.c)
 
 
+def _kv_stream(kv: Kv, stream) -> int:
+    """The raw stream of a call: the device's current one by its number alone (a Stream object costs 3 us)."""
+    return torch._C._cuda_getCurrentRawStream(kv.index) if stream is None else _stream(stream).value
+
+
 def _rows(kv: Kv, t: torch.Tensor, n: int, heads: tuple) -> int:
     """Checks [n][heads][width] with dense tokens and returns the elements between tokens."""
     assert t.device == kv.device and t.dtype == kv.dtype and tuple(t.shape) == (n, *heads), (t.device, t.dtype, t.shape, (n, *heads))
@@ -557,7 +563,7 @@ def kv_append(kv: Kv, pages: KvPages, table: torch.Tensor, pos: torch.Tensor, q:
                            q.data_ptr(), _rows(kv, q, T, kv.heads), k.data_ptr(), _rows(kv, k, T, (kv.k_page[0], kv.k_page[2])),
                            v.data_ptr(), _rows(kv, v, T, (kv.v_page[0], kv.v_page[2])),
                            None if inv_freq is None else inv_freq.data_ptr(), 0 if inv_freq is None else 2 * inv_freq.numel(),
-                           interleaved, q_out.data_ptr(), _stream(stream)))
+                           interleaved, q_out.data_ptr(), _kv_stream(kv, stream)))
     return q_out
 
 
@@ -576,7 +582,7 @@ def kv_attend(kv: Kv, pages: KvPages, table: torch.Tensor, lens: torch.Tensor, q
     B = q.shape[0]
     out, lse = _attend_outputs(kv, B, table, lens, out, want_lse)
     _check(lib().kv_attend(kv.h, pages.ref, _ints(kv, table), table.shape[1], _ints(kv, lens), B, q.data_ptr(), _rows(kv, q, B, kv.heads),
-                           scale, window, out.data_ptr(), lse.data_ptr() if want_lse else None, _stream(stream)))
+                           scale, window, out.data_ptr(), lse.data_ptr() if want_lse else None, _kv_stream(kv, stream)))
     return (out, lse) if want_lse else out
 
 
@@ -590,7 +596,7 @@ def kv_attend_blocks(kv: Kv, pages: KvPages, table: torch.Tensor, lens: torch.Te
     blocks = torch.empty((B, kv.k_page[0], max(n_sel, 0)), dtype=torch.int32, device=kv.device) if want_blocks else None
     _check(lib().kv_attend_blocks(kv.h, pages.ref, _ints(kv, table), table.shape[1], _ints(kv, lens), B, q.data_ptr(),
                                   _rows(kv, q, B, kv.heads), scale, n_sel, keep_first, keep_last, out.data_ptr(),
-                                  lse.data_ptr() if want_lse else None, blocks.data_ptr() if want_blocks else None, _stream(stream)))
+                                  lse.data_ptr() if want_lse else None, blocks.data_ptr() if want_blocks else None, _kv_stream(kv, stream)))
     got = (out,) + ((lse,) if want_lse else ()) + ((blocks,) if want_blocks else ())
     return got if len(got) > 1 else out
 

@@ -62,8 +62,7 @@ enum KernelId {
     K_KV_APPEND,
     K_KV_SUMMARY,
     K_KV_ATTEND,
-    K_KV_SCORE,
-    K_KV_SELECT,
+    K_KV_BLOCKS,
     K_COUNT
 };
 extern bool g_prof_on;

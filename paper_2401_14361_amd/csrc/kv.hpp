@@ -51,7 +51,9 @@ struct KvBlocksArgs {
     const int32_t* table;
     const int32_t* lens;
     int B, n_kv, group, k_dim, width, page_shift, n_pages, n_sel, keep_first, keep_last;
+    int per;                   // pages of a workgroup
     unsigned long long* keys;  // [B][n_kv][width] scratch
+    unsigned* arrived;         // [B][n_kv] workgroups whose keys are there; zero between launches
     int32_t* list;             // [B][n_kv][n_sel] out
     int32_t* flags;
 };
@@ -67,6 +69,7 @@ struct moei_kv {
     float* d_stat = nullptr;
     unsigned* d_arrived = nullptr;
     unsigned long long* d_keys = nullptr;
+    unsigned* d_scored = nullptr;
     int32_t* d_list = nullptr;
     int32_t* d_flags = nullptr;
 };
@@ -74,7 +77,7 @@ struct moei_kv {
 namespace moei {
 
 int launch_kv_attend(const moei_kv& kv, const KvAttendArgs& a, hipStream_t s);
-int launch_kv_blocks(const moei_kv& kv, const KvBlocksArgs& a, hipStream_t s);
+int launch_kv_blocks(const moei_kv& kv, KvBlocksArgs a, hipStream_t s);
 
 #if defined(__HIPCC__)
 

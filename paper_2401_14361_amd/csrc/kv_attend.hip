@@ -17,7 +17,6 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kWaves = 4;  // of a workgroup; each has a state of its own and every fourth tile
 constexpr int kRows = 16;  // keys of a subtile: the rows of a matrix instruction; a page holds whole ones
 
 // ------------------------------------------------------------------------------------------------ the plan
@@ -62,15 +61,18 @@ struct Stretch {
     unsigned per;         // units of a workgroup
     unsigned first, end;  // this one's, in the line
     int b;                // the sequence in which it begins
-    unsigned base;        // and its first unit in the line
+    unsigned base;        // its first unit in the line
+    int len;              // and its length
 };
 
 template <int kUnit>
 __device__ __forceinline__ Stretch my_stretch(const KvAttendArgs& a, int lane) {
     const unsigned items = a.n_kv * a.blocks_of_heads;
     unsigned total = 0, upto = 0, mine = 0;
+    int len = 0;
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
-        mine = b0 + lane < a.B ? units_of<kUnit>(span_of(a, a.lens[b0 + lane])) * items : 0u;
+        len = b0 + lane < a.B ? a.lens[b0 + lane] : 0;
+        mine = b0 + lane < a.B ? units_of<kUnit>(span_of(a, len)) * items : 0u;
         upto = total + lane_scan(mine);
         total = __builtin_amdgcn_readlane(upto, kWave - 1);
     }
@@ -80,11 +82,13 @@ __device__ __forceinline__ Stretch my_stretch(const KvAttendArgs& a, int lane) {
     s.end = min(s.first + s.per, total);
     s.b = -1;
     s.base = 0;
+    s.len = 0;
     if (s.first >= s.end) return s;
     unsigned before = 0;
     for (int b0 = 0; b0 < a.B; b0 += kWave) {
         if (a.B > kWave) {
-            mine = b0 + lane < a.B ? units_of<kUnit>(span_of(a, a.lens[b0 + lane])) * items : 0u;
+            len = b0 + lane < a.B ? a.lens[b0 + lane] : 0;
+            mine = b0 + lane < a.B ? units_of<kUnit>(span_of(a, len)) * items : 0u;
             upto = before + lane_scan(mine);
             before = __builtin_amdgcn_readlane(upto, kWave - 1);
         }
@@ -93,6 +97,7 @@ __device__ __forceinline__ Stretch my_stretch(const KvAttendArgs& a, int lane) {
             const int l = __builtin_ctzll(who);
             s.b = b0 + l;
             s.base = __builtin_amdgcn_readlane(upto - mine, l);
+            s.len = __builtin_amdgcn_readlane(len, l);
             break;
         }
     }
@@ -195,8 +200,9 @@ __device__ __forceinline__ void write_out(const KvAttendArgs& a, long long head,
 }
 
 // ------------------------------------------------------------------------------------------------ a stretch of units
-template <typename T, int KC, int VC, int NS>
+template <typename T, int KC, int VC, int NS, int NW>
 struct Shape {
+    static constexpr int kWaves = NW;  // of a workgroup; each has a state of its own and takes the tiles in turn with the others
     static constexpr int kTile = T::kSub * kRows;                       // keys
     static constexpr int kUnit = kWaves * kTile;
     static constexpr int kPiecesK = KC * T::kBytes / 16, kPiecesV = VC * T::kBytes / 16;  // 16-byte pieces of a row
@@ -221,9 +227,10 @@ __device__ __forceinline__ void wait_stage(int rest) {
     wait_vm_fence<EXTRA>();
 }
 
-template <typename T, int KC, int VC, int NS>
-__global__ void __launch_bounds__(kWaves * kWave, (Shape<T, KC, VC, NS>::kResident)) kv_attend_kernel(KvAttendArgs a) {
-    using S = Shape<T, KC, VC, NS>;
+template <typename T, int KC, int VC, int NS, int NW>
+__global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kResident * NW / 4)) kv_attend_kernel(KvAttendArgs a) {
+    using S = Shape<T, KC, VC, NS, NW>;
+    constexpr int kWaves = NW;
     typedef typename T::io io;
     constexpr int kUnits = KC * T::kBytes / 64;  // of 64 bytes of a key: a 16-byte piece for each of the four lane groups
     constexpr int kOut = VC / 16;                // tiles of sixteen output columns
@@ -255,7 +262,7 @@ __global__ void __launch_bounds__(kWaves * kWave, (Shape<T, KC, VC, NS>::kReside
     unsigned base = mine_of.base;  // of the sequence, in the line
     unsigned at_unit = mine_of.first;
     do {
-    const int len = ((kv_const_ints)(uintptr_t)a.lens)[b];
+    const int len = b == mine_of.b ? mine_of.len : ((kv_const_ints)(uintptr_t)a.lens)[b];
     const Span sp = span_of(a, len);
     const unsigned units = units_of<S::kUnit>(sp);
     const unsigned item = (at_unit - base) / units, u0 = at_unit - base - item * units;
@@ -595,12 +602,13 @@ __global__ void __launch_bounds__(kWaves * kWave, (Shape<T, KC, VC, NS>::kReside
 
 LdsLimits<64> g_limits;
 
-template <typename T, int KC, int VC>
+template <typename T, int KC, int VC, int NWX>
 int launch_shape(const KvAttendArgs& a, int cus, hipStream_t s) {
-    constexpr int NS = Shape<T, KC, VC, 2>::kLds <= 160 * 1024 ? 2 : 1;
-    using S = Shape<T, KC, VC, NS>;
+    constexpr int NW = NWX;
+    constexpr int NS = Shape<T, KC, VC, 2, NW>::kLds <= 160 * 1024 ? 2 : 1;
+    using S = Shape<T, KC, VC, NS, NW>;
     static_assert(S::kLds <= 160 * 1024, "the rings fit a compute unit");
-    const auto kernel = kv_attend_kernel<T, KC, VC, NS>;
+    const auto kernel = kv_attend_kernel<T, KC, VC, NS, NW>;
     if (S::kLds > 64 * 1024) {
         const int rc = g_limits.at_least(reinterpret_cast<const void*>(kernel), S::kLds, [&]() -> int {
             MOEI_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds));
@@ -611,7 +619,7 @@ int launch_shape(const KvAttendArgs& a, int cus, hipStream_t s) {
     const long long units = ((long long)a.width << a.page_shift) / S::kUnit + 1, line = units * a.B * a.n_kv * a.blocks_of_heads;
     if (line > 0x7fffffffll) MOEI_FAIL(MOEI_ECAPACITY, "kv_attend: %d sequences of up to %lld tokens are more than one call takes", a.B, (long long)a.width << a.page_shift);
     const int grid = cus * S::kResident;
-    launch(K_KV_ATTEND, kernel, dim3((unsigned)(line < grid ? line : grid)), dim3(kWaves * kWave), S::kLds, s, a);
+    launch(K_KV_ATTEND, kernel, dim3((unsigned)(line < grid ? line : grid)), dim3(NW * kWave), S::kLds, s, a);
     MOEI_LAUNCH_CHECK();
     return MOEI_OK;
 }
@@ -619,10 +627,10 @@ int launch_shape(const KvAttendArgs& a, int cus, hipStream_t s) {
 // Heads are padded in LDS to the next of four widths; the classes are the pairs in use, others round both widths up.
 template <typename T>
 int launch_type(const KvAttendArgs& a, int cus, hipStream_t s) {
-    if (a.k_dim <= 64 && a.v_dim <= 64) return launch_shape<T, 64, 64>(a, cus, s);
-    if (a.k_dim <= 128 && a.v_dim <= 128) return launch_shape<T, 128, 128>(a, cus, s);
-    if (a.k_dim <= 192 && a.v_dim <= 128) return launch_shape<T, 192, 128>(a, cus, s);
-    return launch_shape<T, 256, 256>(a, cus, s);
+    if (a.k_dim <= 64 && a.v_dim <= 64) return launch_shape<T, 64, 64, 8>(a, cus, s);
+    if (a.k_dim <= 128 && a.v_dim <= 128) return launch_shape<T, 128, 128, (T::kBytes == 4 ? 4 : 8)>(a, cus, s);
+    if (a.k_dim <= 192 && a.v_dim <= 128) return launch_shape<T, 192, 128, (T::kBytes == 4 ? 4 : 8)>(a, cus, s);
+    return launch_shape<T, 256, 256, 4>(a, cus, s);
 }
 
 }  // namespace
