@@ -166,17 +166,7 @@ __device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi) {
 struct Sums {
     float m, l;
     f32x4 o;
-    __device__ __forceinline__ void raise(float to) {
-        if (m == to) return;  // (of nothing: m is -inf, and l and o are zero)
-        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - to);
-        m = to;
-        l *= f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[i] *= f;
-    }
-    __device__ __forceinline__ void add(float pm, float pl, f32x4 po) {  // pm <= m
-        if (pm == -INFINITY) return;
-        const float f = __builtin_amdgcn_exp2f(pm - m);
+    __device__ __forceinline__ void add(float f, float pl, f32x4 po) {
         l = __builtin_fmaf(f, pl, l);
 #pragma unroll
         for (int i = 0; i < 4; ++i) o[i] = __builtin_fmaf(f, po[i], o[i]);
@@ -294,30 +284,20 @@ __global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kReside
     const long long head_k = (long long)hk * a.k_dim << a.page_shift, head_v = (long long)hk * a.v_dim << a.page_shift;
     const int in_page = (1 << a.page_shift) - 1;
 
-    // the page of a tile's subtile, -1: none
+    // the page of a tile's subtile (past the last one: the last one's again)
     auto page_of = [&](int k, int st) -> int {
-        const int tok = c0 + (wv + k * kWaves) * S::kTile + st * kRows;
-        if (tok >= c1) return -1;
-        int at = tok >> a.page_shift;
-        if (a.list) {
-            at = list[at];
-            if (at < 0 || at >= a.width) return -1;
-        }
-        const int pg = table[at];
-        return pg;
+        int at = min(c0 + (wv + k * kWaves) * S::kTile + st * kRows, c1 - 1) >> a.page_shift;
+        if (a.list) at = list[at];
+        return table[min((unsigned)at, (unsigned)a.width - 1u)];
     };
     int next[T::kSub];
     unsigned gone = 0;  // a bit per stage and subtile: its page is none of the pool's
     const unsigned char *src_k[T::kSub], *src_v[T::kSub];
-    auto look_up = [&](int k) {
-#pragma unroll
-        for (int st = 0; st < T::kSub; ++st) next[st] = k < mine ? page_of(k, st) : -1;
-    };
-    auto place = [&](int k, int stage) {
+    auto place = [&](int k, int stage, const int (&pages)[T::kSub]) {
 #pragma unroll
         for (int st = 0; st < T::kSub; ++st) {
             const int tok = c0 + (wv + k * kWaves) * S::kTile + st * kRows;
-            int pg = next[st];
+            int pg = pages[st];
             const bool ok = pg >= 0 && pg < a.n_pages;
             const unsigned bit = 1u << (stage * T::kSub + st);
             gone = ok ? gone & ~bit : gone | bit;
@@ -325,7 +305,7 @@ __global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kReside
             const long long row = tok & in_page;
             src_k[st] = a.k + ((long long)pg * a.k_stride + head_k + row * a.k_dim) * T::kBytes;
             src_v[st] = a.v + ((long long)pg * a.v_stride + head_v + row * a.v_dim) * T::kBytes;
-            if (!ok && tok < c1) {
+            if (!ok) {
                 if (lane == 0) atomicOr(a.flags, kKvBadPage);
                 wait_vm_fence<0>();  // the waits below count loads, which need not stay in order with an atomic
             }
@@ -351,15 +331,29 @@ __global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kReside
     for (int t = 0; t < kOut; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
     const float scale2 = a.k_scale ? a.scale2 * a.k_scale[hk] : a.scale2;
 
-    look_up(0);
-    for (int k = 0; k < NS && k < mine; ++k) {
-        place(k, k);
-        look_up(k + 1);
-        bring_k(k);
-        bring_v(k);
+    if (mine > 0) {
+        int pages[NS][T::kSub];
+#pragma unroll
+        for (int k = 0; k < NS; ++k)
+#pragma unroll
+            for (int st = 0; st < T::kSub; ++st) pages[k][st] = page_of(k, st);
+#pragma unroll
+        for (int st = 0; st < T::kSub; ++st) next[st] = page_of(NS, st);
+#pragma unroll
+        for (int k = 0; k < NS; ++k)
+            if (k < mine) {
+                place(k, k, pages[k]);
+                bring_k(k);
+                bring_v(k);
+            }
     }
     int stage = 0;
+    const int together = n_tiles / kWaves;  // steps that every wavefront has
     for (int k = 0; k < mine; ++k) {
+        // The wavefronts step together: the first four, which a compute unit prefers, would end a seventh earlier than the others, and leave
+        // them with half as many bytes under way (one sequence of 131,072 tokens 88 -> 85 us).
+        if constexpr (kWaves > 4)
+            if (k < together) __builtin_amdgcn_s_barrier();
         const int rest = min(mine - 1 - k, NS - 1);  // stages under way behind this one
         const bool more = k + NS < mine;
         const uint32_t at_k = ring + stage * S::kStage, at_v = at_k + S::kTileK;
@@ -390,9 +384,10 @@ __global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kReside
         }
         if (more) {
             wait_lds_fence();
-            place(k + NS, stage);
-            look_up(k + NS + 1);
+            place(k + NS, stage, next);
             bring_k(stage);
+#pragma unroll
+            for (int st = 0; st < T::kSub; ++st) next[st] = page_of(k + NS + 1, st);
         }
 
         // lane (col, grp) holds the logits of head col with keys 4 grp + r of every subtile
@@ -494,14 +489,15 @@ __global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kReside
     // the wavefronts' sums, joined in LDS
     __syncthreads();  // the rings are read
     float* out = reinterpret_cast<float*>(smem);                              // [kWaves][kKvHeads][kOutRow]
-    float* stat = out + kWaves * kKvHeads * S::kOutRow;                        // [kWaves][kKvHeads][2]
+    float* s_m = out + kWaves * kKvHeads * S::kOutRow;                         // [kKvHeads][kWaves] maxima
+    float* s_l = s_m + kWaves * kKvHeads;                                      // and sums
     if (col < heads) {
 #pragma unroll
         for (int t = 0; t < kOut; ++t)
             *reinterpret_cast<f32x4*>(out + (wv * kKvHeads + col) * S::kOutRow + t * 16 + grp * 4) = acc[t];
         if (grp == 0) {
-            stat[(wv * kKvHeads + col) * 2] = top;
-            stat[(wv * kKvHeads + col) * 2 + 1] = sum;
+            s_m[col * kWaves + wv] = top;
+            s_l[col * kWaves + wv] = sum;
         }
     }
     __syncthreads();
@@ -511,27 +507,31 @@ __global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kReside
     const int rows = min(kKvHeads, a.group);
     const unsigned w0 = item_first / mine_of.per;  // the workgroup in whose stretch the item begins
     // A workgroup leaves two partial results at most: of an item that began before its stretch and of one that ends behind it.
-    auto slot_of = [&](unsigned w) -> long long { return (2ll * w + (w == w0 ? 1 : 0)) * rows; };
+    auto slot_of = [&](unsigned w) -> unsigned { return (2 * w + (w == w0 ? 1 : 0)) * rows; };
     for (int n = threadIdx.x; n < cols; n += kWaves * kWave) {
         const int h = n / quads, d = (n - h * quads) * 4;
         Sums r{-INFINITY, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
+        float f[kWaves];
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) r.m = fmaxf(r.m, stat[(w * kKvHeads + h) * 2]);
+        for (int w = 0; w < kWaves; ++w) r.m = fmaxf(r.m, f[w] = s_m[h * kWaves + w]);
+        const float from = r.m == -INFINITY ? 0.f : r.m;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w)
-            r.add(stat[(w * kKvHeads + h) * 2], stat[(w * kKvHeads + h) * 2 + 1], *reinterpret_cast<const f32x4*>(out + (w * kKvHeads + h) * S::kOutRow + d));
+        for (int w = 0; w < kWaves; ++w) {  // (a wavefront without a tile has -inf, and zeros)
+            f[w] = __builtin_amdgcn_exp2f(f[w] - from);
+            r.add(f[w], s_l[h * kWaves + w], *reinterpret_cast<const f32x4*>(out + (w * kKvHeads + h) * S::kOutRow + d));
+        }
         if (whole) {
             write_out<io>(a, head0 + h, d, hk, r);
         } else {  // past the caches: another workgroup, on another die, may read it before this launch ends
-            const long long row = slot_of(blockIdx.x) + h;
-            unsigned long long* to = reinterpret_cast<unsigned long long*>(a.part + row * a.v_dim + d);
+            const unsigned row = slot_of(blockIdx.x) + h;
+            unsigned long long* to = reinterpret_cast<unsigned long long*>(a.part + (row * a.v_dim + d));
             store_past(to, r.o[0], r.o[1]);
             store_past(to + 1, r.o[2], r.o[3]);
             if (d == 0) store_past(reinterpret_cast<unsigned long long*>(a.stat) + row, r.m, r.l);
         }
     }
     if (!whole) {
-        int* last = reinterpret_cast<int*>(smem + 8192);  // behind what the join below uses
+        int* last = reinterpret_cast<int*>(smem + 16384);  // behind what the join below uses
         const unsigned w1 = (item_first + units - 1) / mine_of.per, parts = w1 - w0 + 1;
         wait_vm_fence<0>();  // the partial result has arrived before it is counted
         __syncthreads();
@@ -550,42 +550,50 @@ __global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kReside
                 const int h = n / quads, d = (n - h * quads) * 4;
                 const bool here = g < groups && n < cols;
                 if (here) {
-                    constexpr int kAhead = 8;
+                    constexpr unsigned kAhead = 8;  // parts under way
                     for (unsigned p0 = g; p0 < parts; p0 += kAhead * groups) {
                         float2 ps[kAhead], lo[kAhead], hi[kAhead];
-                        float m = r.m;
 #pragma unroll
-                        for (int j = 0; j < kAhead; ++j) {
-                            const unsigned p = min(p0 + j * groups, parts - 1);
-                            const long long row = slot_of(w0 + p) + h;
-                            const unsigned long long* from = reinterpret_cast<const unsigned long long*>(a.part + row * a.v_dim + d);
+                        for (unsigned j = 0; j < kAhead; ++j) {
+                            const unsigned row = slot_of(w0 + min(p0 + j * groups, parts - 1)) + h;
+                            const unsigned long long* from = reinterpret_cast<const unsigned long long*>(a.part + (row * a.v_dim + d));
                             ps[j] = load_past(reinterpret_cast<const unsigned long long*>(a.stat) + row);
                             lo[j] = load_past(from);
                             hi[j] = load_past(from + 1);
                         }
+                        float m = r.m;
 #pragma unroll
-                        for (int j = 0; j < kAhead; ++j)
-                            if (p0 + j * groups < parts) m = fmaxf(m, ps[j].x);
-                        r.raise(m);
+                        for (unsigned j = 0; j < kAhead; ++j) m = fmaxf(m, ps[j].x);
+                        const float from = m == -INFINITY ? 0.f : m, fade = __builtin_amdgcn_exp2f(r.m - from);
+                        r.m = m;
+                        r.l *= fade;
+                        r.o *= fade;
 #pragma unroll
-                        for (int j = 0; j < kAhead; ++j)
-                            if (p0 + j * groups < parts) r.add(ps[j].x, ps[j].y, f32x4{lo[j].x, lo[j].y, hi[j].x, hi[j].y});
+                        for (unsigned j = 0; j < kAhead; ++j)
+                            r.add(p0 + j * groups < parts ? __builtin_amdgcn_exp2f(ps[j].x - from) : 0.f, ps[j].y, f32x4{lo[j].x, lo[j].y, hi[j].x, hi[j].y});
                     }
                 }
-                if (groups > 1) {
-                    float* mine = sh + threadIdx.x * 6;
+                if (groups > 1) {  // the groups' sums, by columns: [groups][6][lanes]
                     if (here) {
-                        mine[0] = r.m; mine[1] = r.l;
+                        float* mine = sh + g * 6 * lanes + i;
+                        mine[0] = r.m;
+                        mine[lanes] = r.l;
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) mine[2 + j] = r.o[j];
+                        for (int j = 0; j < 4; ++j) mine[(2 + j) * lanes] = r.o[j];
                     }
                     __syncthreads();
-                    if (here && g == 0)
+                    if (here && g == 0) {
+                        float m = r.m;
+                        for (int k = 1; k < groups; ++k) m = fmaxf(m, sh[k * 6 * lanes + i]);
+                        const float from = m == -INFINITY ? 0.f : m, fade = __builtin_amdgcn_exp2f(r.m - from);
+                        r.m = m;
+                        r.l *= fade;
+                        r.o *= fade;
                         for (int k = 1; k < groups; ++k) {
-                            const float* x = sh + (k * lanes + i) * 6;
-                            r.raise(fmaxf(r.m, x[0]));
-                            r.add(x[0], x[1], f32x4{x[2], x[3], x[4], x[5]});
+                            const float* x = sh + k * 6 * lanes + i;
+                            r.add(__builtin_amdgcn_exp2f(x[0] - from), x[lanes], f32x4{x[2 * lanes], x[3 * lanes], x[4 * lanes], x[5 * lanes]});
                         }
+                    }
                 }
                 if (here && g == 0) write_out<io>(a, head0 + h, d, hk, r);
             }
