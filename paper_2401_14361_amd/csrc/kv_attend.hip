@@ -17,6 +17,14 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef int i32x2 __attribute__((ext_vector_type(2)));
 
+// The arguments are read where they are used: held from the start they would be 60 scalar registers more than there are, moved to lanes and
+// back at every phase.  (A launch runs most of its code once, from memory: 2 KB a microsecond.)
+typedef const __attribute__((address_space(4))) KvAttendArgs* Args;
+__device__ __forceinline__ Args again(Args p) {
+    asm volatile("" : "+s"(p));
+    return p;
+}
+
 constexpr int kRows = 16;  // keys of a subtile: the rows of a matrix instruction; a page holds whole ones
 
 // ------------------------------------------------------------------------------------------------ the plan
@@ -28,15 +36,16 @@ struct Span {
     int begin, end, start;  // tokens [begin, end) of the (listed) sequence; units are counted from `start`, a whole subtile
 };
 
-__device__ __forceinline__ Span span_of(const KvAttendArgs& a, int len) {
-    const long long room = (long long)a.width << a.page_shift;
+template <typename A>
+__device__ __forceinline__ Span span_of(A a, int len) {
+    const long long room = (long long)a->width << a->page_shift;
     len = len < 0 ? 0 : len > room ? (int)room : len;
     Span s{0, len, 0};
-    if (a.list) {
-        const int nb = (len + (1 << a.page_shift) - 1) >> a.page_shift;
-        if (nb > a.n_sel) s.end = len - ((nb - a.n_sel) << a.page_shift);  // the last page, whole or not, is always listed
-    } else if (a.window > 0 && len > a.window) {
-        s.begin = len - a.window;
+    if (a->list) {
+        const int nb = (len + (1 << a->page_shift) - 1) >> a->page_shift;
+        if (nb > a->n_sel) s.end = len - ((nb - a->n_sel) << a->page_shift);  // the last page, whole or not, is always listed
+    } else if (a->window > 0 && len > a->window) {
+        s.begin = len - a->window;
         s.start = s.begin & ~(kRows - 1);
     }
     return s;
@@ -66,13 +75,13 @@ struct Stretch {
 };
 
 template <int kUnit>
-__device__ __forceinline__ Stretch my_stretch(const KvAttendArgs& a, int lane) {
-    const unsigned items = a.n_kv * a.blocks_of_heads;
+__device__ __forceinline__ Stretch my_stretch(Args a, int lane) {
+    const unsigned items = a->n_kv * a->blocks_of_heads;
     unsigned total = 0, upto = 0, mine = 0;
     int len = 0;
-    for (int b0 = 0; b0 < a.B; b0 += kWave) {
-        len = b0 + lane < a.B ? a.lens[b0 + lane] : 0;
-        mine = b0 + lane < a.B ? units_of<kUnit>(span_of(a, len)) * items : 0u;
+    for (int b0 = 0; b0 < a->B; b0 += kWave) {
+        len = b0 + lane < a->B ? a->lens[b0 + lane] : 0;
+        mine = b0 + lane < a->B ? units_of<kUnit>(span_of(a, len)) * items : 0u;
         upto = total + lane_scan(mine);
         total = __builtin_amdgcn_readlane(upto, kWave - 1);
     }
@@ -85,10 +94,10 @@ __device__ __forceinline__ Stretch my_stretch(const KvAttendArgs& a, int lane) {
     s.len = 0;
     if (s.first >= s.end) return s;
     unsigned before = 0;
-    for (int b0 = 0; b0 < a.B; b0 += kWave) {
-        if (a.B > kWave) {
-            len = b0 + lane < a.B ? a.lens[b0 + lane] : 0;
-            mine = b0 + lane < a.B ? units_of<kUnit>(span_of(a, len)) * items : 0u;
+    for (int b0 = 0; b0 < a->B; b0 += kWave) {
+        if (a->B > kWave) {
+            len = b0 + lane < a->B ? a->lens[b0 + lane] : 0;
+            mine = b0 + lane < a->B ? units_of<kUnit>(span_of(a, len)) * items : 0u;
             upto = before + lane_scan(mine);
             before = __builtin_amdgcn_readlane(upto, kWave - 1);
         }
@@ -179,15 +188,6 @@ __device__ __forceinline__ float2 load_past(const unsigned long long* p) {
     const unsigned long long v = __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     return make_float2(__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32)));
 }
-template <typename io>
-__device__ __forceinline__ void write_out(const KvAttendArgs& a, long long head, int d, int hk, const Sums& r) {
-    const float f = r.m == -INFINITY ? 0.f : (a.v_scale ? a.v_scale[hk] : 1.f) / r.l;
-    if constexpr (sizeof(io) == 2)
-        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(a.out) + head * a.v_dim + d) = make_uint2(pack_bf16(r.o[0] * f, r.o[1] * f), pack_bf16(r.o[2] * f, r.o[3] * f));
-    else
-        *reinterpret_cast<f32x4*>(static_cast<float*>(a.out) + head * a.v_dim + d) = r.o * f;
-    if (d == 0 && a.lse) a.lse[head] = r.m == -INFINITY ? -INFINITY : (r.m + log2f(r.l)) * 0.69314718055994531f;
-}
 
 // ------------------------------------------------------------------------------------------------ a stretch of units
 template <typename T, int KC, int VC, int NS, int NW>
@@ -218,7 +218,7 @@ __device__ __forceinline__ void wait_stage(int rest) {
 }
 
 template <typename T, int KC, int VC, int NS, int NW>
-__global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kResident * NW / 4)) kv_attend_kernel(KvAttendArgs a) {
+__global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kResident * NW / 4)) kv_attend_kernel(KvAttendArgs) {
     using S = Shape<T, KC, VC, NS, NW>;
     constexpr int kWaves = NW;
     typedef typename T::io io;
@@ -228,383 +228,389 @@ __global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kReside
     const int lane = threadIdx.x & (kWave - 1);
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int col = lane & 15, grp = lane >> 4;
+    Args a = (Args)__builtin_amdgcn_kernarg_segment_ptr();
 
     const Stretch mine_of = my_stretch<S::kUnit>(a, lane);
     if (mine_of.b < 0) return;
-    const unsigned items = a.n_kv * a.blocks_of_heads;
 
     // where a lane's pieces of a tile come from, behind the subtile's first byte
+    a = again(a);
     uint32_t off_k[S::kLoadsK / T::kSub], off_v[S::kLoadsV];
+    {
+        const int k_row = a->k_dim * T::kBytes, v_row = a->v_dim * T::kBytes;
 #pragma unroll
-    for (int i = 0; i < S::kLoadsK / T::kSub; ++i) {
-        const int n = i * kWave + lane, row = n / S::kPiecesK, at = n % S::kPiecesK;
-        const int piece = at ^ k_key(row, S::kPiecesK);
-        off_k[i] = row * a.k_dim * T::kBytes + (piece * 16 < a.k_dim * T::kBytes ? piece * 16 : 0);  // (past the row: any valid piece, the query is zero there)
-    }
+        for (int i = 0; i < S::kLoadsK / T::kSub; ++i) {
+            const int n = i * kWave + lane, row = n / S::kPiecesK, at = n % S::kPiecesK;
+            const int piece = (at ^ k_key(row, S::kPiecesK)) * 16;
+            off_k[i] = row * k_row + (piece < k_row ? piece : 0);  // (past the row: any valid piece, the query is zero there)
+        }
 #pragma unroll
-    for (int i = 0; i < S::kLoadsV; ++i) {
-        const int n = i * kWave + lane, row = n / S::kPiecesV, at = n % S::kPiecesV;
-        const int piece = at ^ v_key<T>(row, S::kPiecesV);
-        off_v[i] = (row % kRows) * a.v_dim * T::kBytes + (piece * 16 < a.v_dim * T::kBytes ? piece * 16 : 0);
+        for (int i = 0; i < S::kLoadsV; ++i) {
+            const int n = i * kWave + lane, row = n / S::kPiecesV, at = n % S::kPiecesV;
+            const int piece = (at ^ v_key<T>(row, S::kPiecesV)) * 16;
+            off_v[i] = (row % kRows) * v_row + (piece < v_row ? piece : 0);
+        }
     }
 
     int b = mine_of.b;
     unsigned base = mine_of.base;  // of the sequence, in the line
     unsigned at_unit = mine_of.first;
     do {
-    const int len = b == mine_of.b ? mine_of.len : ((kv_const_ints)(uintptr_t)a.lens)[b];
-    const Span sp = span_of(a, len);
-    const unsigned units = units_of<S::kUnit>(sp);
-    const unsigned item = (at_unit - base) / units, u0 = at_unit - base - item * units;
-    const unsigned u1 = min(units, u0 + (mine_of.end - at_unit));
-    const unsigned item_first = base + item * units;  // the item's first unit in the line
-    const int hk = item / a.blocks_of_heads, h0 = (item - hk * a.blocks_of_heads) * kKvHeads;
-    const int heads = min(kKvHeads, a.group - h0);
-    const int c0 = sp.start + u0 * S::kUnit, c1 = min(sp.start + (int)u1 * S::kUnit, sp.end);
-    if (item == 0 && u0 == 0 && threadIdx.x == 0 && (len < 0 || len > (long long)a.width << a.page_shift)) atomicOr(a.flags, kKvBadLength);
-
-    // the queries, as the second operand of the products: lane (col, grp) holds piece grp of every unit of head col
-    constexpr int kQ = T::kBytes == 1 ? 2 * kUnits : kUnits;  // 16-byte pieces
-    uint4 q[kQ];
-    {
-        const io* src = static_cast<const io*>(a.q) + (long long)b * a.q_stride + (long long)(hk * a.group + h0 + col) * a.k_dim;
-#pragma unroll
-        for (int u = 0; u < kQ; ++u) {
-            const int d = T::kBytes == 1 ? (u >> 1) * 64 + grp * 16 + (u & 1) * 8 : T::kBytes == 2 ? u * 32 + grp * 8 : u * 16 + grp * 4;
-            q[u] = make_uint4(0u, 0u, 0u, 0u);
-            if (col < heads && d < a.k_dim) q[u] = *reinterpret_cast<const uint4*>(src + d);
+        a = again(a);
+        const int len = b == mine_of.b ? mine_of.len : ((kv_const_ints)(uintptr_t)a->lens)[b];
+        const Span sp = span_of(a, len);
+        const unsigned units = units_of<S::kUnit>(sp);
+        const unsigned item = (at_unit - base) / units, u0 = at_unit - base - item * units;
+        const unsigned u1 = min(units, u0 + (mine_of.end - at_unit));
+        const unsigned item_first = base + item * units;  // the item's first unit in the line
+        int hk = item, h0 = 0;
+        if (a->blocks_of_heads > 1) {
+            hk = item / a->blocks_of_heads;
+            h0 = (item - hk * a->blocks_of_heads) * kKvHeads;
         }
-    }
+        const int heads = min(kKvHeads, a->group - h0);
+        const int c0 = sp.start + u0 * S::kUnit, c1 = min(sp.start + (int)u1 * S::kUnit, sp.end);
+        if (item == 0 && u0 == 0 && (len < 0 || len > (long long)a->width << a->page_shift) && threadIdx.x == 0) atomicOr(a->flags, kKvBadLength);
 
-    const uint32_t ring = lds_address(smem) + wv * S::kRing;
-    const int n_tiles = c1 > c0 ? (c1 - c0 + S::kTile - 1) / S::kTile : 0;
-    const int mine = n_tiles > wv ? (n_tiles - wv + kWaves - 1) / kWaves : 0;
-    const kv_const_ints table = (kv_const_ints)(uintptr_t)(a.table + (long long)b * a.width);
-    const kv_const_ints list = (kv_const_ints)(uintptr_t)(a.list ? a.list + ((long long)b * a.n_kv + hk) * a.n_sel : nullptr);
-    const long long head_k = (long long)hk * a.k_dim << a.page_shift, head_v = (long long)hk * a.v_dim << a.page_shift;
-    const int in_page = (1 << a.page_shift) - 1;
+        const uint32_t ring = lds_address(smem) + wv * S::kRing;
+        const int n_tiles = c1 > c0 ? (c1 - c0 + S::kTile - 1) / S::kTile : 0;
+        const int mine = n_tiles > wv ? (n_tiles - wv + kWaves - 1) / kWaves : 0;
+        const int page_shift = a->page_shift, last_page = a->width - 1, n_pages = a->n_pages;
+        const kv_const_ints table = (kv_const_ints)(uintptr_t)(a->table + (long long)b * a->width);
+        const kv_const_ints list = (kv_const_ints)(uintptr_t)(a->list ? a->list + ((long long)b * a->n_kv + hk) * a->n_sel : nullptr);
 
-    // the page of a tile's subtile (past the last one: the last one's again)
-    auto page_of = [&](int k, int st) -> int {
-        int at = min(c0 + (wv + k * kWaves) * S::kTile + st * kRows, c1 - 1) >> a.page_shift;
-        if (a.list) at = list[at];
-        return table[min((unsigned)at, (unsigned)a.width - 1u)];
-    };
-    int next[T::kSub];
-    unsigned gone = 0;  // a bit per stage and subtile: its page is none of the pool's
-    const unsigned char *src_k[T::kSub], *src_v[T::kSub];
-    auto place = [&](int k, int stage, const int (&pages)[T::kSub]) {
+        // the page of a tile's subtile (past the last one: the last one's again)
+        auto page_of = [&](int k, int st) -> int {
+            int at = min(c0 + (wv + k * kWaves) * S::kTile + st * kRows, c1 - 1) >> page_shift;
+            if (list) at = list[at];
+            return table[min((unsigned)at, (unsigned)last_page)];
+        };
+        int next[T::kSub], after[T::kSub];  // pages of the tiles to be brought next
+        if (mine > 0) {
 #pragma unroll
-        for (int st = 0; st < T::kSub; ++st) {
-            const int tok = c0 + (wv + k * kWaves) * S::kTile + st * kRows;
-            int pg = pages[st];
-            const bool ok = pg >= 0 && pg < a.n_pages;
-            const unsigned bit = 1u << (stage * T::kSub + st);
-            gone = ok ? gone & ~bit : gone | bit;
-            pg = ok ? pg : 0;
-            const long long row = tok & in_page;
-            src_k[st] = a.k + ((long long)pg * a.k_stride + head_k + row * a.k_dim) * T::kBytes;
-            src_v[st] = a.v + ((long long)pg * a.v_stride + head_v + row * a.v_dim) * T::kBytes;
-            if (!ok) {
-                if (lane == 0) atomicOr(a.flags, kKvBadPage);
-                wait_vm_fence<0>();  // the waits below count loads, which need not stay in order with an atomic
+            for (int st = 0; st < T::kSub; ++st) {
+                next[st] = page_of(0, st);
+                after[st] = page_of(1, st);
             }
         }
-    };
-    auto bring_k = [&](int stage) {
-        const uint32_t to = ring + stage * S::kStage;
-#pragma unroll
-        for (int i = 0; i < S::kLoadsK; ++i)
-            load16_once_to_lds_at(src_k[i / (S::kLoadsK / T::kSub)], off_k[i % (S::kLoadsK / T::kSub)], to + i * (kWave * 16));
-    };
-    auto bring_v = [&](int stage) {
-        const uint32_t to = ring + stage * S::kStage + S::kTileK;
-#pragma unroll
-        for (int i = 0; i < S::kLoadsV; ++i) {
-            load16_once_to_lds_at(src_v[i / (S::kLoadsV / T::kSub)], off_v[i], to + i * (kWave * 16));
-        }
-    };
 
-    float top = -INFINITY, sum = 0.f;  // of head col: the running maximum (of what exp2 takes) and this lane's share of the sum
-    f32x4 acc[kOut];
+        // the queries, as the second operand of the products: lane (col, grp) holds piece grp of every unit of head col
+        constexpr int kQ = T::kBytes == 1 ? 2 * kUnits : kUnits;  // 16-byte pieces
+        u32x4 q[kQ];
+        {
+            const io* src = static_cast<const io*>(a->q) + (long long)b * a->q_stride + (hk * a->group + h0 + col) * a->k_dim;
+            const int k_dim = col < heads ? a->k_dim : 0;
 #pragma unroll
-    for (int t = 0; t < kOut; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const float scale2 = a.k_scale ? a.scale2 * a.k_scale[hk] : a.scale2;
-
-    if (mine > 0) {
-        int pages[NS][T::kSub];
-#pragma unroll
-        for (int k = 0; k < NS; ++k)
-#pragma unroll
-            for (int st = 0; st < T::kSub; ++st) pages[k][st] = page_of(k, st);
-#pragma unroll
-        for (int st = 0; st < T::kSub; ++st) next[st] = page_of(NS, st);
-#pragma unroll
-        for (int k = 0; k < NS; ++k)
-            if (k < mine) {
-                place(k, k, pages[k]);
-                bring_k(k);
-                bring_v(k);
+            for (int u = 0; u < kQ; ++u) {
+                const int d = T::kBytes == 1 ? (u >> 1) * 64 + grp * 16 + (u & 1) * 8 : T::kBytes == 2 ? u * 32 + grp * 8 : u * 16 + grp * 4;
+                q[u] = u32x4{0u, 0u, 0u, 0u};
+                if (d < k_dim) q[u] = *reinterpret_cast<const u32x4*>(src + d);
             }
-    }
-    int stage = 0;
-    const int together = n_tiles / kWaves;  // steps that every wavefront has
-    for (int k = 0; k < mine; ++k) {
-        // The wavefronts step together: the first four, which a compute unit prefers, would end a seventh earlier than the others, and leave
-        // them with half as many bytes under way (one sequence of 131,072 tokens 88 -> 85 us).
-        if constexpr (kWaves > 4)
-            if (k < together) __builtin_amdgcn_s_barrier();
-        const int rest = min(mine - 1 - k, NS - 1);  // stages under way behind this one
-        const bool more = k + NS < mine;
-        const uint32_t at_k = ring + stage * S::kStage, at_v = at_k + S::kTileK;
-        const int t0 = c0 + (wv + k * kWaves) * S::kTile;
-        const unsigned lost = (gone >> (stage * T::kSub)) & ((1u << T::kSub) - 1);
-        const bool edge = t0 < sp.begin || t0 + S::kTile > c1 || lost;
+        }
 
-        wait_stage<NS, S::kLoadsK + S::kLoadsV, S::kLoadsV>(rest);
-        f32x4 s[T::kSub];
+        unsigned gone = 0;  // a bit per stage and subtile: its page is none of the pool's
+        const unsigned char *src_k[T::kSub], *src_v[T::kSub];
+        const unsigned char* const head_k = a->k + ((long long)hk * a->k_dim << page_shift) * T::kBytes;
+        const unsigned char* const head_v = a->v + ((long long)hk * a->v_dim << page_shift) * T::kBytes;
+        const long long k_stride = a->k_stride * T::kBytes, v_stride = a->v_stride * T::kBytes;
+        const int k_row = a->k_dim * T::kBytes, v_row = a->v_dim * T::kBytes, in_page = (1 << page_shift) - 1;
+        auto place = [&](int k, int stage) {  // where tile k comes from, and the pages behind
 #pragma unroll
-        for (int st = 0; st < T::kSub; ++st) {
-            s[st] = f32x4{0.f, 0.f, 0.f, 0.f};
-            const uint32_t row = at_k + (st * kRows + col) * (KC * T::kBytes);
+            for (int st = 0; st < T::kSub; ++st) {
+                const int row = (c0 + (wv + k * kWaves) * S::kTile + st * kRows) & in_page;
+                int pg = next[st];
+                const unsigned bit = 1u << (stage * T::kSub + st);
+                gone &= ~bit;
+                if ((unsigned)pg >= (unsigned)n_pages) {
+                    gone |= bit;
+                    pg = 0;
+                    if (lane == 0) atomicOr(again(a)->flags, kKvBadPage);
+                    wait_vm_fence<0>();  // the waits below count loads, which need not stay in order with an atomic
+                }
+                src_k[st] = head_k + (pg * k_stride + row * k_row);
+                src_v[st] = head_v + (pg * v_stride + row * v_row);
+            }
 #pragma unroll
-            for (int u = 0; u < kUnits; ++u) {
-                const u32x4 kk = lds_16(row + (((4 * u + grp) ^ k_key(col, S::kPiecesK)) << 4));
-                if constexpr (T::kBytes == 2) {
-                    s[st] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kk), __builtin_bit_cast(bf16x8, q[u]), s[st], 0, 0, 0);
-                } else if constexpr (T::kBytes == 1) {
-                    s[st] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(kk.x, kk.y), __builtin_bit_cast(bf16x8, q[2 * u]), s[st], 0, 0, 0);
-                    s[st] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(kk.z, kk.w), __builtin_bit_cast(bf16x8, q[2 * u + 1]), s[st], 0, 0, 0);
-                } else {
-                    const f32x4 x = __builtin_bit_cast(f32x4, kk), y = __builtin_bit_cast(f32x4, q[u]);
+            for (int st = 0; st < T::kSub; ++st) {
+                next[st] = after[st];
+                after[st] = page_of(k + 2, st);
+            }
+        };
+        auto bring_k = [&](int stage) {
+            const uint32_t to = ring + stage * S::kStage;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) s[st] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], s[st], 0, 0, 0);
+            for (int i = 0; i < S::kLoadsK; ++i)
+                load16_once_to_lds_at(src_k[i / (S::kLoadsK / T::kSub)], off_k[i % (S::kLoadsK / T::kSub)], to + i * (kWave * 16));
+        };
+        auto bring_v = [&](int stage) {
+            const uint32_t to = ring + stage * S::kStage + S::kTileK;
+#pragma unroll
+            for (int i = 0; i < S::kLoadsV; ++i) load16_once_to_lds_at(src_v[i / (S::kLoadsV / T::kSub)], off_v[i], to + i * (kWave * 16));
+        };
+
+        float top = -INFINITY, sum = 0.f;  // of head col: the running maximum (of what exp2 takes) and this lane's share of the sum
+        f32x4 acc[kOut];
+#pragma unroll
+        for (int t = 0; t < kOut; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const float scale2 = a->k_scale ? a->scale2 * ((const __attribute__((address_space(4))) float*)(uintptr_t)a->k_scale)[hk] : a->scale2;
+
+#pragma nounroll
+        for (int k = 0; k < min(NS, mine); ++k) {
+            place(k, k);
+            bring_k(k);
+            bring_v(k);
+        }
+        int stage = 0;
+        const int together = n_tiles / kWaves;  // steps that every wavefront has
+        for (int k = 0; k < mine; ++k) {
+            // The wavefronts step together: the first four, which a compute unit prefers, would end a seventh earlier than the others, and leave
+            // them with half as many bytes under way (one sequence of 131,072 tokens 88 -> 85 us).
+            if constexpr (kWaves > 4)
+                if (k < together) __builtin_amdgcn_s_barrier();
+            const int rest = min(mine - 1 - k, NS - 1);  // stages under way behind this one
+            const bool more = k + NS < mine;
+            const uint32_t at_k = ring + stage * S::kStage, at_v = at_k + S::kTileK;
+            const int t0 = c0 + (wv + k * kWaves) * S::kTile;
+            const unsigned lost = (gone >> (stage * T::kSub)) & ((1u << T::kSub) - 1);
+            const bool edge = t0 < sp.begin || t0 + S::kTile > c1 || lost;
+
+            wait_stage<NS, S::kLoadsK + S::kLoadsV, S::kLoadsV>(rest);
+            f32x4 s[T::kSub];
+#pragma unroll
+            for (int st = 0; st < T::kSub; ++st) {
+                s[st] = f32x4{0.f, 0.f, 0.f, 0.f};
+                const uint32_t row = at_k + (st * kRows + col) * (KC * T::kBytes);
+#pragma unroll
+                for (int u = 0; u < kUnits; ++u) {
+                    const u32x4 kk = lds_16(row + (((4 * u + grp) ^ k_key(col, S::kPiecesK)) << 4));
+                    if constexpr (T::kBytes == 2) {
+                        s[st] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kk), __builtin_bit_cast(bf16x8, q[u]), s[st], 0, 0, 0);
+                    } else if constexpr (T::kBytes == 1) {
+                        s[st] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(kk.x, kk.y), __builtin_bit_cast(bf16x8, q[2 * u]), s[st], 0, 0, 0);
+                        s[st] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(kk.z, kk.w), __builtin_bit_cast(bf16x8, q[2 * u + 1]), s[st], 0, 0, 0);
+                    } else {
+                        const f32x4 x = __builtin_bit_cast(f32x4, kk), y = __builtin_bit_cast(f32x4, q[u]);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) s[st] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], s[st], 0, 0, 0);
+                    }
                 }
             }
-        }
-        if (more) {
-            wait_lds_fence();
-            place(k + NS, stage, next);
-            bring_k(stage);
-#pragma unroll
-            for (int st = 0; st < T::kSub; ++st) next[st] = page_of(k + NS + 1, st);
-        }
+            if (more) {
+                wait_lds_fence();
+                place(k + NS, stage);
+                bring_k(stage);
+            }
 
-        // lane (col, grp) holds the logits of head col with keys 4 grp + r of every subtile
-        if (edge) {
+            // lane (col, grp) holds the logits of head col with keys 4 grp + r of every subtile
+            if (edge) {
+#pragma unroll
+                for (int st = 0; st < T::kSub; ++st) {
+                    const int first = t0 + st * kRows + 4 * grp;
+                    const int from = sp.begin - first, to = lost >> st & 1 ? 0 : c1 - first;  // which of the four are the sequence's
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) s[st][r] = r >= from && r < to ? s[st][r] : -INFINITY;
+                }
+            }
+            float best = s[0][0];
+#pragma unroll
+            for (int st = 0; st < T::kSub; ++st)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) best = fmaxf(best, s[st][r]);
+            best = quad_max(best) * scale2;
+            if (__ballot(best > top)) {
+                const float higher = fmaxf(top, best);
+                const float fade = higher == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top - higher);
+                top = higher;
+                sum *= fade;
+#pragma unroll
+                for (int t = 0; t < kOut; ++t) acc[t] *= fade;
+            }
+            const float from = top == -INFINITY ? 0.f : top;
+            f32x4 e[T::kSub];
 #pragma unroll
             for (int st = 0; st < T::kSub; ++st)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int tok = t0 + st * kRows + 4 * grp + r;
-                    if (tok < sp.begin || tok >= c1 || (lost >> st & 1)) s[st][r] = -INFINITY;
+                    e[st][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[st][r], scale2, -from));
+                    sum += e[st][r];
                 }
-        }
-        float best = s[0][0];
-#pragma unroll
-        for (int st = 0; st < T::kSub; ++st)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) best = fmaxf(best, s[st][r]);
-        best = quad_max(best) * scale2;
-        if (__ballot(best > top)) {
-            const float higher = fmaxf(top, best);
-            const float fade = higher == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(top - higher);
-            top = higher;
-            sum *= fade;
-#pragma unroll
-            for (int t = 0; t < kOut; ++t) acc[t] *= fade;
-        }
-        const float from = top == -INFINITY ? 0.f : top;
-        f32x4 e[T::kSub];
-#pragma unroll
-        for (int st = 0; st < T::kSub; ++st)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                e[st][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[st][r], scale2, -from));
-                sum += e[st][r];
-            }
 
-        if (more) wait_vm_fence<(NS - 1) * (S::kLoadsK + S::kLoadsV) + S::kLoadsK>();
-        else wait_stage<NS, S::kLoadsK + S::kLoadsV, 0>(rest);
-        if (edge) {  // what lies in rows that are not the sequence's may be anything, and 0 times it not 0
-#pragma unroll
-            for (int i = 0; i < S::kLoadsV; ++i) {
-                const int row = (i * kWave + lane) / S::kPiecesV, tok = t0 + row;
-                if (tok < sp.begin || tok >= c1 || (lost >> (row / kRows) & 1))
-                    *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(at_v + (i * kWave + lane) * 16) = u32x4{0u, 0u, 0u, 0u};
+            if (more) wait_vm_fence<(NS - 1) * (S::kLoadsK + S::kLoadsV) + S::kLoadsK>();
+            else wait_stage<NS, S::kLoadsK + S::kLoadsV, 0>(rest);
+            if (edge) {  // what lies in rows that are not the sequence's may be anything, and 0 times it not 0
+#pragma nounroll
+                for (int i = lane; i < S::kLoadsV * kWave; i += kWave) {
+                    const int row = i / S::kPiecesV, tok = t0 + row;
+                    if (tok < sp.begin || tok >= c1 || (lost >> (row / kRows) & 1))
+                        *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(at_v + i * 16) = u32x4{0u, 0u, 0u, 0u};
+                }
+                wait_lds_fence();
             }
-            wait_lds_fence();
+            // The weights go to the products as they lie: a lane's keys are the summation indices of its group.  As bf16 they are split in two,
+            // the value and what rounding took from it: the matrix cores have the time, and the sums are as exact as the logits.
+            if constexpr (T::kBytes == 2) {
+                const uint2 hi = make_uint2(pack_bf16(e[0][0], e[0][1]), pack_bf16(e[0][2], e[0][3]));
+                const uint2 lo = make_uint2(pack_bf16(e[0][0] - bf16_lo(hi.x), e[0][1] - bf16_hi(hi.x)), pack_bf16(e[0][2] - bf16_lo(hi.y), e[0][3] - bf16_hi(hi.y)));
+                const uint32_t row = at_v + (4 * grp + (col >> 2)) * (VC * 2) + ((col & 1) << 3);
+                const int key = v_key<T>(4 * grp + (col >> 2), S::kPiecesV);
+#pragma unroll
+                for (int t = 0; t < kOut; ++t) {
+                    const s16x4 vt = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (__attribute__((address_space(3))) s16x4*)(uintptr_t)(row + (((2 * t + ((col >> 1) & 1)) ^ key) << 4)));
+                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vt, __builtin_bit_cast(s16x4, hi), acc[t], 0, 0, 0);
+                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vt, __builtin_bit_cast(s16x4, lo), acc[t], 0, 0, 0);
+                }
+            } else if constexpr (T::kBytes == 1) {
+                uint4 hi, lo;
+                hi.x = pack_bf16(e[0][0], e[0][1]); hi.y = pack_bf16(e[0][2], e[0][3]);
+                hi.z = pack_bf16(e[1][0], e[1][1]); hi.w = pack_bf16(e[1][2], e[1][3]);
+                lo.x = pack_bf16(e[0][0] - bf16_lo(hi.x), e[0][1] - bf16_hi(hi.x)); lo.y = pack_bf16(e[0][2] - bf16_lo(hi.y), e[0][3] - bf16_hi(hi.y));
+                lo.z = pack_bf16(e[1][0] - bf16_lo(hi.z), e[1][1] - bf16_hi(hi.z)); lo.w = pack_bf16(e[1][2] - bf16_lo(hi.w), e[1][3] - bf16_hi(hi.w));
+                // eight rows of sixteen 8-bit columns, lanes 2r and 2r + 1 name row r's: the keys of the lane group in both subtiles
+                const int r8 = col >> 1, vrow = (r8 >> 2) * kRows + 4 * grp + (r8 & 3);
+                const uint32_t row = at_v + vrow * VC + ((col & 1) << 3);
+                const int key = v_key<T>(vrow, S::kPiecesV);
+#pragma unroll
+                for (int t = 0; t < kOut; ++t) {
+                    const i32x2 vt = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+                        (__attribute__((address_space(3))) i32x2*)(uintptr_t)(row + ((t ^ key) << 4)));
+                    const bf16x8 w = widen8(vt[0], vt[1]);
+                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(bf16x8, hi), acc[t], 0, 0, 0);
+                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(bf16x8, lo), acc[t], 0, 0, 0);
+                }
+            } else {
+#pragma unroll
+                for (int t = 0; t < kOut; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const int vrow = 4 * grp + r, piece = 4 * t + (col >> 2);
+                        const float x = *(const __attribute__((address_space(3))) float*)(uintptr_t)(
+                            at_v + vrow * (VC * 4) + ((piece ^ v_key<T>(vrow, S::kPiecesV)) << 4) + ((col & 3) << 2));
+                        acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, e[0][r], acc[t], 0, 0, 0);
+                    }
+            }
+            if (more) {
+                wait_lds_fence();
+                bring_v(stage);
+            }
+            stage = stage + 1 == NS ? 0 : stage + 1;
         }
-        // The weights go to the products as they lie: a lane's keys are the summation indices of its group.  As bf16 they are split in two,
-        // the value and what rounding took from it: the matrix cores have the time, and the sums are as exact as the logits.
-        if constexpr (T::kBytes == 2) {
-            const uint2 hi = make_uint2(pack_bf16(e[0][0], e[0][1]), pack_bf16(e[0][2], e[0][3]));
-            const uint2 lo = make_uint2(pack_bf16(e[0][0] - bf16_lo(hi.x), e[0][1] - bf16_hi(hi.x)), pack_bf16(e[0][2] - bf16_lo(hi.y), e[0][3] - bf16_hi(hi.y)));
-            const uint32_t row = at_v + (4 * grp + (col >> 2)) * (VC * 2) + ((col & 1) << 3);
-            const int key = v_key<T>(4 * grp + (col >> 2), S::kPiecesV);
-#pragma unroll
-            for (int t = 0; t < kOut; ++t) {
-                const s16x4 vt = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (__attribute__((address_space(3))) s16x4*)(uintptr_t)(row + (((2 * t + ((col >> 1) & 1)) ^ key) << 4)));
-                acc[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vt, __builtin_bit_cast(s16x4, hi), acc[t], 0, 0, 0);
-                acc[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vt, __builtin_bit_cast(s16x4, lo), acc[t], 0, 0, 0);
-            }
-        } else if constexpr (T::kBytes == 1) {
-            uint4 hi, lo;
-            hi.x = pack_bf16(e[0][0], e[0][1]); hi.y = pack_bf16(e[0][2], e[0][3]);
-            hi.z = pack_bf16(e[1][0], e[1][1]); hi.w = pack_bf16(e[1][2], e[1][3]);
-            lo.x = pack_bf16(e[0][0] - bf16_lo(hi.x), e[0][1] - bf16_hi(hi.x)); lo.y = pack_bf16(e[0][2] - bf16_lo(hi.y), e[0][3] - bf16_hi(hi.y));
-            lo.z = pack_bf16(e[1][0] - bf16_lo(hi.z), e[1][1] - bf16_hi(hi.z)); lo.w = pack_bf16(e[1][2] - bf16_lo(hi.w), e[1][3] - bf16_hi(hi.w));
-            // eight rows of sixteen 8-bit columns, lanes 2r and 2r + 1 name row r's: the keys of the lane group in both subtiles
-            const int r8 = col >> 1, vrow = (r8 >> 2) * kRows + 4 * grp + (r8 & 3);
-            const uint32_t row = at_v + vrow * VC + ((col & 1) << 3);
-            const int key = v_key<T>(vrow, S::kPiecesV);
-#pragma unroll
-            for (int t = 0; t < kOut; ++t) {
-                const i32x2 vt = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-                    (__attribute__((address_space(3))) i32x2*)(uintptr_t)(row + ((t ^ key) << 4)));
-                const bf16x8 w = widen8(vt[0], vt[1]);
-                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(bf16x8, hi), acc[t], 0, 0, 0);
-                acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(bf16x8, lo), acc[t], 0, 0, 0);
-            }
-        } else {
+        sum = quad_sum(sum);
+
+        // The wavefronts' sums, joined in LDS: a thread takes four output columns of a head, of more than kThreads of them in turns.
+        barrier_lds();  // the rings are read
+        constexpr int kThreads = kWaves * kWave, kQuads = VC / 4, kAtOnce = kThreads / kQuads;  // heads at once
+        float* out = reinterpret_cast<float*>(smem);         // [kWaves][kKvHeads][kOutRow]
+        float* s_m = out + kWaves * kKvHeads * S::kOutRow;   // [kKvHeads][kWaves] maxima
+        float* s_l = s_m + kWaves * kKvHeads;                // and sums
+        if (col < heads) {
 #pragma unroll
             for (int t = 0; t < kOut; ++t)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const int vrow = 4 * grp + r, piece = 4 * t + (col >> 2);
-                    const float x = *(const __attribute__((address_space(3))) float*)(uintptr_t)(
-                        at_v + vrow * (VC * 4) + ((piece ^ v_key<T>(vrow, S::kPiecesV)) << 4) + ((col & 3) << 2));
-                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, e[0][r], acc[t], 0, 0, 0);
-                }
-        }
-        if (more) {
-            wait_lds_fence();
-            bring_v(stage);
-        }
-        stage = stage + 1 == NS ? 0 : stage + 1;
-    }
-    sum = quad_sum(sum);
-
-    // the wavefronts' sums, joined in LDS
-    __syncthreads();  // the rings are read
-    float* out = reinterpret_cast<float*>(smem);                              // [kWaves][kKvHeads][kOutRow]
-    float* s_m = out + kWaves * kKvHeads * S::kOutRow;                         // [kKvHeads][kWaves] maxima
-    float* s_l = s_m + kWaves * kKvHeads;                                      // and sums
-    if (col < heads) {
-#pragma unroll
-        for (int t = 0; t < kOut; ++t)
-            *reinterpret_cast<f32x4*>(out + (wv * kKvHeads + col) * S::kOutRow + t * 16 + grp * 4) = acc[t];
-        if (grp == 0) {
-            s_m[col * kWaves + wv] = top;
-            s_l[col * kWaves + wv] = sum;
-        }
-    }
-    __syncthreads();
-    const long long head0 = (long long)b * a.n_kv * a.group + hk * a.group + h0;
-    const int quads = a.v_dim / 4, cols = heads * quads;
-    const bool whole = u0 == 0 && u1 == units;
-    const int rows = min(kKvHeads, a.group);
-    const unsigned w0 = item_first / mine_of.per;  // the workgroup in whose stretch the item begins
-    // A workgroup leaves two partial results at most: of an item that began before its stretch and of one that ends behind it.
-    auto slot_of = [&](unsigned w) -> unsigned { return (2 * w + (w == w0 ? 1 : 0)) * rows; };
-    for (int n = threadIdx.x; n < cols; n += kWaves * kWave) {
-        const int h = n / quads, d = (n - h * quads) * 4;
-        Sums r{-INFINITY, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
-        float f[kWaves];
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) r.m = fmaxf(r.m, f[w] = s_m[h * kWaves + w]);
-        const float from = r.m == -INFINITY ? 0.f : r.m;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {  // (a wavefront without a tile has -inf, and zeros)
-            f[w] = __builtin_amdgcn_exp2f(f[w] - from);
-            r.add(f[w], s_l[h * kWaves + w], *reinterpret_cast<const f32x4*>(out + (w * kKvHeads + h) * S::kOutRow + d));
-        }
-        if (whole) {
-            write_out<io>(a, head0 + h, d, hk, r);
-        } else {  // past the caches: another workgroup, on another die, may read it before this launch ends
-            const unsigned row = slot_of(blockIdx.x) + h;
-            unsigned long long* to = reinterpret_cast<unsigned long long*>(a.part + (row * a.v_dim + d));
-            store_past(to, r.o[0], r.o[1]);
-            store_past(to + 1, r.o[2], r.o[3]);
-            if (d == 0) store_past(reinterpret_cast<unsigned long long*>(a.stat) + row, r.m, r.l);
-        }
-    }
-    if (!whole) {
-        int* last = reinterpret_cast<int*>(smem + 16384);  // behind what the join below uses
-        const unsigned w1 = (item_first + units - 1) / mine_of.per, parts = w1 - w0 + 1;
-        wait_vm_fence<0>();  // the partial result has arrived before it is counted
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            const unsigned n = __hip_atomic_fetch_add(&a.arrived[w0], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            *last = n == parts - 1;
-            if (*last) __hip_atomic_store(&a.arrived[w0], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // for the next launch
-        }
-        __syncthreads();
-        if (*last) {  // the last of the item's workgroups joins the parts, in their order in the line
-            const int lanes = cols < kWaves * kWave ? cols : kWaves * kWave, groups = kWaves * kWave / lanes;
-            float* sh = reinterpret_cast<float*>(smem);  // [groups][lanes][6]
-            for (int c = 0; c < cols; c += lanes) {
-                const int g = threadIdx.x / lanes, i = threadIdx.x - g * lanes, n = c + i;
-                Sums r{-INFINITY, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
-                const int h = n / quads, d = (n - h * quads) * 4;
-                const bool here = g < groups && n < cols;
-                if (here) {
-                    constexpr unsigned kAhead = 8;  // parts under way
-                    for (unsigned p0 = g; p0 < parts; p0 += kAhead * groups) {
-                        float2 ps[kAhead], lo[kAhead], hi[kAhead];
-#pragma unroll
-                        for (unsigned j = 0; j < kAhead; ++j) {
-                            const unsigned row = slot_of(w0 + min(p0 + j * groups, parts - 1)) + h;
-                            const unsigned long long* from = reinterpret_cast<const unsigned long long*>(a.part + (row * a.v_dim + d));
-                            ps[j] = load_past(reinterpret_cast<const unsigned long long*>(a.stat) + row);
-                            lo[j] = load_past(from);
-                            hi[j] = load_past(from + 1);
-                        }
-                        float m = r.m;
-#pragma unroll
-                        for (unsigned j = 0; j < kAhead; ++j) m = fmaxf(m, ps[j].x);
-                        const float from = m == -INFINITY ? 0.f : m, fade = __builtin_amdgcn_exp2f(r.m - from);
-                        r.m = m;
-                        r.l *= fade;
-                        r.o *= fade;
-#pragma unroll
-                        for (unsigned j = 0; j < kAhead; ++j)
-                            r.add(p0 + j * groups < parts ? __builtin_amdgcn_exp2f(ps[j].x - from) : 0.f, ps[j].y, f32x4{lo[j].x, lo[j].y, hi[j].x, hi[j].y});
-                    }
-                }
-                if (groups > 1) {  // the groups' sums, by columns: [groups][6][lanes]
-                    if (here) {
-                        float* mine = sh + g * 6 * lanes + i;
-                        mine[0] = r.m;
-                        mine[lanes] = r.l;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) mine[(2 + j) * lanes] = r.o[j];
-                    }
-                    __syncthreads();
-                    if (here && g == 0) {
-                        float m = r.m;
-                        for (int k = 1; k < groups; ++k) m = fmaxf(m, sh[k * 6 * lanes + i]);
-                        const float from = m == -INFINITY ? 0.f : m, fade = __builtin_amdgcn_exp2f(r.m - from);
-                        r.m = m;
-                        r.l *= fade;
-                        r.o *= fade;
-                        for (int k = 1; k < groups; ++k) {
-                            const float* x = sh + k * 6 * lanes + i;
-                            r.add(__builtin_amdgcn_exp2f(x[0] - from), x[lanes], f32x4{x[2 * lanes], x[3 * lanes], x[4 * lanes], x[5 * lanes]});
-                        }
-                    }
-                }
-                if (here && g == 0) write_out<io>(a, head0 + h, d, hk, r);
+                *reinterpret_cast<f32x4*>(out + (wv * kKvHeads + col) * S::kOutRow + t * 16 + grp * 4) = acc[t];
+            if (grp == 0) {
+                s_m[col * kWaves + wv] = top;
+                s_l[col * kWaves + wv] = sum;
             }
         }
-    }
-    at_unit = item_first + u1;
-    if (item + 1 == items && u1 == units) {
-        base += items * units;
-        ++b;
-    }
-    if (at_unit < mine_of.end) __syncthreads();  // what the joins read in LDS is the next item's ring
+        barrier_lds();
+        a = again(a);
+        const bool whole = u0 == 0 && u1 == units;
+        const int rows = min(kKvHeads, a->group), v_dim = a->v_dim;
+        // A workgroup leaves two partial results at most: of an item that began before its stretch and of one that ends behind it.  They are stored
+        // past the caches: a workgroup on another die may read them before this launch ends.
+        float* const part = a->part;
+        unsigned long long* const part_stat = reinterpret_cast<unsigned long long*>(a->stat);
+        const int my_head = threadIdx.x / kQuads, d = threadIdx.x % kQuads * 4;
+        bool write = whole;
+        for (;;) {
+            for (int h = my_head; h < heads; h += kAtOnce) {
+                if (d >= v_dim) break;
+                Sums r{-INFINITY, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
+                float f[kWaves];
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w) r.m = fmaxf(r.m, f[w] = s_m[h * kWaves + w]);
+                const float from = r.m == -INFINITY ? 0.f : r.m;
+#pragma unroll
+                for (int w = 0; w < kWaves; ++w)  // (a wavefront without a tile has -inf, and zeros)
+                    r.add(__builtin_amdgcn_exp2f(f[w] - from), s_l[h * kWaves + w], *reinterpret_cast<const f32x4*>(out + (w * kKvHeads + h) * S::kOutRow + d));
+                if (write) {
+                    const Args z = again(a);
+                    const long long head = (long long)b * z->n_kv * z->group + hk * z->group + h0 + h;
+                    // (the reciprocal is good to an ulp of fp32; of no weights it is not taken)
+                    const float g = r.m == -INFINITY ? 0.f : __builtin_amdgcn_rcpf(r.l) * (z->v_scale ? z->v_scale[hk] : 1.f);
+                    if constexpr (sizeof(io) == 2)
+                        *reinterpret_cast<uint2*>(static_cast<uint16_t*>(z->out) + head * v_dim + d) = make_uint2(pack_bf16(r.o[0] * g, r.o[1] * g), pack_bf16(r.o[2] * g, r.o[3] * g));
+                    else
+                        *reinterpret_cast<f32x4*>(static_cast<float*>(z->out) + head * v_dim + d) = r.o * g;
+                    if (d == 0 && z->lse) z->lse[head] = r.m == -INFINITY ? -INFINITY : (r.m + __builtin_amdgcn_logf(r.l)) * 0.69314718055994531f;
+                } else {
+                    const unsigned row = (2 * blockIdx.x + (u0 == 0 ? 1 : 0)) * rows + h;
+                    unsigned long long* to = reinterpret_cast<unsigned long long*>(part + (row * v_dim + d));
+                    store_past(to, r.o[0], r.o[1]);
+                    store_past(to + 1, r.o[2], r.o[3]);
+                    if (d == 0) store_past(part_stat + row, r.m, r.l);
+                }
+            }
+            if (write) break;
+            const unsigned w0 = item_first / mine_of.per, w1 = (item_first + units - 1) / mine_of.per;  // the workgroups that the item's units lie in
+            const unsigned parts = w1 - w0 + 1;
+            int* last = reinterpret_cast<int*>(smem);
+            wait_vm_fence<0>();  // the partial result has arrived before it is counted
+            barrier_lds();
+            if (threadIdx.x == 0) {
+                unsigned* arrived = again(a)->arrived + w0;
+                const bool all = __hip_atomic_fetch_add(arrived, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == parts - 1;
+                if (all) __hip_atomic_store(arrived, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // for the next launch
+                *last = all;
+            }
+            barrier_lds();
+            if (!*last) break;
+            // The last of the item's workgroups joins the parts: up to kWaves groups of threads take some each, in their order in the line, and
+            // leave their sums where the wavefronts' were.
+            barrier_lds();  // (`last` is read)
+            write = true;
+            const int groups = min(kWaves, max(1, kAtOnce / heads));
+            for (int i = my_head; i < heads * groups; i += kAtOnce) {
+                const int g = i / heads, h = i - g * heads;
+                if (d >= v_dim) break;
+                Sums r{-INFINITY, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
+                constexpr unsigned kAhead = 8;  // under way
+                for (unsigned p0 = g * kAhead; p0 < parts; p0 += groups * kAhead) {
+                    float2 ps[kAhead], lo[kAhead], hi[kAhead];
+#pragma unroll
+                    for (unsigned j = 0; j < kAhead; ++j) {
+                        const unsigned p = min(p0 + j, parts - 1), row = (2 * (w0 + p) + (p ? 0 : 1)) * rows + h;
+                        const unsigned long long* at = reinterpret_cast<const unsigned long long*>(part + (row * v_dim + d));
+                        ps[j] = load_past(part_stat + row);
+                        lo[j] = load_past(at);
+                        hi[j] = load_past(at + 1);
+                    }
+                    const float before = r.m;
+#pragma unroll
+                    for (unsigned j = 0; j < kAhead; ++j) r.m = fmaxf(r.m, ps[j].x);
+                    const float from = r.m == -INFINITY ? 0.f : r.m, fade = __builtin_amdgcn_exp2f(before - from);
+                    r.l *= fade;
+                    r.o *= fade;
+#pragma unroll
+                    for (unsigned j = 0; j < kAhead; ++j)
+                        r.add(p0 + j < parts ? __builtin_amdgcn_exp2f(ps[j].x - from) : 0.f, ps[j].y, f32x4{lo[j].x, lo[j].y, hi[j].x, hi[j].y});
+                }
+                *reinterpret_cast<f32x4*>(out + (g * kKvHeads + h) * S::kOutRow + d) = r.o;
+                if (d == 0) {
+                    s_m[h * kWaves + g] = r.m;
+                    s_l[h * kWaves + g] = r.l;
+                }
+            }
+            for (int i = threadIdx.x; i < heads * kWaves; i += kThreads)
+                if (i % kWaves >= groups) s_m[i] = -INFINITY;
+            barrier_lds();
+        }
+        at_unit = item_first + u1;
+        if (u1 == units && item + 1 == (unsigned)(a->n_kv * a->blocks_of_heads)) {
+            base = at_unit;
+            ++b;
+        }
+        if (at_unit < mine_of.end) barrier_lds();  // what was read in LDS is the next item's ring
     } while (at_unit < mine_of.end);
 }
 
