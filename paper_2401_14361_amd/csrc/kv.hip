@@ -25,43 +25,56 @@ struct KvAppendArgs {
     long long k_stride, v_stride;
     const float *k_scale, *v_scale;
     void *k_min, *k_max;
+    int parts;  // workgroups that share a token out
     int32_t* flags;
 };
 
 // ------------------------------------------------------------------------------------------------ element access
-// W elements at p as fp32 and back; p is aligned to them.
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+// W elements: 16 bytes, or one
 template <typename IO, int W>
-__device__ __forceinline__ void get(const IO* p, float* f) {
-    if constexpr (sizeof(IO) == 4 && W == 4) {
-        const float4 v = *reinterpret_cast<const float4*>(p);
-        f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
-    } else if constexpr (sizeof(IO) == 2 && W == 8) {
-        const uint4 v = *reinterpret_cast<const uint4*>(p);
-        f[0] = bf16_lo(v.x); f[1] = bf16_hi(v.x); f[2] = bf16_lo(v.y); f[3] = bf16_hi(v.y);
-        f[4] = bf16_lo(v.z); f[5] = bf16_hi(v.z); f[6] = bf16_lo(v.w); f[7] = bf16_hi(v.w);
-    } else if constexpr (sizeof(IO) == 4) {
-        static_assert(W == 1);
-        f[0] = *p;
-    } else {
-        static_assert(W == 1);
-        f[0] = bf16_one(*p);
+struct Vec {
+    static_assert(W * sizeof(IO) == 16);
+    typedef u32x4 raw;
+    static __device__ __forceinline__ raw load(const IO* p) { return *reinterpret_cast<const u32x4*>(p); }
+    static __device__ __forceinline__ void unpack(raw v, float* f) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (sizeof(IO) == 4) f[i] = __uint_as_float(v[i]);
+            else f[2 * i] = bf16_lo(v[i]), f[2 * i + 1] = bf16_hi(v[i]);
+        }
     }
-}
-template <typename IO, int W>
-__device__ __forceinline__ void put(IO* p, const float* f) {
-    if constexpr (sizeof(IO) == 4 && W == 4) *reinterpret_cast<float4*>(p) = make_float4(f[0], f[1], f[2], f[3]);
-    else if constexpr (sizeof(IO) == 2 && W == 8)
-        *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3]), pack_bf16(f[4], f[5]), pack_bf16(f[6], f[7]));
-    else if constexpr (sizeof(IO) == 4) *p = f[0];
-    else *p = (uint16_t)pack_bf16(f[0], 0.f);
-}
+    static __device__ __forceinline__ void store(IO* p, const float* f) {
+        u32x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (sizeof(IO) == 4) v[i] = __float_as_uint(f[i]);
+            else v[i] = pack_bf16(f[2 * i], f[2 * i + 1]);
+        }
+        *reinterpret_cast<u32x4*>(p) = v;
+    }
+};
+template <typename IO>
+struct Vec<IO, 1> {
+    typedef IO raw;
+    static __device__ __forceinline__ raw load(const IO* p) { return *p; }
+    static __device__ __forceinline__ void unpack(raw v, float* f) {
+        if constexpr (sizeof(IO) == 4) f[0] = v;
+        else f[0] = bf16_one(v);
+    }
+    static __device__ __forceinline__ void store(IO* p, const float* f) {
+        if constexpr (sizeof(IO) == 4) *p = f[0];
+        else *p = (uint16_t)pack_bf16(f[0], 0.f);
+    }
+};
 // 8-bit values: divided by the head's scale, limited to the largest that the type has (what is no number stays none), rounded to nearest even
 __device__ __forceinline__ float for_fp8(float x, float scale) {
     const float y = x / scale;
     return y > kFp8Max ? kFp8Max : y < -kFp8Max ? -kFp8Max : y;
 }
 template <int W>
-__device__ __forceinline__ void put8(uint8_t* p, const float* f, float scale) {
+__device__ __forceinline__ void store_fp8(uint8_t* p, const float* f, float scale) {
     if constexpr (W == 8) {
         int a = 0, b = 0;
         a = __builtin_amdgcn_cvt_pk_fp8_f32(for_fp8(f[0], scale), for_fp8(f[1], scale), a, false);
@@ -82,131 +95,232 @@ __device__ __forceinline__ float2 turn(int pos, float freq) {
     sincospif((float)(2.0 * (turns - rint(turns))), &cs.y, &cs.x);
     return cs;
 }
+__device__ __forceinline__ void turn_pair(float& x1, float& x2, float2 cs) {
+    const float y1 = __builtin_fmaf(x1, cs.x, -(x2 * cs.y));
+    x2 = __builtin_fmaf(x2, cs.x, x1 * cs.y);
+    x1 = y1;
+}
 
-// A workgroup takes a share of one token's heads: the turns of all pairs first, in LDS, then units of W pairs (of rotated heads), W plain
-// elements of keys and queries behind them, W elements of values.
-template <typename IO, typename PG, int W>
-__global__ void __launch_bounds__(kAppThreads) kv_append_kernel(KvAppendArgs a) {
-    __shared__ float2 s_turn[kKvMaxDim / 2];
-    const int t = blockIdx.x;
-    const int pos = a.pos[t];
-    if (pos < 0) return;  // a place of the batch without a token
-    const int seq = a.seq ? a.seq[t] : t;
-    const int at = pos >> a.page_shift;
-    bool ok = seq >= 0 && seq < a.B && at < a.width;
-    if (!ok) {
-        if (threadIdx.x == 0 && blockIdx.y == 0) atomicOr(a.flags, kKvBadLength);
-        return;
+typedef const __attribute__((address_space(4))) KvAppendArgs* Args;  // (in place: a copy would go to private memory)
+
+// The page that holds a token's row, -1: none (a flag is raised by the thread that `tell` names).
+__device__ __forceinline__ int page_of(Args a, int t, int pos, bool tell) {
+    const int seq = a->seq ? a->seq[t] : t, at = pos >> a->page_shift;
+    if (pos < 0) return -1;
+    if (seq < 0 || seq >= a->B || at >= a->width) {
+        if (tell) atomicOr(a->flags, kKvBadLength);
+        return -1;
     }
-    const int page = a.table[(long long)seq * a.width + at];
-    if (page < 0 || page >= a.n_pages) {
-        if (threadIdx.x == 0 && blockIdx.y == 0) atomicOr(a.flags, kKvBadPage);
-        return;
-    }
-    const int half = a.rot / 2;
-    for (int i = threadIdx.x; i < half; i += kAppThreads) s_turn[i] = turn(pos, a.inv_freq[i]);
-    __syncthreads();
-    const int row = pos & ((1 << a.page_shift) - 1);
-    const int turned = half / W, plain = (a.k_dim - a.rot) / W, of_head = turned + plain, of_v = a.v_dim / W;
-    const int n_rot = (a.n_q + a.n_kv) * of_head, n = n_rot + a.n_kv * of_v;
-    for (int i = blockIdx.y * kAppThreads + threadIdx.x; i < n; i += gridDim.y * kAppThreads) {
-        if (i >= n_rot) {
-            const int h = (i - n_rot) / of_v, d = (i - n_rot - h * of_v) * W;
-            float f[W];
-            get<IO, W>(static_cast<const IO*>(a.v) + t * a.v_row + h * a.v_dim + d, f);
-            PG* to = static_cast<PG*>(a.v_pages) + page * a.v_stride + (((long long)h << a.page_shift) + row) * a.v_dim + d;
-            if constexpr (sizeof(PG) == 1) put8<W>(to, f, a.v_scale[h]);
-            else put<PG, W>(to, f);
-            continue;
-        }
-        const int head = i / of_head, u = i - head * of_head;
-        const bool is_q = head < a.n_q;
-        const int h = is_q ? head : head - a.n_q;
-        const IO* src = is_q ? static_cast<const IO*>(a.q) + t * a.q_stride + h * a.k_dim : static_cast<const IO*>(a.k) + t * a.k_row + h * a.k_dim;
-        IO* q_to = static_cast<IO*>(a.q_out) + ((long long)t * a.n_q + h) * a.k_dim;
-        PG* k_to = static_cast<PG*>(a.k_pages) + page * a.k_stride + (((long long)h << a.page_shift) + row) * a.k_dim;
-        auto store = [&](int d, const float* f) {
-            if (is_q) put<IO, W>(q_to + d, f);
-            else if constexpr (sizeof(PG) == 1) put8<W>(k_to + d, f, a.k_scale[h]);
-            else put<PG, W>(k_to + d, f);
-        };
-        if (u >= turned) {
-            const int d = a.rot + (u - turned) * W;
-            float f[W];
-            get<IO, W>(src + d, f);
-            store(d, f);
-            continue;
-        }
-        // W pairs: elements i and i + half, or 2 i and 2 i + 1
-        const int d1 = a.interleaved ? 2 * u * W : u * W, d2 = a.interleaved ? d1 + W : d1 + half;
-        float x[2 * W], y[2 * W];
-        get<IO, W>(src + d1, x);
-        get<IO, W>(src + d2, x + W);
+    const int page = a->table[(long long)seq * a->width + at];
+    if (page >= 0 && page < a->n_pages) return page;
+    if (tell) atomicOr(a->flags, kKvBadPage);
+    return -1;
+}
+
+// Smallest and largest value of every dimension of a page's keys, by a workgroup; `own` (LDS) stands for row `own_row`, as stored values.
+// A thread takes 16 bytes of a row, and every so many rows.
+template <typename IO, typename PG>
+__device__ __forceinline__ void summarise(Args a, int page, int h, const float* own, int own_row) {
+    constexpr int N = 16 / sizeof(PG);
+    __shared__ IO s_lo[kAppThreads * N], s_hi[kAppThreads * N];  // (the type holds them exactly)
+    const int pieces = a->k_dim / N, size = 1 << a->page_shift, groups = kAppThreads / pieces;
+    const int g = threadIdx.x / pieces, p = threadIdx.x - g * pieces;
+    const PG* src = static_cast<const PG*>(a->k_pages) + page * a->k_stride + ((long long)h << a->page_shift) * a->k_dim + p * N;
+    float lo[N], hi[N];
 #pragma unroll
-        for (int j = 0; j < W; ++j) {
-            const float2 cs = s_turn[u * W + j];
-            const float x1 = a.interleaved ? x[2 * j] : x[j], x2 = a.interleaved ? x[2 * j + 1] : x[W + j];
-            const float y1 = __builtin_fmaf(x1, cs.x, -(x2 * cs.y)), y2 = __builtin_fmaf(x2, cs.x, x1 * cs.y);
-            if (a.interleaved) { y[2 * j] = y1; y[2 * j + 1] = y2; }
-            else { y[j] = y1; y[W + j] = y2; }
+    for (int j = 0; j < N; ++j) lo[j] = INFINITY, hi[j] = -INFINITY;
+    if (g < groups)
+#pragma unroll 4
+        for (int r = g; r < size; r += groups) {
+            const u32x4 v = *reinterpret_cast<const u32x4*>(src + r * a->k_dim);
+            float x[N];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if constexpr (sizeof(PG) == 1) {
+                    x[4 * i] = __builtin_amdgcn_cvt_f32_fp8((int)v[i], 0); x[4 * i + 1] = __builtin_amdgcn_cvt_f32_fp8((int)v[i], 1);
+                    x[4 * i + 2] = __builtin_amdgcn_cvt_f32_fp8((int)v[i], 2); x[4 * i + 3] = __builtin_amdgcn_cvt_f32_fp8((int)v[i], 3);
+                } else if constexpr (sizeof(PG) == 2) {
+                    x[2 * i] = bf16_lo(v[i]); x[2 * i + 1] = bf16_hi(v[i]);
+                } else {
+                    x[i] = __uint_as_float(v[i]);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const float y = r == own_row ? own[p * N + j] : x[j];
+                lo[j] = fminf(lo[j], y);
+                hi[j] = fmaxf(hi[j], y);
+            }
         }
-        store(d1, y);
-        store(d2, y + W);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {  // [N][threads]: a column's values side by side
+        Vec<IO, 1>::store(&s_lo[j * kAppThreads + threadIdx.x], &lo[j]);
+        Vec<IO, 1>::store(&s_hi[j * kAppThreads + threadIdx.x], &hi[j]);
+    }
+    __syncthreads();
+    for (int d = threadIdx.x; d < a->k_dim; d += kAppThreads) {
+        const int at = d % N * kAppThreads + d / N;
+        float l, u;
+        Vec<IO, 1>::unpack(s_lo[at], &l);
+        Vec<IO, 1>::unpack(s_hi[at], &u);
+        for (int j = 1; j < groups; ++j) {
+            float x, y;
+            Vec<IO, 1>::unpack(s_lo[at + j * pieces], &x);
+            Vec<IO, 1>::unpack(s_hi[at + j * pieces], &y);
+            l = fminf(l, x);
+            u = fmaxf(u, y);
+        }
+        const long long to = ((long long)page * a->n_kv + h) * a->k_dim + d;
+        Vec<IO, 1>::store(static_cast<IO*>(a->k_min) + to, &l);
+        Vec<IO, 1>::store(static_cast<IO*>(a->k_max) + to, &u);
+    }
+    __syncthreads();
+}
+
+// A workgroup takes a share of a token's heads.  A thread's unit is two vectors of W elements of a head, which hold W pairs or are plain; it keeps
+// its place and goes from head to head, so that the turns of its pairs are read once and nothing is divided on the way, and has the next
+// head's unit under way.  Bound by memory: 8,192 tokens of 32 + 8 + 8 heads of 128 in bf16, 202 MB, 39 us (a copy of as many bytes 42);
+// units dealt out one by one, with two divisions each, 42 - 48.
+// kSums: each token is its sequence's only one, and further workgroups (blockIdx.y >= parts) form the summaries of the pages that
+// are completed, one for a key/value head: the page's other rows are there from earlier calls, the new one is formed a second time.
+template <typename IO, typename PG, int W, bool kSums>
+__global__ void __launch_bounds__(kAppThreads, kSums ? 4 : 6) kv_append_kernel(KvAppendArgs) {
+    const Args a = (Args)__builtin_amdgcn_kernarg_segment_ptr();
+    using V = Vec<IO, W>;
+    __shared__ float2 s_turn[kKvMaxDim / 2];
+    const int tid = threadIdx.x, half = a->rot / 2;
+    const int t = blockIdx.x;
+    const int size = 1 << a->page_shift;
+    if constexpr (kSums)
+    if ((int)blockIdx.y >= a->parts) {
+        const int pos = a->pos[t], h = blockIdx.y - a->parts;
+        if (pos < 0 || (pos & (size - 1)) != size - 1) return;
+        const int page = page_of(a, t, pos, false);
+        if (page < 0) return;
+        __shared__ float own[kKvMaxDim];
+        for (int i = tid; i < half; i += kAppThreads) s_turn[i] = turn(pos, a->inv_freq[i]);
+        __syncthreads();
+        const IO* k = static_cast<const IO*>(a->k) + t * a->k_row + h * a->k_dim;
+        for (int d = tid; d < a->k_dim; d += kAppThreads) {
+            const int i = a->interleaved ? d >> 1 : d < half ? d : d - half;
+            const bool second = a->interleaved ? d & 1 : d >= half;
+            float x, y;
+            Vec<IO, 1>::unpack(k[d], &x);
+            if (d < a->rot) {
+                Vec<IO, 1>::unpack(k[a->interleaved ? d ^ 1 : second ? i : i + half], &y);
+                if (second) turn_pair(y, x, s_turn[i]);
+                else turn_pair(x, y, s_turn[i]);
+            }
+            if constexpr (sizeof(PG) == 1) x = __builtin_amdgcn_cvt_f32_fp8(__builtin_amdgcn_cvt_pk_fp8_f32(for_fp8(x, a->k_scale[h]), 0.f, 0, false), 0);
+            else if constexpr (sizeof(PG) == 2) x = bf16_lo(pack_bf16(x, 0.f));
+            own[d] = x;
+        }
+        __syncthreads();
+        summarise<IO, PG>(a, page, h, own, size - 1);
+        return;
+    }
+
+    // A thread keeps its place in a head and takes one head after another, queries first: the turns of its pairs are read once.
+    const int of_head = a->k_dim / (2 * W), at_once = blockDim.x / of_head, per_step = a->parts * at_once;
+    const int u = tid % of_head, n_heads = a->n_q + a->n_kv;
+    const bool is_turned = u < half / W, apart = is_turned && !a->interleaved;
+    const int d1 = apart ? u * W : u * 2 * W;  // (plain elements lie behind the rotated ones, two vectors a unit like these)
+    const int d2 = d1 + (apart ? half : W);
+    int head = tid < at_once * of_head ? blockIdx.y * at_once + tid / of_head : n_heads;
+    typename V::raw r1{}, r2{};
+    auto load = [&]() __attribute__((always_inline)) {
+        const bool is_q = head < a->n_q;
+        const IO* src = is_q ? static_cast<const IO*>(a->q) + t * a->q_stride + head * a->k_dim
+                             : static_cast<const IO*>(a->k) + t * a->k_row + (head - a->n_q) * a->k_dim;
+        r1 = V::load(src + d1);
+        r2 = V::load(src + d2);
+    };
+    if (head < n_heads) load();  // on its way while the turns are formed
+    const int pos = a->pos[t];
+    const int page = page_of(a, t, pos, tid == 0 && blockIdx.y == 0);
+    if (page < 0) return;  // (all threads see the same)
+    for (int j = tid; j < half; j += blockDim.x) s_turn[j] = turn(pos, a->inv_freq[j]);
+    __syncthreads();
+    const int row = pos & (size - 1);
+    {
+        float2 cs[W];
+#pragma unroll
+        for (int k = 0; k < W; ++k) cs[k] = is_turned ? s_turn[u * W + k] : make_float2(1.f, 0.f);
+        PG* k_page = static_cast<PG*>(a->k_pages) + page * a->k_stride + (long long)row * a->k_dim;
+        while (head < n_heads) {
+            float f[2 * W];
+            V::unpack(r1, f);
+            V::unpack(r2, f + W);
+            if (is_turned) {
+                if (a->interleaved) {
+#pragma unroll
+                    for (int k = 0; k < W; ++k) turn_pair(f[2 * k], f[2 * k + 1], cs[k]);
+                } else {
+#pragma unroll
+                    for (int k = 0; k < W; ++k) turn_pair(f[k], f[W + k], cs[k]);
+                }
+            }
+            const int now = head;
+            head += per_step;
+            if (head < n_heads) load();
+            if (now < a->n_q) {
+                IO* to = static_cast<IO*>(a->q_out) + ((long long)t * a->n_q + now) * a->k_dim;
+                V::store(to + d1, f);
+                V::store(to + d2, f + W);
+            } else {
+                const int h = now - a->n_q;
+                PG* to = k_page + ((long long)h << a->page_shift) * a->k_dim;
+                if constexpr (sizeof(PG) == 1) {
+                    const float scale = a->k_scale[h];
+                    store_fp8<W>(to + d1, f, scale);
+                    store_fp8<W>(to + d2, f + W, scale);
+                } else {
+                    Vec<PG, W>::store(to + d1, f);
+                    Vec<PG, W>::store(to + d2, f + W);
+                }
+            }
+        }
+    }
+    const int of_v = a->v_dim / W;
+    const IO* v = static_cast<const IO*>(a->v) + t * a->v_row;
+    PG* v_page = static_cast<PG*>(a->v_pages) + page * a->v_stride + (long long)row * a->v_dim;
+    for (int i = blockIdx.y * blockDim.x + tid; i < a->n_kv * of_v; i += a->parts * blockDim.x) {
+        const int h = i / of_v;
+        PG* to = v_page + ((long long)h << a->page_shift) * a->v_dim + (i - h * of_v) * W;
+        const typename V::raw r = V::load(v + i * W);
+        float f[W];
+        V::unpack(r, f);
+        if constexpr (sizeof(PG) == 1) store_fp8<W>(to, f, a->v_scale[h]);
+        else Vec<PG, W>::store(to, f);
     }
 }
 
-// Smallest and largest value of every key dimension of the pages that a call has completed.  A workgroup looks at kEndTokens tokens for one
-// head; runs of a sequence complete a page in every page_size tokens.
-constexpr int kEndTokens = 16;
+// The summaries of the pages that a call with several tokens of a sequence has completed, when all of its rows are there.  A workgroup looks at
+// 64 tokens for one head.
 template <typename IO, typename PG>
-__global__ void __launch_bounds__(kAppThreads) kv_summary_kernel(KvAppendArgs a) {
-    __shared__ float s_lo[kAppThreads], s_hi[kAppThreads];
-    const int h = blockIdx.y;
-    const int size = 1 << a.page_shift;
-    for (int t = blockIdx.x * kEndTokens; t < min(a.T, (int)(blockIdx.x + 1) * kEndTokens); ++t) {
-        const int pos = a.pos[t];
-        if (pos < 0 || (pos & (size - 1)) != size - 1) continue;
-        const int seq = a.seq ? a.seq[t] : t, at = pos >> a.page_shift;
-        if (seq < 0 || seq >= a.B || at >= a.width) continue;
-        const int page = a.table[(long long)seq * a.width + at];
-        if (page < 0 || page >= a.n_pages) continue;
-        const PG* src = static_cast<const PG*>(a.k_pages) + page * a.k_stride + ((long long)h << a.page_shift) * a.k_dim;
-        // threads: k_dim columns (up to 256), rows shared among the rest
-        const int groups = kAppThreads / a.k_dim > 0 ? kAppThreads / a.k_dim : 1;
-        const int d = threadIdx.x % a.k_dim, g = threadIdx.x / a.k_dim;
-        float lo = INFINITY, hi = -INFINITY;
-        if (g < groups)
-            for (int r = g; r < size; r += groups) {
-                const PG raw = src[(long long)r * a.k_dim + d];
-                float x;
-                if constexpr (sizeof(PG) == 1) x = __builtin_amdgcn_cvt_f32_fp8((int)raw, 0);
-                else if constexpr (sizeof(PG) == 2) x = bf16_one(raw);
-                else x = raw;
-                lo = fminf(lo, x);
-                hi = fmaxf(hi, x);
-            }
-        s_lo[threadIdx.x] = lo;
-        s_hi[threadIdx.x] = hi;
-        __syncthreads();
-        if (g == 0) {
-            for (int j = 1; j < groups; ++j) {
-                lo = fminf(lo, s_lo[j * a.k_dim + d]);
-                hi = fmaxf(hi, s_hi[j * a.k_dim + d]);
-            }
-            const long long to = ((long long)page * a.n_kv + h) * a.k_dim + d;
-            put<IO, 1>(static_cast<IO*>(a.k_min) + to, &lo);
-            put<IO, 1>(static_cast<IO*>(a.k_max) + to, &hi);
-        }
-        __syncthreads();
-    }
+__global__ void __launch_bounds__(kAppThreads) kv_summary_kernel(KvAppendArgs) {
+    const Args a = (Args)__builtin_amdgcn_kernarg_segment_ptr();
+    const int h = blockIdx.y, lane = threadIdx.x & (kWave - 1), size = 1 << a->page_shift;
+    const int t = blockIdx.x * kWave + lane;
+    const int pos = t < a->T ? a->pos[t] : -1;
+    const bool done = pos >= 0 && (pos & (size - 1)) == size - 1;
+    const int mine = done ? page_of(a, t, pos, false) : -1;
+    for (unsigned long long left = __ballot(mine >= 0); left; left &= left - 1)  // (all wavefronts see the same)
+        summarise<IO, PG>(a, __builtin_amdgcn_readlane(mine, __builtin_ctzll(left)), h, nullptr, -1);
 }
 
 template <typename IO, typename PG>
-void launch_append(const KvAppendArgs& a, bool wide, int parts, hipStream_t s) {
-    constexpr int W = 16 / sizeof(IO);
-    launch(K_KV_APPEND, wide ? kv_append_kernel<IO, PG, W> : kv_append_kernel<IO, PG, 1>, dim3((unsigned)a.T, (unsigned)parts), dim3(kAppThreads), 0, s, a);
-    if (a.k_min)
-        launch(K_KV_SUMMARY, kv_summary_kernel<IO, PG>, dim3((unsigned)((a.T + kEndTokens - 1) / kEndTokens), (unsigned)a.n_kv), dim3(kAppThreads), 0, s, a);
+void launch_append(KvAppendArgs a, bool wide, int cus, hipStream_t s) {
+    constexpr int N = 16 / sizeof(IO);
+    const int W = wide ? N : 1;
+    const int at_once = kAppThreads / (a.k_dim / (2 * W));
+    a.parts = a.T >= 8 * cus ? 1 : (a.n_q + a.n_kv + at_once - 1) / at_once;  // few tokens: as many workgroups as a token has heads for
+    const bool sums = a.k_min && !a.seq;
+    const dim3 grid((unsigned)a.T, (unsigned)(a.parts + (sums ? a.n_kv : 0)));
+    const auto kernel = sums ? (wide ? kv_append_kernel<IO, PG, N, true> : kv_append_kernel<IO, PG, 1, true>)
+                             : (wide ? kv_append_kernel<IO, PG, N, false> : kv_append_kernel<IO, PG, 1, false>);
+    launch(K_KV_APPEND, kernel, grid, dim3(kAppThreads), 0, s, a);
+    if (a.k_min && a.seq) launch(K_KV_SUMMARY, kv_summary_kernel<IO, PG>, dim3((unsigned)((a.T + kWave - 1) / kWave), (unsigned)a.n_kv), dim3(kAppThreads), 0, s, a);
 }
 
 int log2_of(int v) { return 31 - __builtin_clz((unsigned)v); }
@@ -394,15 +508,10 @@ extern "C" int kv_append(moei_kv* kv, const moei_kv_pages* pages, const int32_t*
     const int W = 16 / io;
     auto even = [&](const void* p, long long stride) { return (uintptr_t)p % 16 == 0 && stride % W == 0; };
     const bool wide = rot_dim / 2 % W == 0 && even(d_q, a.q_stride) && even(d_k, a.k_row) && even(d_v, a.v_row) && even(d_q_out, 0);
-    const int w = wide ? W : 1;
-    const int units = (d.n_q_heads + d.n_kv_heads) * (rot_dim / 2 / w + (d.k_dim - rot_dim) / w) + d.n_kv_heads * (d.v_dim / w);
-    int parts = (units + kAppThreads - 1) / kAppThreads;  // few tokens: a thread a unit
-    const int enough = (8 * kv->cus + T - 1) / T;
-    if (parts > enough) parts = enough;
     hipStream_t s = as_stream(stream);
-    if (d.dtype == MOEI_WDTYPE_FP32) launch_append<float, float>(a, wide, parts, s);
-    else if (d.dtype == MOEI_WDTYPE_BF16) launch_append<uint16_t, uint16_t>(a, wide, parts, s);
-    else launch_append<uint16_t, uint8_t>(a, wide, parts, s);
+    if (d.dtype == MOEI_WDTYPE_FP32) launch_append<float, float>(a, wide, kv->cus, s);
+    else if (d.dtype == MOEI_WDTYPE_BF16) launch_append<uint16_t, uint16_t>(a, wide, kv->cus, s);
+    else launch_append<uint16_t, uint8_t>(a, wide, kv->cus, s);
     MOEI_LAUNCH_CHECK();
     return MOEI_OK;
 }
