@@ -403,7 +403,7 @@ extern "C" int moei_kv_destroy(moei_kv* kv) {
     if (!kv) return MOEI_OK;
     int dev = -1;
     const bool other = hipGetDevice(&dev) == hipSuccess && dev != kv->device && hipSetDevice(kv->device) == hipSuccess;
-    for (void* p : {(void*)kv->d_part, (void*)kv->d_stat, (void*)kv->d_arrived, (void*)kv->d_keys, (void*)kv->d_scored, (void*)kv->d_list, (void*)kv->d_flags})
+    for (void* p : {(void*)kv->d_part, (void*)kv->d_stat, (void*)kv->d_arrived, (void*)kv->d_keys, (void*)kv->d_scores, (void*)kv->d_scored, (void*)kv->d_list, (void*)kv->d_flags})
         if (p) (void)hipFree(p);
     if (other) (void)hipSetDevice(dev);
     delete kv;
@@ -437,10 +437,10 @@ extern "C" int moei_kv_create(const moei_kv_desc* desc, moei_kv** out) {
     kv->rows = group < kKvHeads ? group : kKvHeads;
     const size_t groups = (size_t)kKvResident * kv->cus, rows = 2 * groups * kv->rows, sel = d.max_sel ? (size_t)d.max_batch * d.n_kv_heads : 0;
     auto room = [&](auto*& p, size_t n) { return n == 0 || (e = hipMalloc(reinterpret_cast<void**>(&p), n * sizeof(*p))) == hipSuccess; };
-    if (!room(kv->d_part, rows * d.v_dim) || !room(kv->d_stat, rows * 2) || !room(kv->d_arrived, groups) || !room(kv->d_keys, sel * d.max_pages) || !room(kv->d_scored, sel) ||
+    if (!room(kv->d_part, rows * d.v_dim) || !room(kv->d_stat, rows * 2) || !room(kv->d_arrived, groups) || !room(kv->d_keys, sel * d.max_pages) || !room(kv->d_scores, sel * d.max_pages) || !room(kv->d_scored, 2 * sel) ||
         !room(kv->d_list, sel * d.max_sel) || !room(kv->d_flags, 1) || (e = hipMemset(kv->d_flags, 0, 4)) != hipSuccess ||
         (e = hipMemset(kv->d_arrived, 0, groups * sizeof(unsigned))) != hipSuccess ||
-        (sel && (e = hipMemset(kv->d_scored, 0, sel * sizeof(unsigned))) != hipSuccess) ||
+        (sel && (e = hipMemset(kv->d_scored, 0, 2 * sel * sizeof(unsigned))) != hipSuccess) ||
         (e = hipDeviceSynchronize()) != hipSuccess) {
         (void)hipGetLastError();
         moei_kv_destroy(kv);
@@ -557,7 +557,9 @@ extern "C" int kv_attend_blocks(moei_kv* kv, const moei_kv_pages* pages, const i
     c.width = table_width; c.page_shift = a.page_shift; c.n_pages = a.n_pages;
     c.n_sel = n_sel; c.keep_first = keep_first; c.keep_last = keep_last;
     c.keys = kv->d_keys;
+    c.scores = kv->d_scores;
     c.arrived = kv->d_scored;
+    c.eps = kv->d_scored + (size_t)kv->d.max_batch * kv->d.n_kv_heads;
     c.list = d_blocks ? d_blocks : kv->d_list;
     c.flags = kv->d_flags;
     rc = launch_kv_blocks(*kv, c, as_stream(stream));

@@ -52,8 +52,10 @@ struct KvBlocksArgs {
     const int32_t* lens;
     int B, n_kv, group, k_dim, width, page_shift, n_pages, n_sel, keep_first, keep_last;
     int per;                   // pages of a workgroup
-    unsigned long long* keys;  // [B][n_kv][width] scratch
-    unsigned* arrived;         // [B][n_kv] workgroups whose keys are there; zero between launches
+    float* scores;             // [B][n_kv][width] scratch: sums in fp32 ...
+    unsigned long long* keys;  // ... and keys of those in 64 bits that the choice needs
+    unsigned* arrived;         // [B][n_kv] workgroups whose scores are there; zero between launches
+    unsigned* eps;             // [B][n_kv] largest error of the scores, fp32 bits; zero between launches
     int32_t* list;             // [B][n_kv][n_sel] out
     int32_t* flags;
 };
@@ -69,7 +71,8 @@ struct moei_kv {
     float* d_stat = nullptr;
     unsigned* d_arrived = nullptr;
     unsigned long long* d_keys = nullptr;
-    unsigned* d_scored = nullptr;
+    float* d_scores = nullptr;
+    unsigned* d_scored = nullptr;  // [2][max_batch][n_kv_heads]
     int32_t* d_list = nullptr;
     int32_t* d_flags = nullptr;
 };
@@ -82,6 +85,19 @@ int launch_kv_blocks(const moei_kv& kv, KvBlocksArgs a, hipStream_t s);
 #if defined(__HIPCC__)
 
 typedef const __attribute__((address_space(4))) int32_t* kv_const_ints;  // uniform reads of memory that the launch doesn't write
+
+// inclusive sum over the lanes
+__device__ __forceinline__ unsigned wave_scan_u32(unsigned v) {
+#define MOEI_DPP_ADD(ctrl, rows) v += (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, rows, 0xF, false)
+    MOEI_DPP_ADD(0x111, 0xF);  // row_shr 1, 2, 4, 8: inside rows of sixteen lanes
+    MOEI_DPP_ADD(0x112, 0xF);
+    MOEI_DPP_ADD(0x114, 0xF);
+    MOEI_DPP_ADD(0x118, 0xF);
+    MOEI_DPP_ADD(0x142, 0xA);  // the rows before
+    MOEI_DPP_ADD(0x143, 0xC);
+#undef MOEI_DPP_ADD
+    return v;
+}
 
 // Two fp32 values rounded to bf16 (nearest, ties to even), the first in the low half.
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {

@@ -53,19 +53,6 @@ __device__ __forceinline__ Span span_of(A a, int len) {
 template <int kUnit>
 __device__ __forceinline__ int units_of(const Span& s) { return max(1, (s.end - s.start + kUnit - 1) / kUnit); }  // (an empty one has its zeros to write)
 
-// inclusive sum over the lanes
-__device__ __forceinline__ unsigned lane_scan(unsigned v) {
-#define MOEI_DPP_ADD(ctrl, rows) v += (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, ctrl, rows, 0xF, false)
-    MOEI_DPP_ADD(0x111, 0xF);  // row_shr 1, 2, 4, 8: inside rows of sixteen lanes
-    MOEI_DPP_ADD(0x112, 0xF);
-    MOEI_DPP_ADD(0x114, 0xF);
-    MOEI_DPP_ADD(0x118, 0xF);
-    MOEI_DPP_ADD(0x142, 0xA);  // the rows before
-    MOEI_DPP_ADD(0x143, 0xC);
-#undef MOEI_DPP_ADD
-    return v;
-}
-
 struct Stretch {
     unsigned per;         // units of a workgroup
     unsigned first, end;  // this one's, in the line
@@ -82,7 +69,7 @@ __device__ __forceinline__ Stretch my_stretch(Args a, int lane) {
     for (int b0 = 0; b0 < a->B; b0 += kWave) {
         len = b0 + lane < a->B ? a->lens[b0 + lane] : 0;
         mine = b0 + lane < a->B ? units_of<kUnit>(span_of(a, len)) * items : 0u;
-        upto = total + lane_scan(mine);
+        upto = total + wave_scan_u32(mine);
         total = __builtin_amdgcn_readlane(upto, kWave - 1);
     }
     Stretch s;
@@ -98,7 +85,7 @@ __device__ __forceinline__ Stretch my_stretch(Args a, int lane) {
         if (a->B > kWave) {
             len = b0 + lane < a->B ? a->lens[b0 + lane] : 0;
             mine = b0 + lane < a->B ? units_of<kUnit>(span_of(a, len)) * items : 0u;
-            upto = before + lane_scan(mine);
+            upto = before + wave_scan_u32(mine);
             before = __builtin_amdgcn_readlane(upto, kWave - 1);
         }
         const unsigned long long who = __ballot(upto > s.first && upto - mine <= s.first);

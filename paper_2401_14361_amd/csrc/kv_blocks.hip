@@ -1,8 +1,9 @@
 // Which pages of a paged KV cache a new token attends to.
 //
 // A page's score for a key/value head is the largest of its query heads' bounds sum_d max(q_d k_min_d, q_d k_max_d): no logit
-// of the page exceeds it.  The sums are formed in 64 bits, where those of bf16 values are exact for all but absurd ranges, so
-// that the choice does not hang on an order of summation.  A few pages at either end are always taken, then the highest scores.
+// of the page exceeds it.  A few pages at either end are always taken, then the highest scores.  The choice is made by the sums
+// in 64 bits, but nearly all pages are told apart by sums in fp32 whose error is bounded: those come from the matrix cores at the rate at
+// which the summaries are read, and only pages so near the last one chosen that their order is open are summed again in 64 bits.
 #include "kv.hpp"
 #include "wtypes.hpp"
 
@@ -10,325 +11,478 @@ namespace moei {
 
 namespace {
 
-constexpr int kScoreWaves = 4;
-constexpr int kScoreThreads = kScoreWaves * kWave;
-constexpr int kScorePages = 512;  // of a workgroup, at most
-constexpr int kQuad = 4;          // query heads whose values a lane holds
-constexpr int kAhead = 3;         // steps whose pages are under way
-constexpr int kHeld = 16;         // keys of a thread in the selection; longer rows are read again from memory
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef unsigned short u16x8 __attribute__((ext_vector_type(8)));
+typedef unsigned long long u64;
 
-__device__ __forceinline__ int kv_length(const KvBlocksArgs& a, int b, bool* bad) {
-    const int len = ((kv_const_ints)(uintptr_t)a.lens)[b];
-    const long long room = (long long)a.width << a.page_shift;
+constexpr int kWaves = 4;
+constexpr int kThreads = kWaves * kWave;
+constexpr int kMostPages = 512;  // of a workgroup
+constexpr int kHeld = 8192;      // scores that the choice keeps in LDS; longer rows are read from memory each time
+constexpr int kFew = kWave;      // pages of open order that are ranked by one wavefront
+
+typedef const __attribute__((address_space(4))) KvBlocksArgs* Args;  // (read where they are used: there are too few scalar registers for all)
+__device__ __forceinline__ Args again(Args p) {
+    asm volatile("" : "+s"(p));
+    return p;
+}
+
+__device__ __forceinline__ int kv_length(Args a, int b, bool* bad) {
+    const int len = ((kv_const_ints)(uintptr_t)a->lens)[b];
+    const long long room = (long long)a->width << a->page_shift;
     *bad = len < 0 || len > room;
     return len < 0 ? 0 : len > room ? (int)room : len;
 }
 
-// 64-bit keys in the order of the scores; a score that is no number goes behind all others
-__device__ __forceinline__ unsigned long long key_of(double s) {
-    const double z = s == s ? s + 0.0 : -INFINITY;
-    const unsigned long long u = __builtin_bit_cast(unsigned long long, z);
+// keys in the order of the scores
+__device__ __forceinline__ unsigned key_of(float s) {
+    const unsigned u = __float_as_uint(s + 0.f);
+    return u >> 31 ? ~u : u | 1u << 31;
+}
+__device__ __forceinline__ float score_of(unsigned k) { return __uint_as_float(k >> 31 ? k & 0x7fffffffu : ~k); }
+__device__ __forceinline__ u64 key_of(double s) {  // a score that is no number goes behind all others
+    const u64 u = __builtin_bit_cast(u64, s == s ? s + 0.0 : -(double)INFINITY);
     return u >> 63 ? ~u : u | 1ull << 63;
 }
+template <typename V>
+__device__ __forceinline__ V load_past(const V* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+template <typename V>
+__device__ __forceinline__ void store_past(V* p, V v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
-template <int ctrl>
-__device__ __forceinline__ double dpp_f64(double v) {
-    const unsigned long long u = __builtin_bit_cast(unsigned long long, v);
-    const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)u, ctrl, 0xF, 0xF, false);
-    const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)(u >> 32), ctrl, 0xF, 0xF, false);
-    return __builtin_bit_cast(double, (unsigned long long)hi << 32 | lo);
-}
-__device__ __forceinline__ double larger(double a, double b) { return b > a || a != a ? b : a; }  // a number, if there is one
-
-// The largest of four heads' sums, each over LP lanes: halves of the lanes keep half of the heads in the first two steps.
-template <int LP>
-__device__ __forceinline__ double sum_and_pick(const double (&s)[kQuad], int lane) {
-    constexpr int kXor1 = 0xB1, kXor2 = 0x4E;  // quad_perm
-    const bool odd = lane & 1, second = lane & 2;
-    // lanes l and l ^ 1 exchange two heads each, then l and l ^ 2 one
-    const double a0 = (odd ? s[2] : s[0]) + dpp_f64<kXor1>(odd ? s[0] : s[2]);
-    const double a1 = (odd ? s[3] : s[1]) + dpp_f64<kXor1>(odd ? s[1] : s[3]);
-    double v = (second ? a1 : a0) + dpp_f64<kXor2>(second ? a0 : a1);
-    // lanes 4 apart hold the same head
-    if constexpr (LP >= 16) {
-        v += dpp_f64<0x124>(v);  // row_ror 4
-        v += dpp_f64<0x128>(v);  // row_ror 8
-    } else {
-        v += __shfl_xor(v, 4, kWave);
-    }
-    if constexpr (LP >= 32) v += __shfl_xor(v, 16, kWave);
-    if constexpr (LP >= 64) v += __shfl_xor(v, 32, kWave);
-    v = larger(v, dpp_f64<kXor1>(v));
-    return larger(v, dpp_f64<kXor2>(v));
-}
-
-// The list of a (sequence, key/value head) from its keys, by one workgroup: the smallest key that is in is found eight bits at a time, from
-// the first bit on in which the keys differ; then the pages are written in ascending order.
-__device__ __forceinline__ void select_pages(const KvBlocksArgs& a, const unsigned long long* keys, int nb, int32_t* out) {
-    const int tid = threadIdx.x, lane = tid & (kWave - 1), wv = tid / kWave;
-    __shared__ int s_count[256];
-    __shared__ int s_found[3];
-    __shared__ unsigned long long s_low[kScoreWaves], s_high[kScoreWaves];
-    __shared__ int s_equal[kScoreWaves], s_in[kScoreWaves];
-    const int lo = a.keep_first, hi = nb - a.keep_last;
-    int need = a.n_sel - a.keep_first - a.keep_last;
-    const bool held = hi - lo <= kHeld * kScoreThreads;
-    unsigned long long mine[kHeld];
-    auto key_at = [&](int i) { return __hip_atomic_load(&keys[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); };  // (written by other workgroups of this launch)
-    unsigned long long cut = ~0ull;  // keys whose highest bits exceed it are in; of those that have it the first `need`
-    int shift = 0;
-    if (need > 0) {
-        unsigned long long low = ~0ull, high = 0ull;
-        if (held) {
-#pragma unroll
-            for (int j = 0; j < kHeld; ++j) {
-                const int i = lo + j * kScoreThreads + tid;
-                mine[j] = i < hi ? key_at(i) : 0ull;
-            }
-#pragma unroll
-            for (int j = 0; j < kHeld; ++j)
-                if (lo + j * kScoreThreads + tid < hi) {
-                    low = mine[j] < low ? mine[j] : low;
-                    high = mine[j] > high ? mine[j] : high;
-                }
-        } else {
-            for (int i = lo + tid; i < hi; i += kScoreThreads) {
-                const unsigned long long k = key_at(i);
-                low = k < low ? k : low;
-                high = k > high ? k : high;
-            }
-        }
-#pragma unroll
-        for (int off = 32; off > 0; off >>= 1) {
-            const unsigned long long l = __shfl_xor(low, off, kWave), h = __shfl_xor(high, off, kWave);
-            low = l < low ? l : low;
-            high = h > high ? h : high;
-        }
-        if (lane == 0) {
-            s_low[wv] = low;
-            s_high[wv] = high;
-        }
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < kScoreWaves; ++w) {
-            low = s_low[w] < low ? s_low[w] : low;
-            high = s_high[w] > high ? s_high[w] : high;
-        }
-        const unsigned long long differ = low ^ high;
-        int bits = differ ? __clzll(differ) : 64;  // the highest bits that all keys share
-        cut = bits == 0 ? 0ull : bits == 64 ? high : high >> (64 - bits);
-        while (bits < 64) {
-            const int step = min(8, 64 - bits), down = 64 - bits - step;
-            for (int i = tid; i < 256; i += kScoreThreads) s_count[i] = 0;
-            __syncthreads();
-            auto count = [&](unsigned long long k) {
-                if (bits == 0 || k >> (64 - bits) == cut) atomicAdd(&s_count[(k >> down) & ((1u << step) - 1)], 1);
-            };
-            if (held) {
-#pragma unroll
-                for (int j = 0; j < kHeld; ++j)
-                    if (lo + j * kScoreThreads + tid < hi) count(mine[j]);
-            } else {
-                for (int i = lo + tid; i < hi; i += kScoreThreads) count(key_at(i));
-            }
-            __syncthreads();
-            if (wv == 0) {  // four bins a lane, from the highest down: the bin in which the count reaches `need`
-                int c[4], sum = 0;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) sum += c[j] = s_count[255 - 4 * lane - j];
-                int upto = sum;
-#pragma unroll
-                for (int off = 1; off < kWave; off <<= 1) {
-                    const int up = __shfl_up(upto, off, kWave);
-                    if (lane >= off) upto += up;
-                }
-                int before = upto - sum;
-                if (before < need && upto >= need) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        if (before < need && before + c[j] >= need) {
-                            s_found[0] = 255 - 4 * lane - j;
-                            s_found[1] = before;
-                            s_found[2] = c[j];
-                        }
-                        before += c[j];
-                    }
-                }
-            }
-            __syncthreads();
-            cut = cut << step | (unsigned)s_found[0];
-            need -= s_found[1];
-            bits += step;
-            if (s_found[2] == need) break;  // every key with these bits is in
-            __syncthreads();
-        }
-        shift = 64 - bits;
-    }
-    int written = 0, equal_before = 0;
-    const unsigned long long below = (1ull << lane) - 1;
-    auto place = [&](int i, unsigned long long key) {  // pages of one step, a thread each
-        bool in = i < nb && (i < lo || i >= hi), equal = false;
-        if (i >= lo && i < hi) {
-            in = key >> shift > cut;
-            equal = key >> shift == cut && need > 0;
-        }
-        const unsigned long long eq = __ballot(equal);
-        if (lane == 0) s_equal[wv] = __popcll(eq);
-        __syncthreads();
-        int e = equal_before;
-#pragma unroll
-        for (int w = 0; w < kScoreWaves; ++w) {
-            e += w < wv ? s_equal[w] : 0;
-            equal_before += s_equal[w];
-        }
-        if (equal && e + __popcll(eq & below) < need) in = true;
-        const unsigned long long ins = __ballot(in);
-        if (lane == 0) s_in[wv] = __popcll(ins);
-        __syncthreads();
-        int at = written;
-#pragma unroll
-        for (int w = 0; w < kScoreWaves; ++w) {
-            at += w < wv ? s_in[w] : 0;
-            written += s_in[w];
-        }
-        at += __popcll(ins & below);
-        if (in && at < a.n_sel) out[at] = i;
-    };
-    for (int i0 = 0; i0 < lo; i0 += kScoreThreads) place(i0 + tid < lo ? i0 + tid : nb, 0ull);
-    if (need > 0 || a.n_sel > a.keep_first + a.keep_last) {
-        if (held) {
-#pragma unroll
-            for (int j = 0; j < kHeld; ++j)
-                if (lo + j * kScoreThreads < hi) {
-                    const int i = lo + j * kScoreThreads + tid;
-                    place(i < hi ? i : nb, mine[j]);
-                }
-        } else {
-            for (int i0 = lo; i0 < hi; i0 += kScoreThreads) {
-                const int i = i0 + tid;
-                place(i < hi ? i : nb, i < hi ? key_at(i) : 0ull);
-            }
-        }
-    }
-    for (int i0 = hi; i0 < nb; i0 += kScoreThreads) place(i0 + tid, 0ull);
-}
-
-// LP lanes share a page, a 16-byte piece of its summary each.  A wavefront has kQuad query heads in registers, in 64 bits and split by
-// sign; wavefronts share the group's heads out among them, and the pages where there are wavefronts left.  The last
-// workgroup of a (sequence, key/value head) to store its keys selects.
+// ------------------------------------------------------------------------------------------------ scores in 64 bits
+// The exact keys of up to kWave / LP pages by one wavefront: LP lanes share a page (`pg`, the same in all of them; -1: none), 16 bytes of its
+// summary each.  All of a page's lanes get its key.
 template <typename IO, int LP>
-__global__ void __launch_bounds__(kScoreThreads, 2) kv_blocks_kernel(KvBlocksArgs a) {
-    constexpr int VE = WVec<IO>::N, kPer = kWave / LP;  // pages of a step
+__device__ __forceinline__ u64 exact_key(Args a, int b, int hk, int pg, int lane) {
+    constexpr int VE = WVec<IO>::N;
+    const int d0 = (lane & (LP - 1)) * VE;
+    const bool in = d0 < a->k_dim;
+    const IO* q = static_cast<const IO*>(a->q) + (long long)b * a->q_stride + (long long)hk * a->group * a->k_dim + d0;
+    const int at = pg >= 0 ? a->table[(long long)b * a->width + pg] : -1;
+    const bool ok = at >= 0 && at < a->n_pages;
+    float lo[VE], hi[VE];
+    const long long row = ((long long)at * a->n_kv + hk) * a->k_dim + d0;
+    WVec<IO>::unpack(ok && in ? WVec<IO>::load(static_cast<const IO*>(a->k_min) + row) : WVec<IO>::zero(), lo);
+    WVec<IO>::unpack(ok && in ? WVec<IO>::load(static_cast<const IO*>(a->k_max) + row) : WVec<IO>::zero(), hi);
+    double best = -(double)INFINITY;
+    for (int h = 0; h < a->group; ++h) {
+        float x[VE];
+        WVec<IO>::unpack(in ? WVec<IO>::load(q + h * a->k_dim) : WVec<IO>::zero(), x);
+        double sum = 0.0;
+#pragma unroll
+        for (int j = 0; j < VE; ++j) sum = __builtin_fma((double)x[j], (double)(x[j] > 0.f ? hi[j] : lo[j]), sum);
+#pragma unroll
+        for (int off = 1; off < LP; off <<= 1) sum += __shfl_xor(sum, off, kWave);
+        best = sum > best ? sum : best;
+    }
+    return ok ? key_of(best) : key_of(-(double)INFINITY);
+}
+
+// ------------------------------------------------------------------------------------------------ the choice
+struct Shared {
+    int count[256];
+    int found[2];
+    unsigned low[kWaves], high[kWaves];
+    int sure[kWaves], in[kWaves], equal[kWaves];
+    int n_few;
+    int few[kFew];  // pages whose order is open
+    u64 key[kFew];
+    unsigned held[kHeld];
+};
+
+// The need-th largest of the keys that `each` hands to its argument, found eight bits at a time from the first bit on in which
+// they differ; *need becomes its number among the keys equal to it.
+template <typename K, typename E>
+__device__ __forceinline__ K nth_largest(Shared& sh, K low, K high, E each, int* need, int tid) {
+    const int lane = tid & (kWave - 1);
+    constexpr int kBits = sizeof(K) * 8;
+    const K differ = low ^ high;
+    int bits = differ == 0 ? kBits : sizeof(K) == 8 ? __clzll((long long)differ) : __clz((int)differ);  // the highest bits that all keys share
+    K cut = bits == 0 ? 0 : high >> (kBits - bits);
+    while (bits < kBits) {
+        const int step = min(8, kBits - bits), down = kBits - bits - step;
+        sh.count[tid] = 0;
+        barrier_lds();
+        each([&](K k) __attribute__((always_inline)) {
+            if (bits == 0 || k >> (kBits - bits) == cut) atomicAdd(&sh.count[(int)(k >> down) & ((1 << step) - 1)], 1);
+        });
+        barrier_lds();
+        if (tid < kWave) {  // four bins a lane, from the highest down: the bin in which the count reaches `need`
+            int c[4], sum = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum += c[j] = sh.count[255 - 4 * lane - j];
+            int upto = (int)wave_scan_u32((unsigned)sum);
+            int before = upto - sum;
+            if (before < *need && upto >= *need) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (before < *need && before + c[j] >= *need) {
+                        sh.found[0] = 255 - 4 * lane - j;
+                        sh.found[1] = before;
+                    }
+                    before += c[j];
+                }
+            }
+        }
+        barrier_lds();
+        cut = cut << step | (K)sh.found[0];
+        *need -= sh.found[1];
+        bits += step;
+    }
+    return cut;
+}
+
+// The list of a (sequence, key/value head) from its scores in fp32, whose error is at most `eps`, by one workgroup.
+template <typename IO, int LP>
+__device__ __forceinline__ void choose(Args a, Shared& sh, long long row, int b, int hk, int nb, float eps, int32_t* out) {
+    const int tid = threadIdx.x, lane = tid & (kWave - 1);
+    const int wv = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int lo = a->keep_first, n = nb - a->keep_last - lo;
+    const int want = a->n_sel - a->keep_first - a->keep_last;
+    for (int i = tid; i < lo; i += kThreads) out[i] = i;
+    for (int i = tid; i < a->keep_last; i += kThreads) out[lo + want + i] = lo + n + i;
+    if (want == 0) return;
+    const float* scores = a->scores + row * a->width + lo;
+    u64* keys = a->keys + row * a->width + lo;
+    const bool held = n <= kHeld;
+    auto key_at = [&](int i) __attribute__((always_inline)) { return held ? sh.held[i] : key_of(load_past(&scores[i])); };
+
+    unsigned low = ~0u, high = 0u;
+#pragma unroll 4
+    for (int i = tid; i < n; i += kThreads) {
+        const unsigned k = key_of(load_past(&scores[i]));
+        if (held) sh.held[i] = k;
+        low = min(low, k);
+        high = max(high, k);
+    }
+    low = wave_min_u32_dpp(low);
+    high = ~wave_min_u32_dpp(~high);
+    if (lane == 0) {
+        sh.low[wv] = low;
+        sh.high[wv] = high;
+    }
+    if (tid == 0) sh.n_few = 0;
+    barrier_lds();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        low = min(low, sh.low[w]);
+        high = max(high, sh.high[w]);
+    }
+    unsigned above = ~0u, below = 0u;  // keys over `above` are in, keys under `below` out, those between are open
+    if (eps < INFINITY) {              // (else something was no number, or infinite: all are open)
+        int need = want;
+        const float t = score_of(nth_largest<unsigned>(sh, low, high, [&](auto f) __attribute__((always_inline)) {
+            for (int i = tid; i < n; i += kThreads) f(key_at(i));
+        }, &need, tid));
+        // The want-th largest exact score lies within eps of t: what is further than 2 eps from t lies on its side of it.  (Rounded outward.)
+        const float up = t + 2.f * eps, down = t - 2.f * eps;
+        above = key_of(up + fabsf(up) * 0x1p-22f);
+        below = key_of(down - fabsf(down) * 0x1p-22f);
+    }
+    int n_in = 0;
+    for (int i = tid; i < n; i += kThreads) {
+        const unsigned k = key_at(i);
+        n_in += k > above;
+        if (k <= above && k >= below) {
+            const int at = atomicAdd(&sh.n_few, 1);
+            if (at < kFew) sh.few[at] = i;
+        }
+    }
+    n_in = (int)wave_sum_u32_dpp((unsigned)n_in);
+    if (lane == 0) sh.sure[wv] = n_in;
+    barrier_lds();
+    int rest = want;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) rest -= sh.sure[w];  // how many of the open ones are in
+    const int all_open = sh.n_few;
+    constexpr int kPer = kWave / LP;  // pages of a wavefront at a time, in 64 bits
+    unsigned line = below;            // keys from here on are in
+    bool by_key = false;              // ... and open ones by their exact keys in memory: above `cut`, or equal to it and among the first `rest`
+    u64 cut = 0;
+    if (all_open != rest) {
+        line = above + 1;
+        if (all_open <= kFew && held) {
+            for (int i0 = wv * kPer; i0 < all_open; i0 += kWaves * kPer) {
+                const int i = i0 + lane / LP;
+                const u64 k = exact_key<IO, LP>(a, b, hk, i < all_open ? lo + sh.few[i] : -1, lane);
+                if ((lane & (LP - 1)) == 0 && i < all_open) sh.key[i] = k;
+            }
+            barrier_lds();
+            if (tid < all_open) {  // (they stand in no order: equal ones go by their pages)
+                const u64 k = sh.key[tid];
+                const int me = sh.few[tid];
+                int better = 0;
+                for (int j = 0; j < all_open; ++j) better += sh.key[j] > k || (sh.key[j] == k && sh.few[j] < me);
+                sh.held[me] = better < rest ? ~0u : 0u;
+            }
+            if (above == ~0u) line = ~0u;  // (all were open)
+            barrier_lds();
+        } else {
+            by_key = true;
+            if (above == ~0u) line = ~0u;  // no key reaches it: a score has no such bits
+            u64 lowest = ~0ull, highest = 0ull;
+            for (int i0 = wv * kPer; i0 < n; i0 += kWaves * kPer) {
+                const int i = i0 + lane / LP;
+                const unsigned s = i < n ? key_at(i) : 0u;
+                const bool open = i < n && s <= above && s >= below;
+                if (!__ballot(open)) continue;
+                const u64 k = exact_key<IO, LP>(a, b, hk, open ? lo + i : -1, lane);
+                if (open) {
+                    lowest = k < lowest ? k : lowest;
+                    highest = k > highest ? k : highest;
+                    if ((lane & (LP - 1)) == 0) store_past(&keys[i], k);
+                }
+            }
+#pragma unroll
+            for (int off = 32; off > 0; off >>= 1) {
+                const u64 l = __shfl_xor(lowest, off, kWave), h = __shfl_xor(highest, off, kWave);
+                lowest = l < lowest ? l : lowest;
+                highest = h > highest ? h : highest;
+            }
+            if (lane == 0) {
+                sh.key[wv] = lowest;
+                sh.key[kWaves + wv] = highest;
+            }
+            wait_vm_fence<0>();  // the keys are there
+            barrier_lds();
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                lowest = sh.key[w] < lowest ? sh.key[w] : lowest;
+                highest = sh.key[kWaves + w] > highest ? sh.key[kWaves + w] : highest;
+            }
+            cut = nth_largest<u64>(sh, lowest, highest, [&](auto f) __attribute__((always_inline)) {
+                for (int i = tid; i < n; i += kThreads) {
+                    const unsigned k = key_at(i);
+                    if (k <= above && k >= below) f(load_past(&keys[i]));
+                }
+            }, &rest, tid);
+        }
+    }
+    // A wavefront writes a run of the pages, behind those of the wavefronts before it.
+    const int run = (n + kThreads - 1) / kThreads * kWave, from = wv * run, to = min(n, from + run);
+    int at = lo, equal_before = 0;
+    for (int pass = 0; pass < 2; ++pass) {  // counted, then written
+        int in_here = 0, equal_here = 0;
+        for (int i0 = from; i0 < to; i0 += kWave) {
+            const int i = i0 + lane;
+            const unsigned k = i < to ? key_at(i) : 0u;
+            bool in = i < to && k >= line, equal = false;
+            if (by_key && i < to && k <= above && k >= below) {
+                const u64 e = load_past(&keys[i]);
+                in = e > cut;
+                equal = e == cut;
+            }
+            const u64 eq = __ballot(equal), under = (1ull << lane) - 1;
+            if (pass) {
+                in |= equal && equal_before + __popcll(eq & under) < rest;
+                const u64 ins = __ballot(in);
+                if (in) out[at + __popcll(ins & under)] = lo + i;
+                at += __popcll(ins);
+                equal_before += __popcll(eq);
+            } else {
+                in_here += __popcll(__ballot(in));
+                equal_here += __popcll(eq);
+            }
+        }
+        if (pass == 0) {
+            if (lane == 0) {
+                sh.in[wv] = in_here;
+                sh.equal[wv] = equal_here;
+            }
+            barrier_lds();
+            for (int w = 0; w < wv; ++w) {
+                at += sh.in[w] + max(0, min(sh.equal[w], rest - equal_before));
+                equal_before += sh.equal[w];
+            }
+            if (!by_key) equal_before = 0;
+        }
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ scores in fp32
+// 64 bytes of a summary's row are a unit: a 16-byte piece for each of the four lane groups, as the first operand of the matrix
+// instructions (sixteen pages); the query heads, sixteen at a time and split by sign, are the second one.
+template <typename IO, int KC>
+struct Mm {
+    static constexpr int kUnits = KC * (int)sizeof(IO) / 64;
+    static __device__ __forceinline__ f32x4 mul(u32x4 x, u32x4 y, f32x4 c) {
+        if constexpr (sizeof(IO) == 2) {
+            return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), c, 0, 0, 0);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x[j]), __uint_as_float(y[j]), c, 0, 0, 0);
+            return c;
+        }
+    }
+    static __device__ __forceinline__ u32x4 magnitude(u32x4 x) { return x & (sizeof(IO) == 2 ? 0x7fff7fffu : 0x7fffffffu); }
+    static __device__ __forceinline__ u32x4 larger(u32x4 x, u32x4 y) {  // of magnitudes
+        if constexpr (sizeof(IO) == 2) return __builtin_bit_cast(u32x4, __builtin_elementwise_max(__builtin_bit_cast(u16x8, x), __builtin_bit_cast(u16x8, y)));
+        else return __builtin_elementwise_max(x, y);
+    }
+    // the elements that are positive
+    static __device__ __forceinline__ u32x4 positive(u32x4 x) {
+        if constexpr (sizeof(IO) == 2) {
+            typedef short s16x8 __attribute__((ext_vector_type(8)));
+            const s16x8 v = __builtin_bit_cast(s16x8, x);
+            return __builtin_bit_cast(u32x4, __builtin_elementwise_max(v, s16x8{}));
+        } else {
+            typedef int i32x4 __attribute__((ext_vector_type(4)));
+            return __builtin_bit_cast(u32x4, __builtin_elementwise_max(__builtin_bit_cast(i32x4, x), i32x4{}));
+        }
+    }
+};
+#define MOEI_ROW_MAX(v, ctrl) v = fmaxf(v, MOEI_DPP_F32(v, ctrl))
+__device__ __forceinline__ float row_max(float v) {  // over sixteen lanes
+    MOEI_ROW_MAX(v, 0xB1);
+    MOEI_ROW_MAX(v, 0x4E);
+    MOEI_ROW_MAX(v, 0x141);
+    MOEI_ROW_MAX(v, 0x140);
+    return v;
+}
+#undef MOEI_ROW_MAX
+
+// A workgroup scores a share of a (sequence, key/value head)'s pages, a wavefront sixteen at a time; the last workgroup of a head to store its
+// scores chooses.
+//
+// The error of a score: 2 k_dim products, exact for bf16, are added in fp32 in some order; each addition is off by at most 2^-23 of what
+// the magnitudes sum up to (twice what rounding to nearest would allow), as is an fp32 product: (4 k_dim + 4) 2^-23 sum_d |q_d| max(|k_min_d|, |k_max_d|),
+// which is summed up alongside.  Products and elements below the normal range may be lost: 2^-125 of the largest query for each.
+template <typename IO, int KC, int LP>
+__global__ void __launch_bounds__(kThreads, KC > 128 ? 1 : 3) kv_blocks_kernel(KvBlocksArgs) {
+    const Args a = (Args)__builtin_amdgcn_kernarg_segment_ptr();
+    using M = Mm<IO, KC>;
+    constexpr int VE = 16 / sizeof(IO);
     const int b = blockIdx.z, hk = blockIdx.y, x = blockIdx.x;
     const long long row = (long long)b * gridDim.y + hk;
-    const int tid = threadIdx.x, lane = tid & (kWave - 1);
+    const int tid = threadIdx.x, lane = tid & (kWave - 1), col = lane & 15, grp = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(tid / kWave);
     bool bad;
     const int len = kv_length(a, b, &bad);
-    const int nb = (len + (1 << a.page_shift) - 1) >> a.page_shift;
-    int32_t* out = a.list + row * a.n_sel;
-    if (nb <= a.n_sel) {  // all are taken
+    const int nb = (len + (1 << a->page_shift) - 1) >> a->page_shift;
+    int32_t* out = a->list + row * a->n_sel;
+    if (nb <= a->n_sel) {  // all are taken
         if (x == 0) {
-            for (int i = tid; i < a.n_sel; i += kScoreThreads) out[i] = i < nb ? i : -1;
-            if (bad && hk == 0 && tid == 0) atomicOr(a.flags, kKvBadLength);
+            for (int i = tid; i < a->n_sel; i += kThreads) out[i] = i < nb ? i : -1;
+            if (bad && hk == 0 && tid == 0) atomicOr(a->flags, kKvBadLength);
         }
         return;
     }
-    const bool none = a.n_sel == a.keep_first + a.keep_last;  // nothing is left to choose
-    const int lo = a.keep_first, hi = nb - a.keep_last;
-    const int x0 = none ? 0 : lo / a.per, x1 = none ? 0 : (hi - 1) / a.per;  // the workgroups that have pages
+    const bool none = a->n_sel == a->keep_first + a->keep_last;  // nothing is left to choose
+    const int lo = a->keep_first, hi = nb - a->keep_last;
+    const int x0 = none ? 0 : lo / a->per, x1 = none ? 0 : (hi - 1) / a->per;  // the workgroups that have pages
     if (x < x0 || x > x1) return;
-    if (bad && hk == 0 && x == x0 && tid == 0) atomicOr(a.flags, kKvBadLength);
-    const int from = max(lo, x * a.per), to = min(hi, (x + 1) * a.per);
-    __shared__ double s_best[kScoreWaves][kScorePages];
-    __shared__ unsigned s_arrived;
+    if (bad && hk == 0 && x == x0 && tid == 0) atomicOr(a->flags, kKvBadLength);
+    __shared__ Shared sh;
+    __shared__ float s_score[kMostPages];
+    __shared__ float s_eps[kWaves];
+    __shared__ unsigned s_arrived, s_row_eps;
+    float eps = 0.f;
     if (!none) {
-        const int quads = (a.group + kQuad - 1) / kQuad;
-        const int split = quads >= 3 ? 4 : quads;  // wavefronts that share the heads out
-        const int my_quad = wv & (split - 1), my_pages = wv / split, page_waves = kScoreWaves / split;
-        const int piece = lane & (LP - 1), sub = lane / LP;
-        const int d0 = piece * VE;
-        const bool in = d0 < a.k_dim;
-        const IO* q = static_cast<const IO*>(a.q) + (long long)b * a.q_stride + (long long)hk * a.group * a.k_dim;
-        const IO *lows = static_cast<const IO*>(a.k_min) + (long long)hk * a.k_dim + d0, *highs = static_cast<const IO*>(a.k_max) + (long long)hk * a.k_dim + d0;
-        const int32_t* table = a.table + (long long)b * a.width;
-        const long long page_row = (long long)gridDim.y * a.k_dim;
-        for (int i = tid; i < to - from; i += kScoreThreads)
+        const int from = max(lo, x * a->per), to = min(hi, (x + 1) * a->per);
+        const IO* q0 = static_cast<const IO*>(a->q) + (long long)b * a->q_stride + (long long)hk * a->group * a->k_dim;
+        const long long page_row = (long long)gridDim.y * a->k_dim;
+        const IO *lows = static_cast<const IO*>(a->k_min) + (long long)hk * a->k_dim, *highs = static_cast<const IO*>(a->k_max) + (long long)hk * a->k_dim;
+        bool odd = false;     // something is no number, infinite, or a query element below the normal range
+        float most = 0.f;     // largest bound of the magnitudes
+        float biggest = 0.f;  // largest query element
+        bool lost = false;
+        for (int h0 = 0; h0 < a->group; h0 += kKvHeads) {
+            u32x4 up[M::kUnits], down[M::kUnits];
+            {
+                const IO* src = q0 + (long long)min(h0 + col, a->group - 1) * a->k_dim;  // (a repeated head changes no maximum)
 #pragma unroll
-            for (int w = 0; w < kScoreWaves; ++w) s_best[w][i] = -INFINITY;
-        __syncthreads();
-        const int step = page_waves * kPer, first = from + my_pages * kPer + sub;
-        for (int quad = my_quad; quad < quads; quad += split) {
-            double up[kQuad][VE], down[kQuad][VE];
-#pragma unroll
-            for (int h = 0; h < kQuad; ++h) {
-                float v[VE];
-                const int head = min(quad * kQuad + h, a.group - 1);  // (a repeated head changes no maximum)
-                WVec<IO>::unpack(in ? WVec<IO>::load(q + (long long)head * a.k_dim + d0) : WVec<IO>::zero(), v);
-#pragma unroll
-                for (int j = 0; j < VE; ++j) {
-                    up[h][j] = v[j] > 0.f ? (double)v[j] : 0.0;
-                    down[h][j] = v[j] > 0.f ? 0.0 : (double)v[j];
-                }
-            }
-            typename WVec<IO>::raw rl[kAhead], rh[kAhead];
-            bool there[kAhead];
-            auto fetch = [&](int slot, int pg) {
-                const int at = pg < to ? table[pg] : -1;
-                there[slot] = at >= 0 && at < a.n_pages;
-                const bool ok = there[slot] && in;
-                rl[slot] = ok ? WVec<IO>::load(lows + at * page_row) : WVec<IO>::zero();
-                rh[slot] = ok ? WVec<IO>::load(highs + at * page_row) : WVec<IO>::zero();
-            };
-#pragma unroll
-            for (int s = 0; s < kAhead; ++s) fetch(s, first + s * step);
-            for (int p0 = first; __ballot(p0 < to); p0 += kAhead * step) {
-#pragma unroll
-                for (int s = 0; s < kAhead; ++s) {
-                    const int pg = p0 + s * step;
-                    double sum[kQuad] = {};
-                    float l[VE], h[VE];
-                    WVec<IO>::unpack(rl[s], l);
-                    WVec<IO>::unpack(rh[s], h);
-                    const bool ok = there[s];
-                    fetch(s, pg + kAhead * step);
+                for (int u = 0; u < M::kUnits; ++u) {
+                    const int d = (4 * u + grp) * VE;
+                    u32x4 v{};
+                    if (d < a->k_dim) v = *reinterpret_cast<const u32x4*>(src + d);
+                    up[u] = M::positive(v);
+                    down[u] = v ^ up[u];
+                    float f[VE];
+                    if constexpr (sizeof(IO) == 2) WVec<IO>::unpack(make_uint4(v[0], v[1], v[2], v[3]), f);
+                    else WVec<IO>::unpack(make_float4(__uint_as_float(v[0]), __uint_as_float(v[1]), __uint_as_float(v[2]), __uint_as_float(v[3])), f);
 #pragma unroll
                     for (int j = 0; j < VE; ++j) {
-                        const double dl = l[j], dh = h[j];
-#pragma unroll
-                        for (int i = 0; i < kQuad; ++i) sum[i] = __builtin_fma(up[i][j], dh, __builtin_fma(down[i][j], dl, sum[i]));
+                        const float m = fabsf(f[j]);
+                        odd |= !(m < INFINITY) || (m < 0x1p-126f && m != 0.f);
+                        biggest = fmaxf(biggest, m);
                     }
-                    const double best = sum_and_pick<LP>(sum, lane);
-                    if (piece == 0 && pg < to) {
-                        if (!ok) atomicOr(a.flags, kKvBadPage);
-                        double& mine = s_best[wv][pg - from];
-                        mine = ok && best > mine ? best : mine;  // (a page has one place in a wavefront's row)
+                }
+            }
+            u32x4 l[M::kUnits], h[M::kUnits];
+            bool there = false;
+            const int32_t* table = a->table + (long long)b * a->width;
+            int at = from + wv * 16 + col < to ? table[from + wv * 16 + col] : -1;
+            auto fetch = [&](int p0) __attribute__((always_inline)) {  // summaries of sixteen pages, lane col's
+                there = at >= 0 && at < a->n_pages;
+                const long long r = at * page_row;
+#pragma unroll
+                for (int u = 0; u < M::kUnits; ++u) {
+                    const int d = (4 * u + grp) * VE;
+                    l[u] = h[u] = u32x4{};
+                    if (there && d < a->k_dim) {
+                        l[u] = *reinterpret_cast<const u32x4*>(lows + r + d);
+                        h[u] = *reinterpret_cast<const u32x4*>(highs + r + d);
+                    }
+                }
+                const int pg = p0 + kWaves * 16 + col;  // the pages behind
+                at = pg < to ? table[pg] : -1;
+            };
+            for (int p0 = from + wv * 16; p0 < to; p0 += kWaves * 16) {
+                fetch(p0);
+                f32x4 s{}, m{};
+                lost |= !there && p0 + col < to;
+#pragma unroll
+                for (int u = 0; u < M::kUnits; ++u) {
+                    s = M::mul(h[u], up[u], s);
+                    s = M::mul(l[u], down[u], s);
+                    m = M::mul(M::larger(M::magnitude(l[u]), M::magnitude(h[u])), M::magnitude(up[u] | down[u]), m);
+                }
+                const unsigned long long have = __ballot(there);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {  // lane (col, grp) holds head col's sums of pages 4 grp + r
+                    odd |= !(m[r] < INFINITY);
+                    most = fmaxf(most, m[r]);
+                    const float best = row_max(s[r]);
+                    const int pg = p0 + 4 * grp + r;
+                    if (col == 0 && pg < to) {
+                        const float old = h0 ? s_score[pg - from] : -INFINITY;
+                        s_score[pg - from] = have >> (4 * grp + r) & 1 ? fmaxf(old, best) : -INFINITY;
                     }
                 }
             }
         }
-        __syncthreads();
-        for (int i = tid; i < to - from; i += kScoreThreads) {
-            double best = s_best[0][i];
+        if (lost) atomicOr(a->flags, kKvBadPage);
+        eps = (4 * a->k_dim + 4) * 0x1p-23f * 1.01f * wave_max_dpp(most) + a->k_dim * 0x1p-125f * (wave_max_dpp(biggest) + 1.f);
+        if (__ballot(odd) || !(eps < INFINITY)) eps = INFINITY;
+        if (lane == 0) s_eps[wv] = eps;
+        barrier_lds();
 #pragma unroll
-            for (int w = 1; w < kScoreWaves; ++w) best = s_best[w][i] > best ? s_best[w][i] : best;
-            __hip_atomic_store(&a.keys[row * a.width + from + i], key_of(best), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // past the caches
-        }
+        for (int w = 0; w < kWaves; ++w) eps = fmaxf(eps, s_eps[w]);
+        for (int i = tid; i < to - from; i += kThreads) store_past(&a->scores[row * a->width + from + i], s_score[i]);  // past the caches
         if (x1 > x0) {
-            wait_vm_fence<0>();  // the keys have arrived before they are counted
-            __syncthreads();
+            if (tid == 0) (void)__hip_atomic_fetch_max(&a->eps[row], __float_as_uint(eps), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            wait_vm_fence<0>();  // scores and error have arrived before they are counted
+            barrier_lds();
             if (tid == 0) {
-                s_arrived = __hip_atomic_fetch_add(&a.arrived[row], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                if (s_arrived == (unsigned)(x1 - x0)) __hip_atomic_store(&a.arrived[row], 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);  // for the next launch
+                const unsigned n = __hip_atomic_fetch_add(&a->arrived[row], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                s_arrived = n == (unsigned)(x1 - x0);
+                if (s_arrived) {
+                    s_row_eps = load_past(&a->eps[row]);
+                    store_past(&a->eps[row], 0u);  // both for the next launch
+                    store_past(&a->arrived[row], 0u);
+                }
             }
-            __syncthreads();
-            if (s_arrived != (unsigned)(x1 - x0)) return;
+            barrier_lds();
+            if (!s_arrived) return;
+            eps = __uint_as_float(s_row_eps);
         } else {
             wait_vm_fence<0>();
-            __syncthreads();
+            barrier_lds();
         }
     }
-    select_pages(a, a.keys + row * a.width, nb, out);
+    choose<IO, LP>(again(a), sh, row, b, hk, nb, eps, out);
 }
 
 }  // namespace
@@ -337,12 +491,12 @@ int launch_kv_blocks(const moei_kv& kv, KvBlocksArgs a, hipStream_t s) {
     // Pages of a workgroup: about four workgroups a compute unit where there are enough, a step of every wavefront at least.
     const long long all = (long long)a.width * a.n_kv * a.B;
     long long per = (all / (4 * kv.cus) + 63) / 64 * 64;
-    a.per = (int)(per < 64 ? 64 : per > kScorePages ? kScorePages : per);
-    const dim3 grid((unsigned)((a.width + a.per - 1) / a.per), (unsigned)a.n_kv, (unsigned)a.B), block(kScoreThreads);
+    a.per = (int)(per < 64 ? 64 : per > kMostPages ? kMostPages : per);
+    const dim3 grid((unsigned)((a.width + a.per - 1) / a.per), (unsigned)a.n_kv, (unsigned)a.B), block(kThreads);
     if (kv.d.dtype == MOEI_WDTYPE_FP32)
-        launch(K_KV_BLOCKS, a.k_dim <= 64 ? kv_blocks_kernel<float, 16> : a.k_dim <= 128 ? kv_blocks_kernel<float, 32> : kv_blocks_kernel<float, 64>, grid, block, 0, s, a);
+        launch(K_KV_BLOCKS, a.k_dim <= 64 ? kv_blocks_kernel<float, 64, 16> : a.k_dim <= 128 ? kv_blocks_kernel<float, 128, 32> : kv_blocks_kernel<float, 256, 64>, grid, block, 0, s, a);
     else
-        launch(K_KV_BLOCKS, a.k_dim <= 64 ? kv_blocks_kernel<uint16_t, 8> : a.k_dim <= 128 ? kv_blocks_kernel<uint16_t, 16> : kv_blocks_kernel<uint16_t, 32>, grid, block, 0, s, a);
+        launch(K_KV_BLOCKS, a.k_dim <= 64 ? kv_blocks_kernel<uint16_t, 64, 8> : a.k_dim <= 128 ? kv_blocks_kernel<uint16_t, 128, 16> : kv_blocks_kernel<uint16_t, 256, 32>, grid, block, 0, s, a);
     MOEI_LAUNCH_CHECK();
     return MOEI_OK;
 }
