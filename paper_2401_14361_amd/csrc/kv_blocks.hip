@@ -52,6 +52,13 @@ template <typename V>
 __device__ __forceinline__ void store_past(V* p, V v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
 // ------------------------------------------------------------------------------------------------ scores in 64 bits
+template <int ctrl>
+__device__ __forceinline__ double dpp_f64(double v) {
+    const u64 u = __builtin_bit_cast(u64, v);
+    const unsigned lo = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)u, ctrl, 0xF, 0xF, false);
+    const unsigned hi = (unsigned)__builtin_amdgcn_update_dpp(0, (int)(unsigned)(u >> 32), ctrl, 0xF, 0xF, false);
+    return __builtin_bit_cast(double, (u64)hi << 32 | lo);
+}
 // The exact keys of up to kWave / LP pages by one wavefront: LP lanes share a page (`pg`, the same in all of them; -1: none), 16 bytes of its
 // summary each.  All of a page's lanes get its key.
 template <typename IO, int LP>
@@ -67,72 +74,100 @@ __device__ __forceinline__ u64 exact_key(Args a, int b, int hk, int pg, int lane
     WVec<IO>::unpack(ok && in ? WVec<IO>::load(static_cast<const IO*>(a->k_min) + row) : WVec<IO>::zero(), lo);
     WVec<IO>::unpack(ok && in ? WVec<IO>::load(static_cast<const IO*>(a->k_max) + row) : WVec<IO>::zero(), hi);
     double best = -(double)INFINITY;
-    for (int h = 0; h < a->group; ++h) {
-        float x[VE];
-        WVec<IO>::unpack(in ? WVec<IO>::load(q + h * a->k_dim) : WVec<IO>::zero(), x);
-        double sum = 0.0;
+    for (int h = 0; h < a->group; h += 4) {
+        typename WVec<IO>::raw raw[4];
 #pragma unroll
-        for (int j = 0; j < VE; ++j) sum = __builtin_fma((double)x[j], (double)(x[j] > 0.f ? hi[j] : lo[j]), sum);
+        for (int i = 0; i < 4; ++i) raw[i] = in ? WVec<IO>::load(q + min(h + i, a->group - 1) * a->k_dim) : WVec<IO>::zero();  // (a repeated head changes no maximum)
 #pragma unroll
-        for (int off = 1; off < LP; off <<= 1) sum += __shfl_xor(sum, off, kWave);
-        best = sum > best ? sum : best;
+        for (int i = 0; i < 4; ++i) {
+            float x[VE];
+            WVec<IO>::unpack(raw[i], x);
+            double sum = 0.0;
+#pragma unroll
+            for (int j = 0; j < VE; ++j) sum = __builtin_fma((double)x[j], (double)(x[j] > 0.f ? hi[j] : lo[j]), sum);
+            sum += dpp_f64<0xB1>(sum);   // quad_perm [1,0,3,2]
+            sum += dpp_f64<0x4E>(sum);   // quad_perm [2,3,0,1]
+            sum += dpp_f64<0x141>(sum);  // row_half_mirror
+            if constexpr (LP >= 16) sum += dpp_f64<0x140>(sum);  // row_mirror
+            if constexpr (LP >= 32) sum += __shfl_xor(sum, 16, kWave);
+            if constexpr (LP >= 64) sum += __shfl_xor(sum, 32, kWave);
+            best = sum > best ? sum : best;
+        }
     }
     return ok ? key_of(best) : key_of(-(double)INFINITY);
 }
 
 // ------------------------------------------------------------------------------------------------ the choice
+constexpr int kDigit = 11;         // bits of a key that a step looks at
+constexpr int kBins = 1 << kDigit;
+
 struct Shared {
-    int count[256];
-    int found[2];
+    int count[kBins];
+    int found[3];
     unsigned low[kWaves], high[kWaves];
-    int sure[kWaves], in[kWaves], equal[kWaves];
+    int part[kWaves], sure[kWaves], open[kWaves], in[kWaves], equal[kWaves];
     int n_few;
     int few[kFew];  // pages whose order is open
     u64 key[kFew];
     unsigned held[kHeld];
 };
 
-// The need-th largest of the keys that `each` hands to its argument, found eight bits at a time from the first bit on in which
-// they differ; *need becomes its number among the keys equal to it.
-template <typename K, typename E>
-__device__ __forceinline__ K nth_largest(Shared& sh, K low, K high, E each, int* need, int tid) {
-    const int lane = tid & (kWave - 1);
-    constexpr int kBits = sizeof(K) * 8;
-    const K differ = low ^ high;
-    int bits = differ == 0 ? kBits : sizeof(K) == 8 ? __clzll((long long)differ) : __clz((int)differ);  // the highest bits that all keys share
-    K cut = bits == 0 ? 0 : high >> (kBits - bits);
-    while (bits < kBits) {
-        const int step = min(8, kBits - bits), down = kBits - bits - step;
-        sh.count[tid] = 0;
+// Where the need-th largest of some keys lies: `prefix` are its highest `bits` bits, `need` its number among the `count` keys that share them.
+template <typename K>
+struct Place {
+    static constexpr int kBits = sizeof(K) * 8;
+    K prefix;
+    int bits, need, count;
+    // before any step: the bits that all keys share
+    __device__ __forceinline__ Place(K low, K high, int n, int nth) : need(nth), count(n) {
+        const K differ = low ^ high;
+        bits = differ == 0 ? kBits : sizeof(K) == 8 ? __clzll((long long)differ) : __clz((int)differ);
+        prefix = bits == 0 ? 0 : high >> (kBits - bits);
+    }
+    __device__ __forceinline__ K lowest() const { return bits == 0 ? 0 : prefix << (kBits - bits); }
+    __device__ __forceinline__ K highest() const { return bits == kBits ? prefix : lowest() + ((K)(~(K)0) >> bits); }
+    // the next bits, by the whole workgroup; `each` hands every key to its argument
+    template <typename E>
+    __device__ __forceinline__ void step(Shared& sh, E each, int tid) {
+        const int lane = tid & (kWave - 1), wv = tid / kWave;
+        const int digit = min(kDigit, kBits - bits), down = kBits - bits - digit;
+        constexpr int kEach = kBins / kThreads;
+        static_assert(kEach == 8, "two 16-byte pieces of bins a thread");
+        u32x4* bins = reinterpret_cast<u32x4*>(sh.count) + 2 * (kThreads - 1 - tid);  // the highest ones first
+        bins[0] = bins[1] = u32x4{};
         barrier_lds();
         each([&](K k) __attribute__((always_inline)) {
-            if (bits == 0 || k >> (kBits - bits) == cut) atomicAdd(&sh.count[(int)(k >> down) & ((1 << step) - 1)], 1);
+            if (bits == 0 || k >> (kBits - bits) == prefix) atomicAdd(&sh.count[(int)(k >> down) & ((1 << digit) - 1)], 1);
         });
         barrier_lds();
-        if (tid < kWave) {  // four bins a lane, from the highest down: the bin in which the count reaches `need`
-            int c[4], sum = 0;
+        const u32x4 x = bins[1], y = bins[0];
+        const int c[8] = {(int)x[3], (int)x[2], (int)x[1], (int)x[0], (int)y[3], (int)y[2], (int)y[1], (int)y[0]};
+        const int sum = c[0] + c[1] + c[2] + c[3] + c[4] + c[5] + c[6] + c[7];
+        const int upto = (int)wave_scan_u32((unsigned)sum);
+        if (lane == kWave - 1) sh.part[wv] = upto;
+        barrier_lds();
+        int before = upto - sum;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) sum += c[j] = sh.count[255 - 4 * lane - j];
-            int upto = (int)wave_scan_u32((unsigned)sum);
-            int before = upto - sum;
-            if (before < *need && upto >= *need) {
+        for (int w = 0; w < kWaves; ++w) before += w < wv ? sh.part[w] : 0;
+        if (before < need && before + sum >= need) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (before < *need && before + c[j] >= *need) {
-                        sh.found[0] = 255 - 4 * lane - j;
-                        sh.found[1] = before;
-                    }
-                    before += c[j];
+            for (int j = 0; j < 8; ++j) {
+                if (before < need && before + c[j] >= need) {
+                    sh.found[0] = kBins - 1 - 8 * tid - j;
+                    sh.found[1] = before;
+                    sh.found[2] = c[j];
                 }
+                before += c[j];
             }
         }
         barrier_lds();
-        cut = cut << step | (K)sh.found[0];
-        *need -= sh.found[1];
-        bits += step;
+        prefix = prefix << digit | (K)sh.found[0];
+        need -= sh.found[1];
+        count = sh.found[2];
+        bits += digit;
+        barrier_lds();  // (read before another step)
     }
-    return cut;
-}
+};
 
 // The list of a (sequence, key/value head) from its scores in fp32, whose error is at most `eps`, by one workgroup.
 template <typename IO, int LP>
@@ -150,12 +185,17 @@ __device__ __forceinline__ void choose(Args a, Shared& sh, long long row, int b,
     auto key_at = [&](int i) __attribute__((always_inline)) { return held ? sh.held[i] : key_of(load_past(&scores[i])); };
 
     unsigned low = ~0u, high = 0u;
-#pragma unroll 4
-    for (int i = tid; i < n; i += kThreads) {
-        const unsigned k = key_of(load_past(&scores[i]));
-        if (held) sh.held[i] = k;
-        low = min(low, k);
-        high = max(high, k);
+    for (int i0 = tid; i0 < n; i0 += 8 * kThreads) {  // (eight under way)
+        float s[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s[j] = load_past(&scores[min(i0 + j * kThreads, n - 1)]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const unsigned k = key_of(s[j]);
+            if (held && i0 + j * kThreads < n) sh.held[i0 + j * kThreads] = k;
+            low = min(low, k);
+            high = max(high, k);
+        }
     }
     low = wave_min_u32_dpp(low);
     high = ~wave_min_u32_dpp(~high);
@@ -172,132 +212,155 @@ __device__ __forceinline__ void choose(Args a, Shared& sh, long long row, int b,
     }
     unsigned above = ~0u, below = 0u;  // keys over `above` are in, keys under `below` out, those between are open
     if (eps < INFINITY) {              // (else something was no number, or infinite: all are open)
-        int need = want;
-        const float t = score_of(nth_largest<unsigned>(sh, low, high, [&](auto f) __attribute__((always_inline)) {
-            for (int i = tid; i < n; i += kThreads) f(key_at(i));
-        }, &need, tid));
-        // The want-th largest exact score lies within eps of t: what is further than 2 eps from t lies on its side of it.  (Rounded outward.)
-        const float up = t + 2.f * eps, down = t - 2.f * eps;
-        above = key_of(up + fabsf(up) * 0x1p-22f);
-        below = key_of(down - fabsf(down) * 0x1p-22f);
+        Place<unsigned> at(low, high, n, want);
+        while (at.bits < 32 && (at.bits == 0 || at.count > kFew / 4))  // near enough: the few that share its bits stay open
+            at.step(sh, [&](auto f) __attribute__((always_inline)) {
+                for (int i = tid; i < n; i += kThreads) f(key_at(i));
+            }, tid);
+        // The want-th largest exact score lies within eps of the want-th largest score: what is further than 2 eps from where that lies is on
+        // its side of it.  (Rounded outward.)
+        const float up = score_of(at.highest()) + 2.f * eps, down = score_of(at.lowest()) - 2.f * eps;
+        const float over = up + fabsf(up) * 0x1p-22f, under = down - fabsf(down) * 0x1p-22f;
+        if (over == over) above = key_of(over);  // (at the ends there are keys of no number)
+        if (under == under) below = key_of(under);
     }
-    int n_in = 0;
-    for (int i = tid; i < n; i += kThreads) {
+    // A wavefront has a run of the pages.
+    const int run = (n + kThreads - 1) / kThreads * kWave, from = wv * run, to = min(n, from + run);
+    int n_in = 0, n_open = 0;
+    for (int i = from + lane; i < to; i += kWave) {
         const unsigned k = key_at(i);
         n_in += k > above;
         if (k <= above && k >= below) {
+            ++n_open;
             const int at = atomicAdd(&sh.n_few, 1);
             if (at < kFew) sh.few[at] = i;
         }
     }
     n_in = (int)wave_sum_u32_dpp((unsigned)n_in);
-    if (lane == 0) sh.sure[wv] = n_in;
+    n_open = (int)wave_sum_u32_dpp((unsigned)n_open);
+    if (lane == 0) {
+        sh.sure[wv] = n_in;
+        sh.open[wv] = n_open;
+    }
     barrier_lds();
-    int rest = want;
+    int rest = want, at = lo;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) rest -= sh.sure[w];  // how many of the open ones are in
+    for (int w = 0; w < kWaves; ++w) {
+        rest -= sh.sure[w];  // how many of the open ones are in
+        at += w < wv ? sh.sure[w] : 0;
+    }
     const int all_open = sh.n_few;
     constexpr int kPer = kWave / LP;  // pages of a wavefront at a time, in 64 bits
-    unsigned line = below;            // keys from here on are in
-    bool by_key = false;              // ... and open ones by their exact keys in memory: above `cut`, or equal to it and among the first `rest`
+    const unsigned no_key = ~0u;      // (a score has no such bits)
+    unsigned line = above == no_key ? no_key : above + 1;  // keys from here on are in
+    bool by_key = false;  // ... and open ones by their exact keys in memory: above `cut`, or equal to it and among the first `rest`
     u64 cut = 0;
-    if (all_open != rest) {
-        line = above + 1;
-        if (all_open <= kFew && held) {
-            for (int i0 = wv * kPer; i0 < all_open; i0 += kWaves * kPer) {
-                const int i = i0 + lane / LP;
-                const u64 k = exact_key<IO, LP>(a, b, hk, i < all_open ? lo + sh.few[i] : -1, lane);
-                if ((lane & (LP - 1)) == 0 && i < all_open) sh.key[i] = k;
+    int equal_before = 0;
+    if (all_open == rest) {  // all of them
+        line = below;
+        for (int w = 0; w < wv; ++w) at += sh.open[w];
+    } else if (all_open <= kFew && held) {
+        for (int i0 = wv * kPer; i0 < all_open; i0 += kWaves * kPer) {
+            const int i = i0 + lane / LP;
+            const u64 k = exact_key<IO, LP>(a, b, hk, i < all_open ? lo + sh.few[i] : -1, lane);
+            if ((lane & (LP - 1)) == 0 && i < all_open) sh.key[i] = k;
+        }
+        barrier_lds();
+        // every wavefront ranks them (they stand in no order: equal ones go by their pages) and counts those before its run
+        int page = n;
+        bool taken = false;
+        if (lane < all_open) {
+            page = sh.few[lane];
+            const u64 k = sh.key[lane];
+            int better = 0;
+            for (int j = 0; j < all_open; ++j) better += sh.key[j] > k || (sh.key[j] == k && sh.few[j] < page);
+            taken = better < rest;
+        }
+        at += __popcll(__ballot(taken && page < from));
+        if (page >= from && page < to) sh.held[page] = taken ? no_key : 0u;  // its own run's: nobody else reads them
+        wait_lds_fence();
+    } else {
+        by_key = true;
+        u64 lowest = ~0ull, highest = 0ull;
+        for (int i0 = wv * kPer; i0 < n; i0 += kWaves * kPer) {
+            const int i = i0 + lane / LP;
+            const unsigned s = i < n ? key_at(i) : 0u;
+            const bool open = i < n && s <= above && s >= below;
+            if (!__ballot(open)) continue;
+            const u64 k = exact_key<IO, LP>(a, b, hk, open ? lo + i : -1, lane);
+            if (open) {
+                lowest = k < lowest ? k : lowest;
+                highest = k > highest ? k : highest;
+                if ((lane & (LP - 1)) == 0) store_past(&keys[i], k);
             }
-            barrier_lds();
-            if (tid < all_open) {  // (they stand in no order: equal ones go by their pages)
-                const u64 k = sh.key[tid];
-                const int me = sh.few[tid];
-                int better = 0;
-                for (int j = 0; j < all_open; ++j) better += sh.key[j] > k || (sh.key[j] == k && sh.few[j] < me);
-                sh.held[me] = better < rest ? ~0u : 0u;
-            }
-            if (above == ~0u) line = ~0u;  // (all were open)
-            barrier_lds();
-        } else {
-            by_key = true;
-            if (above == ~0u) line = ~0u;  // no key reaches it: a score has no such bits
-            u64 lowest = ~0ull, highest = 0ull;
-            for (int i0 = wv * kPer; i0 < n; i0 += kWaves * kPer) {
-                const int i = i0 + lane / LP;
-                const unsigned s = i < n ? key_at(i) : 0u;
-                const bool open = i < n && s <= above && s >= below;
-                if (!__ballot(open)) continue;
-                const u64 k = exact_key<IO, LP>(a, b, hk, open ? lo + i : -1, lane);
-                if (open) {
-                    lowest = k < lowest ? k : lowest;
-                    highest = k > highest ? k : highest;
-                    if ((lane & (LP - 1)) == 0) store_past(&keys[i], k);
-                }
-            }
+        }
 #pragma unroll
-            for (int off = 32; off > 0; off >>= 1) {
-                const u64 l = __shfl_xor(lowest, off, kWave), h = __shfl_xor(highest, off, kWave);
-                lowest = l < lowest ? l : lowest;
-                highest = h > highest ? h : highest;
-            }
-            if (lane == 0) {
-                sh.key[wv] = lowest;
-                sh.key[kWaves + wv] = highest;
-            }
-            wait_vm_fence<0>();  // the keys are there
-            barrier_lds();
+        for (int off = 32; off > 0; off >>= 1) {
+            const u64 l = __shfl_xor(lowest, off, kWave), h = __shfl_xor(highest, off, kWave);
+            lowest = l < lowest ? l : lowest;
+            highest = h > highest ? h : highest;
+        }
+        if (lane == 0) {
+            sh.key[wv] = lowest;
+            sh.key[kWaves + wv] = highest;
+        }
+        wait_vm_fence<0>();  // the keys are there
+        barrier_lds();
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                lowest = sh.key[w] < lowest ? sh.key[w] : lowest;
-                highest = sh.key[kWaves + w] > highest ? sh.key[kWaves + w] : highest;
-            }
-            cut = nth_largest<u64>(sh, lowest, highest, [&](auto f) __attribute__((always_inline)) {
+        for (int w = 0; w < kWaves; ++w) {
+            lowest = sh.key[w] < lowest ? sh.key[w] : lowest;
+            highest = sh.key[kWaves + w] > highest ? sh.key[kWaves + w] : highest;
+        }
+        Place<u64> place(lowest, highest, all_open, rest);
+        while (place.bits < 64)
+            place.step(sh, [&](auto f) __attribute__((always_inline)) {
                 for (int i = tid; i < n; i += kThreads) {
                     const unsigned k = key_at(i);
                     if (k <= above && k >= below) f(load_past(&keys[i]));
                 }
-            }, &rest, tid);
+            }, tid);
+        cut = place.prefix;
+        rest = place.need;
+        int more = 0, equal = 0;
+        for (int i = from + lane; i < to; i += kWave) {
+            const unsigned k = key_at(i);
+            if (k <= above && k >= below) {
+                const u64 e = load_past(&keys[i]);
+                more += e > cut;
+                equal += e == cut;
+            }
+        }
+        more = (int)wave_sum_u32_dpp((unsigned)more);
+        equal = (int)wave_sum_u32_dpp((unsigned)equal);
+        if (lane == 0) {
+            sh.in[wv] = more;
+            sh.equal[wv] = equal;
+        }
+        barrier_lds();
+        for (int w = 0; w < wv; ++w) {
+            at += sh.in[w] + max(0, min(sh.equal[w], rest - equal_before));
+            equal_before += sh.equal[w];
         }
     }
-    // A wavefront writes a run of the pages, behind those of the wavefronts before it.
-    const int run = (n + kThreads - 1) / kThreads * kWave, from = wv * run, to = min(n, from + run);
-    int at = lo, equal_before = 0;
-    for (int pass = 0; pass < 2; ++pass) {  // counted, then written
-        int in_here = 0, equal_here = 0;
-        for (int i0 = from; i0 < to; i0 += kWave) {
-            const int i = i0 + lane;
-            const unsigned k = i < to ? key_at(i) : 0u;
-            bool in = i < to && k >= line, equal = false;
-            if (by_key && i < to && k <= above && k >= below) {
+    for (int i0 = from; i0 < to; i0 += kWave) {
+        const int i = i0 + lane;
+        const unsigned k = i < to ? key_at(i) : 0u;
+        bool in = i < to && k >= line;
+        const u64 under = (1ull << lane) - 1;
+        if (by_key) {
+            bool equal = false;
+            if (i < to && k <= above && k >= below) {
                 const u64 e = load_past(&keys[i]);
                 in = e > cut;
                 equal = e == cut;
             }
-            const u64 eq = __ballot(equal), under = (1ull << lane) - 1;
-            if (pass) {
-                in |= equal && equal_before + __popcll(eq & under) < rest;
-                const u64 ins = __ballot(in);
-                if (in) out[at + __popcll(ins & under)] = lo + i;
-                at += __popcll(ins);
-                equal_before += __popcll(eq);
-            } else {
-                in_here += __popcll(__ballot(in));
-                equal_here += __popcll(eq);
-            }
+            const u64 eq = __ballot(equal);
+            in |= equal && equal_before + __popcll(eq & under) < rest;
+            equal_before += __popcll(eq);
         }
-        if (pass == 0) {
-            if (lane == 0) {
-                sh.in[wv] = in_here;
-                sh.equal[wv] = equal_here;
-            }
-            barrier_lds();
-            for (int w = 0; w < wv; ++w) {
-                at += sh.in[w] + max(0, min(sh.equal[w], rest - equal_before));
-                equal_before += sh.equal[w];
-            }
-            if (!by_key) equal_before = 0;
-        }
+        const u64 ins = __ballot(in);
+        if (in) out[at + __popcll(ins & under)] = lo + i;
+        at += __popcll(ins);
     }
 }
 
