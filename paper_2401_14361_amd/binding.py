@@ -483,7 +483,7 @@ class Kv:
         self.dtype = torch.float32 if dtype == "fp32" else torch.bfloat16  # of queries, new keys and values, outputs, summaries
         self.k_page = (n_kv_heads, page_size, k_dim)
         self.v_page = (n_kv_heads, page_size, v_dim)
-        self.heads = (n_q_heads, k_dim)
+        self.heads, self.k_heads, self.v_heads = (n_q_heads, k_dim), (n_kv_heads, k_dim), (n_kv_heads, v_dim)
         self.out_heads = (n_q_heads, v_dim)
 
     def error_flags(self, stream=None) -> int:
@@ -535,15 +535,23 @@ def _kv_stream(kv: Kv, stream) -> int:
 
 
 def _rows(kv: Kv, t: torch.Tensor, n: int, heads: tuple) -> int:
-    """Checks [n][heads][width] with dense tokens and returns the elements between tokens."""
-    assert t.device == kv.device and t.dtype == kv.dtype and tuple(t.shape) == (n, *heads), (t.device, t.dtype, t.shape, (n, *heads))
+    """Checks [n][heads][width] with dense tokens and returns the elements between tokens (0: dense)."""
+    assert t.get_device() == kv.index and t.dtype is kv.dtype and t.shape == (n, *heads), (t.device, t.dtype, t.shape, (n, *heads))
+    if t.is_contiguous():
+        return 0
     s = t.stride()
-    assert n == 0 or ((s[2] == 1 or heads[1] == 1) and (s[1] == heads[1] or heads[0] == 1)), "a token's heads must be dense"
+    assert (s[2] == 1 or heads[1] == 1) and (s[1] == heads[1] or heads[0] == 1), "a token's heads must be dense"
     return s[0] if n > 1 else 0
 
 
 def _ints(kv: Kv, t: torch.Tensor) -> int:
-    assert t.device == kv.device and t.dtype == torch.int32 and t.is_contiguous(), (t.device, t.dtype)
+    assert t.dtype is torch.int32 and t.get_device() == kv.index and t.is_contiguous(), (t.device, t.dtype)
+    return t.data_ptr()
+
+
+def _given(kv: Kv, t: torch.Tensor, n: int, heads: tuple) -> int:
+    """Checks a caller's output [n][heads][width] and returns its address."""
+    assert t.dtype is kv.dtype and t.get_device() == kv.index and t.is_contiguous() and t.numel() == n * heads[0] * heads[1], (t.device, t.dtype, t.shape)
     return t.data_ptr()
 
 
@@ -556,33 +564,34 @@ def kv_append(kv: Kv, pages: KvPages, table: torch.Tensor, pos: torch.Tensor, q:
     B, width = table.shape
     if q_out is None:
         q_out = torch.empty((T, *kv.heads), dtype=kv.dtype, device=kv.device)
-    assert q_out.is_contiguous() and q_out.dtype == kv.dtype and q_out.numel() == T * kv.heads[0] * kv.heads[1] and q_out.device == kv.device
-    assert inv_freq is None or (inv_freq.device == kv.device and _dev(inv_freq, torch.float32) is inv_freq)
+    assert inv_freq is None or (inv_freq.dtype is torch.float32 and inv_freq.get_device() == kv.index and inv_freq.is_contiguous()), (inv_freq.device, inv_freq.dtype)
     assert seq is None or seq.numel() == T
     _check(lib().kv_append(kv.h, pages.ref, _ints(kv, table), width, B, None if seq is None else _ints(kv, seq), _ints(kv, pos), T,
-                           q.data_ptr(), _rows(kv, q, T, kv.heads), k.data_ptr(), _rows(kv, k, T, (kv.k_page[0], kv.k_page[2])),
-                           v.data_ptr(), _rows(kv, v, T, (kv.v_page[0], kv.v_page[2])),
+                           q.data_ptr(), _rows(kv, q, T, kv.heads), k.data_ptr(), _rows(kv, k, T, kv.k_heads),
+                           v.data_ptr(), _rows(kv, v, T, kv.v_heads),
                            None if inv_freq is None else inv_freq.data_ptr(), 0 if inv_freq is None else 2 * inv_freq.numel(),
-                           interleaved, q_out.data_ptr(), _kv_stream(kv, stream)))
+                           interleaved, _given(kv, q_out, T, kv.heads), _kv_stream(kv, stream)))
     return q_out
 
 
-def _attend_outputs(kv: Kv, B: int, table, lens, out, want_lse):
+def _attend_outputs(kv: Kv, q, table, lens, out, want_lse):
+    B = q.shape[0]
     assert table.shape[0] == B and lens.numel() == B
     if out is None:
-        out = torch.empty((B, *kv.out_heads), dtype=kv.dtype, device=kv.device)
-    assert out.is_contiguous() and out.dtype == kv.dtype and out.numel() == B * kv.out_heads[0] * kv.out_heads[1] and out.device == kv.device
-    return out, torch.empty((B, kv.heads[0]), dtype=torch.float32, device=kv.device) if want_lse else None
+        out = torch.empty_like(q, memory_format=torch.contiguous_format) if kv.out_heads == kv.heads else q.new_empty((B, *kv.out_heads))
+        at = out.data_ptr()
+    else:
+        at = _given(kv, out, B, kv.out_heads)
+    return B, out, at, q.new_empty((B, kv.heads[0]), dtype=torch.float32) if want_lse else None
 
 
 def kv_attend(kv: Kv, pages: KvPages, table: torch.Tensor, lens: torch.Tensor, q: torch.Tensor, scale: float, window: int = 0,
               out: torch.Tensor | None = None, want_lse: bool = False, stream=None):
     """q [B][Hq][k_dim] (any stride between sequences) over the first lens [B] tokens of each sequence, or the last `window` of them
     -> out [B][Hq][v_dim], or (out, lse [B][Hq] fp32) with want_lse."""
-    B = q.shape[0]
-    out, lse = _attend_outputs(kv, B, table, lens, out, want_lse)
+    B, out, at, lse = _attend_outputs(kv, q, table, lens, out, want_lse)
     _check(lib().kv_attend(kv.h, pages.ref, _ints(kv, table), table.shape[1], _ints(kv, lens), B, q.data_ptr(), _rows(kv, q, B, kv.heads),
-                           scale, window, out.data_ptr(), lse.data_ptr() if want_lse else None, _kv_stream(kv, stream)))
+                           scale, window, at, lse.data_ptr() if want_lse else None, _kv_stream(kv, stream)))
     return (out, lse) if want_lse else out
 
 
@@ -591,11 +600,10 @@ def kv_attend_blocks(kv: Kv, pages: KvPages, table: torch.Tensor, lens: torch.Te
                      want_blocks: bool = False, stream=None):
     """kv_attend over at most n_sel pages a sequence and key/value head: the first keep_first, the last keep_last and those whose
     logits have the highest bounds.  Returns out, or a tuple with lse [B][Hq] and blocks [B][Hkv][n_sel] int32 as wanted."""
-    B = q.shape[0]
-    out, lse = _attend_outputs(kv, B, table, lens, out, want_lse)
+    B, out, at, lse = _attend_outputs(kv, q, table, lens, out, want_lse)
     blocks = torch.empty((B, kv.k_page[0], max(n_sel, 0)), dtype=torch.int32, device=kv.device) if want_blocks else None
     _check(lib().kv_attend_blocks(kv.h, pages.ref, _ints(kv, table), table.shape[1], _ints(kv, lens), B, q.data_ptr(),
-                                  _rows(kv, q, B, kv.heads), scale, n_sel, keep_first, keep_last, out.data_ptr(),
+                                  _rows(kv, q, B, kv.heads), scale, n_sel, keep_first, keep_last, at,
                                   lse.data_ptr() if want_lse else None, blocks.data_ptr() if want_blocks else None, _kv_stream(kv, stream)))
     got = (out,) + ((lse,) if want_lse else ()) + ((blocks,) if want_blocks else ())
     return got if len(got) > 1 else out
