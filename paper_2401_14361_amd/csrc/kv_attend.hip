@@ -55,48 +55,66 @@ __device__ __forceinline__ int units_of(const Span& s) { return max(1, (s.end - 
 
 struct Stretch {
     unsigned per;         // units of a workgroup
+    unsigned step;        // items begin at multiples of it in the line: `per` where every item has workgroups of its own, else 1
     unsigned first, end;  // this one's, in the line
     int b;                // the sequence in which it begins
     unsigned base;        // its first unit in the line
     int len;              // and its length
 };
 
+// An item more in a stretch costs as much as two units or so: where the items are no more than the workgroups, a stretch may be longer by a
+// quarter, or by two units, if then none crosses from an item to the next.
 template <int kUnit>
 __device__ __forceinline__ Stretch my_stretch(Args a, int lane) {
-    const unsigned items = a->n_kv * a->blocks_of_heads;
-    unsigned total = 0, upto = 0, mine = 0;
+    const unsigned items = a->n_kv * a->blocks_of_heads, grid = gridDim.x;
+    unsigned units = 0;  // of an item of this lane's sequence
     int len = 0;
-    for (int b0 = 0; b0 < a->B; b0 += kWave) {
+    auto look = [&](int b0) __attribute__((always_inline)) {
         len = b0 + lane < a->B ? a->lens[b0 + lane] : 0;
-        mine = b0 + lane < a->B ? units_of<kUnit>(span_of(a, len)) * items : 0u;
-        upto = total + wave_scan_u32(mine);
-        total = __builtin_amdgcn_readlane(upto, kWave - 1);
+        units = b0 + lane < a->B ? units_of<kUnit>(span_of(a, len)) : 0u;
+    };
+    unsigned total = 0;
+    for (int b0 = 0; b0 < a->B; b0 += kWave) {
+        look(b0);
+        total += wave_sum_u32_dpp(units) * items;
     }
     Stretch s;
-    s.per = (total + gridDim.x - 1) / gridDim.x;
+    s.per = (total + grid - 1) / grid;
+    s.step = 1;
+    if (a->B * items <= grid) {
+        const unsigned most = s.per + max(2u, s.per / 4);
+        for (unsigned per = s.per; per <= most; per += max(1u, s.per / 16)) {
+            unsigned parts = 0;
+            for (int b0 = 0; b0 < a->B; b0 += kWave) {
+                if (a->B > kWave) look(b0);
+                parts += wave_sum_u32_dpp((units + per - 1) / per) * items;
+            }
+            if (parts <= grid) {
+                s.per = s.step = per;
+                break;
+            }
+        }
+    }
     s.first = blockIdx.x * s.per;
-    s.end = min(s.first + s.per, total);
+    s.end = s.first + s.per;
     s.b = -1;
     s.base = 0;
     s.len = 0;
-    if (s.first >= s.end) return s;
     unsigned before = 0;
     for (int b0 = 0; b0 < a->B; b0 += kWave) {
-        if (a->B > kWave) {
-            len = b0 + lane < a->B ? a->lens[b0 + lane] : 0;
-            mine = b0 + lane < a->B ? units_of<kUnit>(span_of(a, len)) * items : 0u;
-            upto = before + wave_scan_u32(mine);
-            before = __builtin_amdgcn_readlane(upto, kWave - 1);
-        }
+        if (a->B > kWave) look(b0);
+        const unsigned mine = (units + s.step - 1) / s.step * s.step * items, upto = before + wave_scan_u32(mine);
         const unsigned long long who = __ballot(upto > s.first && upto - mine <= s.first);
-        if (who) {
+        if (who && s.b < 0) {
             const int l = __builtin_ctzll(who);
             s.b = b0 + l;
             s.base = __builtin_amdgcn_readlane(upto - mine, l);
             s.len = __builtin_amdgcn_readlane(len, l);
-            break;
         }
+        before = __builtin_amdgcn_readlane(upto, kWave - 1);
+        if (s.b >= 0 && before >= s.end) break;
     }
+    s.end = min(s.end, before);  // (the line's end, if that comes first)
     return s;
 }
 
@@ -247,9 +265,10 @@ __global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kReside
         const int len = b == mine_of.b ? mine_of.len : ((kv_const_ints)(uintptr_t)a->lens)[b];
         const Span sp = span_of(a, len);
         const unsigned units = units_of<S::kUnit>(sp);
-        const unsigned item = (at_unit - base) / units, u0 = at_unit - base - item * units;
+        const unsigned room = mine_of.step == 1 ? units : (units + mine_of.step - 1) / mine_of.step * mine_of.step;  // of an item, in the line
+        const unsigned item = (at_unit - base) / room, u0 = at_unit - base - item * room;
         const unsigned u1 = min(units, u0 + (mine_of.end - at_unit));
-        const unsigned item_first = base + item * units;  // the item's first unit in the line
+        const unsigned item_first = base + item * room;  // the item's first unit in the line
         int hk = item, h0 = 0;
         if (a->blocks_of_heads > 1) {
             hk = item / a->blocks_of_heads;
@@ -596,7 +615,7 @@ __global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kReside
                 if (i % kWaves >= groups) s_m[i] = -INFINITY;
             barrier_lds();
         }
-        at_unit = item_first + u1;
+        at_unit = item_first + (u1 == units ? room : u1);
         if (u1 == units && item + 1 == (unsigned)(a->n_kv * a->blocks_of_heads)) {
             base = at_unit;
             ++b;
