@@ -296,13 +296,13 @@ __global__ void __launch_bounds__(kAppThreads, kSums ? 4 : 6) kv_append_kernel(K
 }
 
 // The summaries of the pages that a call with several tokens of a sequence has completed, when all of its rows are there.  A workgroup looks at
-// 64 tokens for one head.
+// as many tokens as a page holds, 64 at most, for one head: a page or so (64 of them for pages of 16, four pages one after another: 703 tokens 32 us a call, now 16).
 template <typename IO, typename PG>
 __global__ void __launch_bounds__(kAppThreads) kv_summary_kernel(KvAppendArgs) {
     const Args a = (Args)__builtin_amdgcn_kernarg_segment_ptr();
     const int h = blockIdx.y, lane = threadIdx.x & (kWave - 1), size = 1 << a->page_shift;
-    const int t = blockIdx.x * kWave + lane;
-    const int pos = t < a->T ? a->pos[t] : -1;
+    const int look = min(size, kWave), t = blockIdx.x * look + lane;
+    const int pos = lane < look && t < a->T ? a->pos[t] : -1;
     const bool done = pos >= 0 && (pos & (size - 1)) == size - 1;
     const int mine = done ? page_of(a, t, pos, false) : -1;
     for (unsigned long long left = __ballot(mine >= 0); left; left &= left - 1)  // (all wavefronts see the same)
@@ -320,7 +320,8 @@ void launch_append(KvAppendArgs a, bool wide, int cus, hipStream_t s) {
     const auto kernel = sums ? (wide ? kv_append_kernel<IO, PG, N, true> : kv_append_kernel<IO, PG, 1, true>)
                              : (wide ? kv_append_kernel<IO, PG, N, false> : kv_append_kernel<IO, PG, 1, false>);
     launch(K_KV_APPEND, kernel, grid, dim3(kAppThreads), 0, s, a);
-    if (a.k_min && a.seq) launch(K_KV_SUMMARY, kv_summary_kernel<IO, PG>, dim3((unsigned)((a.T + kWave - 1) / kWave), (unsigned)a.n_kv), dim3(kAppThreads), 0, s, a);
+    const int look = 1 << (a.page_shift < 6 ? a.page_shift : 6);
+    if (a.k_min && a.seq) launch(K_KV_SUMMARY, kv_summary_kernel<IO, PG>, dim3((unsigned)((a.T + look - 1) / look), (unsigned)a.n_kv), dim3(kAppThreads), 0, s, a);
 }
 
 int log2_of(int v) { return 31 - __builtin_clz((unsigned)v); }
@@ -385,7 +386,7 @@ int fill_attend(const char* who, const moei_kv* kv, const moei_kv_pages* p, cons
     a->width = width;
     a->page_shift = log2_of(d.page_size);
     a->n_pages = p->n_pages;
-    a->scale2 = scale * 1.4426950408889634f;
+    a->scale2 = (float)((double)scale * 1.4426950408889634);
     a->part = kv->d_part;
     a->stat = kv->d_stat;
     a->arrived = kv->d_arrived;

@@ -389,6 +389,7 @@ __global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kReside
 #pragma unroll
             for (int st = 0; st < T::kSub; ++st) {
                 s[st] = f32x4{0.f, 0.f, 0.f, 0.f};
+                [[maybe_unused]] f32x4 s4[4] = {};  // fp32: four sums, which are a quarter as long each
                 const uint32_t row = at_k + (st * kRows + col) * (KC * T::kBytes);
 #pragma unroll
                 for (int u = 0; u < kUnits; ++u) {
@@ -401,9 +402,10 @@ __global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kReside
                     } else {
                         const f32x4 x = __builtin_bit_cast(f32x4, kk), y = __builtin_bit_cast(f32x4, q[u]);
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) s[st] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], s[st], 0, 0, 0);
+                        for (int j = 0; j < 4; ++j) s4[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[j], y[j], s4[j], 0, 0, 0);
                     }
                 }
+                if constexpr (T::kBytes == 4) s[st] = (s4[0] + s4[1]) + (s4[2] + s4[3]);
             }
             if (more) {
                 wait_lds_fence();
