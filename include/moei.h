@@ -392,8 +392,8 @@ int moei_kv_destroy(moei_kv* kv);
 int moei_kv_error_flags(moei_kv* kv, int32_t* h_flags, void* stream);
 
 /* Appends T tokens: d_q[T][n_q_heads][k_dim], d_k[T][n_kv_heads][k_dim], d_v[T][n_kv_heads][v_dim], *_stride elements between tokens (0: dense).
- * Token t has position d_pos[t] in sequence d_seq[t] (d_seq NULL: sequence t, T <= B); a negative position is no token, and nothing of it
- * is read or written.  The first rot_dim elements of every query and key head are rotated by the angles position * d_inv_freq[i],
+ * Token t has position d_pos[t] in sequence d_seq[t] (d_seq NULL: sequence t, T <= B, and no two tokens share a page); a negative
+ * position is no token, and nothing is written for it.  The first rot_dim elements of every query and key head are rotated by the angles position * d_inv_freq[i],
  * 0 <= i < rot_dim / 2, formed in 64 bits: elements i and i + rot_dim / 2 (interleaved: 2i and 2i + 1) are turned as a pair in fp32.
  * Rotated queries go to d_q_out[T][n_q_heads][k_dim] (dense; d_q itself if that is dense), keys and values into row position % page_size
  * of page d_table[sequence][position / page_size] (d_table [B][table_width] int32), rounded once; 8-bit pages hold value / scale, limited to +-448.
@@ -411,7 +411,8 @@ int kv_append(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, i
  * between sequences (0: dense; multiples of 16 bytes), d_out[B][n_q_heads][v_dim].  Sums are fp32 and bit-reproducible run to run for the same
  * batch.  A sequence without tokens gets zeros and -inf.  Rows behind a sequence's last token may hold anything.  A page id outside the pool
  * counts as a page that is masked, a length outside [0, table_width * page_size] as the nearest one inside; both raise an error flag.
- * scale must be positive. */
+ * scale must be positive.  Outputs must not overlap inputs.  MOEI_ECAPACITY when B * key/value heads * table_width * page_size (for each 16
+ * query heads of a group) passes 2^37 tokens. */
 int kv_attend(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, int32_t table_width, const int32_t* d_len, int32_t B,
               const void* d_q, int64_t q_stride, float scale, int32_t window, void* d_out, float* d_lse, void* stream);
 

@@ -363,6 +363,9 @@ int fill_attend(const char* who, const moei_kv* kv, const moei_kv_pages* p, cons
     MOEI_REQUIRE(q_stride == 0 || (q_stride >= dense && q_stride * io % 16 == 0), "%s: q_stride = %lld is shorter than a token (%lld) or no multiple of 16 bytes",
                  who, (long long)q_stride, dense);
     MOEI_REQUIRE((uintptr_t)d_q % 16 == 0 && (uintptr_t)d_out % 16 == 0, "%s: d_q and d_out must begin at multiples of 16 bytes", who);
+    const long long units = ((long long)width * d.page_size / 64 + 1) * B * d.n_kv_heads * ((d.n_q_heads / d.n_kv_heads + kKvHeads - 1) / kKvHeads);
+    if (units > 0x7fffffffll)
+        MOEI_FAIL(MOEI_ECAPACITY, "%s: %d sequences of up to %lld tokens are more than one call takes", who, B, (long long)width * d.page_size);
     *a = KvAttendArgs{};
     a->q = d_q;
     a->q_stride = q_stride ? q_stride : dense;
@@ -548,6 +551,7 @@ extern "C" int kv_attend_blocks(moei_kv* kv, const moei_kv_pages* pages, const i
     KvAttendArgs a;
     rc = fill_attend(who, kv, pages, d_table, table_width, d_len, B, d_q, q_stride, scale, d_out, d_lse, &a);
     if (rc) return rc;
+    if (table_width <= n_sel && !d_blocks) return launch_kv_attend(*kv, a, as_stream(stream));  // every page is taken, and nobody asks
     KvBlocksArgs c{};
     c.q = d_q;
     c.q_stride = a.q_stride;

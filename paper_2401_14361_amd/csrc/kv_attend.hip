@@ -626,25 +626,25 @@ __global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kReside
     } while (at_unit < mine_of.end);
 }
 
-LdsLimits<64> g_limits;
+LdsLimits<16> g_limits[8];  // of a device
 
 template <typename T, int KC, int VC, int NWX>
-int launch_shape(const KvAttendArgs& a, int cus, hipStream_t s) {
+int launch_shape(const moei_kv& kv, const KvAttendArgs& a, hipStream_t s) {
     constexpr int NW = NWX;
     constexpr int NS = Shape<T, KC, VC, 2, NW>::kLds <= 160 * 1024 ? 2 : 1;
     using S = Shape<T, KC, VC, NS, NW>;
     static_assert(S::kLds <= 160 * 1024, "the rings fit a compute unit");
     const auto kernel = kv_attend_kernel<T, KC, VC, NS, NW>;
     if (S::kLds > 64 * 1024) {
-        const int rc = g_limits.at_least(reinterpret_cast<const void*>(kernel), S::kLds, [&]() -> int {
+        const auto raise = [&]() -> int {
             MOEI_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, S::kLds));
             return MOEI_OK;
-        });
+        };
+        const int rc = kv.device < 8 ? g_limits[kv.device].at_least(reinterpret_cast<const void*>(kernel), S::kLds, raise) : raise();
         if (rc) return rc;
     }
-    const long long units = ((long long)a.width << a.page_shift) / S::kUnit + 1, line = units * a.B * a.n_kv * a.blocks_of_heads;
-    if (line > 0x7fffffffll) MOEI_FAIL(MOEI_ECAPACITY, "kv_attend: %d sequences of up to %lld tokens are more than one call takes", a.B, (long long)a.width << a.page_shift);
-    const int grid = cus * S::kResident;
+    const long long line = (((long long)a.width << a.page_shift) / S::kUnit + 1) * a.B * a.n_kv * a.blocks_of_heads;  // units, at most
+    const int grid = kv.cus * S::kResident;
     launch(K_KV_ATTEND, kernel, dim3((unsigned)(line < grid ? line : grid)), dim3(NW * kWave), S::kLds, s, a);
     MOEI_LAUNCH_CHECK();
     return MOEI_OK;
@@ -652,20 +652,20 @@ int launch_shape(const KvAttendArgs& a, int cus, hipStream_t s) {
 
 // Heads are padded in LDS to the next of four widths; the classes are the pairs in use, others round both widths up.
 template <typename T>
-int launch_type(const KvAttendArgs& a, int cus, hipStream_t s) {
-    if (a.k_dim <= 64 && a.v_dim <= 64) return launch_shape<T, 64, 64, 8>(a, cus, s);
-    if (a.k_dim <= 128 && a.v_dim <= 128) return launch_shape<T, 128, 128, (T::kBytes == 4 ? 4 : 8)>(a, cus, s);
-    if (a.k_dim <= 192 && a.v_dim <= 128) return launch_shape<T, 192, 128, 4>(a, cus, s);
-    return launch_shape<T, 256, 256, 4>(a, cus, s);
+int launch_type(const moei_kv& kv, const KvAttendArgs& a, hipStream_t s) {
+    if (a.k_dim <= 64 && a.v_dim <= 64) return launch_shape<T, 64, 64, 8>(kv, a, s);
+    if (a.k_dim <= 128 && a.v_dim <= 128) return launch_shape<T, 128, 128, (T::kBytes == 4 ? 4 : 8)>(kv, a, s);
+    if (a.k_dim <= 192 && a.v_dim <= 128) return launch_shape<T, 192, 128, 4>(kv, a, s);
+    return launch_shape<T, 256, 256, 4>(kv, a, s);
 }
 
 }  // namespace
 
 int launch_kv_attend(const moei_kv& kv, const KvAttendArgs& a, hipStream_t s) {
     switch (kv.d.dtype) {
-        case MOEI_WDTYPE_FP32: return launch_type<Fp32>(a, kv.cus, s);
-        case MOEI_WDTYPE_BF16: return launch_type<Bf16>(a, kv.cus, s);
-        default: return launch_type<Fp8>(a, kv.cus, s);
+        case MOEI_WDTYPE_FP32: return launch_type<Fp32>(kv, a, s);
+        case MOEI_WDTYPE_BF16: return launch_type<Bf16>(kv, a, s);
+        default: return launch_type<Fp8>(kv, a, s);
     }
 }
 

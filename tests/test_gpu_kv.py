@@ -465,6 +465,37 @@ def test_attend_blocks_of_many_pages(m, n_sel):
     _check_blocks(c, n_sel, 1, 1)
 
 
+@pytest.mark.parametrize("alike", [False, True])
+def test_attend_blocks_of_more_pages_than_a_workgroup_holds(m, alike):
+    c = Case(m, "bf16", 2, 1, 64, 64, 16, [16 * 9000 - 3, 16 * 8500], seed=5, summaries=True, max_sel=40)
+    if alike:
+        c.lo[c.table.long()[:, :8500]], c.hi[c.table.long()[:, :8500]] = -1.0, 1.0
+    _check_blocks(c, 40, 2, 1)
+
+
+def test_attend_blocks_scores_that_differ_in_the_last_bits_of_fp32(m):
+    # every page has the same large summary but for one small element: fp32 sums cannot tell them apart, sums in 64 bits can
+    c = Case(m, "bf16", 4, 2, 128, 128, 16, [16 * 1500], seed=6, summaries=True, max_sel=64)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    c.lo.copy_(torch.full_like(c.lo, -1000.0))
+    c.hi.copy_(torch.full_like(c.hi, 1000.0))
+    c.hi[:, :, 77] = (1e-4 * torch.rand(c.hi.shape[:2], generator=g, device="cuda")).to(c.hi.dtype)
+    c.q[:, :, 77] = c.q[:, :, 77].abs()
+    _check_blocks(c, 50, 1, 1)
+
+
+def test_attend_blocks_huge_and_tiny_summaries(m):
+    for value in (3e38, 1e-39):
+        c = Case(m, "bf16", 4, 1, 64, 64, 16, [16 * 300], seed=7, summaries=True, max_sel=20)
+        g = torch.Generator(device="cuda")
+        g.manual_seed(2)
+        r = torch.rand(c.hi.shape, generator=g, device="cuda")
+        c.hi.copy_(r * value)
+        c.lo.copy_(-r * value)
+        _check_blocks(c, 20, 0, 2)
+
+
 def test_attend_blocks_equal_and_undefined_scores(m):
     # all pages alike but a few: ties go to the lower page; a score that is no number comes last, also among ties
     c = Case(m, "bf16", 4, 1, 64, 64, 16, [16 * 2000], seed=1, summaries=True, max_sel=64)
@@ -576,6 +607,37 @@ def test_calls_in_captured_graphs_and_on_other_streams(m):
         for a, b in zip(got, (q_out, out_a, out_b, c.k, c.v, c.lo)):
             assert (bits(a) == bits(b)).all()
     assert c.kv.error_flags() == 0
+
+
+def test_two_handles_on_two_streams_at_once(m):
+    cs = [Case(m, "bf16", 8, 2, 128, 128, 16, [5000, 300, 20], seed=s, summaries=True, max_sel=16) for s in (1, 2)]
+    want = [(m.kv_attend(c.kv, c.pages, c.table, c.len_t, c.q, c.scale), m.kv_attend_blocks(c.kv, c.pages, c.table, c.len_t, c.q, c.scale, 9)) for c in cs]
+    streams = [torch.cuda.Stream() for _ in cs]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(20):
+        for c, s, g in zip(cs, streams, got):
+            g.append((m.kv_attend(c.kv, c.pages, c.table, c.len_t, c.q, c.scale, out=torch.empty_like(c.q), stream=s),
+                      m.kv_attend_blocks(c.kv, c.pages, c.table, c.len_t, c.q, c.scale, 9, out=torch.empty_like(c.q), stream=s)))
+    torch.cuda.synchronize()
+    for w, g in zip(want, got):
+        for pair in g:
+            assert all((bits(a) == bits(b)).all() for a, b in zip(pair, w))
+
+
+def test_the_largest_batch(m):
+    # 4,096 slots, most of them without a token
+    rng = np.random.default_rng(0)
+    lens = np.where(rng.random(4096) < 0.05, rng.integers(1, 60, 4096), 0).tolist()
+    lens[4095], lens[64] = 33, 500
+    c = Case(m, "bf16", 2, 1, 64, 64, 16, lens, seed=3)
+    out, lse = m.kv_attend(c.kv, c.pages, c.table, c.len_t, c.q, c.scale, want_lse=True)
+    c.check(out, lse, *c.oracle())
+
+
+def test_whole_sequences_when_the_table_has_no_more_pages_than_wanted(m):
+    c = Case(m, "bf16", 4, 2, 64, 64, 16, [50, 64, 0], seed=1, summaries=True, max_sel=4)
+    assert (bits(m.kv_attend_blocks(c.kv, c.pages, c.table, c.len_t, c.q, c.scale, 4)) == bits(m.kv_attend(c.kv, c.pages, c.table, c.len_t, c.q, c.scale))).all()
 
 
 def test_a_decoder_layer(m):

@@ -4,6 +4,8 @@ import os
 
 import pytest
 
+from tests.test_kernel_resources import kernels  # noqa: F401 (a fixture)
+
 
 @pytest.fixture(scope="module")
 def m():
@@ -54,3 +56,16 @@ def test_null_pointers_are_refused_on_the_host(m):
     assert "negative" in err(L.kv_attend(None, one, one, 1, one, -1, one, 0, 1.0, 0, one, None, None))
     assert "null" in err(L.moei_kv_error_flags(None, None, None))
     assert L.moei_kv_destroy(None) == 0
+
+
+def test_kernels_keep_to_their_registers(kernels):
+    """No private memory, and as few registers as the workgroups that a compute unit is to hold at once allow."""
+    named = {n: k for n, k in kernels.items() if n.startswith("kv_")}
+    assert len(named) >= 4 * 3 + 12 + 6 + 3
+    for n, k in named.items():
+        assert k[".private_segment_fixed_size"] == 0 and k[".vgpr_spill_count"] == 0, n
+    for n, waves_a_simd in (("kv_attend_kernel<moei::Bf16, 128, 128, 2, 8>", 2), ("kv_attend_kernel<moei::Fp8, 128, 128, 2, 8>", 2),
+                            ("kv_attend_kernel<moei::Bf16, 64, 64, 2, 8>", 4), ("kv_attend_kernel<moei::Bf16, 192, 128, 2, 4>", 2),
+                            ("kv_blocks_kernel<unsigned short, 128, 16>", 3), ("kv_append_kernel<unsigned short, unsigned short, 8, false>", 6)):
+        got, = [k for name, k in named.items() if name.startswith(n)]
+        assert waves_a_simd * (got[".vgpr_count"] + 7 & ~7) <= 512, (n, got[".vgpr_count"])
