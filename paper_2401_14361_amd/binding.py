@@ -535,12 +535,13 @@ def _kv_stream(kv: Kv, stream) -> int:
 
 
 def _rows(kv: Kv, t: torch.Tensor, n: int, heads: tuple) -> int:
-    """Checks [n][heads][width] with dense tokens and returns the elements between tokens (0: dense)."""
-    assert t.get_device() == kv.index and t.dtype is kv.dtype and t.shape == (n, *heads), (t.device, t.dtype, t.shape, (n, *heads))
-    if t.is_contiguous():
+    """Checks n tokens' heads - a contiguous tensor of as many elements, or [n][heads][width] with dense tokens - and returns the
+    elements between tokens (0: dense)."""
+    assert t.dtype is kv.dtype and t.get_device() == kv.index, (t.device, t.dtype)
+    if t.is_contiguous() and t.numel() == n * heads[0] * heads[1]:
         return 0
     s = t.stride()
-    assert (s[2] == 1 or heads[1] == 1) and (s[1] == heads[1] or heads[0] == 1), "a token's heads must be dense"
+    assert t.shape == (n, *heads) and (s[2] == 1 or heads[1] == 1) and (s[1] == heads[1] or heads[0] == 1), (t.shape, s, (n, *heads))
     return s[0] if n > 1 else 0
 
 

@@ -417,8 +417,9 @@ __global__ void __launch_bounds__(kThreads, KC > 128 ? 1 : 3) kv_blocks_kernel(K
     const Args a = (Args)__builtin_amdgcn_kernarg_segment_ptr();
     using M = Mm<IO, KC>;
     constexpr int VE = 16 / sizeof(IO);
-    const int b = blockIdx.z, hk = blockIdx.y, x = blockIdx.x;
-    const long long row = (long long)b * gridDim.y + hk;
+    // heads side by side: the dies, which take workgroups in turns, get equal shares of every sequence whatever its length
+    const int b = blockIdx.y, x = blockIdx.x / a->n_kv, hk = blockIdx.x - x * a->n_kv;
+    const long long row = (long long)b * a->n_kv + hk;
     const int tid = threadIdx.x, lane = tid & (kWave - 1), col = lane & 15, grp = lane >> 4;
     const int wv = __builtin_amdgcn_readfirstlane(tid / kWave);
     bool bad;
@@ -445,7 +446,7 @@ __global__ void __launch_bounds__(kThreads, KC > 128 ? 1 : 3) kv_blocks_kernel(K
     if (!none) {
         const int from = max(lo, x * a->per), to = min(hi, (x + 1) * a->per);
         const IO* q0 = static_cast<const IO*>(a->q) + (long long)b * a->q_stride + (long long)hk * a->group * a->k_dim;
-        const long long page_row = (long long)gridDim.y * a->k_dim;
+        const long long page_row = (long long)a->n_kv * a->k_dim;
         const IO *lows = static_cast<const IO*>(a->k_min) + (long long)hk * a->k_dim, *highs = static_cast<const IO*>(a->k_max) + (long long)hk * a->k_dim;
         bool odd = false;     // something is no number, infinite, or a query element below the normal range
         float most = 0.f;     // largest bound of the magnitudes
@@ -555,7 +556,7 @@ int launch_kv_blocks(const moei_kv& kv, KvBlocksArgs a, hipStream_t s) {
     const long long all = (long long)a.width * a.n_kv * a.B;
     long long per = (all / (4 * kv.cus) + 63) / 64 * 64;
     a.per = (int)(per < 64 ? 64 : per > kMostPages ? kMostPages : per);
-    const dim3 grid((unsigned)((a.width + a.per - 1) / a.per), (unsigned)a.n_kv, (unsigned)a.B), block(kThreads);
+    const dim3 grid((unsigned)((a.width + a.per - 1) / a.per * a.n_kv), (unsigned)a.B), block(kThreads);
     if (kv.d.dtype == MOEI_WDTYPE_FP32)
         launch(K_KV_BLOCKS, a.k_dim <= 64 ? kv_blocks_kernel<float, 64, 16> : a.k_dim <= 128 ? kv_blocks_kernel<float, 128, 32> : kv_blocks_kernel<float, 256, 64>, grid, block, 0, s, a);
     else
