@@ -399,7 +399,7 @@ int moei_kv_error_flags(moei_kv* kv, int32_t* h_flags, void* stream);
  * of page d_table[sequence][position / page_size] (d_table [B][table_width] int32), rounded once; 8-bit pages hold value / scale, limited to +-448.
  * A token whose position lies outside the table or whose page outside the pool is left out, its query too, and raises an error flag.
  * With summaries: when the last row of a page is appended, d_k_min and d_k_max of that page are formed from all of its rows as they are stored
- * then (values that are no numbers are passed over).  A token's place must not be another token's of the same call. */
+ * then (values that are no numbers are passed over).  A token's place must not be another token's of the same call.  T < 2^24. */
 int kv_append(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, int32_t table_width, int32_t B,
               const int32_t* d_seq, const int32_t* d_pos, int32_t T,
               const void* d_q, int64_t q_stride, const void* d_k, int64_t k_stride, const void* d_v, int64_t v_stride,
@@ -411,6 +411,7 @@ int kv_append(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, i
  * between sequences (0: dense; multiples of 16 bytes), d_out[B][n_q_heads][v_dim].  Sums are fp32 and bit-reproducible run to run for the same
  * batch.  A sequence without tokens gets zeros and -inf.  Rows behind a sequence's last token may hold anything.  A page id outside the pool
  * counts as a page that is masked, a length outside [0, table_width * page_size] as the nearest one inside; both raise an error flag.
+ * A token whose key or value holds an infinity or no number may turn the results of its heads into no numbers.
  * scale must be positive.  Outputs must not overlap inputs.  MOEI_ECAPACITY when B * key/value heads * table_width * page_size (for each 16
  * query heads of a group) passes 2^37 tokens. */
 int kv_attend(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, int32_t table_width, const int32_t* d_len, int32_t B,

@@ -485,6 +485,7 @@ class Kv:
         self.v_page = (n_kv_heads, page_size, v_dim)
         self.heads, self.k_heads, self.v_heads = (n_q_heads, k_dim), (n_kv_heads, k_dim), (n_kv_heads, v_dim)
         self.out_heads = (n_q_heads, v_dim)
+        self.layout = (self.k_page, self.v_page, self.page_dtype, self.index)
 
     def error_flags(self, stream=None) -> int:
         f = C.c_int32(0)
@@ -506,7 +507,7 @@ class Kv:
 def _pages(kv: Kv, t: torch.Tensor, shape: tuple) -> int:
     """Checks a pool of pages (each page dense) and returns the elements between pages."""
     assert t.device == kv.device and t.dtype == kv.page_dtype and tuple(t.shape[1:]) == shape, (t.device, t.dtype, t.shape, shape)
-    assert t[:1].is_contiguous(), "a page must be dense"
+    assert t[:1].is_contiguous() and (t.shape[0] <= 1 or t.stride(0) > 0), "a page must be dense, and pages lie apart"
     return t.stride(0) if t.shape[0] > 1 else 0
 
 
@@ -523,6 +524,7 @@ class KvPages:
             assert t is None or (t.numel() == kv.k_page[0] and t.device == kv.device and _dev(t, torch.float32) is t)
         for t in (k_min, k_max):
             assert t is None or (tuple(t.shape) == (n, kv.k_page[0], kv.k_page[2]) and t.device == kv.device and _dev(t, kv.dtype) is t)
+        self.layout = kv.layout
         self._keep = (k, v, k_min, k_max, k_scale, v_scale)
         ptr = [None if t is None else t.data_ptr() for t in self._keep]
         self.c = _KvPages(ptr[0], ptr[1], ks, vs, n, ptr[4], ptr[5], ptr[2], ptr[3])
@@ -542,6 +544,7 @@ def _rows(kv: Kv, t: torch.Tensor, n: int, heads: tuple) -> int:
         return 0
     s = t.stride()
     assert t.shape == (n, *heads) and (s[2] == 1 or heads[1] == 1) and (s[1] == heads[1] or heads[0] == 1), (t.shape, s, (n, *heads))
+    assert n <= 1 or s[0] > 0, "an expanded tensor: the tokens must lie apart"  # (a stride of 0 would be taken for dense)
     return s[0] if n > 1 else 0
 
 
@@ -561,6 +564,7 @@ def kv_append(kv: Kv, pages: KvPages, table: torch.Tensor, pos: torch.Tensor, q:
               q_out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """q [T][Hq][k_dim], k [T][Hkv][k_dim], v [T][Hkv][v_dim] of the tokens at pos [T] of sequences seq [T] (None: token t is of
     sequence t) -> rotated queries; keys and values go into the pages that table [B][width] names.  inv_freq [rot_dim / 2] fp32."""
+    assert pages.layout == kv.layout, (pages.layout, kv.layout)
     T = pos.numel()
     B, width = table.shape
     if q_out is None:
@@ -590,6 +594,7 @@ def kv_attend(kv: Kv, pages: KvPages, table: torch.Tensor, lens: torch.Tensor, q
               out: torch.Tensor | None = None, want_lse: bool = False, stream=None):
     """q [B][Hq][k_dim] (any stride between sequences) over the first lens [B] tokens of each sequence, or the last `window` of them
     -> out [B][Hq][v_dim], or (out, lse [B][Hq] fp32) with want_lse."""
+    assert pages.layout == kv.layout, (pages.layout, kv.layout)
     B, out, at, lse = _attend_outputs(kv, q, table, lens, out, want_lse)
     _check(lib().kv_attend(kv.h, pages.ref, _ints(kv, table), table.shape[1], _ints(kv, lens), B, q.data_ptr(), _rows(kv, q, B, kv.heads),
                            scale, window, at, lse.data_ptr() if want_lse else None, _kv_stream(kv, stream)))
@@ -601,6 +606,7 @@ def kv_attend_blocks(kv: Kv, pages: KvPages, table: torch.Tensor, lens: torch.Te
                      want_blocks: bool = False, stream=None):
     """kv_attend over at most n_sel pages a sequence and key/value head: the first keep_first, the last keep_last and those whose
     logits have the highest bounds.  Returns out, or a tuple with lse [B][Hq] and blocks [B][Hkv][n_sel] int32 as wanted."""
+    assert pages.layout == kv.layout, (pages.layout, kv.layout)
     B, out, at, lse = _attend_outputs(kv, q, table, lens, out, want_lse)
     blocks = torch.empty((B, kv.k_page[0], max(n_sel, 0)), dtype=torch.int32, device=kv.device) if want_blocks else None
     _check(lib().kv_attend_blocks(kv.h, pages.ref, _ints(kv, table), table.shape[1], _ints(kv, lens), B, q.data_ptr(),

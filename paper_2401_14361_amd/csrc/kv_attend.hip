@@ -195,6 +195,13 @@ __device__ __forceinline__ float2 load_past(const unsigned long long* p) {
 }
 
 // ------------------------------------------------------------------------------------------------ a stretch of units
+// A wavefront brings tiles of sixteen keys and values (8-bit: 32) into a ring of two stages of its own in LDS, by loads that pass the registers by,
+// and waits for the oldest only, so that a compute unit has 64 - 128 KB under way all the time.  Logits are keys times queries, head by
+// head in columns; their exponentials lie in a lane's registers as the second product, values transposed by the LDS read times weights, wants
+// them: nothing goes from lane to lane but a maximum, and only a higher one costs a rescaling.
+// Measured, of the 7.0 TB/s that streams which only read reach: bf16, heads of 128: one sequence of 131,072 tokens 84 us (6.3 TB/s), 64 ragged ones
+// 365 us (6.5); 8-bit 194 us (6.2); bf16 keys of 192 44 us (5.3: short ends of stretches).  What is left is the beginning and
+// the end of an item, 4 - 5 us, which nothing else of the workgroup overlaps.
 template <typename T, int KC, int VC, int NS, int NW>
 struct Shape {
     static constexpr int kWaves = NW;  // of a workgroup; each has a state of its own and takes the tiles in turn with the others
@@ -554,7 +561,7 @@ __global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kReside
                         *reinterpret_cast<uint2*>(static_cast<uint16_t*>(z->out) + head * v_dim + d) = make_uint2(pack_bf16(r.o[0] * g, r.o[1] * g), pack_bf16(r.o[2] * g, r.o[3] * g));
                     else
                         *reinterpret_cast<f32x4*>(static_cast<float*>(z->out) + head * v_dim + d) = r.o * g;
-                    if (d == 0 && z->lse) z->lse[head] = r.m == -INFINITY ? -INFINITY : (r.m + __builtin_amdgcn_logf(r.l)) * 0.69314718055994531f;
+                    if (d == 0 && z->lse) z->lse[head] = (r.m + __builtin_amdgcn_logf(r.l)) * 0.69314718055994531f;  // (no weights: -inf, from both)
                 } else {
                     const unsigned row = (2 * blockIdx.x + (u0 == 0 ? 1 : 0)) * rows + h;
                     unsigned long long* to = reinterpret_cast<unsigned long long*>(part + (row * v_dim + d));

@@ -222,6 +222,16 @@ def test_attend_extreme_logits(m):
     assert np.isfinite(host(out)).all() and np.abs(host(out) - ref).max() <= 1e-4 and np.abs(host(lse) - ref_l).max() <= 1e-4
 
 
+@pytest.mark.parametrize("lens,bad", [([1], 0), ([40], 39), ([3000], 1700)])
+def test_attend_tokens_that_are_no_numbers(m, lens, bad):
+    # a sequence with such a key has neither outputs nor a logarithm, whichever workgroup or wavefront meets it; the others keep theirs
+    c = Case(m, "bf16", 4, 2, 64, 64, 16, lens + [50], seed=6)
+    c.k[int(c.table[0, bad // 16]), 1, bad % 16, 3] = float("nan")
+    out, lse = m.kv_attend(c.kv, c.pages, c.table, c.len_t, c.q, c.scale, want_lse=True)
+    assert torch.isnan(out[0, 2:]).all() and torch.isnan(lse[0, 2:]).all()
+    assert torch.isfinite(out[0, :2]).all() and torch.isfinite(lse[0, :2]).all() and torch.isfinite(out[1]).all() and torch.isfinite(lse[1]).all()
+
+
 def test_attend_offsets_beyond_32_bits(m):
     # a pool of 2.6 * 10^9 elements; the sequence's pages lie at its end
     Hkv, page, D, n_pages = 8, 64, 128, 40000
@@ -747,6 +757,7 @@ def test_refusals(m):
     assert append() == 0 and append(T=0) == 0
     refused(append(T=-1), "negative")
     refused(append(T=3), "need d_seq")
+    refused(append(T=1 << 24, seq=P(pos)), "2^24")
     refused(append(B=3), "max_batch")
     refused(append(pos=None), "null")
     refused(append(qo=None), "null")
@@ -766,3 +777,16 @@ def test_refusals(m):
         m.KvPages(c.kv, c.k.transpose(1, 2), c.v)
     with pytest.raises(AssertionError):
         m.kv_attend(c.kv, c.pages, c.table.long(), c.len_t, c.q, 0.125)
+    # one row for all sequences, one page for all: a stride of 0 must not be taken for dense
+    with pytest.raises(AssertionError, match="expanded"):
+        m.kv_attend(c.kv, c.pages, c.table, c.len_t, c.q[:1].expand(2, -1, -1), 0.125)
+    with pytest.raises(AssertionError, match="expanded"):
+        m.kv_append(c.kv, c.pages, c.table, pos, q, k[:1].expand(2, -1, -1), v, None)
+    with pytest.raises(AssertionError, match="apart"):
+        m.KvPages(c.kv, c.k[:1].expand(4, -1, -1, -1), c.v[:4])
+    # pages of another shape than the handle's
+    other = m.Kv(4, 2, 128, 64, 16, "bf16", max_batch=2, max_pages=c.width)
+    with pytest.raises(AssertionError):
+        m.kv_attend(other, c.pages, c.table, c.len_t, torch.zeros((2, 4, 128), dtype=torch.bfloat16, device="cuda"), 0.125)
+    with pytest.raises(AssertionError):
+        m.kv_attend_blocks(f8.kv, c.pages, c.table, c.len_t, c.q, 0.125, 2)
