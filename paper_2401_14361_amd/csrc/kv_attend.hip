@@ -62,8 +62,9 @@ struct Stretch {
     int len;              // and its length
 };
 
-// An item more in a stretch costs as much as two units or so: where the items are no more than the workgroups, a stretch may be longer by a
-// quarter, or by two units, if then none crosses from an item to the next.
+// An item more in a stretch costs as much as two to four units: where the items are no more than the workgroups, a stretch may be longer by a
+// quarter, or by four units, if then none crosses from an item to the next.  (64 sequences of up to 1,000 tokens, four heads of 128: 19.7 us, with
+// two units 26.5; of up to 2,000 in 8 bits 21.6 and 31.8; with six units as with four.)
 template <int kUnit>
 __device__ __forceinline__ Stretch my_stretch(Args a, int lane) {
     const unsigned items = a->n_kv * a->blocks_of_heads, grid = gridDim.x;
@@ -82,7 +83,7 @@ __device__ __forceinline__ Stretch my_stretch(Args a, int lane) {
     s.per = (total + grid - 1) / grid;
     s.step = 1;
     if (a->B * items <= grid) {
-        const unsigned most = s.per + max(2u, s.per / 4);
+        const unsigned most = s.per + max(4u, s.per / 4);
         for (unsigned per = s.per; per <= most; per += max(1u, s.per / 16)) {
             unsigned parts = 0;
             for (int b0 = 0; b0 < a->B; b0 += kWave) {
@@ -658,10 +659,28 @@ int launch_shape(const moei_kv& kv, const KvAttendArgs& a, hipStream_t s) {
 }
 
 // Heads are padded in LDS to the next of four widths; the classes are the pairs in use, others round both widths up.
+// Many short items: four wavefronts, so that a compute unit holds twice as many workgroups, of which one streams while another goes from an item
+// to the next.  Up to 1 MB an item, and half as many items as compute units at least: 64 sequences of up to 2,000 tokens with four heads of 128
+// 30.8 us (eight wavefronts: 36.3), 160 of up to 200 18.5 (22.8), in 8 bits 100 of up to 1,000 25 (31); long ones the other way round: 64 of up to
+// 16,384 with eight heads 384 (380), 100 of up to 4,000 86 (76).  Items of one length, as lists and windows make them, keep eight wavefronts while each
+// has a workgroup to itself: 24 lists of 1,536 tokens with eight heads 19.7 (four: 24.2).
+template <typename T>
+bool many_short_items(const moei_kv& kv, const KvAttendArgs& a) {
+    const long long items = (long long)a.B * a.n_kv * a.blocks_of_heads;
+    long long longest = (long long)a.width << a.page_shift;
+    if (a.list) longest = min(longest, (long long)a.n_sel << a.page_shift);
+    if (a.window > 0) longest = min(longest, (long long)a.window);
+    return items > (a.list || a.window > 0 ? kv.cus : kv.cus / 2) && longest * (a.k_dim + a.v_dim) * T::kBytes <= 1 << 20;
+}
+
 template <typename T>
 int launch_type(const moei_kv& kv, const KvAttendArgs& a, hipStream_t s) {
-    if (a.k_dim <= 64 && a.v_dim <= 64) return launch_shape<T, 64, 64, 8>(kv, a, s);
-    if (a.k_dim <= 128 && a.v_dim <= 128) return launch_shape<T, 128, 128, (T::kBytes == 4 ? 4 : 8)>(kv, a, s);
+    const bool many = many_short_items<T>(kv, a);
+    if (a.k_dim <= 64 && a.v_dim <= 64) return many ? launch_shape<T, 64, 64, 4>(kv, a, s) : launch_shape<T, 64, 64, 8>(kv, a, s);
+    if (a.k_dim <= 128 && a.v_dim <= 128) {
+        if (T::kBytes == 4 || many) return launch_shape<T, 128, 128, 4>(kv, a, s);
+        if constexpr (T::kBytes != 4) return launch_shape<T, 128, 128, 8>(kv, a, s);
+    }
     if (a.k_dim <= 192 && a.v_dim <= 128) return launch_shape<T, 192, 128, 4>(kv, a, s);
     return launch_shape<T, 256, 256, 4>(kv, a, s);
 }

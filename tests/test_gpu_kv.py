@@ -222,6 +222,19 @@ def test_attend_extreme_logits(m):
     assert np.isfinite(host(out)).all() and np.abs(host(out) - ref).max() <= 1e-4 and np.abs(host(lse) - ref_l).max() <= 1e-4
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp8", "fp32"])
+@pytest.mark.parametrize("D,top", [(64, 300), (80, 200), (128, 700)])
+@pytest.mark.parametrize("window", [0, 90])
+def test_attend_many_short_sequences(m, dtype, D, top, window):
+    # 280 heads of sequences, empty ones and full tables among them: more than a compute unit each
+    lens = [(37 * b * b + 11 * b) % (top + 1) for b in range(139)] + [top]
+    c = Case(m, dtype, 4, 2, D, D, 32, lens, seed=D + window)
+    out, lse = m.kv_attend(c.kv, c.pages, c.table, c.len_t, c.q, c.scale, window=window, want_lse=True)
+    c.check(out, lse, *c.oracle(window=window))
+    again, lse2 = m.kv_attend(c.kv, c.pages, c.table, c.len_t, c.q, c.scale, window=window, want_lse=True)
+    assert torch.equal(out, again) and torch.equal(lse, lse2)
+
+
 @pytest.mark.parametrize("lens,bad", [([1], 0), ([40], 39), ([3000], 1700)])
 def test_attend_tokens_that_are_no_numbers(m, lens, bad):
     # a sequence with such a key has neither outputs nor a logarithm, whichever workgroup or wavefront meets it; the others keep theirs
