@@ -74,10 +74,15 @@ __device__ __forceinline__ u64 exact_key(Args a, int b, int hk, int pg, int lane
     WVec<IO>::unpack(ok && in ? WVec<IO>::load(static_cast<const IO*>(a->k_min) + row) : WVec<IO>::zero(), lo);
     WVec<IO>::unpack(ok && in ? WVec<IO>::load(static_cast<const IO*>(a->k_max) + row) : WVec<IO>::zero(), hi);
     double best = -(double)INFINITY;
-    for (int h = 0; h < a->group; h += 4) {
-        typename WVec<IO>::raw raw[4];
+    typename WVec<IO>::raw next[4];
+    auto fetch = [&](int h) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) raw[i] = in ? WVec<IO>::load(q + min(h + i, a->group - 1) * a->k_dim) : WVec<IO>::zero();  // (a repeated head changes no maximum)
+        for (int i = 0; i < 4; ++i) next[i] = in ? WVec<IO>::load(q + min(h + i, a->group - 1) * a->k_dim) : WVec<IO>::zero();  // (a repeated head changes no maximum)
+    };
+    fetch(0);
+    for (int h = 0; h < a->group; h += 4) {
+        typename WVec<IO>::raw raw[4] = {next[0], next[1], next[2], next[3]};
+        if (h + 4 < a->group) fetch(h + 4);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             float x[VE];
@@ -169,9 +174,10 @@ struct Place {
     }
 };
 
-// The list of a (sequence, key/value head) from its scores in fp32, whose error is at most `eps`, by one workgroup.
+// The list of a (sequence, key/value head) from its scores in fp32, whose error is at most `eps`, by one workgroup.  They are in memory or, where
+// the workgroup has scored all of the pages itself (`alone`), in `own` (LDS).
 template <typename IO, int LP>
-__device__ __forceinline__ void choose(Args a, Shared& sh, long long row, int b, int hk, int nb, float eps, int32_t* out) {
+__device__ __forceinline__ void choose(Args a, Shared& sh, const float* own, bool alone, long long row, int b, int hk, int nb, float eps, int32_t* out) {
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
     const int wv = __builtin_amdgcn_readfirstlane(tid / kWave);
     const int lo = a->keep_first, n = nb - a->keep_last - lo;
@@ -182,13 +188,17 @@ __device__ __forceinline__ void choose(Args a, Shared& sh, long long row, int b,
     const float* scores = a->scores + row * a->width + lo;
     u64* keys = a->keys + row * a->width + lo;
     const bool held = n <= kHeld;
+    constexpr int kPer = kWave / LP;  // pages of a wavefront at a time, in 64 bits
     auto key_at = [&](int i) __attribute__((always_inline)) { return held ? sh.held[i] : key_of(load_past(&scores[i])); };
 
     unsigned low = ~0u, high = 0u;
     for (int i0 = tid; i0 < n; i0 += 8 * kThreads) {  // (eight under way)
         float s[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) s[j] = load_past(&scores[min(i0 + j * kThreads, n - 1)]);
+        for (int j = 0; j < 8; ++j) {
+            const int i = min(i0 + j * kThreads, n - 1);
+            s[j] = alone ? own[min(i, kMostPages - 1)] : load_past(&scores[i]);
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const unsigned k = key_of(s[j]);
@@ -213,7 +223,7 @@ __device__ __forceinline__ void choose(Args a, Shared& sh, long long row, int b,
     unsigned above = ~0u, below = 0u;  // keys over `above` are in, keys under `below` out, those between are open
     if (eps < INFINITY) {              // (else something was no number, or infinite: all are open)
         Place<unsigned> at(low, high, n, want);
-        while (at.bits < 32 && (at.bits == 0 || at.count > kFew / 4))  // near enough: the few that share its bits stay open
+        while (at.bits < 32 && (at.bits == 0 || at.count > 4))  // near enough: the few that share its bits stay open
             at.step(sh, [&](auto f) __attribute__((always_inline)) {
                 for (int i = tid; i < n; i += kThreads) f(key_at(i));
             }, tid);
@@ -250,7 +260,6 @@ __device__ __forceinline__ void choose(Args a, Shared& sh, long long row, int b,
         at += w < wv ? sh.sure[w] : 0;
     }
     const int all_open = sh.n_few;
-    constexpr int kPer = kWave / LP;  // pages of a wavefront at a time, in 64 bits
     const unsigned no_key = ~0u;      // (a score has no such bits)
     unsigned line = above == no_key ? no_key : above + 1;  // keys from here on are in
     bool by_key = false;  // ... and open ones by their exact keys in memory: above `cut`, or equal to it and among the first `rest`
@@ -526,8 +535,8 @@ __global__ void __launch_bounds__(kThreads, KC > 128 ? 1 : 3) kv_blocks_kernel(K
         barrier_lds();
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) eps = fmaxf(eps, s_eps[w]);
-        for (int i = tid; i < to - from; i += kThreads) store_past(&a->scores[row * a->width + from + i], s_score[i]);  // past the caches
         if (x1 > x0) {
+            for (int i = tid; i < to - from; i += kThreads) store_past(&a->scores[row * a->width + from + i], s_score[i]);  // past the caches
             if (tid == 0) (void)__hip_atomic_fetch_max(&a->eps[row], __float_as_uint(eps), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
             wait_vm_fence<0>();  // scores and error have arrived before they are counted
             barrier_lds();
@@ -543,12 +552,9 @@ __global__ void __launch_bounds__(kThreads, KC > 128 ? 1 : 3) kv_blocks_kernel(K
             barrier_lds();
             if (!s_arrived) return;
             eps = __uint_as_float(s_row_eps);
-        } else {
-            wait_vm_fence<0>();
-            barrier_lds();
         }
     }
-    choose<IO, LP>(again(a), sh, row, b, hk, nb, eps, out);
+    choose<IO, LP>(again(a), sh, s_score, x0 == x1, row, b, hk, nb, eps, out);
 }
 
 }  // namespace
