@@ -659,11 +659,12 @@ int launch_shape(const moei_kv& kv, const KvAttendArgs& a, hipStream_t s) {
 }
 
 // Heads are padded in LDS to the next of four widths; the classes are the pairs in use, others round both widths up.
-// Many short items: four wavefronts, so that a compute unit holds twice as many workgroups, of which one streams while another goes from an item
+// Many short items: half as many wavefronts, so that a compute unit holds twice as many workgroups, of which one streams while another goes from an item
 // to the next.  Up to 1 MB an item, and half as many items as compute units at least: 64 sequences of up to 2,000 tokens with four heads of 128
 // 30.8 us (eight wavefronts: 36.3), 160 of up to 200 18.5 (22.8), in 8 bits 100 of up to 1,000 25 (31); long ones the other way round: 64 of up to
 // 16,384 with eight heads 384 (380), 100 of up to 4,000 86 (76).  Items of one length, as lists and windows make them, keep eight wavefronts while each
-// has a workgroup to itself: 24 lists of 1,536 tokens with eight heads 19.7 (four: 24.2).
+// has a workgroup to itself: 24 lists of 1,536 tokens with eight heads 19.7 (four: 24.2).  Heads of 256, where two take the place of four: 48 lists of 384 tokens with
+// eight heads 32.4 (36.2).
 template <typename T>
 bool many_short_items(const moei_kv& kv, const KvAttendArgs& a) {
     const long long items = (long long)a.B * a.n_kv * a.blocks_of_heads;
@@ -682,6 +683,8 @@ int launch_type(const moei_kv& kv, const KvAttendArgs& a, hipStream_t s) {
         if constexpr (T::kBytes != 4) return launch_shape<T, 128, 128, 8>(kv, a, s);
     }
     if (a.k_dim <= 192 && a.v_dim <= 128) return launch_shape<T, 192, 128, 4>(kv, a, s);
+    if constexpr (T::kBytes != 4)
+        if (many) return launch_shape<T, 256, 256, 2>(kv, a, s);
     return launch_shape<T, 256, 256, 4>(kv, a, s);
 }
 

@@ -424,7 +424,7 @@ __device__ __forceinline__ float row_max(float v) {  // over sixteen lanes
 // the magnitudes sum up to (twice what rounding to nearest would allow), as is an fp32 product: (4 k_dim + 4) 2^-23 sum_d |q_d| max(|k_min_d|, |k_max_d|),
 // which is summed up alongside.  Products and elements below the normal range may be lost: 2^-125 of the largest query for each.
 template <typename IO, int KC, int LP>
-__global__ void __launch_bounds__(kThreads, KC > 128 ? 1 : 3) kv_blocks_kernel(KvBlocksArgs) {
+__global__ void __launch_bounds__(kThreads, KC > 128 ? 1 : KC * sizeof(IO) > 256 ? 2 : 3) kv_blocks_kernel(KvBlocksArgs) {
     const Args a = (Args)__builtin_amdgcn_kernarg_segment_ptr();
     using M = Mm<IO, KC>;
     constexpr int VE = 16 / sizeof(IO);
@@ -464,27 +464,7 @@ __global__ void __launch_bounds__(kThreads, KC > 128 ? 1 : 3) kv_blocks_kernel(K
         float biggest = 0.f;  // largest query element
         bool lost = false;
         for (int h0 = 0; h0 < a->group; h0 += kKvHeads) {
-            u32x4 up[M::kUnits], down[M::kUnits];
-            {
-                const IO* src = q0 + (long long)min(h0 + col, a->group - 1) * a->k_dim;  // (a repeated head changes no maximum)
-#pragma unroll
-                for (int u = 0; u < M::kUnits; ++u) {
-                    const int d = (4 * u + grp) * VE;
-                    u32x4 v{};
-                    if (d < a->k_dim) v = *reinterpret_cast<const u32x4*>(src + d);
-                    up[u] = M::positive(v);
-                    down[u] = v ^ up[u];
-                    float f[VE];
-                    if constexpr (sizeof(IO) == 2) WVec<IO>::unpack(make_uint4(v[0], v[1], v[2], v[3]), f);
-                    else WVec<IO>::unpack(make_float4(__uint_as_float(v[0]), __uint_as_float(v[1]), __uint_as_float(v[2]), __uint_as_float(v[3])), f);
-#pragma unroll
-                    for (int j = 0; j < VE; ++j) {
-                        const float m = fabsf(f[j]);
-                        odd |= !(m < INFINITY) || (m < 0x1p-126f && m != 0.f);
-                        biggest = fmaxf(biggest, m);
-                    }
-                }
-            }
+            // Pages' numbers, queries and the first summaries are under way together.
             u32x4 l[M::kUnits], h[M::kUnits];
             bool there = false;
             const int32_t* table = a->table + (long long)b * a->width;
@@ -504,8 +484,33 @@ __global__ void __launch_bounds__(kThreads, KC > 128 ? 1 : 3) kv_blocks_kernel(K
                 const int pg = p0 + kWaves * 16 + col;  // the pages behind
                 at = pg < to ? table[pg] : -1;
             };
+            u32x4 up[M::kUnits], down[M::kUnits];
+            const IO* src = q0 + (long long)min(h0 + col, a->group - 1) * a->k_dim;  // (a repeated head changes no maximum)
+#pragma unroll
+            for (int u = 0; u < M::kUnits; ++u) {
+                const int d = (4 * u + grp) * VE;
+                up[u] = u32x4{};
+                if (d < a->k_dim) up[u] = *reinterpret_cast<const u32x4*>(src + d);
+            }
+            constexpr bool kAhead = KC * sizeof(IO) <= 512;  // (a wider row's summaries and queries are all that the registers hold)
+            if (kAhead) fetch(from + wv * 16);
+#pragma unroll
+            for (int u = 0; u < M::kUnits; ++u) {
+                const u32x4 v = up[u];
+                up[u] = M::positive(v);
+                down[u] = v ^ up[u];
+                float f[VE];
+                if constexpr (sizeof(IO) == 2) WVec<IO>::unpack(make_uint4(v[0], v[1], v[2], v[3]), f);
+                else WVec<IO>::unpack(make_float4(__uint_as_float(v[0]), __uint_as_float(v[1]), __uint_as_float(v[2]), __uint_as_float(v[3])), f);
+#pragma unroll
+                for (int j = 0; j < VE; ++j) {
+                    const float m = fabsf(f[j]);
+                    odd |= !(m < INFINITY) || (m < 0x1p-126f && m != 0.f);
+                    biggest = fmaxf(biggest, m);
+                }
+            }
             for (int p0 = from + wv * 16; p0 < to; p0 += kWaves * 16) {
-                fetch(p0);
+                if (!kAhead) fetch(p0);
                 f32x4 s{}, m{};
                 lost |= !there && p0 + col < to;
 #pragma unroll
@@ -515,6 +520,7 @@ __global__ void __launch_bounds__(kThreads, KC > 128 ? 1 : 3) kv_blocks_kernel(K
                     m = M::mul(M::larger(M::magnitude(l[u]), M::magnitude(h[u])), M::magnitude(up[u] | down[u]), m);
                 }
                 const unsigned long long have = __ballot(there);
+                if (kAhead && p0 + kWaves * 16 < to) fetch(p0 + kWaves * 16);
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {  // lane (col, grp) holds head col's sums of pages 4 grp + r
                     odd |= !(m[r] < INFINITY);

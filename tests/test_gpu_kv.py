@@ -223,7 +223,7 @@ def test_attend_extreme_logits(m):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "fp8", "fp32"])
-@pytest.mark.parametrize("D,top", [(64, 300), (80, 200), (128, 700)])
+@pytest.mark.parametrize("D,top", [(64, 300), (80, 200), (128, 700), (256, 150)])
 @pytest.mark.parametrize("window", [0, 90])
 def test_attend_many_short_sequences(m, dtype, D, top, window):
     # 280 heads of sequences, empty ones and full tables among them: more than a compute unit each
