@@ -579,25 +579,32 @@ def kv_append(kv: Kv, pages: KvPages, table: torch.Tensor, pos: torch.Tensor, q:
     return q_out
 
 
-def _attend_outputs(kv: Kv, q, table, lens, out, want_lse):
-    B = q.shape[0]
-    assert table.shape[0] == B and lens.numel() == B
+def _attend_args(kv: Kv, pages: KvPages, table, lens, q, out, want_lse):
+    """Checks what kv_attend and kv_attend_blocks have in common, once: their library call takes as long as these lines."""
+    assert pages.layout == kv.layout, (pages.layout, kv.layout)
+    B, width = table.shape
+    at, i32 = kv.index, torch.int32
+    assert table.dtype is i32 and lens.dtype is i32 and table.get_device() == at and lens.get_device() == at, (table.device, table.dtype, lens.device, lens.dtype)
+    assert table.is_contiguous() and lens.is_contiguous() and lens.numel() == B, (table.shape, lens.shape)
+    stride = _rows(kv, q, B, kv.heads)
     if out is None:
-        out = torch.empty_like(q, memory_format=torch.contiguous_format) if kv.out_heads == kv.heads else q.new_empty((B, *kv.out_heads))
-        at = out.data_ptr()
+        if kv.out_heads != kv.heads:
+            out = q.new_empty((B, *kv.out_heads))
+        else:
+            out = torch.empty_like(q) if stride == 0 else torch.empty_like(q, memory_format=torch.contiguous_format)
+        to = out.data_ptr()
     else:
-        at = _given(kv, out, B, kv.out_heads)
-    return B, out, at, q.new_empty((B, kv.heads[0]), dtype=torch.float32) if want_lse else None
+        to = _given(kv, out, B, kv.out_heads)
+    lse = q.new_empty((B, kv.heads[0]), dtype=torch.float32) if want_lse else None
+    return B, width, table.data_ptr(), lens.data_ptr(), stride, out, to, lse, lse.data_ptr() if want_lse else None
 
 
 def kv_attend(kv: Kv, pages: KvPages, table: torch.Tensor, lens: torch.Tensor, q: torch.Tensor, scale: float, window: int = 0,
               out: torch.Tensor | None = None, want_lse: bool = False, stream=None):
     """q [B][Hq][k_dim] (any stride between sequences) over the first lens [B] tokens of each sequence, or the last `window` of them
     -> out [B][Hq][v_dim], or (out, lse [B][Hq] fp32) with want_lse."""
-    assert pages.layout == kv.layout, (pages.layout, kv.layout)
-    B, out, at, lse = _attend_outputs(kv, q, table, lens, out, want_lse)
-    _check(lib().kv_attend(kv.h, pages.ref, _ints(kv, table), table.shape[1], _ints(kv, lens), B, q.data_ptr(), _rows(kv, q, B, kv.heads),
-                           scale, window, at, lse.data_ptr() if want_lse else None, _kv_stream(kv, stream)))
+    B, width, table_at, lens_at, stride, out, out_at, lse, lse_at = _attend_args(kv, pages, table, lens, q, out, want_lse)
+    _check(lib().kv_attend(kv.h, pages.ref, table_at, width, lens_at, B, q.data_ptr(), stride, scale, window, out_at, lse_at, _kv_stream(kv, stream)))
     return (out, lse) if want_lse else out
 
 
@@ -606,12 +613,10 @@ def kv_attend_blocks(kv: Kv, pages: KvPages, table: torch.Tensor, lens: torch.Te
                      want_blocks: bool = False, stream=None):
     """kv_attend over at most n_sel pages a sequence and key/value head: the first keep_first, the last keep_last and those whose
     logits have the highest bounds.  Returns out, or a tuple with lse [B][Hq] and blocks [B][Hkv][n_sel] int32 as wanted."""
-    assert pages.layout == kv.layout, (pages.layout, kv.layout)
-    B, out, at, lse = _attend_outputs(kv, q, table, lens, out, want_lse)
+    B, width, table_at, lens_at, stride, out, out_at, lse, lse_at = _attend_args(kv, pages, table, lens, q, out, want_lse)
     blocks = torch.empty((B, kv.k_page[0], max(n_sel, 0)), dtype=torch.int32, device=kv.device) if want_blocks else None
-    _check(lib().kv_attend_blocks(kv.h, pages.ref, _ints(kv, table), table.shape[1], _ints(kv, lens), B, q.data_ptr(),
-                                  _rows(kv, q, B, kv.heads), scale, n_sel, keep_first, keep_last, at,
-                                  lse.data_ptr() if want_lse else None, blocks.data_ptr() if want_blocks else None, _kv_stream(kv, stream)))
+    _check(lib().kv_attend_blocks(kv.h, pages.ref, table_at, width, lens_at, B, q.data_ptr(), stride, scale, n_sel, keep_first, keep_last,
+                                  out_at, lse_at, blocks.data_ptr() if want_blocks else None, _kv_stream(kv, stream)))
     got = (out,) + ((lse,) if want_lse else ()) + ((blocks,) if want_blocks else ())
     return got if len(got) > 1 else out
 
