@@ -540,7 +540,7 @@ __global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kReside
         // past the caches: a workgroup on another die may read them before this launch ends.
         float* const part = a->part;
         unsigned long long* const part_stat = reinterpret_cast<unsigned long long*>(a->stat);
-        const int my_head = threadIdx.x / kQuads, d = threadIdx.x % kQuads * 4;
+        const int my_head = threadIdx.x < kAtOnce * kQuads ? threadIdx.x / kQuads : 1 << 20, d = threadIdx.x % kQuads * 4;
         bool write = whole;
         for (;;) {
             for (int h = my_head; h < heads; h += kAtOnce) {
@@ -636,12 +636,12 @@ __global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kReside
 
 LdsLimits<16> g_limits[8];  // of a device
 
-template <typename T, int KC, int VC, int NWX>
+template <typename T, int KC, int VC, int NW>
 int launch_shape(const moei_kv& kv, const KvAttendArgs& a, hipStream_t s) {
-    constexpr int NW = NWX;
-    constexpr int NS = Shape<T, KC, VC, 2, NW>::kLds <= 160 * 1024 ? 2 : 1;
+    constexpr int kMost = 160 * 1024;
+    constexpr int NS = KC == 96 && Shape<T, KC, VC, 3, NW>::kLds <= kMost ? 3 : Shape<T, KC, VC, 2, NW>::kLds <= kMost ? 2 : 1;
     using S = Shape<T, KC, VC, NS, NW>;
-    static_assert(S::kLds <= 160 * 1024, "the rings fit a compute unit");
+    static_assert(S::kLds <= kMost, "the rings fit a compute unit");
     const auto kernel = kv_attend_kernel<T, KC, VC, NS, NW>;
     if (S::kLds > 64 * 1024) {
         const auto raise = [&]() -> int {
@@ -658,7 +658,9 @@ int launch_shape(const moei_kv& kv, const KvAttendArgs& a, hipStream_t s) {
     return MOEI_OK;
 }
 
-// Heads are padded in LDS to the next of four widths; the classes are the pairs in use, others round both widths up.
+// Heads are padded in LDS to the next of four widths; the classes are the pairs in use, others round both widths up.  In fp32, whose rings
+// leave room for one workgroup of four wavefronts, 96 is one more: its three stages hold as many bytes that count as two of 128 with padding
+// hold in all (16 sequences of 8,192 tokens, four heads of 96: 66 us, by the class of 128 84; in bf16 36 both ways).
 // Many short items: half as many wavefronts, so that a compute unit holds twice as many workgroups, of which one streams while another goes from an item
 // to the next.  Up to 1 MB an item, and half as many items as compute units at least: 64 sequences of up to 2,000 tokens with four heads of 128
 // 30.8 us (eight wavefronts: 36.3), 160 of up to 200 18.5 (22.8), in 8 bits 100 of up to 1,000 25 (31); long ones the other way round: 64 of up to
@@ -678,6 +680,8 @@ template <typename T>
 int launch_type(const moei_kv& kv, const KvAttendArgs& a, hipStream_t s) {
     const bool many = many_short_items<T>(kv, a);
     if (a.k_dim <= 64 && a.v_dim <= 64) return many ? launch_shape<T, 64, 64, 4>(kv, a, s) : launch_shape<T, 64, 64, 8>(kv, a, s);
+    if constexpr (T::kBytes == 4)
+        if (a.k_dim <= 96 && a.v_dim <= 96) return launch_shape<T, 96, 96, 4>(kv, a, s);
     if (a.k_dim <= 128 && a.v_dim <= 128) {
         if (T::kBytes == 4 || many) return launch_shape<T, 128, 128, 4>(kv, a, s);
         if constexpr (T::kBytes != 4) return launch_shape<T, 128, 128, 8>(kv, a, s);

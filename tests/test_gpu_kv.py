@@ -133,6 +133,8 @@ ATTEND = [
     ("fp32", 3, 1, 128, 112, 32, [65, 200]),
     ("fp32", 2, 2, 192, 128, 16, [31]),
     ("fp32", 5, 1, 256, 240, 64, [130, 64]),
+    ("fp32", 6, 2, 96, 80, 32, [1000, 31, 0, 65]),   # three stages
+    ("fp32", 16, 1, 80, 96, 16, [2000]),
 ]
 
 
