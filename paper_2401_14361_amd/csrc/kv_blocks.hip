@@ -417,8 +417,8 @@ __device__ __forceinline__ float row_max(float v) {  // over sixteen lanes
 
 // A workgroup scores a share of a (sequence, key/value head)'s pages, a wavefront sixteen at a time; the last workgroup of a head to store its
 // scores chooses: a launch of its own for the choice would begin when this one has ended for all heads.  One sequence of 2,048 pages and eight
-// heads 18 us: reading 4, arrival 2.4 - 4, the choice 8 (bound by the trips through LDS of its two or three steps).  24 sequences of up to 2,048 pages
-// 36 - 41 us, of which the summaries, 100 MB in rows of 256 bytes, take 24 (4.8 TB/s).
+// heads 17 us: reading 3.3, arrival 2.4 - 4, the choice 8 (bound by the trips through LDS of its two or three steps).  24 sequences of up to 2,048
+// pages 34 - 39 us, of which the summaries, 100 MB in rows of 256 bytes, take 21 (4.8 TB/s).
 //
 // The error of a score: 2 k_dim products, exact for bf16, are added in fp32 in some order; each addition is off by at most 2^-23 of what
 // the magnitudes sum up to (twice what rounding to nearest would allow), as is an fp32 product: (4 k_dim + 4) 2^-23 sum_d |q_d| max(|k_min_d|, |k_max_d|),
