@@ -498,6 +498,30 @@ def test_attend_blocks_of_more_pages_than_a_workgroup_holds(m, alike):
     _check_blocks(c, 40, 2, 1)
 
 
+@pytest.mark.parametrize("dtype,D", [("bf16", 32), ("fp32", 16), ("fp32", 144)])
+def test_attend_blocks_of_large_batches(m, dtype, D):
+    # 128 sequences of up to 500 pages with eight heads, over a small pool that they share: a workgroup has all pages of a head, several steps of them
+    B, Hkv, width, n_pages, n_sel = 128, 8, 500, 40, 12
+    g = torch.Generator(device="cuda")
+    g.manual_seed(D)
+    kv = m.Kv(2 * Hkv, Hkv, D, 16, 16, dtype, max_batch=B, max_pages=width, max_sel=n_sel)
+    k = torch.randn((n_pages, Hkv, 16, D), generator=g, device="cuda").to(kv.dtype)
+    v = torch.randn((n_pages, Hkv, 16, 16), generator=g, device="cuda").to(kv.dtype)
+    lo, hi = k.amin(2), k.amax(2)
+    pages = m.KvPages(kv, k, v, k_min=lo, k_max=hi)
+    table = torch.randint(0, n_pages, (B, width), generator=g, device="cuda", dtype=torch.int32)
+    n_blocks = [(b * 73) % 480 + 21 if b else width for b in range(B)]
+    lens = torch.tensor([16 * n - b % 16 for b, n in enumerate(n_blocks)], dtype=torch.int32, device="cuda")
+    q = torch.randn((B, 2 * Hkv, D), generator=g, device="cuda").to(kv.dtype)
+    _, blocks = m.kv_attend_blocks(kv, pages, table, lens, q, D ** -0.5, n_sel, keep_first=1, keep_last=2, want_blocks=True)
+    got, tab, qh, lo, hi = blocks.cpu().numpy(), table.cpu().numpy(), host(q), host(lo), host(hi)
+    for b in (0, 1, 2, 3, 60, 127):  # (many scores are equal: pages are repeated)
+        for h in (0, 3, 7):
+            at = tab[b, :n_blocks[b]]
+            assert got[b, h].tolist() == O.choose(qh[b, 2 * h:2 * h + 2], lo[at, h], hi[at, h], n_blocks[b], n_sel, 1, 2), (b, h)
+    assert kv.error_flags() == 0
+
+
 def test_attend_blocks_scores_that_differ_in_the_last_bits_of_fp32(m):
     # every page has the same large summary but for one small element: fp32 sums cannot tell them apart, sums in 64 bits can
     c = Case(m, "bf16", 4, 2, 128, 128, 16, [16 * 1500], seed=6, summaries=True, max_sel=64)
