@@ -354,6 +354,12 @@ void strides_of(const moei_kv* kv, const moei_kv_pages* p, long long* k, long lo
     *v = p->v_stride ? p->v_stride : rows * kv->d.v_dim;
 }
 
+// Whether `n` rows of `row` bytes, `stride` bytes apart, reach into `m` bytes at `b`.
+bool overlap(const void* a, long long n, long long stride, long long row, const void* b, long long m) {
+    const uintptr_t p = (uintptr_t)a, q = (uintptr_t)b;
+    return p < q + (uintptr_t)m && q < p + (uintptr_t)((n - 1) * stride + row);
+}
+
 int fill_attend(const char* who, const moei_kv* kv, const moei_kv_pages* p, const int32_t* d_table, int32_t width, const int32_t* d_len,
                 int32_t B, const void* d_q, int64_t q_stride, float scale, void* d_out, float* d_lse, KvAttendArgs* a) {
     const moei_kv_desc& d = kv->d;
@@ -364,6 +370,8 @@ int fill_attend(const char* who, const moei_kv* kv, const moei_kv_pages* p, cons
     MOEI_REQUIRE(q_stride == 0 || (q_stride >= dense && q_stride * io % 16 == 0), "%s: q_stride = %lld is shorter than a token (%lld) or no multiple of 16 bytes",
                  who, (long long)q_stride, dense);
     MOEI_REQUIRE((uintptr_t)d_q % 16 == 0 && (uintptr_t)d_out % 16 == 0, "%s: d_q and d_out must begin at multiples of 16 bytes", who);
+    const long long rows = (q_stride ? q_stride : dense) * io;
+    MOEI_REQUIRE(!overlap(d_q, B, rows, dense * io, d_out, (long long)B * d.n_q_heads * d.v_dim * io), "%s: d_out overlaps d_q", who);  // (other workgroups read it still)
     const long long units = ((long long)width * d.page_size / 64 + 1) * B * d.n_kv_heads * ((d.n_q_heads / d.n_kv_heads + kKvHeads - 1) / kKvHeads);
     if (units > 0x7fffffffll)
         MOEI_FAIL(MOEI_ECAPACITY, "%s: %d sequences of up to %lld tokens are more than one call takes", who, B, (long long)width * d.page_size);
@@ -491,6 +499,8 @@ extern "C" int kv_append(moei_kv* kv, const moei_kv_pages* pages, const int32_t*
                  "%s: strides %lld, %lld, %lld are shorter than a token (%lld, %lld, %lld)", who, (long long)q_stride, (long long)k_stride, (long long)v_stride, nq, nk, nv);
     const int io = kv_io_bytes(d.dtype);
     MOEI_REQUIRE((uintptr_t)d_q % io == 0 && (uintptr_t)d_k % io == 0 && (uintptr_t)d_v % io == 0 && (uintptr_t)d_q_out % io == 0, "%s: elements are not aligned", who);
+    MOEI_REQUIRE((d_q_out == d_q && (T == 1 || q_stride == 0 || q_stride == nq)) || !overlap(d_q, T, (q_stride ? q_stride : nq) * io, nq * io, d_q_out, (long long)T * nq * io),
+                 "%s: d_q_out overlaps d_q, but is not the same dense tensor", who);
     KvAppendArgs a{};
     a.q = d_q; a.k = d_k; a.v = d_v;
     a.q_stride = q_stride ? q_stride : nq;

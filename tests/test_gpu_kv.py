@@ -757,6 +757,8 @@ def test_refusals(m):
     refused(attend(stride=260), "q_stride")
     refused(attend(q=P(c.q) + 2), "16 bytes")
     refused(attend(window=-1), "window")
+    refused(attend(o=P(c.q)), "overlaps")
+    refused(attend(o=P(c.q) + 256), "overlaps")
     for s in (0.0, -1.0, float("inf"), float("nan")):
         refused(attend(scale=s), "scale")
     C = type(c.pages.c)
@@ -808,6 +810,9 @@ def test_refusals(m):
     refused(append(ks=100), "strides")
     refused(append(vs=100), "strides")
     refused(append(q=P(q) + 1), "aligned")
+    refused(append(qo=P(q) + 16), "overlaps")
+    refused(append(qo=P(q), qs=264), "overlaps")
+    assert append(qo=P(q)) == 0 and append(T=1, qo=P(q), qs=264) == 0
     torch.cuda.synchronize()
     assert c.kv.error_flags() == 0
     with pytest.raises(AssertionError):
