@@ -177,6 +177,13 @@ __device__ __forceinline__ bf16x8 widen8(uint32_t lo, uint32_t hi) {
     return r;
 }
 
+// The next eight bits of four weights, as bf16, and what they leave: three parts add up to the weights exactly.
+__device__ __forceinline__ uint2 next_part(f32x4& left) {
+    const uint2 p = make_uint2(pack_bf16(left[0], left[1]), pack_bf16(left[2], left[3]));
+    left -= f32x4{bf16_lo(p.x), bf16_hi(p.x), bf16_lo(p.y), bf16_hi(p.y)};
+    return p;
+}
+
 // Sums of a head's weighted values and of its weights, relative to exponents of m.
 struct Sums {
     float m, l;
@@ -466,26 +473,30 @@ __global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kReside
                 }
                 wait_lds_fence();
             }
-            // The weights go to the products as they lie: a lane's keys are the summation indices of its group.  As bf16 they are split in two,
-            // the value and what rounding took from it: the matrix cores have the time, and the sums are as exact as the logits.
+            // The weights go to the products as they lie: a lane's keys are the summation indices of its group.  The bf16 products take them in
+            // three parts of eight bits, so that nothing of their 24 is lost.  The matrix cores have the time: one sequence of 131,072 tokens takes 85 us with
+            // three parts and with two (17 bits), 32 of up to 32,768 in 8 bits 201 and 199.
+            constexpr int kParts = 3;
             if constexpr (T::kBytes == 2) {
-                const uint2 hi = make_uint2(pack_bf16(e[0][0], e[0][1]), pack_bf16(e[0][2], e[0][3]));
-                const uint2 lo = make_uint2(pack_bf16(e[0][0] - bf16_lo(hi.x), e[0][1] - bf16_hi(hi.x)), pack_bf16(e[0][2] - bf16_lo(hi.y), e[0][3] - bf16_hi(hi.y)));
+                s16x4 w[kParts];
+#pragma unroll
+                for (int i = 0; i < kParts; ++i) w[i] = __builtin_bit_cast(s16x4, next_part(e[0]));
                 const uint32_t row = at_v + (4 * grp + (col >> 2)) * (VC * 2) + ((col & 1) << 3);
                 const int key = v_key<T>(4 * grp + (col >> 2), S::kPiecesV);
 #pragma unroll
                 for (int t = 0; t < kOut; ++t) {
                     const s16x4 vt = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                         (__attribute__((address_space(3))) s16x4*)(uintptr_t)(row + (((2 * t + ((col >> 1) & 1)) ^ key) << 4)));
-                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vt, __builtin_bit_cast(s16x4, hi), acc[t], 0, 0, 0);
-                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vt, __builtin_bit_cast(s16x4, lo), acc[t], 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < kParts; ++i) acc[t] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(vt, w[i], acc[t], 0, 0, 0);
                 }
             } else if constexpr (T::kBytes == 1) {
-                uint4 hi, lo;
-                hi.x = pack_bf16(e[0][0], e[0][1]); hi.y = pack_bf16(e[0][2], e[0][3]);
-                hi.z = pack_bf16(e[1][0], e[1][1]); hi.w = pack_bf16(e[1][2], e[1][3]);
-                lo.x = pack_bf16(e[0][0] - bf16_lo(hi.x), e[0][1] - bf16_hi(hi.x)); lo.y = pack_bf16(e[0][2] - bf16_lo(hi.y), e[0][3] - bf16_hi(hi.y));
-                lo.z = pack_bf16(e[1][0] - bf16_lo(hi.z), e[1][1] - bf16_hi(hi.z)); lo.w = pack_bf16(e[1][2] - bf16_lo(hi.w), e[1][3] - bf16_hi(hi.w));
+                bf16x8 w[kParts];
+#pragma unroll
+                for (int i = 0; i < kParts; ++i) {
+                    const uint2 x = next_part(e[0]), y = next_part(e[1]);
+                    w[i] = __builtin_bit_cast(bf16x8, make_uint4(x.x, x.y, y.x, y.y));
+                }
                 // eight rows of sixteen 8-bit columns, lanes 2r and 2r + 1 name row r's: the keys of the lane group in both subtiles
                 const int r8 = col >> 1, vrow = (r8 >> 2) * kRows + 4 * grp + (r8 & 3);
                 const uint32_t row = at_v + vrow * VC + ((col & 1) << 3);
@@ -494,9 +505,9 @@ __global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kReside
                 for (int t = 0; t < kOut; ++t) {
                     const i32x2 vt = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
                         (__attribute__((address_space(3))) i32x2*)(uintptr_t)(row + ((t ^ key) << 4)));
-                    const bf16x8 w = widen8(vt[0], vt[1]);
-                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(bf16x8, hi), acc[t], 0, 0, 0);
-                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, __builtin_bit_cast(bf16x8, lo), acc[t], 0, 0, 0);
+                    const bf16x8 x = widen8(vt[0], vt[1]);
+#pragma unroll
+                    for (int i = 0; i < kParts; ++i) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, w[i], acc[t], 0, 0, 0);
                 }
             } else {
 #pragma unroll

@@ -1,0 +1,70 @@
+"""The paged KV cache's attention where its answer shows a single weight: inputs whose sums are known in 64 bits and whose
+losses would be larger than what is allowed, by what is derived beside each."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def m():
+    import paper_2401_14361_amd as mod
+    mod.lib()
+    return mod
+
+
+def bf16(x):
+    return torch.from_numpy(np.asarray(x, dtype=np.float64)).bfloat16().double().numpy()
+
+
+def e4m3(x):
+    return torch.from_numpy(np.asarray(x, dtype=np.float64)).to(torch.float8_e4m3fn).double().numpy()
+
+
+def logits_whose_weights_need_24_bits(n, dtype, rng):
+    """x in (0.05, 0.69), held by a key of `dtype` (8 bits: by the scale of a code of one), for which p = exp(-x) is at least 0.8 2^-18 off
+    the sum of two bf16 numbers (2^-18 is as far as that gets)."""
+    x = rng.uniform(0.05, 0.69, 4000)
+    x = np.unique(bf16(x) if dtype == "bf16" else x.astype(np.float32).astype(np.float64))
+    p = np.exp(-x)
+    hi = bf16(p)
+    rest = p - hi - bf16(p - hi)
+    x = x[np.abs(rest) >= 0.8 * 2.0 ** -18]
+    return rng.choice(x, n, replace=len(x) < n)
+
+
+@pytest.mark.parametrize("D", [64, 128, 192, 256])
+@pytest.mark.parametrize("dtype", ["bf16", "fp8", "fp32"])
+def test_weights_keep_24_bits(m, dtype, D):
+    # Five tokens: one of weight p = exp(-x) and value 256, four of weight 1 whose values take away 256 times the nearest two bf16 numbers.  What is
+    # left is 256 (p - hi - lo) / (4 + p), at least 12.8 2^-14 before the division.  Allowed: the weight is off by 2^-22.5 (the exponent's factor and
+    # its rounding 2^-23, exp2 2^-24), seven additions of magnitudes up to 512 p by 2^-23 each (twice what rounding to nearest would): 5.8 2^-14.
+    Hkv, page, Dv = 32, 16, min(D, 128) if D != 256 else 256
+    io = torch.float32 if dtype == "fp32" else torch.bfloat16
+    x = logits_whose_weights_need_24_bits(Hkv, dtype, np.random.default_rng(D))
+    p = np.exp(-x)
+    hi = bf16(p)
+    lo = bf16(p - hi)
+    take = []
+    for part in (256 * hi, 256 * lo):  # four bits each, so that 8-bit pages hold them
+        a = e4m3(part)
+        take += [a, part - a]
+        assert (e4m3(part - a) == part - a).all()
+    kv = m.Kv(Hkv, Hkv, D, Dv, page, dtype, max_batch=1, max_pages=1)
+    k = torch.zeros((1, Hkv, page, D), dtype=torch.float64)
+    v = torch.zeros((1, Hkv, page, Dv), dtype=torch.float64)
+    k[0, :, 4, 0] = torch.from_numpy(-np.ones(Hkv) if dtype == "fp8" else -x)
+    for t, a in enumerate(take):
+        v[0, :, t] = torch.from_numpy(-a)[:, None]
+    v[0, :, 4] = 256
+    k, v = k.to(kv.page_dtype).cuda(), v.to(kv.page_dtype).cuda()
+    scales = dict(k_scale=torch.from_numpy(x).float().cuda(), v_scale=torch.ones(Hkv, device="cuda")) if dtype == "fp8" else {}
+    q = torch.zeros((1, Hkv, D), dtype=io, device="cuda")
+    q[:, :, 0] = 1
+    out = m.kv_attend(kv, m.KvPages(kv, k, v, **scales), torch.zeros((1, 1), dtype=torch.int32, device="cuda"),
+                      torch.tensor([5], dtype=torch.int32, device="cuda"), q, 1.0)
+    ref = 256 * (p - hi - lo) / (4 + p)
+    tol = (256 * 2.0 ** -22.5 + 7 * 2.0 ** -23 * 512 * p) / (4 + p) + 2.0 ** -8 * np.abs(ref)
+    assert (np.abs(ref) > 1.5 * tol).all()  # (two parts would give 0)
+    assert (np.abs(out[0].double().cpu().numpy() - ref[:, None]) <= tol[:, None]).all()
