@@ -87,13 +87,14 @@ __device__ __forceinline__ void store_fp8(uint8_t* p, const float* f, float scal
     }
 }
 
-// cos and sin of position times frequency.  The product and its reduction to a turn are formed in 64 bits: at position 10^5 the fp32 product
-// would be off by up to 2^-8.
+// cos and sin of position times frequency, in 64 bits and rounded once: at position 10^5 an fp32 angle would be off by up to 2^-8, and an fp32 turn,
+// reduced in 64 bits, by as much as the rounding of sine and cosine themselves.  (1 / (2 pi) in two numbers: positions reach 2^30.)
 __device__ __forceinline__ float2 turn(int pos, float freq) {
-    const double turns = (double)pos * (double)freq * 0.15915494309189535;  // 1 / (2 pi)
-    float2 cs;
-    sincospif((float)(2.0 * (turns - rint(turns))), &cs.y, &cs.x);
-    return cs;
+    const double angle = (double)pos * (double)freq, turns = angle * 0x1.45f306dc9c883p-3;
+    const double rest = __builtin_fma(angle, 0x1.45f306dc9c883p-3, -turns) + angle * -0x1.6b01ec5417056p-57;
+    double s, c;
+    sincospi(2.0 * (turns - rint(turns) + rest), &s, &c);
+    return make_float2((float)c, (float)s);
 }
 __device__ __forceinline__ void turn_pair(float& x1, float& x2, float2 cs) {
     const float y1 = __builtin_fmaf(x1, cs.x, -(x2 * cs.y));

@@ -68,3 +68,40 @@ def test_weights_keep_24_bits(m, dtype, D):
     tol = (256 * 2.0 ** -22.5 + 7 * 2.0 ** -23 * 512 * p) / (4 + p) + 2.0 ** -8 * np.abs(ref)
     assert (np.abs(ref) > 1.5 * tol).all()  # (two parts would give 0)
     assert (np.abs(out[0].double().cpu().numpy() - ref[:, None]) <= tol[:, None]).all()
+
+
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("D,rot", [(128, 128), (64, 64), (48, 6), (256, 256)])  # (6: element by element)
+def test_rotation_rounds_sine_and_cosine_once(m, D, rot, interleaved):
+    # x1 c - x2 s in fp32: c and s, which are at most 1, are off by 2^-25 each, the first product by 2^-24 of itself, the result by 2^-24 of itself.
+    rng = np.random.default_rng(D + rot)
+    T, page = 64, 256
+    pos = np.concatenate([[0, 1, 2, 131071, 10 ** 6 - 1, 2 ** 24 + 1, 2 ** 30 - 1, 2 ** 30 - 2], rng.integers(0, 131072, T - 16), rng.integers(0, 2 ** 30, 8)]).astype(np.int64)
+    width = 2 ** 30 // page
+    kv = m.Kv(4, 2, D, 16, page, "fp32", max_batch=1, max_pages=width, max_sel=0)
+    at = np.unique(pos // page)
+    table = torch.full((1, width), -1, dtype=torch.int32, device="cuda")
+    table[0, torch.from_numpy(at).cuda()] = torch.arange(len(at), dtype=torch.int32, device="cuda")
+    k_pages, v_pages = torch.zeros((len(at), 2, page, D), device="cuda"), torch.zeros((len(at), 2, page, 16), device="cuda")
+    assert len(np.unique(pos)) == T
+    g = torch.Generator(device="cuda")
+    g.manual_seed(D)
+    q, k = torch.randn((T, 4, D), generator=g, device="cuda"), torch.randn((T, 2, D), generator=g, device="cuda")
+    v = torch.randn((T, 2, 16), generator=g, device="cuda")
+    freq = (10000.0 ** (-torch.arange(rot // 2, dtype=torch.float64) * 2 / rot)).float()
+    q_out = m.kv_append(kv, m.KvPages(kv, k_pages, v_pages), table, torch.from_numpy(pos).int().cuda(), q, k, v, freq.cuda(),
+                        seq=torch.zeros(T, dtype=torch.int32, device="cuda"), interleaved=interleaved)
+    k_out = k_pages[torch.from_numpy(np.searchsorted(at, pos // page)).cuda(), :, torch.from_numpy(pos % page).cuda()]
+    angle = pos[:, None] * freq.double().numpy()
+    c, s = np.cos(angle)[:, None], np.sin(angle)[:, None]
+    first = np.arange(0, rot, 2) if interleaved else np.arange(rot // 2)
+    second = first + (1 if interleaved else rot // 2)
+    for x, y in ((q, q_out), (k, k_out)):
+        x, y = x.double().cpu().numpy(), y.double().cpu().numpy()
+        a, b = x[..., first], x[..., second]
+        for got, one, other, sign in ((y[..., first], a, b, -1), (y[..., second], b, a, 1)):
+            ref = one * c + sign * other * s
+            tol = 2.0 ** -25 * (np.abs(a) + np.abs(b)) + 2.0 ** -24 * (np.abs(other * s) + np.abs(ref)) + 1e-12
+            assert (np.abs(got - ref) <= tol).all(), (np.abs(got - ref) / tol).max()
+        assert (y[..., rot:] == x[..., rot:]).all()
+    assert kv.error_flags() == 0
