@@ -418,8 +418,10 @@ int kv_attend(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, i
               const void* d_q, int64_t q_stride, float scale, int32_t window, void* d_out, float* d_lse, void* stream);
 
 /* kv_attend over at most n_sel pages of a sequence for each key/value head: its first keep_first and last keep_last (>= 1) pages, and of the
- * others those with the largest score  max over the head's queries of sum_d max(q_d k_min_d, q_d k_max_d),  which no logit of the page exceeds
- * (formed in 64 bits; equal scores go to the lower page; one that is no number comes last).  A sequence of at most n_sel pages is attended to whole.
+ * others those with the largest score  max over the head's queries of sum_d q_d (q_d > 0 ? k_max_d : k_min_d),  which no logit of the page exceeds
+ * (formed in 64 bits; equal scores go to the lower page).  A query whose sum is no number is passed over in that maximum.  A page for which no query
+ * has a number comes last, and so does one with a dimension that holds no number in any row (k_min +inf, k_max -inf).
+ * A sequence of at most n_sel pages is attended to whole.
  * d_blocks[B][n_kv_heads][n_sel] int32 (may be NULL): the pages' numbers within their sequence, ascending, -1 behind the last.
  * The pages between the kept ones need their summaries. */
 int kv_attend_blocks(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, int32_t table_width, const int32_t* d_len, int32_t B,

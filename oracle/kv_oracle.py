@@ -36,15 +36,21 @@ def span(n, page, window, n_sel, chosen):
 
 
 def choose(q, k_min, k_max, n_blocks, n_sel, first, last):
-    """Pages for one key/value head: q [G][D], k_min / k_max [n_blocks][D] -> ascending page numbers."""
+    """Pages for one key/value head: q [G][D], k_min / k_max [n_blocks][D] -> ascending page numbers.
+
+    A page's score is the largest of its heads' sums of q_d k_max_d where q_d is positive and q_d k_min_d elsewhere; sums that are no numbers are
+    passed over, and a page without any comes last.  So does one with a dimension that holds no number (k_min +inf, k_max -inf): its sums
+    are -inf or no numbers.
+    """
     if n_blocks <= n_sel:
         return list(range(n_blocks))
     always = set(range(first)) | set(range(n_blocks - last, n_blocks))
     score = {}
     for p in range(n_blocks):
         if p not in always:
-            s = max(float(np.sum(np.maximum(qh * k_min[p], qh * k_max[p]))) for qh in q)
-            score[p] = -np.inf if np.isnan(s) else s
+            with np.errstate(invalid="ignore"):
+                sums = [float(np.sum(qh * np.where(qh > 0, k_max[p], k_min[p]))) for qh in q]
+            score[p] = max([s for s in sums if not np.isnan(s)], default=-np.inf)
     order = sorted(score, key=lambda p: (-score[p], p))
     return sorted(always | set(order[:n_sel - len(always)]))
 

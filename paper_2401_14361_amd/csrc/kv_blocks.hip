@@ -1,7 +1,7 @@
 // Which pages of a paged KV cache a new token attends to.
 //
-// A page's score for a key/value head is the largest of its query heads' bounds sum_d max(q_d k_min_d, q_d k_max_d): no logit
-// of the page exceeds it.  A few pages at either end are always taken, then the highest scores.  The choice is made by the sums
+// A page's score for a key/value head is the largest of its query heads' bounds sum_d q_d (q_d > 0 ? k_max_d : k_min_d): no logit
+// of the page exceeds it.  Bounds that are no numbers are passed over; a page without any comes last.  A few pages at either end are always taken, then the highest scores.  The choice is made by the sums
 // in 64 bits, but nearly all pages are told apart by sums in fp32 whose error is bounded: those come from the matrix cores at the rate at
 // which the summaries are read, and only pages so near the last one chosen that their order is open are summed again in 64 bits.
 #include "kv.hpp"
@@ -96,7 +96,7 @@ __device__ __forceinline__ u64 exact_key(Args a, int b, int hk, int pg, int lane
             if constexpr (LP >= 16) sum += dpp_f64<0x140>(sum);  // row_mirror
             if constexpr (LP >= 32) sum += __shfl_xor(sum, 16, kWave);
             if constexpr (LP >= 64) sum += __shfl_xor(sum, 32, kWave);
-            best = sum > best ? sum : best;
+            best = sum > best ? sum : best;  // (never one that is no number)
         }
     }
     return ok ? key_of(best) : key_of(-(double)INFINITY);
