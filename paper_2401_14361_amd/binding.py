@@ -4,6 +4,10 @@ Every function has the name of the C entry point it calls (include/moei.h) and
 takes torch CUDA tensors for device buffers; outputs are allocated with torch
 (device memory plumbing) and filled by the library's kernels.  A missing library
 is an error: there is no CPU fallback.
+
+With `stream=` a call's work is queued there, and the tensors that it allocates belong to that stream, as those of any
+torch operation under torch.cuda.stream(stream) do.  Ordering is the caller's: `stream` waits for whoever wrote the inputs, and
+whoever uses the outputs waits for `stream` (events, wait_stream; record_stream for tensors given up while another stream uses them).
 """
 from __future__ import annotations
 
@@ -108,6 +112,27 @@ def _stream(stream=None) -> C.c_void_p:
     if stream is None:
         stream = torch.cuda.current_stream()
     return C.c_void_p(stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream))
+
+
+def _elsewhere(stream, device: int):
+    """The torch stream that `stream` (a torch stream or a handle) names, None if it is the device's current one."""
+    if stream is None:
+        return None
+    at = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+    if at == torch._C._cuda_getCurrentRawStream(device):
+        return None
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    return torch.cuda.ExternalStream(at, device=device) if at else torch.cuda.default_stream(device)
+
+
+def _new(shape, dtype, device: torch.device, stream) -> torch.Tensor:
+    """A tensor that the call on `stream` fills: from that stream's memory, which nothing queued on another one still uses."""
+    on = _elsewhere(stream, device.index)
+    if on is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(on):
+        return torch.empty(shape, dtype=dtype, device=device)
 
 
 def _dev(t: torch.Tensor, dtype) -> torch.Tensor:
@@ -330,8 +355,8 @@ def moe_route_topk(logits: torch.Tensor, k: int, renorm: bool, stream=None):
     """logits [B][E] fp32 (device) -> (idx [B][k] int32, w [B][k] fp32) on the device."""
     _dev(logits, torch.float32)
     B, E = logits.shape
-    idx = torch.empty((B, k), dtype=torch.int32, device=logits.device)
-    w = torch.empty((B, k), dtype=torch.float32, device=logits.device)
+    idx = _new((B, k), torch.int32, logits.device, stream)
+    w = _new((B, k), torch.float32, logits.device, stream)
     _check(lib().moe_route_topk(_p(logits), B, E, k, int(renorm), _p(idx), _p(w), _stream(stream)))
     return idx, w
 
@@ -354,9 +379,9 @@ def eamc_match(eamc: Eamc, eam: torch.Tensor, layer_hi: int | None = None, want_
         eam = eam.unsqueeze(0)
     B = eam.shape[0]
     assert tuple(eam.shape[1:]) == (eamc.desc.L, eamc.desc.E)
-    best = torch.empty(B, dtype=torch.int32, device=eam.device)
-    sim = torch.empty(B, dtype=torch.float32, device=eam.device)
-    sims = torch.empty((B, eamc.size), dtype=torch.float32, device=eam.device) if want_sims else None
+    best = _new(B, torch.int32, eam.device, stream)
+    sim = _new(B, torch.float32, eam.device, stream)
+    sims = _new((B, eamc.size), torch.float32, eam.device, stream) if want_sims else None
     lh = eamc.desc.L - 1 if layer_hi is None else layer_hi
     _check(lib().eamc_match(eamc.h, _p(eam), B, lh, _p(best), _p(sim), _p(sims), _stream(stream)))
     return best, sim, sims
@@ -369,9 +394,9 @@ def eamc_match_topm(eamc: Eamc, eam: torch.Tensor, m: int, layer_hi: int | None 
     _dev(eam, torch.int32)
     assert tuple(eam.shape) == (eamc.desc.L, eamc.desc.E)
     n = max(int(m), 1)
-    top = torch.empty(n, dtype=torch.int32, device=eam.device)
-    sim = torch.empty(n, dtype=torch.float32, device=eam.device)
-    sims = torch.empty(eamc.size, dtype=torch.float32, device=eam.device) if want_sims else None
+    top = _new(n, torch.int32, eam.device, stream)
+    sim = _new(n, torch.float32, eam.device, stream)
+    sims = _new(eamc.size, torch.float32, eam.device, stream) if want_sims else None
     lh = eamc.desc.L - 1 if layer_hi is None else layer_hi
     _check(lib().eamc_match_topm(eamc.h, _p(eam), lh, int(m), _p(top), _p(sim), _p(sims), _stream(stream)))
     return top, sim, sims
@@ -384,12 +409,12 @@ def expert_priority(eamc: Eamc, best: torch.Tensor, cur_layer: int, slot_of, eps
     _dev(best, torch.int32)
     L, E = eamc.desc.L, eamc.desc.E
     dev = best.device
-    P = torch.empty((L, E), dtype=torch.float32, device=dev)
-    V = torch.empty((L, E), dtype=torch.float32, device=dev)
-    pf = torch.empty(L * E, dtype=torch.int32, device=dev)
-    ev = torch.empty(L * E, dtype=torch.int32, device=dev)
-    n_pf = torch.empty(1, dtype=torch.int32, device=dev)  # (the kernel writes both counts: no launches to clear them)
-    n_ev = torch.empty(1, dtype=torch.int32, device=dev)
+    P = _new((L, E), torch.float32, dev, stream)
+    V = _new((L, E), torch.float32, dev, stream)
+    pf = _new(L * E, torch.int32, dev, stream)
+    ev = _new(L * E, torch.int32, dev, stream)
+    n_pf = _new(1, torch.int32, dev, stream)  # (the kernel writes both counts: no launches to clear them)
+    n_ev = _new(1, torch.int32, dev, stream)
     k = 0
     if cur_idx is not None:
         _dev(cur_idx, torch.int32)
@@ -405,7 +430,7 @@ def expert_ffn_gemv(cache: Cache, slot_ids: torch.Tensor, gate_w: torch.Tensor, 
     _dev(slot_ids, torch.int32)
     _dev(gate_w, torch.float32)
     assert x.is_cuda and x.is_contiguous() and x.numel() == cache.desc.H
-    y = out if out is not None else torch.empty(cache.desc.H, dtype=torch.float32, device=x.device)
+    y = out if out is not None else _new(cache.desc.H, torch.float32, x.device, stream)
     _check(lib().expert_ffn_gemv(cache.h, _p(slot_ids), _p(gate_w), slot_ids.numel(), _p(x), _p(y), _stream(stream)))
     return y
 
@@ -430,7 +455,7 @@ def expert_ffn_grouped(cache: Cache, layer: int, idx: torch.Tensor, w: torch.Ten
     _dev(w, torch.float32)
     B = idx.shape[0]
     assert x.is_cuda and x.is_contiguous() and x.numel() == B * cache.desc.H
-    y = torch.empty((B, cache.desc.H), dtype=torch.float32, device=x.device)
+    y = _new((B, cache.desc.H), torch.float32, x.device, stream)
     _check(lib().expert_ffn_grouped(cache.h, layer, _p(idx), _p(w), B, _p(x), _p(y), _stream(stream)))
     return y
 
@@ -553,9 +578,9 @@ def _ints(kv: Kv, t: torch.Tensor) -> int:
     return t.data_ptr()
 
 
-def _given(kv: Kv, t: torch.Tensor, n: int, heads: tuple) -> int:
+def _given(kv: Kv, t: torch.Tensor, n: int, heads: tuple, dtype=None) -> int:
     """Checks a caller's output [n][heads][width] and returns its address."""
-    assert t.dtype is kv.dtype and t.get_device() == kv.index and t.is_contiguous() and t.numel() == n * heads[0] * heads[1], (t.device, t.dtype, t.shape)
+    assert t.dtype is (dtype or kv.dtype) and t.get_device() == kv.index and t.is_contiguous() and t.numel() == n * heads[0] * heads[1], (t.device, t.dtype, t.shape)
     return t.data_ptr()
 
 
@@ -568,7 +593,7 @@ def kv_append(kv: Kv, pages: KvPages, table: torch.Tensor, pos: torch.Tensor, q:
     T = pos.numel()
     B, width = table.shape
     if q_out is None:
-        q_out = torch.empty((T, *kv.heads), dtype=kv.dtype, device=kv.device)
+        q_out = _new((T, *kv.heads), kv.dtype, kv.device, stream)
     assert inv_freq is None or (inv_freq.dtype is torch.float32 and inv_freq.get_device() == kv.index and inv_freq.is_contiguous()), (inv_freq.device, inv_freq.dtype)
     assert seq is None or seq.numel() == T
     _check(lib().kv_append(kv.h, pages.ref, _ints(kv, table), width, B, None if seq is None else _ints(kv, seq), _ints(kv, pos), T,
@@ -579,7 +604,7 @@ def kv_append(kv: Kv, pages: KvPages, table: torch.Tensor, pos: torch.Tensor, q:
     return q_out
 
 
-def _attend_args(kv: Kv, pages: KvPages, table, lens, q, out, want_lse):
+def _attend_args(kv: Kv, pages: KvPages, table, lens, q, out, want_lse, lse):
     """Checks what kv_attend and kv_attend_blocks have in common, once: their library call takes as long as these lines."""
     assert pages.layout == kv.layout, (pages.layout, kv.layout)
     B, width = table.shape
@@ -595,29 +620,43 @@ def _attend_args(kv: Kv, pages: KvPages, table, lens, q, out, want_lse):
         to = out.data_ptr()
     else:
         to = _given(kv, out, B, kv.out_heads)
-    lse = q.new_empty((B, kv.heads[0]), dtype=torch.float32) if want_lse else None
-    return B, width, table.data_ptr(), lens.data_ptr(), stride, out, to, lse, lse.data_ptr() if want_lse else None
+    if lse is not None:
+        lse_to = _given(kv, lse, B, (kv.heads[0], 1), torch.float32)
+    else:
+        lse = q.new_empty((B, kv.heads[0]), dtype=torch.float32) if want_lse else None
+        lse_to = lse.data_ptr() if want_lse else None
+    return B, width, table.data_ptr(), lens.data_ptr(), stride, out, to, lse, lse_to
 
 
 def kv_attend(kv: Kv, pages: KvPages, table: torch.Tensor, lens: torch.Tensor, q: torch.Tensor, scale: float, window: int = 0,
-              out: torch.Tensor | None = None, want_lse: bool = False, stream=None):
+              out: torch.Tensor | None = None, want_lse: bool = False, stream=None, lse: torch.Tensor | None = None):
     """q [B][Hq][k_dim] (any stride between sequences) over the first lens [B] tokens of each sequence, or the last `window` of them
-    -> out [B][Hq][v_dim], or (out, lse [B][Hq] fp32) with want_lse."""
-    B, width, table_at, lens_at, stride, out, out_at, lse, lse_at = _attend_args(kv, pages, table, lens, q, out, want_lse)
-    _check(lib().kv_attend(kv.h, pages.ref, table_at, width, lens_at, B, q.data_ptr(), stride, scale, window, out_at, lse_at, _kv_stream(kv, stream)))
-    return (out, lse) if want_lse else out
+    -> out [B][Hq][v_dim], or (out, lse [B][Hq] fp32) with want_lse or where lse is given."""
+    if stream is not None and (on := _elsewhere(stream, kv.index)) is not None:
+        with torch.cuda.stream(on):
+            return kv_attend(kv, pages, table, lens, q, scale, window, out, want_lse, None, lse)
+    B, width, table_at, lens_at, stride, out, out_at, lse, lse_at = _attend_args(kv, pages, table, lens, q, out, want_lse, lse)
+    _check(lib().kv_attend(kv.h, pages.ref, table_at, width, lens_at, B, q.data_ptr(), stride, scale, window, out_at, lse_at, _kv_stream(kv, None)))
+    return out if lse is None else (out, lse)
 
 
 def kv_attend_blocks(kv: Kv, pages: KvPages, table: torch.Tensor, lens: torch.Tensor, q: torch.Tensor, scale: float, n_sel: int,
                      keep_first: int = 1, keep_last: int = 1, out: torch.Tensor | None = None, want_lse: bool = False,
-                     want_blocks: bool = False, stream=None):
+                     want_blocks: bool = False, stream=None, lse: torch.Tensor | None = None, blocks: torch.Tensor | None = None):
     """kv_attend over at most n_sel pages a sequence and key/value head: the first keep_first, the last keep_last and those whose
-    logits have the highest bounds.  Returns out, or a tuple with lse [B][Hq] and blocks [B][Hkv][n_sel] int32 as wanted."""
-    B, width, table_at, lens_at, stride, out, out_at, lse, lse_at = _attend_args(kv, pages, table, lens, q, out, want_lse)
-    blocks = torch.empty((B, kv.k_page[0], max(n_sel, 0)), dtype=torch.int32, device=kv.device) if want_blocks else None
+    logits have the highest bounds.  Returns out, or a tuple with lse [B][Hq] and blocks [B][Hkv][n_sel] int32 as wanted or given."""
+    if stream is not None and (on := _elsewhere(stream, kv.index)) is not None:
+        with torch.cuda.stream(on):
+            return kv_attend_blocks(kv, pages, table, lens, q, scale, n_sel, keep_first, keep_last, out, want_lse, want_blocks, None, lse, blocks)
+    B, width, table_at, lens_at, stride, out, out_at, lse, lse_at = _attend_args(kv, pages, table, lens, q, out, want_lse, lse)
+    if blocks is not None:
+        blocks_at = _given(kv, blocks, B, (kv.k_page[0], n_sel), torch.int32)
+    else:
+        blocks = torch.empty((B, kv.k_page[0], max(n_sel, 0)), dtype=torch.int32, device=kv.device) if want_blocks else None
+        blocks_at = blocks.data_ptr() if want_blocks else None
     _check(lib().kv_attend_blocks(kv.h, pages.ref, table_at, width, lens_at, B, q.data_ptr(), stride, scale, n_sel, keep_first, keep_last,
-                                  out_at, lse_at, blocks.data_ptr() if want_blocks else None, _kv_stream(kv, stream)))
-    got = (out,) + ((lse,) if want_lse else ()) + ((blocks,) if want_blocks else ())
+                                  out_at, lse_at, blocks_at, _kv_stream(kv, None)))
+    got = (out,) + (() if lse is None else (lse,)) + (() if blocks is None else (blocks,))
     return got if len(got) > 1 else out
 
 
@@ -630,9 +669,9 @@ def moe_prefill_layer(cache: Cache, eam: torch.Tensor, layer: int, router_w: tor
     n, H = X.shape
     assert H == cache.desc.H and X.is_contiguous()
     if Y is None:
-        Y = torch.empty((n, H), dtype=torch.float32, device=X.device)
-    idx = torch.empty((n, cache.desc.k), dtype=torch.int32, device=X.device) if want_picks else None
-    w = torch.empty((n, cache.desc.k), dtype=torch.float32, device=X.device) if want_picks else None
+        Y = _new((n, H), torch.float32, X.device, stream)
+    idx = _new((n, cache.desc.k), torch.int32, X.device, stream) if want_picks else None
+    w = _new((n, cache.desc.k), torch.float32, X.device, stream) if want_picks else None
     _check(lib().moe_prefill_layer(cache.h, _p(eam), layer, _p(router_w), _p(router_bias), _p(X), n, _p(Y),
                                    _p(idx), _p(w), _stream(stream)))
     return (Y, idx, w) if want_picks else Y
