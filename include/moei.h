@@ -395,7 +395,7 @@ int moei_kv_error_flags(moei_kv* kv, int32_t* h_flags, void* stream);
  * Token t has position d_pos[t] in sequence d_seq[t] (d_seq NULL: sequence t, T <= B, and no two tokens share a page); a negative
  * position is no token, and nothing is written for it.  The first rot_dim elements of every query and key head are rotated by the angles position * d_inv_freq[i],
  * 0 <= i < rot_dim / 2, whose sine and cosine are formed in 64 bits and rounded once: elements i and i + rot_dim / 2 (interleaved: 2i and 2i + 1) are turned as a pair in fp32.
- * Rotated queries go to d_q_out[T][n_q_heads][k_dim] (dense; d_q itself if that is dense), keys and values into row position % page_size
+ * Rotated queries go to d_q_out[T][n_q_heads][k_dim] (dense; d_q itself if that is dense, else no part of d_q, d_k or d_v), keys and values into row position % page_size
  * of page d_table[sequence][position / page_size] (d_table [B][table_width] int32), rounded once; 8-bit pages hold value / scale, limited to +-448.
  * A token whose position lies outside the table or whose page outside the pool is left out, its query too, and raises an error flag.
  * With summaries: when the last row of a page is appended, d_k_min and d_k_max of that page are formed from all of its rows as they are stored

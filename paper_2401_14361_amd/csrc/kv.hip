@@ -355,10 +355,11 @@ void strides_of(const moei_kv* kv, const moei_kv_pages* p, long long* k, long lo
     *v = p->v_stride ? p->v_stride : rows * kv->d.v_dim;
 }
 
-// Whether `n` rows of `row` bytes, `stride` bytes apart, reach into `m` bytes at `b`.
+// Whether one of `n` rows of `row` bytes, `stride` bytes apart, reaches into `m` bytes at `b`.
 bool overlap(const void* a, long long n, long long stride, long long row, const void* b, long long m) {
-    const uintptr_t p = (uintptr_t)a, q = (uintptr_t)b;
-    return p < q + (uintptr_t)m && q < p + (uintptr_t)((n - 1) * stride + row);
+    const long long ahead = (long long)((uintptr_t)b - (uintptr_t)a);
+    const long long i = ahead < row ? 0 : (ahead - row) / stride + 1;  // the first row that ends behind b
+    return i < n && i * stride < ahead + m;
 }
 
 int fill_attend(const char* who, const moei_kv* kv, const moei_kv_pages* p, const int32_t* d_table, int32_t width, const int32_t* d_len,
@@ -502,6 +503,9 @@ extern "C" int kv_append(moei_kv* kv, const moei_kv_pages* pages, const int32_t*
     MOEI_REQUIRE((uintptr_t)d_q % io == 0 && (uintptr_t)d_k % io == 0 && (uintptr_t)d_v % io == 0 && (uintptr_t)d_q_out % io == 0, "%s: elements are not aligned", who);
     MOEI_REQUIRE((d_q_out == d_q && (T == 1 || q_stride == 0 || q_stride == nq)) || !overlap(d_q, T, (q_stride ? q_stride : nq) * io, nq * io, d_q_out, (long long)T * nq * io),
                  "%s: d_q_out overlaps d_q, but is not the same dense tensor", who);
+    MOEI_REQUIRE(!overlap(d_k, T, (k_stride ? k_stride : nk) * io, nk * io, d_q_out, (long long)T * nq * io) &&
+                     !overlap(d_v, T, (v_stride ? v_stride : nv) * io, nv * io, d_q_out, (long long)T * nq * io),
+                 "%s: d_q_out overlaps d_k or d_v", who);  // (other workgroups read them still)
     KvAppendArgs a{};
     a.q = d_q; a.k = d_k; a.v = d_v;
     a.q_stride = q_stride ? q_stride : nq;

@@ -139,3 +139,27 @@ def test_decode_batches_of_eight_sequences_a_compute_unit(m, dtype, Hq, Hkv, Dk,
     pos[::3] = pos[::3] // page * page + page - 1
     pos[5::50] = -1
     check(m, dtype, Hq, Hkv, Dk, Dv, page, rot, interleaved, layout, in_place, B, None, pos)
+
+
+def test_rotated_queries_over_keys_or_values_are_refused(m):  # (no kernel runs but for the calls that are taken)
+    kv = m.Kv(4, 2, 64, 64, 16, "bf16", max_batch=4, max_pages=1, max_sel=0)
+    pages = m.KvPages(kv, *(torch.zeros((4, 2, 16, 64), dtype=torch.bfloat16, device="cuda") for _ in range(2)))
+    table = torch.arange(4, dtype=torch.int32, device="cuda")[:, None].contiguous()
+    room = torch.randn(64 * 1024, device="cuda").bfloat16()
+
+    def append(T, q, k, v, out, stride=0):
+        view = lambda at, h: (torch.as_strided(room, (T, h, 64), (stride or h * 64, 64, 1), at))  # noqa: E731
+        pos = torch.zeros(T, dtype=torch.int32, device="cuda")
+        return m.kv_append(kv, pages, table, pos, view(q, 4), view(k, 2), view(v, 2), None, q_out=torch.as_strided(room, (T, 4, 64), (256, 64, 1), out))
+
+    for bad in ((4096, 8192, 4096 + 511), (4096, 8192, 4096 - 1023), (8192, 4096, 4096 + 511), (4096, 4096, 4096)):
+        with pytest.raises(m.MoeiError, match="overlaps d_k or d_v"):
+            append(4, 0, *bad)
+    append(4, 0, 4096, 4608, 4096 + 1024)                       # right behind
+    append(4, 0, 4096, 8192, 4096 - 1024)                       # right before
+    with pytest.raises(m.MoeiError, match="overlaps d_k or d_v"):  # one row of packed tokens
+        append(4, 0, 256, 384, 3 * 4096 + 256, stride=4096)
+    append(4, 0, 256, 384, 3 * 4096 - 1024, stride=4096)         # between two rows
+    append(1, 0, 256, 384, 0)                                    # in place, keys right behind
+    torch.cuda.synchronize()
+    assert kv.error_flags() == 0
