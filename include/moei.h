@@ -412,7 +412,7 @@ int kv_append(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, i
  * batch.  A sequence without tokens gets zeros and -inf.  Rows behind a sequence's last token may hold anything.  A page id outside the pool
  * counts as a page that is masked, a length outside [0, table_width * page_size] as the nearest one inside; both raise an error flag.
  * A token whose key or value holds an infinity or no number may turn the results of its heads into no numbers.
- * scale must be positive.  Outputs must not overlap inputs.  MOEI_ECAPACITY when B * key/value heads * table_width * page_size (for each 16
+ * scale must be positive and, times log2(e), finite.  Outputs must not overlap inputs.  MOEI_ECAPACITY when B * key/value heads * table_width * page_size (for each 16
  * query heads of a group) passes 2^37 tokens. */
 int kv_attend(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, int32_t table_width, const int32_t* d_len, int32_t B,
               const void* d_q, int64_t q_stride, float scale, int32_t window, void* d_out, float* d_lse, void* stream);

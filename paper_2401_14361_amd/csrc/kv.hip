@@ -366,7 +366,8 @@ int fill_attend(const char* who, const moei_kv* kv, const moei_kv_pages* p, cons
                 int32_t B, const void* d_q, int64_t q_stride, float scale, void* d_out, float* d_lse, KvAttendArgs* a) {
     const moei_kv_desc& d = kv->d;
     MOEI_REQUIRE(d_len && d_q && d_out, "%s: null pointer", who);
-    MOEI_REQUIRE(scale > 0.f && scale < INFINITY, "%s: scale must be positive and finite", who);
+    const float scale2 = (float)((double)scale * 1.4426950408889634);
+    MOEI_REQUIRE(scale > 0.f && scale2 < INFINITY, "%s: scale must be positive, and finite times log2(e)", who);
     const int io = kv_io_bytes(d.dtype);
     const long long dense = (long long)d.n_q_heads * d.k_dim;
     MOEI_REQUIRE(q_stride == 0 || (q_stride >= dense && q_stride * io % 16 == 0), "%s: q_stride = %lld is shorter than a token (%lld) or no multiple of 16 bytes",
@@ -400,7 +401,7 @@ int fill_attend(const char* who, const moei_kv* kv, const moei_kv_pages* p, cons
     a->width = width;
     a->page_shift = log2_of(d.page_size);
     a->n_pages = p->n_pages;
-    a->scale2 = (float)((double)scale * 1.4426950408889634);
+    a->scale2 = scale2;
     a->part = kv->d_part;
     a->stat = kv->d_stat;
     a->arrived = kv->d_arrived;

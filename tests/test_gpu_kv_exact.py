@@ -105,3 +105,18 @@ def test_rotation_rounds_sine_and_cosine_once(m, D, rot, interleaved):
             assert (np.abs(got - ref) <= tol).all(), (np.abs(got - ref) / tol).max()
         assert (y[..., rot:] == x[..., rot:]).all()
     assert kv.error_flags() == 0
+
+
+def test_the_largest_and_smallest_scales(m):
+    # equal logits of 0 whatever the scale is; one that is infinite times log2(e) in fp32 is refused: 0 times it would be no number
+    kv = m.Kv(2, 1, 64, 64, 16, "fp32", max_batch=1, max_pages=4, max_sel=4)
+    k, v = torch.randn((4, 1, 16, 64), device="cuda"), torch.ones((4, 1, 16, 64), device="cuda")
+    table, n = torch.arange(4, dtype=torch.int32, device="cuda")[None], torch.tensor([50], dtype=torch.int32, device="cuda")
+    pages, q = m.KvPages(kv, k, v, k_min=k.amin(2), k_max=k.amax(2)), torch.zeros((1, 2, 64), device="cuda")
+    for scale in (1e-45, 1e-38, 2.35e38):
+        out, lse = m.kv_attend(kv, pages, table, n, q, scale, want_lse=True)
+        assert (out == 1).all() and ((lse - np.log(50)).abs() < 1e-5).all()
+    for scale in (2.4e38, 3.4e38):
+        for call in (lambda s: m.kv_attend(kv, pages, table, n, q, s), lambda s: m.kv_attend_blocks(kv, pages, table, n, q, s, 3)):
+            with pytest.raises(m.MoeiError, match="scale"):
+                call(scale)
