@@ -613,7 +613,7 @@ def _attend_args(kv: Kv, pages: KvPages, table, lens, q, out, want_lse, lse):
     assert table.is_contiguous() and lens.is_contiguous() and lens.numel() == B, (table.shape, lens.shape)
     stride = _rows(kv, q, B, kv.heads)
     if out is None:
-        if kv.out_heads != kv.heads:
+        if kv.out_heads != kv.heads or q.shape[1:] != kv.heads:
             out = q.new_empty((B, *kv.out_heads))
         else:
             out = torch.empty_like(q) if stride == 0 else torch.empty_like(q, memory_format=torch.contiguous_format)

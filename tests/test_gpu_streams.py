@@ -1,4 +1,4 @@
-"""Calls on a stream that is not the current one: what they allocate belongs to that stream, and holds the same bits."""
+"""What calls allocate: on a stream that is not the current one it belongs to that stream and holds the same bits."""
 import numpy as np
 import pytest
 import torch
@@ -107,3 +107,14 @@ def test_calls_of_the_expert_path(m, by_handle):  # noqa: F811
     assert cache.error_flags() == 0
     cache.close()
     eamc.close()
+
+
+def test_kv_outputs_have_the_documented_shape(m):  # noqa: F811
+    # queries may be any contiguous tensor of a call's elements, as projections leave them: outputs are [B][Hq][v_dim] all the same
+    for Dv in (64, 48):
+        c = Case(m, "bf16", 4, 2, 64, Dv, 16, [90, 40, 1], seed=Dv, summaries=True, max_sel=6)
+        want = m.kv_attend(c.kv, c.pages, c.table, c.len_t, c.q, c.scale)
+        for q in (c.q, c.q.view(3, 256), c.q.view(3, 1, 256), c.q.view(1, 3, 4, 64), c.q.view(-1)):
+            out = m.kv_attend(c.kv, c.pages, c.table, c.len_t, q, c.scale)
+            few = m.kv_attend_blocks(c.kv, c.pages, c.table, c.len_t, q, c.scale, 6)
+            assert torch.equal(out, want) and torch.equal(few, want) and out.shape == few.shape == (3, 4, Dv)
