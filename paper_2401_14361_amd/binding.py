@@ -490,7 +490,10 @@ class _KvPages(C.Structure):
 
 
 class Kv:
-    """Owner of a moei_kv handle: shapes, scratch and error flags of a paged KV cache (the pages are the caller's)."""
+    """Owner of a moei_kv handle: shapes, scratch and error flags of a paged KV cache (the pages are the caller's).
+
+    max_sel, the largest n_sel of kv_attend_blocks (None: 256 or max_pages), costs scratch: 12 bytes for each of max_pages pages of each
+    key/value head of each of max_batch sequences, 25 MB for the defaults and eight heads.  0 where pages are never selected: none."""
 
     DTYPES = {"fp32": WDTYPE_FP32, "bf16": WDTYPE_BF16, "fp8": KVDTYPE_FP8}
     _PAGE = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp8": torch.float8_e4m3fn}

@@ -184,6 +184,8 @@ __device__ __forceinline__ void summarise(Args a, int page, int h, const float* 
 // units dealt out one by one, with two divisions each, 42 - 48.
 // kSums: each token is its sequence's only one, and further workgroups (blockIdx.y >= parts) form the summaries of the pages that
 // are completed, one for a key/value head: the page's other rows are there from earlier calls, the new one is formed a second time.
+// Bound by five trips to memory one after the other - position, table, frequencies, the new key with its scale, the page's rows, which would need
+// the table's entry alone: 64 sequences of eight heads in 8 bits 7.9 us, 4.7 where no page is completed.
 template <typename IO, typename PG, int W, bool kSums>
 __global__ void __launch_bounds__(kAppThreads, kSums ? 4 : 6) kv_append_kernel(KvAppendArgs) {
     const Args a = (Args)__builtin_amdgcn_kernarg_segment_ptr();

@@ -2,7 +2,8 @@
 //
 // out[b][h] = sum_j softmax_j(scale q.k_j) v_j over the sequence's tokens, in one pass over keys and values with the running
 // maximum and sum of the softmax.  Bound by the bytes of the pages: up to sixteen query heads of a group share a pass, and on the matrix
-// cores their products take a tenth of the time that the bytes need.
+// cores their products take a sixth of the time that the bytes need.  Larger groups read the pages once for every sixteen heads: 16 sequences of up to
+// 32,768 tokens, one key/value head of 128, take 42 us for a group of 16, 66 for one of 32 (1.8 times the bytes), 110 for one of 64 (3.0).
 #include <math.h>
 
 #include "kv.hpp"
@@ -53,6 +54,8 @@ __device__ __forceinline__ Span span_of(A a, int len) {
 template <int kUnit>
 __device__ __forceinline__ int units_of(const Span& s) { return max(1, (s.end - s.start + kUnit - 1) / kUnit); }  // (an empty one has its zeros to write)
 
+// (Every workgroup reads all lengths two times or three, 64 at once: 4,096 sequences of up to 200 tokens, one head of 64, take 89 us, of which their
+// bytes need 15, 1,024 of them 37 and 4.)
 struct Stretch {
     unsigned per;         // units of a workgroup
     unsigned step;        // items begin at multiples of it in the line: `per` where every item has workgroups of its own, else 1
@@ -203,8 +206,10 @@ __device__ __forceinline__ float2 load_past(const unsigned long long* p) {
 }
 
 // ------------------------------------------------------------------------------------------------ a stretch of units
-// A wavefront brings tiles of sixteen keys and values (8-bit: 32) into a ring of two stages of its own in LDS, by loads that pass the registers by,
-// and waits for the oldest only, so that a compute unit has 64 - 128 KB under way all the time.  Logits are keys times queries, head by
+// A wavefront brings tiles of sixteen keys and values (8-bit: 32) into a ring of its own in LDS, by loads that pass the registers by, and waits for
+// the oldest only.  Most classes have two stages, 128 KB of rings in a compute unit (192-wide keys 160); fp32 heads of 96 have three, 144 KB;
+// fp32 heads of 256 a single one, 128 KB: a tile's keys are asked for when the tile before has its logits, and its values when that one's are summed, so
+// less than a tile is under way (16 sequences of up to 8,000 tokens, four heads, 155 us, 5.3 TB/s as by heads of 128).  Logits are keys times queries, head by
 // head in columns; their exponentials lie in a lane's registers as the second product, values transposed by the LDS read times weights, wants
 // them: nothing goes from lane to lane but a maximum, and only a higher one costs a rescaling.
 // Measured, of the 7.0 TB/s that streams which only read reach: bf16, heads of 128: one sequence of 131,072 tokens 84 us (6.3 TB/s), 64 ragged ones
@@ -678,6 +683,8 @@ int launch_shape(const moei_kv& kv, const KvAttendArgs& a, hipStream_t s) {
 // 16,384 with eight heads 384 (380), 100 of up to 4,000 86 (76).  Items of one length, as lists and windows make them, keep eight wavefronts while each
 // has a workgroup to itself: 24 lists of 1,536 tokens with eight heads 19.7 (four: 24.2).  Heads of 256, where two take the place of four: 48 lists of 384 tokens with
 // eight heads 32.4 (36.2).
+// The host knows no lengths: a sequence counts as long as its table, list or window allows.  With tables of 4,096 pages the same short sequences have eight
+// wavefronts, 64 of up to 2,000 36.2 us, 160 of up to 200 21.9, in 8 bits 100 of up to 1,000 31.2: a caller that knows better hands in a narrower table.
 template <typename T>
 bool many_short_items(const moei_kv& kv, const KvAttendArgs& a) {
     const long long items = (long long)a.B * a.n_kv * a.blocks_of_heads;
