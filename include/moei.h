@@ -405,6 +405,19 @@ int kv_append(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, i
               const void* d_q, int64_t q_stride, const void* d_k, int64_t k_stride, const void* d_v, int64_t v_stride,
               const float* d_inv_freq, int32_t rot_dim, int32_t interleaved, void* d_q_out, void* stream);
 
+/* kv_append of queries and keys that are normed for each head before they are rotated: x_d becomes
+ *   x_d w_d / sqrt(mean over d of x_d^2 + eps),  in fp32, and is rounded once behind the rotation.
+ * w: d_q_weight and d_k_weight, fp32, [k_dim] for every head or with weight_per_head [n_q_heads][k_dim] and [n_kv_heads][k_dim]; values are not normed.
+ * eps is positive and finite.  Squares are summed in fp32: a head whose sum of squares passes that type's range becomes zeros, and infinities in it no
+ * numbers; a head that holds no number becomes none.
+ * Token t is rotated by position d_turn[t] (any; NULL: d_pos[t]): where a cache has evicted tokens, the place of a new token, d_pos, is not its
+ * position in the text.  d_q_out overlaps no weights. */
+int kv_append_norm(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, int32_t table_width, int32_t B,
+                   const int32_t* d_seq, const int32_t* d_pos, const int32_t* d_turn, int32_t T,
+                   const void* d_q, int64_t q_stride, const void* d_k, int64_t k_stride, const void* d_v, int64_t v_stride,
+                   const float* d_q_weight, const float* d_k_weight, int32_t weight_per_head, float eps,
+                   const float* d_inv_freq, int32_t rot_dim, int32_t interleaved, void* d_q_out, void* stream);
+
 /* Attention of one token per sequence: for every sequence b and query head h,
  *   d_out[b][h] = sum_j softmax_j(scale * q.k_j) v_j  over its tokens j with d_len[b] - window <= j < d_len[b]  (window 0: all of them),
  * d_lse[b][h] (fp32, may be NULL) = the natural logarithm of the softmax's denominator.  d_q[B][n_q_heads][k_dim] with q_stride elements

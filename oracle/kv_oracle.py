@@ -19,6 +19,17 @@ def rotate(x, pos, inv_freq, interleaved):
     return y
 
 
+def norm(x, weight, eps):
+    """x [T][heads][D], weight [D] or [heads][D], float64 -> every head divided by the root of its mean square (and eps), times the weight."""
+    y = np.empty_like(np.asarray(x, dtype=np.float64))
+    weight = np.broadcast_to(np.asarray(weight, dtype=np.float64), y.shape[1:])
+    for t in range(y.shape[0]):
+        for h in range(y.shape[1]):
+            row = np.asarray(x[t, h], dtype=np.float64)
+            y[t, h] = row / np.sqrt(np.mean(row * row) + eps) * weight[h]
+    return y
+
+
 def places(table, seq, pos, page, n_pages):
     """(page, row) of every token, None for one that has no place."""
     got = []

@@ -22,7 +22,7 @@ __all__ = [
     "moe_route_topk", "eam_update", "eamc_match", "eamc_match_topm", "expert_priority", "expert_ffn_gemv",
     "expert_ffn_gemv_static",
     "moe_decode_layer", "moe_prefill_layer", "expert_ffn_grouped", "WDTYPE_FP32", "WDTYPE_BF16", "EXPORTS", "expert_pack", "profile_enable", "profile_disable", "profile_read", "profile_samples",
-    "Kv", "KvDesc", "KvPages", "kv_append", "kv_attend", "kv_attend_blocks", "KVDTYPE_FP8",
+    "Kv", "KvDesc", "KvPages", "kv_append", "kv_append_norm", "kv_attend", "kv_attend_blocks", "KVDTYPE_FP8",
 ]
 
 WDTYPE_FP32, WDTYPE_BF16 = 0, 1
@@ -38,7 +38,7 @@ EXPORTS = [
     "moe_decode_layer", "moei_cache_last_step", "moei_cache_last_heads", "moei_cache_join", "moei_cache_sync",
     "moei_cache_set_match_count", "moei_cache_last_matches",
     "moe_prefill_layer", "moei_cache_set_policy", "moei_cache_prefetch", "moei_cache_set_prefetch", "moei_cache_last_prefetch",
-    "moei_kv_create", "moei_kv_destroy", "moei_kv_error_flags", "kv_append", "kv_attend", "kv_attend_blocks",
+    "moei_kv_create", "moei_kv_destroy", "moei_kv_error_flags", "kv_append", "kv_append_norm", "kv_attend", "kv_attend_blocks",
     "moei_profile_enable", "moei_profile_disable", "moei_profile_kernels", "moei_profile_kernel_name",
     "moei_profile_read", "moei_profile_samples",
 ]
@@ -84,6 +84,7 @@ def lib() -> C.CDLL:
         L.moei_profile_kernel_name.restype = C.c_char_p
         P, i32, i64, f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_float
         L.kv_append.argtypes = [P, P, P, i32, i32, P, P, i32, P, i64, P, i64, P, i64, P, i32, i32, P, P]
+        L.kv_append_norm.argtypes = [P, P, P, i32, i32, P, P, P, i32, P, i64, P, i64, P, i64, P, P, i32, f32, P, i32, i32, P, P]
         L.kv_attend.argtypes = [P, P, P, i32, P, i32, P, i64, f32, i32, P, P, P]
         L.kv_attend_blocks.argtypes = [P, P, P, i32, P, i32, P, i64, f32, i32, i32, i32, P, P, P, P]
         _lib = L
@@ -604,6 +605,32 @@ def kv_append(kv: Kv, pages: KvPages, table: torch.Tensor, pos: torch.Tensor, q:
                            v.data_ptr(), _rows(kv, v, T, kv.v_heads),
                            None if inv_freq is None else inv_freq.data_ptr(), 0 if inv_freq is None else 2 * inv_freq.numel(),
                            interleaved, _given(kv, q_out, T, kv.heads), _kv_stream(kv, stream)))
+    return q_out
+
+
+def kv_append_norm(kv: Kv, pages: KvPages, table: torch.Tensor, pos: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor,
+                   q_weight: torch.Tensor, k_weight: torch.Tensor, inv_freq: torch.Tensor | None, eps: float = 1e-6,
+                   seq: torch.Tensor | None = None, turn: torch.Tensor | None = None, interleaved: bool = False,
+                   q_out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """kv_append of queries and keys that are normed for each head before the rotation, with fp32 weights [k_dim], or [Hq][k_dim] and
+    [Hkv][k_dim].  turn [T]: positions to rotate by, where they are not the tokens' places pos [T]."""
+    assert pages.layout == kv.layout, (pages.layout, kv.layout)
+    T = pos.numel()
+    B, width = table.shape
+    if q_out is None:
+        q_out = _new((T, *kv.heads), kv.dtype, kv.device, stream)
+    assert inv_freq is None or (inv_freq.dtype is torch.float32 and inv_freq.get_device() == kv.index and inv_freq.is_contiguous()), (inv_freq.device, inv_freq.dtype)
+    assert (seq is None or seq.numel() == T) and (turn is None or turn.numel() == T)
+    each = q_weight.dim() == 2
+    assert q_weight.shape == (kv.heads if each else kv.heads[1:]) and k_weight.shape == (kv.k_heads if each else kv.heads[1:]), (q_weight.shape, k_weight.shape)
+    for w in (q_weight, k_weight):
+        assert w.dtype is torch.float32 and w.get_device() == kv.index and w.is_contiguous(), (w.device, w.dtype)
+    _check(lib().kv_append_norm(kv.h, pages.ref, _ints(kv, table), width, B, None if seq is None else _ints(kv, seq), _ints(kv, pos),
+                                None if turn is None else _ints(kv, turn), T,
+                                q.data_ptr(), _rows(kv, q, T, kv.heads), k.data_ptr(), _rows(kv, k, T, kv.k_heads),
+                                v.data_ptr(), _rows(kv, v, T, kv.v_heads), q_weight.data_ptr(), k_weight.data_ptr(), each, eps,
+                                None if inv_freq is None else inv_freq.data_ptr(), 0 if inv_freq is None else 2 * inv_freq.numel(),
+                                interleaved, _given(kv, q_out, T, kv.heads), _kv_stream(kv, stream)))
     return q_out
 
 

@@ -63,6 +63,11 @@ enum KernelId {
     K_KV_SUMMARY,
     K_KV_ATTEND,
     K_KV_BLOCKS,
+    K_KV_APPEND_NORM,
+    K_KV_SHARED,
+    K_KV_WEIGHTS,
+    K_KV_EVICT,
+    K_KV_MOVE,
     K_COUNT
 };
 extern bool g_prof_on;

@@ -3,180 +3,11 @@
 
 #include <new>
 
-#include "kv.hpp"
+#include "kv_append.hpp"
 
 namespace moei {
 
 namespace {
-
-constexpr int kAppThreads = 256;
-constexpr float kFp8Max = 448.f;
-
-struct KvAppendArgs {
-    const void *q, *k, *v;
-    long long q_stride, k_row, v_row;  // elements between tokens
-    void* q_out;                       // [T][Hq][k_dim]
-    const float* inv_freq;             // [rot / 2]
-    const int32_t *seq, *pos;          // seq null: token t belongs to sequence t
-    const int32_t* table;
-    int T, B, width, page_shift, n_pages;
-    int n_q, n_kv, k_dim, v_dim, rot, interleaved;
-    void *k_pages, *v_pages;
-    long long k_stride, v_stride;
-    const float *k_scale, *v_scale;
-    void *k_min, *k_max;
-    int parts;  // workgroups that share a token out
-    int32_t* flags;
-};
-
-// ------------------------------------------------------------------------------------------------ element access
-typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
-
-// W elements: 16 bytes, or one
-template <typename IO, int W>
-struct Vec {
-    static_assert(W * sizeof(IO) == 16);
-    typedef u32x4 raw;
-    static __device__ __forceinline__ raw load(const IO* p) { return *reinterpret_cast<const u32x4*>(p); }
-    static __device__ __forceinline__ void unpack(raw v, float* f) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (sizeof(IO) == 4) f[i] = __uint_as_float(v[i]);
-            else f[2 * i] = bf16_lo(v[i]), f[2 * i + 1] = bf16_hi(v[i]);
-        }
-    }
-    static __device__ __forceinline__ void store(IO* p, const float* f) {
-        u32x4 v;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if constexpr (sizeof(IO) == 4) v[i] = __float_as_uint(f[i]);
-            else v[i] = pack_bf16(f[2 * i], f[2 * i + 1]);
-        }
-        *reinterpret_cast<u32x4*>(p) = v;
-    }
-};
-template <typename IO>
-struct Vec<IO, 1> {
-    typedef IO raw;
-    static __device__ __forceinline__ raw load(const IO* p) { return *p; }
-    static __device__ __forceinline__ void unpack(raw v, float* f) {
-        if constexpr (sizeof(IO) == 4) f[0] = v;
-        else f[0] = bf16_one(v);
-    }
-    static __device__ __forceinline__ void store(IO* p, const float* f) {
-        if constexpr (sizeof(IO) == 4) *p = f[0];
-        else *p = (uint16_t)pack_bf16(f[0], 0.f);
-    }
-};
-// 8-bit values: divided by the head's scale, limited to the largest that the type has (what is no number stays none), rounded to nearest even
-__device__ __forceinline__ float for_fp8(float x, float scale) {
-    const float y = x / scale;
-    return y > kFp8Max ? kFp8Max : y < -kFp8Max ? -kFp8Max : y;
-}
-template <int W>
-__device__ __forceinline__ void store_fp8(uint8_t* p, const float* f, float scale) {
-    if constexpr (W == 8) {
-        int a = 0, b = 0;
-        a = __builtin_amdgcn_cvt_pk_fp8_f32(for_fp8(f[0], scale), for_fp8(f[1], scale), a, false);
-        a = __builtin_amdgcn_cvt_pk_fp8_f32(for_fp8(f[2], scale), for_fp8(f[3], scale), a, true);
-        b = __builtin_amdgcn_cvt_pk_fp8_f32(for_fp8(f[4], scale), for_fp8(f[5], scale), b, false);
-        b = __builtin_amdgcn_cvt_pk_fp8_f32(for_fp8(f[6], scale), for_fp8(f[7], scale), b, true);
-        *reinterpret_cast<uint2*>(p) = make_uint2((unsigned)a, (unsigned)b);
-    } else {
-        *p = (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(for_fp8(f[0], scale), 0.f, 0, false);
-    }
-}
-
-// cos and sin of position times frequency, in 64 bits and rounded once: at position 10^5 an fp32 angle would be off by up to 2^-8, and an fp32 turn,
-// reduced in 64 bits, by as much as the rounding of sine and cosine themselves.  (1 / (2 pi) in two numbers: positions reach 2^30.)
-__device__ __forceinline__ float2 turn(int pos, float freq) {
-    const double angle = (double)pos * (double)freq, turns = angle * 0x1.45f306dc9c883p-3;
-    const double rest = __builtin_fma(angle, 0x1.45f306dc9c883p-3, -turns) + angle * -0x1.6b01ec5417056p-57;
-    double s, c;
-    sincospi(2.0 * (turns - rint(turns) + rest), &s, &c);
-    return make_float2((float)c, (float)s);
-}
-__device__ __forceinline__ void turn_pair(float& x1, float& x2, float2 cs) {
-    const float y1 = __builtin_fmaf(x1, cs.x, -(x2 * cs.y));
-    x2 = __builtin_fmaf(x2, cs.x, x1 * cs.y);
-    x1 = y1;
-}
-
-typedef const __attribute__((address_space(4))) KvAppendArgs* Args;  // (in place: a copy would go to private memory)
-
-// The page that holds a token's row, -1: none (a flag is raised by the thread that `tell` names).
-__device__ __forceinline__ int page_of(Args a, int t, int pos, bool tell) {
-    const int seq = a->seq ? a->seq[t] : t, at = pos >> a->page_shift;
-    if (pos < 0) return -1;
-    if (seq < 0 || seq >= a->B || at >= a->width) {
-        if (tell) atomicOr(a->flags, kKvBadLength);
-        return -1;
-    }
-    const int page = a->table[(long long)seq * a->width + at];
-    if (page >= 0 && page < a->n_pages) return page;
-    if (tell) atomicOr(a->flags, kKvBadPage);
-    return -1;
-}
-
-// Smallest and largest value of every dimension of a page's keys, by a workgroup; `own` (LDS) stands for row `own_row`, as stored values.
-// A thread takes 16 bytes of a row, and every so many rows.
-template <typename IO, typename PG>
-__device__ __forceinline__ void summarise(Args a, int page, int h, const float* own, int own_row) {
-    constexpr int N = 16 / sizeof(PG);
-    __shared__ IO s_lo[kAppThreads * N], s_hi[kAppThreads * N];  // (the type holds them exactly)
-    const int pieces = a->k_dim / N, size = 1 << a->page_shift, groups = kAppThreads / pieces;
-    const int g = threadIdx.x / pieces, p = threadIdx.x - g * pieces;
-    const PG* src = static_cast<const PG*>(a->k_pages) + page * a->k_stride + ((long long)h << a->page_shift) * a->k_dim + p * N;
-    float lo[N], hi[N];
-#pragma unroll
-    for (int j = 0; j < N; ++j) lo[j] = INFINITY, hi[j] = -INFINITY;
-    if (g < groups)
-#pragma unroll 4
-        for (int r = g; r < size; r += groups) {
-            const u32x4 v = *reinterpret_cast<const u32x4*>(src + r * a->k_dim);
-            float x[N];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if constexpr (sizeof(PG) == 1) {
-                    x[4 * i] = __builtin_amdgcn_cvt_f32_fp8((int)v[i], 0); x[4 * i + 1] = __builtin_amdgcn_cvt_f32_fp8((int)v[i], 1);
-                    x[4 * i + 2] = __builtin_amdgcn_cvt_f32_fp8((int)v[i], 2); x[4 * i + 3] = __builtin_amdgcn_cvt_f32_fp8((int)v[i], 3);
-                } else if constexpr (sizeof(PG) == 2) {
-                    x[2 * i] = bf16_lo(v[i]); x[2 * i + 1] = bf16_hi(v[i]);
-                } else {
-                    x[i] = __uint_as_float(v[i]);
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const float y = r == own_row ? own[p * N + j] : x[j];
-                lo[j] = fminf(lo[j], y);
-                hi[j] = fmaxf(hi[j], y);
-            }
-        }
-#pragma unroll
-    for (int j = 0; j < N; ++j) {  // [N][threads]: a column's values side by side
-        Vec<IO, 1>::store(&s_lo[j * kAppThreads + threadIdx.x], &lo[j]);
-        Vec<IO, 1>::store(&s_hi[j * kAppThreads + threadIdx.x], &hi[j]);
-    }
-    __syncthreads();
-    for (int d = threadIdx.x; d < a->k_dim; d += kAppThreads) {
-        const int at = d % N * kAppThreads + d / N;
-        float l, u;
-        Vec<IO, 1>::unpack(s_lo[at], &l);
-        Vec<IO, 1>::unpack(s_hi[at], &u);
-        for (int j = 1; j < groups; ++j) {
-            float x, y;
-            Vec<IO, 1>::unpack(s_lo[at + j * pieces], &x);
-            Vec<IO, 1>::unpack(s_hi[at + j * pieces], &y);
-            l = fminf(l, x);
-            u = fmaxf(u, y);
-        }
-        const long long to = ((long long)page * a->n_kv + h) * a->k_dim + d;
-        Vec<IO, 1>::store(static_cast<IO*>(a->k_min) + to, &l);
-        Vec<IO, 1>::store(static_cast<IO*>(a->k_max) + to, &u);
-    }
-    __syncthreads();
-}
 
 // A workgroup takes a share of a token's heads.  A thread's unit is two vectors of W elements of a head, which hold W pairs or are plain; it keeps
 // its place and goes from head to head, so that the turns of its pairs are read once and nothing is divided on the way, and has the next
@@ -324,8 +155,6 @@ void launch_append(KvAppendArgs a, bool wide, int cus, hipStream_t s) {
     const auto kernel = sums ? (wide ? kv_append_kernel<IO, PG, N, true> : kv_append_kernel<IO, PG, 1, true>)
                              : (wide ? kv_append_kernel<IO, PG, N, false> : kv_append_kernel<IO, PG, 1, false>);
     launch(K_KV_APPEND, kernel, grid, dim3(kAppThreads), 0, s, a);
-    const int look = 1 << (a.page_shift < 6 ? a.page_shift : 6);
-    if (a.k_min && a.seq) launch(K_KV_SUMMARY, kv_summary_kernel<IO, PG>, dim3((unsigned)((a.T + look - 1) / look), (unsigned)a.n_kv), dim3(kAppThreads), 0, s, a);
 }
 
 int log2_of(int v) { return 31 - __builtin_clz((unsigned)v); }
@@ -411,7 +240,66 @@ int fill_attend(const char* who, const moei_kv* kv, const moei_kv_pages* p, cons
     return MOEI_OK;
 }
 
+// Checks what both appends have in common, and their arguments; *wide: sixteen bytes at a time.
+int fill_append(const char* who, const moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, int32_t table_width, int32_t B,
+                const int32_t* d_seq, const int32_t* d_pos, int32_t T,
+                const void* d_q, int64_t q_stride, const void* d_k, int64_t k_stride, const void* d_v, int64_t v_stride,
+                const float* d_inv_freq, int32_t rot_dim, int32_t interleaved, void* d_q_out, KvAppendArgs* args, bool* wide) {
+    const int rc = check_call(who, kv, pages, d_table, table_width);
+    if (rc) return rc;
+    const moei_kv_desc& d = kv->d;
+    MOEI_REQUIRE(d_pos && d_q && d_k && d_v && d_q_out, "%s: null pointer", who);
+    MOEI_REQUIRE(B >= 1 && B <= d.max_batch, "%s: B = %d outside [1, max_batch = %d]", who, B, d.max_batch);
+    MOEI_REQUIRE(d_seq || T <= B, "%s: %d tokens of %d sequences need d_seq", who, T, B);
+    MOEI_REQUIRE(T < (1 << 24), "%s: T = %d must be below 2^24", who, T);  // (a launch counts its threads in 32 bits)
+    MOEI_REQUIRE(rot_dim >= 0 && rot_dim <= d.k_dim && rot_dim % 2 == 0, "%s: rot_dim = %d must be even and at most k_dim = %d", who, rot_dim, d.k_dim);
+    MOEI_REQUIRE(rot_dim == 0 || d_inv_freq, "%s: null d_inv_freq", who);
+    const long long nq = (long long)d.n_q_heads * d.k_dim, nk = (long long)d.n_kv_heads * d.k_dim, nv = (long long)d.n_kv_heads * d.v_dim;
+    MOEI_REQUIRE((q_stride == 0 || q_stride >= nq) && (k_stride == 0 || k_stride >= nk) && (v_stride == 0 || v_stride >= nv),
+                 "%s: strides %lld, %lld, %lld are shorter than a token (%lld, %lld, %lld)", who, (long long)q_stride, (long long)k_stride, (long long)v_stride, nq, nk, nv);
+    const int io = kv_io_bytes(d.dtype);
+    MOEI_REQUIRE((uintptr_t)d_q % io == 0 && (uintptr_t)d_k % io == 0 && (uintptr_t)d_v % io == 0 && (uintptr_t)d_q_out % io == 0, "%s: elements are not aligned", who);
+    MOEI_REQUIRE((d_q_out == d_q && (T == 1 || q_stride == 0 || q_stride == nq)) || !overlap(d_q, T, (q_stride ? q_stride : nq) * io, nq * io, d_q_out, (long long)T * nq * io),
+                 "%s: d_q_out overlaps d_q, but is not the same dense tensor", who);
+    MOEI_REQUIRE(!overlap(d_k, T, (k_stride ? k_stride : nk) * io, nk * io, d_q_out, (long long)T * nq * io) &&
+                     !overlap(d_v, T, (v_stride ? v_stride : nv) * io, nv * io, d_q_out, (long long)T * nq * io),
+                 "%s: d_q_out overlaps d_k or d_v", who);  // (other workgroups read them still)
+    *args = KvAppendArgs{};
+    KvAppendArgs& a = *args;
+    a.q = d_q; a.k = d_k; a.v = d_v;
+    a.q_stride = q_stride ? q_stride : nq;
+    a.k_row = k_stride ? k_stride : nk;
+    a.v_row = v_stride ? v_stride : nv;
+    a.q_out = d_q_out;
+    a.inv_freq = d_inv_freq;
+    a.seq = d_seq; a.pos = d_pos; a.table = d_table;
+    a.T = T; a.B = B; a.width = table_width;
+    a.page_shift = log2_of(d.page_size);
+    a.n_pages = pages->n_pages;
+    a.n_q = d.n_q_heads; a.n_kv = d.n_kv_heads; a.k_dim = d.k_dim; a.v_dim = d.v_dim;
+    a.rot = rot_dim; a.interleaved = interleaved != 0;
+    a.k_pages = pages->d_k; a.v_pages = pages->d_v;
+    strides_of(kv, pages, &a.k_stride, &a.v_stride);
+    a.k_scale = pages->d_k_scale; a.v_scale = pages->d_v_scale;
+    a.k_min = pages->d_k_min; a.k_max = pages->d_k_max;
+    a.flags = kv->d_flags;
+    // Sixteen bytes at a time where every vector of elements begins at a multiple of 16 bytes and a vector of pairs fits the rotated part.
+    const int W = 16 / io;
+    auto even = [&](const void* p, long long stride) { return (uintptr_t)p % 16 == 0 && stride % W == 0; };
+    *wide = rot_dim / 2 % W == 0 && even(d_q, a.q_stride) && even(d_k, a.k_row) && even(d_v, a.v_row) && even(d_q_out, 0);
+    return MOEI_OK;
+}
+
 }  // namespace
+
+
+int launch_kv_summary(int dtype, const KvAppendArgs& a, hipStream_t s) {
+    const int look = 1 << (a.page_shift < 6 ? a.page_shift : 6);
+    const auto kernel = dtype == MOEI_WDTYPE_FP32 ? kv_summary_kernel<float, float> : dtype == MOEI_WDTYPE_BF16 ? kv_summary_kernel<uint16_t, uint16_t> : kv_summary_kernel<uint16_t, uint8_t>;
+    launch(K_KV_SUMMARY, kernel, dim3((unsigned)((a.T + look - 1) / look), (unsigned)a.n_kv), dim3(kAppThreads), 0, s, a);
+    MOEI_LAUNCH_CHECK();
+    return MOEI_OK;
+}
 
 }  // namespace moei
 
@@ -490,53 +378,46 @@ extern "C" int kv_append(moei_kv* kv, const moei_kv_pages* pages, const int32_t*
     const char* who = "kv_append";
     MOEI_REQUIRE(T >= 0 && B >= 0, "%s: T = %d or B = %d is negative", who, T, B);
     if (T == 0) return MOEI_OK;
-    const int rc = check_call(who, kv, pages, d_table, table_width);
+    KvAppendArgs a;
+    bool wide;
+    const int rc = fill_append(who, kv, pages, d_table, table_width, B, d_seq, d_pos, T, d_q, q_stride, d_k, k_stride, d_v, v_stride, d_inv_freq, rot_dim, interleaved, d_q_out, &a, &wide);
+    if (rc) return rc;
+    hipStream_t s = as_stream(stream);
+    switch (kv->d.dtype) {
+        case MOEI_WDTYPE_FP32: launch_append<float, float>(a, wide, kv->cus, s); break;
+        case MOEI_WDTYPE_BF16: launch_append<uint16_t, uint16_t>(a, wide, kv->cus, s); break;
+        default: launch_append<uint16_t, uint8_t>(a, wide, kv->cus, s);
+    }
+    MOEI_LAUNCH_CHECK();
+    if (a.k_min && a.seq) return launch_kv_summary(kv->d.dtype, a, s);
+    return MOEI_OK;
+}
+
+extern "C" int kv_append_norm(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, int32_t table_width, int32_t B,
+                              const int32_t* d_seq, const int32_t* d_pos, const int32_t* d_turn, int32_t T,
+                              const void* d_q, int64_t q_stride, const void* d_k, int64_t k_stride, const void* d_v, int64_t v_stride,
+                              const float* d_q_weight, const float* d_k_weight, int32_t weight_per_head, float eps,
+                              const float* d_inv_freq, int32_t rot_dim, int32_t interleaved, void* d_q_out, void* stream) {
+    const char* who = "kv_append_norm";
+    MOEI_REQUIRE(T >= 0 && B >= 0, "%s: T = %d or B = %d is negative", who, T, B);
+    if (T == 0) return MOEI_OK;
+    KvAppendArgs a;
+    bool wide;
+    const int rc = fill_append(who, kv, pages, d_table, table_width, B, d_seq, d_pos, T, d_q, q_stride, d_k, k_stride, d_v, v_stride, d_inv_freq, rot_dim, interleaved, d_q_out, &a, &wide);
     if (rc) return rc;
     const moei_kv_desc& d = kv->d;
-    MOEI_REQUIRE(d_pos && d_q && d_k && d_v && d_q_out, "%s: null pointer", who);
-    MOEI_REQUIRE(B >= 1 && B <= d.max_batch, "%s: B = %d outside [1, max_batch = %d]", who, B, d.max_batch);
-    MOEI_REQUIRE(d_seq || T <= B, "%s: %d tokens of %d sequences need d_seq", who, T, B);
-    MOEI_REQUIRE(T < (1 << 24), "%s: T = %d must be below 2^24", who, T);  // (a launch counts its threads in 32 bits)
-    MOEI_REQUIRE(rot_dim >= 0 && rot_dim <= d.k_dim && rot_dim % 2 == 0, "%s: rot_dim = %d must be even and at most k_dim = %d", who, rot_dim, d.k_dim);
-    MOEI_REQUIRE(rot_dim == 0 || d_inv_freq, "%s: null d_inv_freq", who);
-    const long long nq = (long long)d.n_q_heads * d.k_dim, nk = (long long)d.n_kv_heads * d.k_dim, nv = (long long)d.n_kv_heads * d.v_dim;
-    MOEI_REQUIRE((q_stride == 0 || q_stride >= nq) && (k_stride == 0 || k_stride >= nk) && (v_stride == 0 || v_stride >= nv),
-                 "%s: strides %lld, %lld, %lld are shorter than a token (%lld, %lld, %lld)", who, (long long)q_stride, (long long)k_stride, (long long)v_stride, nq, nk, nv);
-    const int io = kv_io_bytes(d.dtype);
-    MOEI_REQUIRE((uintptr_t)d_q % io == 0 && (uintptr_t)d_k % io == 0 && (uintptr_t)d_v % io == 0 && (uintptr_t)d_q_out % io == 0, "%s: elements are not aligned", who);
-    MOEI_REQUIRE((d_q_out == d_q && (T == 1 || q_stride == 0 || q_stride == nq)) || !overlap(d_q, T, (q_stride ? q_stride : nq) * io, nq * io, d_q_out, (long long)T * nq * io),
-                 "%s: d_q_out overlaps d_q, but is not the same dense tensor", who);
-    MOEI_REQUIRE(!overlap(d_k, T, (k_stride ? k_stride : nk) * io, nk * io, d_q_out, (long long)T * nq * io) &&
-                     !overlap(d_v, T, (v_stride ? v_stride : nv) * io, nv * io, d_q_out, (long long)T * nq * io),
-                 "%s: d_q_out overlaps d_k or d_v", who);  // (other workgroups read them still)
-    KvAppendArgs a{};
-    a.q = d_q; a.k = d_k; a.v = d_v;
-    a.q_stride = q_stride ? q_stride : nq;
-    a.k_row = k_stride ? k_stride : nk;
-    a.v_row = v_stride ? v_stride : nv;
-    a.q_out = d_q_out;
-    a.inv_freq = d_inv_freq;
-    a.seq = d_seq; a.pos = d_pos; a.table = d_table;
-    a.T = T; a.B = B; a.width = table_width;
-    a.page_shift = log2_of(d.page_size);
-    a.n_pages = pages->n_pages;
-    a.n_q = d.n_q_heads; a.n_kv = d.n_kv_heads; a.k_dim = d.k_dim; a.v_dim = d.v_dim;
-    a.rot = rot_dim; a.interleaved = interleaved != 0;
-    a.k_pages = pages->d_k; a.v_pages = pages->d_v;
-    strides_of(kv, pages, &a.k_stride, &a.v_stride);
-    a.k_scale = pages->d_k_scale; a.v_scale = pages->d_v_scale;
-    a.k_min = pages->d_k_min; a.k_max = pages->d_k_max;
-    a.flags = kv->d_flags;
-    // Sixteen bytes at a time where every vector of elements begins at a multiple of 16 bytes and a vector of pairs fits the rotated part.
-    const int W = 16 / io;
-    auto even = [&](const void* p, long long stride) { return (uintptr_t)p % 16 == 0 && stride % W == 0; };
-    const bool wide = rot_dim / 2 % W == 0 && even(d_q, a.q_stride) && even(d_k, a.k_row) && even(d_v, a.v_row) && even(d_q_out, 0);
-    hipStream_t s = as_stream(stream);
-    if (d.dtype == MOEI_WDTYPE_FP32) launch_append<float, float>(a, wide, kv->cus, s);
-    else if (d.dtype == MOEI_WDTYPE_BF16) launch_append<uint16_t, uint16_t>(a, wide, kv->cus, s);
-    else launch_append<uint16_t, uint8_t>(a, wide, kv->cus, s);
-    MOEI_LAUNCH_CHECK();
-    return MOEI_OK;
+    MOEI_REQUIRE(d_q_weight && d_k_weight, "%s: null weights", who);
+    MOEI_REQUIRE(eps > 0.f && eps < INFINITY, "%s: eps must be positive and finite", who);
+    MOEI_REQUIRE((uintptr_t)d_q_weight % 4 == 0 && (uintptr_t)d_k_weight % 4 == 0, "%s: weights are not aligned", who);
+    const long long out = (long long)T * d.n_q_heads * d.k_dim * kv_io_bytes(d.dtype), row = d.k_dim * 4;
+    const long long wq = (weight_per_head ? d.n_q_heads : 1) * row, wk = (weight_per_head ? d.n_kv_heads : 1) * row;
+    MOEI_REQUIRE(!overlap(d_q_weight, 1, wq, wq, d_q_out, out) && !overlap(d_k_weight, 1, wk, wk, d_q_out, out), "%s: d_q_out overlaps the weights", who);
+    a.q_weight = d_q_weight; a.k_weight = d_k_weight;
+    a.per_head = weight_per_head != 0;
+    a.eps = eps;
+    a.turn = d_turn;
+    wide = wide && (uintptr_t)d_q_weight % 16 == 0 && (uintptr_t)d_k_weight % 16 == 0;
+    return launch_kv_append_norm(*kv, a, wide, as_stream(stream));
 }
 
 extern "C" int kv_attend(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, int32_t table_width, const int32_t* d_len,
