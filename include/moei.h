@@ -387,8 +387,13 @@ typedef struct moei_kv_pages {
 int moei_kv_create(const moei_kv_desc* desc, moei_kv** out);
 /* The caller has waited for every call that names it. */
 int moei_kv_destroy(moei_kv* kv);
-/* Error flags raised since the last call (bit 0: a page id outside the pool, bit 1: a length or position outside the page table, or a
- * sequence number outside the batch).  Synchronises `stream`. */
+/* Scratch of kv_attend_weights: calls of up to max_tokens tokens (B * table_width * page_size), 4 * n_q_heads bytes each; 0 gives it back.  Allocates; the
+ * caller has waited for every call that names the handle, and captures the call in no graph.  What there was stays if there is no memory. */
+int moei_kv_set_weights(moei_kv* kv, int64_t max_tokens);
+/* Scratch of kv_attend_shared, (256 rows a compute unit + max_batch * n_q_heads) * (v_dim + 2) * 4 bytes; on = 0 gives it back.  As moei_kv_set_weights. */
+int moei_kv_set_shared(moei_kv* kv, int32_t on);
+/* Error flags raised since the last call (bit 0: a page id outside the pool, bit 1: a length or position outside the page table, a
+ * sequence number outside the batch, or groups of sequences outside it).  Synchronises `stream`. */
 int moei_kv_error_flags(moei_kv* kv, int32_t* h_flags, void* stream);
 
 /* Appends T tokens: d_q[T][n_q_heads][k_dim], d_k[T][n_kv_heads][k_dim], d_v[T][n_kv_heads][v_dim], *_stride elements between tokens (0: dense).
@@ -440,6 +445,38 @@ int kv_attend(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, i
 int kv_attend_blocks(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, int32_t table_width, const int32_t* d_len, int32_t B,
                      const void* d_q, int64_t q_stride, float scale, int32_t n_sel, int32_t keep_first, int32_t keep_last,
                      void* d_out, float* d_lse, int32_t* d_blocks, void* stream);
+
+/* kv_attend for a batch whose sequences share prefixes: each prefix is read once for all queries of its group.  Group g, 0 <= g < n_groups <= 4096, is the
+ * sequences d_start[g] <= b < d_start[g + 1] (d_start[n_groups + 1], d_prefix[n_groups] int32, device).  Of those that have d_prefix[g]
+ * tokens or more, these first tokens are read by way of the table's row of the first such sequence, the others by way of each one's own; the prefix may end inside a page.
+ * A shorter sequence shares nothing and is read by its own row, and so is one that lies in no group.
+ * Starts that do not ascend within [0, B] count as no groups, a prefix outside [0, table_width * page_size] as the nearest one inside; both raise an error
+ * flag.  The rest is as for kv_attend, but for MOEI_ECAPACITY from 2^31 blocks of 16 query heads and 32 tokens on; sums are in another order, and weights of prefixes enter the
+ * products of 16- and 8-bit pages with 17 bits.  Needs moei_kv_set_shared (MOEI_ESTATE). */
+int kv_attend_shared(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, int32_t table_width, const int32_t* d_len, int32_t B,
+                     const int32_t* d_start, const int32_t* d_prefix, int32_t n_groups,
+                     const void* d_q, int64_t q_stride, float scale, void* d_out, float* d_lse, void* stream);
+
+/* kv_attend that adds up what every token was given: for every sequence b, key/value head hk and token j that it attends to,
+ *   d_weights[b][hk][j] += sum over the group's query heads h of exp(scale * q_h.k_j - d_lse[b][h]),
+ * in fp32, the heads in their order.  d_weights: [B][n_kv_heads] rows that lie w_stride elements apart (0: table_width * page_size, which none is shorter than); j counts within the
+ * sequence, and nothing else of a row is touched.  Out and lse have kv_attend's bits.  A token of a page outside the pool is given nothing.
+ * Needs moei_kv_set_weights (MOEI_ECAPACITY).  d_weights overlaps neither d_q, d_out nor d_lse. */
+int kv_attend_weights(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, int32_t table_width, const int32_t* d_len, int32_t B,
+                      const void* d_q, int64_t q_stride, float scale, int32_t window, float* d_weights, int64_t w_stride,
+                      void* d_out, float* d_lse, void* stream);
+
+/* Moves what is kept of every sequence to other pages of the pool: for each key/value head its first keep_first and last keep_last tokens and, of the others, those with the
+ * largest weights (equal ones: the lower token; one that is no number comes last), n_keep in all; a sequence of at most n_keep tokens is moved whole.
+ * Keys, values and weights of the kept tokens go, in their order, to the first places of d_to_table's pages [B][to_width] and of d_to_weights (rows to_w_stride apart, 0: to_width
+ * * page_size; may be NULL); d_to_len[b] = min(length, n_keep); d_kept[B][n_kv_heads][n_keep]: their numbers within the sequence, ascending, -1 behind the last.  Heads keep tokens of their own:
+ * a place is no position any longer, and windows and positions (kv_append_norm's d_turn) are the caller's to keep.  With summaries: d_k_min and d_k_max of
+ * the pages that are full.  Rows behind the last are left as they are, and so are the old pages, which other sequences may share.
+ * No page of d_to_table is one of d_table's, or stands in it twice.  A token whose old or new page lies outside the pool is not moved (its weight is), and raises a flag,
+ * as a length outside the table does, which counts as the nearest one inside.  d_to_len overlaps not d_len, d_to_table not d_table, d_to_weights not d_weights. */
+int kv_evict(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, int32_t table_width, const int32_t* d_len, int32_t B,
+             const float* d_weights, int64_t w_stride, int32_t n_keep, int32_t keep_first, int32_t keep_last,
+             const int32_t* d_to_table, int32_t to_width, int32_t* d_to_len, float* d_to_weights, int64_t to_w_stride, int32_t* d_kept, void* stream);
 
 /* ------------------------------------------------------------------ kernel timing (diagnostic)
  * While enabled, every kernel launch of the library carries a start and a stop HIP event

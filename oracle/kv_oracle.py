@@ -90,3 +90,56 @@ def attend(q, k, v, table, lens, scale, window=0, chosen=None, k_scale=None, v_s
                 out[b, h] = p @ vals / p.sum()
                 lse[b, h] = m + np.log(p.sum())
     return out, lse
+
+
+def attend_shared(q, k, v, table, lens, scale, starts, prefix, k_scale=None, v_scale=None):
+    """attend, where the first prefix[g] tokens of those of sequences starts[g] to starts[g + 1] that have as many lie where the row of the first of these says."""
+    n_pages, Hkv, page, Dv = v.shape
+    (B, Hq, _), G, room = q.shape, q.shape[1] // Hkv, table.shape[1] * page
+    out, lse = np.zeros((B, Hq, Dv)), np.full((B, Hq), -np.inf)
+    for b in range(B):
+        n = min(max(int(lens[b]), 0), room)
+        rows = [(b, j) for j in range(n)]
+        for g in range(len(prefix)):
+            p = min(max(int(prefix[g]), 0), room)
+            if starts[g] <= b < starts[g + 1] and n >= p:
+                first = next(i for i in range(starts[g], b + 1) if int(lens[i]) >= p)
+                rows = [(first if j < p else b, j) for j in range(n)]
+        at = [(int(table[r][j // page]), j % page) for r, j in rows]
+        at = np.array([(i, r) for i, r in at if 0 <= i < n_pages], dtype=np.int64).reshape(-1, 2)
+        if not len(at):
+            continue
+        for hk in range(Hkv):
+            keys = k[at[:, 0], hk, at[:, 1]] * (1.0 if k_scale is None else float(k_scale[hk]))
+            vals = v[at[:, 0], hk, at[:, 1]] * (1.0 if v_scale is None else float(v_scale[hk]))
+            for h in range(hk * G, (hk + 1) * G):
+                z = scale * (keys @ q[b, h])
+                w = np.exp(z - z.max())
+                out[b, h], lse[b, h] = w @ vals / w.sum(), z.max() + np.log(w.sum())
+    return out, lse
+
+
+def attend_weights(q, k, table, lens, lse, scale, window=0, k_scale=None):
+    """What every token is given: [B][Hkv][tokens of the table] sums over a group's heads of exp(scale q.k - lse), 0 where nothing is."""
+    n_pages, Hkv, page, _ = k.shape
+    B, G, room = q.shape[0], q.shape[1] // Hkv, table.shape[1] * page
+    w = np.zeros((B, Hkv, room))
+    for b in range(B):
+        n = min(max(int(lens[b]), 0), room)
+        at = [j for j in span(n, page, window, None, None) if 0 <= table[b][j // page] < n_pages]
+        if not at:
+            continue
+        pg, row = table[b][np.array(at) // page], np.array(at) % page
+        for hk in range(Hkv):
+            keys = k[pg, hk, row] * (1.0 if k_scale is None else float(k_scale[hk]))
+            for h in range(hk * G, (hk + 1) * G):
+                w[b, hk, at] += np.exp(scale * (keys @ q[b, h]) - lse[b, h])
+    return w
+
+
+def keep(w, n, n_keep, first, last):
+    """Which of n tokens are kept, ascending: the first, the last, and of the others those with the largest w (no number: least; ties: the lower)."""
+    if n <= n_keep:
+        return list(range(n))
+    inner = sorted(range(first, n - last), key=lambda j: (0, -float(w[j]), j) if w[j] == w[j] else (1, 0.0, j))
+    return sorted([*range(first), *inner[:n_keep - first - last], *range(n - last, n)])

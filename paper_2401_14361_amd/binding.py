@@ -22,7 +22,7 @@ __all__ = [
     "moe_route_topk", "eam_update", "eamc_match", "eamc_match_topm", "expert_priority", "expert_ffn_gemv",
     "expert_ffn_gemv_static",
     "moe_decode_layer", "moe_prefill_layer", "expert_ffn_grouped", "WDTYPE_FP32", "WDTYPE_BF16", "EXPORTS", "expert_pack", "profile_enable", "profile_disable", "profile_read", "profile_samples",
-    "Kv", "KvDesc", "KvPages", "kv_append", "kv_append_norm", "kv_attend", "kv_attend_blocks", "KVDTYPE_FP8",
+    "Kv", "KvDesc", "KvPages", "kv_append", "kv_append_norm", "kv_attend", "kv_attend_blocks", "kv_attend_shared", "kv_attend_weights", "kv_evict", "KVDTYPE_FP8",
 ]
 
 WDTYPE_FP32, WDTYPE_BF16 = 0, 1
@@ -38,7 +38,8 @@ EXPORTS = [
     "moe_decode_layer", "moei_cache_last_step", "moei_cache_last_heads", "moei_cache_join", "moei_cache_sync",
     "moei_cache_set_match_count", "moei_cache_last_matches",
     "moe_prefill_layer", "moei_cache_set_policy", "moei_cache_prefetch", "moei_cache_set_prefetch", "moei_cache_last_prefetch",
-    "moei_kv_create", "moei_kv_destroy", "moei_kv_error_flags", "kv_append", "kv_append_norm", "kv_attend", "kv_attend_blocks",
+    "moei_kv_create", "moei_kv_destroy", "moei_kv_error_flags", "moei_kv_set_weights", "moei_kv_set_shared",
+    "kv_append", "kv_append_norm", "kv_attend", "kv_attend_blocks", "kv_attend_shared", "kv_attend_weights", "kv_evict",
     "moei_profile_enable", "moei_profile_disable", "moei_profile_kernels", "moei_profile_kernel_name",
     "moei_profile_read", "moei_profile_samples",
 ]
@@ -84,6 +85,11 @@ def lib() -> C.CDLL:
         L.moei_profile_kernel_name.restype = C.c_char_p
         P, i32, i64, f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_float
         L.kv_append.argtypes = [P, P, P, i32, i32, P, P, i32, P, i64, P, i64, P, i64, P, i32, i32, P, P]
+        L.moei_kv_set_weights.argtypes = [P, i64]
+        L.moei_kv_set_shared.argtypes = [P, i32]
+        L.kv_attend_shared.argtypes = [P, P, P, i32, P, i32, P, P, i32, P, i64, f32, P, P, P]
+        L.kv_attend_weights.argtypes = [P, P, P, i32, P, i32, P, i64, f32, i32, P, i64, P, P, P]
+        L.kv_evict.argtypes = [P, P, P, i32, P, i32, P, i64, i32, i32, i32, P, i32, P, P, i64, P, P]
         L.kv_append_norm.argtypes = [P, P, P, i32, i32, P, P, P, i32, P, i64, P, i64, P, i64, P, P, i32, f32, P, i32, i32, P, P]
         L.kv_attend.argtypes = [P, P, P, i32, P, i32, P, i64, f32, i32, P, P, P]
         L.kv_attend_blocks.argtypes = [P, P, P, i32, P, i32, P, i64, f32, i32, i32, i32, P, P, P, P]
@@ -494,13 +500,15 @@ class Kv:
     """Owner of a moei_kv handle: shapes, scratch and error flags of a paged KV cache (the pages are the caller's).
 
     max_sel, the largest n_sel of kv_attend_blocks (None: 256 or max_pages), costs scratch: 12 bytes for each of max_pages pages of each
-    key/value head of each of max_batch sequences, 25 MB for the defaults and eight heads.  0 where pages are never selected: none."""
+    key/value head of each of max_batch sequences, 25 MB for the defaults and eight heads.  0 where pages are never selected: none.
+    shared: there is scratch for kv_attend_shared; max_weight_tokens, tokens (sequences times the table's) of a kv_attend_weights call, costs 4 bytes for each
+    query head of each of them.  set_shared and set_weights change these later."""
 
     DTYPES = {"fp32": WDTYPE_FP32, "bf16": WDTYPE_BF16, "fp8": KVDTYPE_FP8}
     _PAGE = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp8": torch.float8_e4m3fn}
 
     def __init__(self, n_q_heads: int, n_kv_heads: int, k_dim: int, v_dim: int, page_size: int, dtype: str = "bf16",
-                 max_batch: int = 64, max_pages: int = 4096, max_sel: int | None = None):
+                 max_batch: int = 64, max_pages: int = 4096, max_sel: int | None = None, shared: bool = False, max_weight_tokens: int = 0):
         max_sel = min(256, max_pages) if max_sel is None else max_sel
         self.desc = KvDesc(n_q_heads, n_kv_heads, k_dim, v_dim, page_size, self.DTYPES[dtype], max_batch, max_pages, max_sel)
         self.max_batch, self.max_pages = max_batch, max_pages
@@ -515,6 +523,18 @@ class Kv:
         self.heads, self.k_heads, self.v_heads = (n_q_heads, k_dim), (n_kv_heads, k_dim), (n_kv_heads, v_dim)
         self.out_heads = (n_q_heads, v_dim)
         self.layout = (self.k_page, self.v_page, self.page_dtype, self.index)
+        self.max_weight_tokens = 0
+        if shared:
+            self.set_shared(True)
+        if max_weight_tokens:
+            self.set_weights(max_weight_tokens)
+
+    def set_shared(self, on: bool) -> None:
+        _check(lib().moei_kv_set_shared(self.h, on))
+
+    def set_weights(self, max_tokens: int) -> None:
+        _check(lib().moei_kv_set_weights(self.h, max_tokens))
+        self.max_weight_tokens = max_tokens
 
     def error_flags(self, stream=None) -> int:
         f = C.c_int32(0)
@@ -688,6 +708,65 @@ def kv_attend_blocks(kv: Kv, pages: KvPages, table: torch.Tensor, lens: torch.Te
                                   out_at, lse_at, blocks_at, _kv_stream(kv, None)))
     got = (out,) + (() if lse is None else (lse,)) + (() if blocks is None else (blocks,))
     return got if len(got) > 1 else out
+
+
+def kv_attend_shared(kv: Kv, pages: KvPages, table: torch.Tensor, lens: torch.Tensor, starts: torch.Tensor, prefix: torch.Tensor,
+                     q: torch.Tensor, scale: float, out: torch.Tensor | None = None, want_lse: bool = False, stream=None,
+                     lse: torch.Tensor | None = None):
+    """kv_attend of a batch whose sequences starts[g] to starts[g + 1] (starts [groups + 1] int32) share their first prefix[g] tokens, which are
+    read once for all of them.  The handle is made with shared=True."""
+    if stream is not None and (on := _elsewhere(stream, kv.index)) is not None:
+        with torch.cuda.stream(on):
+            return kv_attend_shared(kv, pages, table, lens, starts, prefix, q, scale, out, want_lse, None, lse)
+    B, width, table_at, lens_at, stride, out, out_at, lse, lse_at = _attend_args(kv, pages, table, lens, q, out, want_lse, lse)
+    n = prefix.numel()
+    assert starts.numel() == n + 1, (starts.shape, prefix.shape)
+    _check(lib().kv_attend_shared(kv.h, pages.ref, table_at, width, lens_at, B, _ints(kv, starts), _ints(kv, prefix), n, q.data_ptr(), stride, scale,
+                                  out_at, lse_at, _kv_stream(kv, None)))
+    return out if lse is None else (out, lse)
+
+
+def _weight_rows(kv: Kv, w: torch.Tensor, B: int, tokens: int) -> int:
+    """Checks weights [B][Hkv][tokens or more] fp32, contiguous, and returns the elements between rows."""
+    assert w.dtype is torch.float32 and w.get_device() == kv.index and w.is_contiguous() and w.dim() == 3, (w.device, w.dtype, w.shape)
+    assert w.shape[:2] == (B, kv.k_page[0]) and w.shape[2] >= max(tokens, 1), (w.shape, (B, kv.k_page[0], tokens))
+    return w.shape[2]
+
+
+def kv_attend_weights(kv: Kv, pages: KvPages, table: torch.Tensor, lens: torch.Tensor, q: torch.Tensor, scale: float, weights: torch.Tensor,
+                      window: int = 0, out: torch.Tensor | None = None, want_lse: bool = False, stream=None, lse: torch.Tensor | None = None):
+    """kv_attend that adds to weights [B][Hkv][tokens] fp32 what the heads of each group give to every token of the sequence (a row holds as many
+    tokens as the table, or more).  The handle is made with max_weight_tokens."""
+    if stream is not None and (on := _elsewhere(stream, kv.index)) is not None:
+        with torch.cuda.stream(on):
+            return kv_attend_weights(kv, pages, table, lens, q, scale, weights, window, out, want_lse, None, lse)
+    B, width, table_at, lens_at, stride, out, out_at, lse, lse_at = _attend_args(kv, pages, table, lens, q, out, want_lse, lse)
+    _check(lib().kv_attend_weights(kv.h, pages.ref, table_at, width, lens_at, B, q.data_ptr(), stride, scale, window, weights.data_ptr(),
+                                   _weight_rows(kv, weights, B, width * kv.k_page[1]), out_at, lse_at, _kv_stream(kv, None)))
+    return out if lse is None else (out, lse)
+
+
+def kv_evict(kv: Kv, pages: KvPages, table: torch.Tensor, lens: torch.Tensor, weights: torch.Tensor, n_keep: int, to_table: torch.Tensor,
+             to_weights: torch.Tensor | None = None, keep_first: int = 0, keep_last: int = 1, to_lens: torch.Tensor | None = None,
+             kept: torch.Tensor | None = None, stream=None):
+    """Moves n_keep tokens of each sequence and key/value head - the first, the last and those with the largest weights [B][Hkv][tokens] - to the
+    pages of to_table [B][pages], and their weights to to_weights -> (to_lens [B], kept [B][Hkv][n_keep] int32, -1 behind the last)."""
+    if stream is not None and (on := _elsewhere(stream, kv.index)) is not None:
+        with torch.cuda.stream(on):
+            return kv_evict(kv, pages, table, lens, weights, n_keep, to_table, to_weights, keep_first, keep_last, to_lens, kept, None)
+    assert pages.layout == kv.layout, (pages.layout, kv.layout)
+    B, width = table.shape
+    assert lens.numel() == B and to_table.dim() == 2 and to_table.shape[0] == B, (lens.shape, to_table.shape)
+    row, to_row = _weight_rows(kv, weights, B, width * kv.k_page[1]), 0 if to_weights is None else _weight_rows(kv, to_weights, B, n_keep)
+    if to_lens is None:
+        to_lens = torch.empty((B,), dtype=torch.int32, device=kv.device)
+    if kept is None:
+        kept = torch.empty((B, kv.k_page[0], max(n_keep, 0)), dtype=torch.int32, device=kv.device)
+    _check(lib().kv_evict(kv.h, pages.ref, _ints(kv, table), width, _ints(kv, lens), B, weights.data_ptr(), row, n_keep, keep_first, keep_last,
+                          _ints(kv, to_table), to_table.shape[1], _given(kv, to_lens, B, (1, 1), torch.int32),
+                          None if to_weights is None else to_weights.data_ptr(), to_row, _given(kv, kept, B, (kv.k_page[0], n_keep), torch.int32),
+                          _kv_stream(kv, None)))
+    return to_lens, kept
 
 
 # -------------------------------------------------------------------- kernel timing

@@ -1,6 +1,7 @@
 // The paged KV cache of a decode step: its handle, appending tokens, and the entry points.
 #include <math.h>
 
+#include <initializer_list>
 #include <new>
 
 #include "kv_append.hpp"
@@ -309,7 +310,8 @@ extern "C" int moei_kv_destroy(moei_kv* kv) {
     if (!kv) return MOEI_OK;
     int dev = -1;
     const bool other = hipGetDevice(&dev) == hipSuccess && dev != kv->device && hipSetDevice(kv->device) == hipSuccess;
-    for (void* p : {(void*)kv->d_part, (void*)kv->d_stat, (void*)kv->d_arrived, (void*)kv->d_keys, (void*)kv->d_scores, (void*)kv->d_scored, (void*)kv->d_list, (void*)kv->d_flags})
+    for (void* p : {(void*)kv->d_part, (void*)kv->d_stat, (void*)kv->d_arrived, (void*)kv->d_keys, (void*)kv->d_scores, (void*)kv->d_scored, (void*)kv->d_list, (void*)kv->d_flags,
+                    (void*)kv->d_logits, (void*)kv->d_tops, (void*)kv->d_told, (void*)kv->d_pre_part, (void*)kv->d_pre_stat})
         if (p) (void)hipFree(p);
     if (other) (void)hipSetDevice(dev);
     delete kv;
@@ -354,6 +356,59 @@ extern "C" int moei_kv_create(const moei_kv_desc* desc, moei_kv** out) {
     }
     *out = kv;
     return MOEI_OK;
+}
+
+namespace {
+
+// Memory of a handle on its device, whichever is the current one: what is there goes when the new is there.
+struct Room {
+    void** at;
+    size_t bytes;
+};
+int exchange(const char* who, const moei_kv* kv, std::initializer_list<Room> rooms) {
+    int dev = -1;
+    MOEI_HIP(hipGetDevice(&dev));
+    if (dev != kv->device) MOEI_FAIL(MOEI_ESTATE, "%s: the handle belongs to device %d, the current one is %d", who, kv->device, dev);
+    void* got[4] = {};
+    hipError_t e = hipSuccess;
+    int n = 0;
+    for (const Room& r : rooms) {
+        if (r.bytes && (e = hipMalloc(&got[n], r.bytes)) != hipSuccess) break;
+        ++n;
+    }
+    if (e != hipSuccess) {
+        (void)hipGetLastError();
+        for (void* p : got)
+            if (p) (void)hipFree(p);
+        MOEI_FAIL(e == hipErrorOutOfMemory ? MOEI_ENOMEM : MOEI_EHIP, "%s: %s", who, hipGetErrorString(e));
+    }
+    n = 0;
+    for (const Room& r : rooms) {
+        if (*r.at) (void)hipFree(*r.at);
+        *r.at = got[n++];
+    }
+    return MOEI_OK;
+}
+
+}  // namespace
+
+extern "C" int moei_kv_set_weights(moei_kv* kv, int64_t max_tokens) {
+    const char* who = "moei_kv_set_weights";
+    MOEI_REQUIRE(kv, "%s: null pointer", who);
+    MOEI_REQUIRE(max_tokens >= 0 && max_tokens <= (1ll << 40), "%s: max_tokens = %lld outside [0, 2^40]", who, (long long)max_tokens);
+    const size_t heads = kv->d.n_q_heads, tokens = ((size_t)max_tokens + 15) / 16 * 16;
+    const int rc = exchange(who, kv, {{reinterpret_cast<void**>(&kv->d_logits), tokens * heads * 4}, {reinterpret_cast<void**>(&kv->d_tops), max_tokens ? (size_t)kv->d.max_batch * heads * 8 : 0}});
+    if (rc == MOEI_OK) kv->weight_tokens = max_tokens;
+    return rc;
+}
+
+extern "C" int moei_kv_set_shared(moei_kv* kv, int32_t on) {
+    const char* who = "moei_kv_set_shared";
+    MOEI_REQUIRE(kv, "%s: null pointer", who);
+    // Parts of prefixes are no longer than the workgroups' shares, but for one of each row: see kv_shared.hip.
+    const size_t rows = on ? (size_t)kKvSharedBlock * kKvSharedResident * kv->cus + (size_t)kv->d.max_batch * kv->d.n_q_heads : 0;
+    return exchange(who, kv, {{reinterpret_cast<void**>(&kv->d_told), on ? kv->d.max_batch * sizeof(KvShared) : 0}, {reinterpret_cast<void**>(&kv->d_pre_part), rows * kv->d.v_dim * 4},
+                              {reinterpret_cast<void**>(&kv->d_pre_stat), rows * 8}});
 }
 
 extern "C" int moei_kv_error_flags(moei_kv* kv, int32_t* h_flags, void* stream) {
@@ -472,4 +527,105 @@ extern "C" int kv_attend_blocks(moei_kv* kv, const moei_kv_pages* pages, const i
     a.list = c.list;
     a.n_sel = n_sel;
     return launch_kv_attend(*kv, a, as_stream(stream));
+}
+
+extern "C" int kv_attend_weights(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, int32_t table_width, const int32_t* d_len,
+                                 int32_t B, const void* d_q, int64_t q_stride, float scale, int32_t window, float* d_weights, int64_t w_stride,
+                                 void* d_out, float* d_lse, void* stream) {
+    const char* who = "kv_attend_weights";
+    MOEI_REQUIRE(B >= 0, "%s: B = %d is negative", who, B);
+    if (B == 0) return MOEI_OK;
+    int rc = check_call(who, kv, pages, d_table, table_width);
+    if (rc) return rc;
+    const moei_kv_desc& d = kv->d;
+    MOEI_REQUIRE(B <= d.max_batch, "%s: B = %d exceeds max_batch = %d", who, B, d.max_batch);
+    MOEI_REQUIRE(window >= 0, "%s: window = %d is negative", who, window);
+    const long long room = (long long)table_width * d.page_size, w_row = w_stride ? w_stride : room;
+    MOEI_REQUIRE(d_weights, "%s: null pointer", who);
+    MOEI_REQUIRE((uintptr_t)d_weights % 4 == 0 && w_row >= room, "%s: w_stride = %lld is shorter than the table's %lld tokens, or d_weights not aligned", who, (long long)w_stride, room);
+    KvWeightsArgs w{};
+    rc = fill_attend(who, kv, pages, d_table, table_width, d_len, B, d_q, q_stride, scale, d_out, d_lse, &w.a);
+    if (rc) return rc;
+    const int io = kv_io_bytes(d.dtype);
+    const long long rows = (long long)B * d.n_kv_heads, bytes = ((rows - 1) * w_row + room) * 4;
+    MOEI_REQUIRE(!overlap(d_weights, 1, bytes, bytes, d_out, (long long)B * d.n_q_heads * d.v_dim * io) &&
+                     !overlap(d_q, B, w.a.q_stride * io, (long long)d.n_q_heads * d.k_dim * io, d_weights, bytes) &&
+                     !(d_lse && overlap(d_weights, 1, bytes, bytes, d_lse, (long long)B * d.n_q_heads * 4)),
+                 "%s: d_weights overlaps d_q, d_out or d_lse", who);
+    if (B * room > kv->weight_tokens)
+        MOEI_FAIL(MOEI_ECAPACITY, "%s: %d sequences of up to %lld tokens are more than the %lld of moei_kv_set_weights", who, B, room, kv->weight_tokens);
+    w.a.window = window;
+    w.a.logits = kv->d_logits;
+    w.a.tops = kv->d_tops;
+    w.weights = d_weights;
+    w.w_row = w_row;
+    w.wide = (uintptr_t)d_weights % 16 == 0 && w_row % 4 == 0;
+    return launch_kv_attend_weights(*kv, w, as_stream(stream));
+}
+
+extern "C" int kv_attend_shared(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, int32_t table_width, const int32_t* d_len,
+                                int32_t B, const int32_t* d_start, const int32_t* d_prefix, int32_t n_groups, const void* d_q, int64_t q_stride,
+                                float scale, void* d_out, float* d_lse, void* stream) {
+    const char* who = "kv_attend_shared";
+    MOEI_REQUIRE(B >= 0, "%s: B = %d is negative", who, B);
+    if (B == 0) return MOEI_OK;
+    int rc = check_call(who, kv, pages, d_table, table_width);
+    if (rc) return rc;
+    MOEI_REQUIRE(B <= kv->d.max_batch, "%s: B = %d exceeds max_batch = %d", who, B, kv->d.max_batch);
+    MOEI_REQUIRE(n_groups >= 0 && n_groups <= kKvMaxBatch, "%s: n_groups = %d outside [0, %d]", who, n_groups, kKvMaxBatch);
+    MOEI_REQUIRE(n_groups == 0 || (d_start && d_prefix), "%s: null pointer", who);
+    if (!kv->d_told) MOEI_FAIL(MOEI_ESTATE, "%s: moei_kv_set_shared has not been called", who);
+    KvSharedArgs a{};
+    rc = fill_attend(who, kv, pages, d_table, table_width, d_len, B, d_q, q_stride, scale, d_out, d_lse, &a.a);
+    if (rc) return rc;
+    if (n_groups == 0) return launch_kv_attend(*kv, a.a, as_stream(stream));
+    const long long stages = (long long)table_width * kv->d.page_size / 32 + 1, blocks = (long long)B * a.a.group / 16 + n_groups;
+    if (stages * blocks * a.a.n_kv > 0x7fffffffll)
+        MOEI_FAIL(MOEI_ECAPACITY, "%s: %d sequences of up to %lld tokens are more than one call takes", who, B, (long long)table_width * kv->d.page_size);
+    a.starts = d_start;
+    a.prefix = d_prefix;
+    a.n_groups = n_groups;
+    a.told = kv->d_told;
+    a.part = kv->d_pre_part;
+    a.stat = kv->d_pre_stat;
+    return launch_kv_attend_shared(*kv, a, as_stream(stream));
+}
+
+extern "C" int kv_evict(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, int32_t table_width, const int32_t* d_len, int32_t B,
+                        const float* d_weights, int64_t w_stride, int32_t n_keep, int32_t keep_first, int32_t keep_last,
+                        const int32_t* d_to_table, int32_t to_width, int32_t* d_to_len, float* d_to_weights, int64_t to_w_stride, int32_t* d_kept, void* stream) {
+    const char* who = "kv_evict";
+    MOEI_REQUIRE(B >= 0, "%s: B = %d is negative", who, B);
+    if (B == 0) return MOEI_OK;
+    const int rc = check_call(who, kv, pages, d_table, table_width);
+    if (rc) return rc;
+    const moei_kv_desc& d = kv->d;
+    MOEI_REQUIRE(B <= d.max_batch, "%s: B = %d exceeds max_batch = %d", who, B, d.max_batch);
+    MOEI_REQUIRE(n_keep >= 1 && keep_first >= 0 && keep_last >= 0 && (long long)keep_first + keep_last <= n_keep,
+                 "%s: keep_first = %d and keep_last = %d must fit n_keep = %d", who, keep_first, keep_last, n_keep);
+    MOEI_REQUIRE(d_len && d_weights && d_to_table && d_to_len && d_kept, "%s: null pointer", who);
+    MOEI_REQUIRE(to_width >= 1 && to_width <= d.max_pages && (long long)to_width * d.page_size >= n_keep, "%s: a table of %d pages does not hold n_keep = %d tokens, or is wider than max_pages = %d",
+                 who, to_width, n_keep, d.max_pages);
+    const long long room = (long long)table_width * d.page_size, w_row = w_stride ? w_stride : room;
+    const long long to_room = (long long)to_width * d.page_size, to_w_row = to_w_stride ? to_w_stride : to_room;
+    MOEI_REQUIRE((uintptr_t)d_weights % 4 == 0 && (uintptr_t)d_to_weights % 4 == 0 && w_row >= room && to_w_row >= n_keep,
+                 "%s: w_stride = %lld or to_w_stride = %lld is shorter than a row, or weights are not aligned", who, (long long)w_stride, (long long)to_w_stride);
+    const long long rows = (long long)B * d.n_kv_heads, from = ((rows - 1) * w_row + room) * 4, to = ((rows - 1) * to_w_row + n_keep) * 4;
+    MOEI_REQUIRE(!overlap(d_len, 1, B * 4ll, B * 4ll, d_to_len, B * 4ll), "%s: d_to_len overlaps d_len", who);  // (other workgroups read it still)
+    MOEI_REQUIRE(!d_to_weights || !overlap(d_weights, 1, from, from, d_to_weights, to), "%s: d_to_weights overlaps d_weights", who);
+    MOEI_REQUIRE(!overlap(d_table, 1, (long long)B * table_width * 4, (long long)B * table_width * 4, d_to_table, (long long)B * to_width * 4), "%s: d_to_table overlaps d_table", who);
+    KvEvictArgs a{};
+    a.append.k_pages = pages->d_k; a.append.v_pages = pages->d_v;
+    strides_of(kv, pages, &a.append.k_stride, &a.append.v_stride);
+    a.append.k_min = pages->d_k_min; a.append.k_max = pages->d_k_max;
+    a.append.k_dim = d.k_dim; a.append.v_dim = d.v_dim; a.append.n_kv = d.n_kv_heads;
+    a.append.page_shift = a.page_shift = log2_of(d.page_size);
+    a.table = d_table; a.to_table = d_to_table; a.lens = d_len;
+    a.to_lens = d_to_len; a.kept = d_kept;
+    a.weights = d_weights; a.to_weights = d_to_weights;
+    a.w_row = w_row; a.to_w_row = to_w_row;
+    a.B = B; a.n_kv = d.n_kv_heads; a.width = table_width; a.to_width = to_width; a.n_pages = pages->n_pages;
+    a.keep = n_keep; a.first = keep_first; a.last = keep_last;
+    a.flags = kv->d_flags;
+    return launch_kv_evict(*kv, a, as_stream(stream));
 }

@@ -18,6 +18,12 @@ constexpr int kKvBadPage = 1, kKvBadLength = 2;
 inline int kv_page_bytes(int dtype) { return dtype == MOEI_WDTYPE_FP32 ? 4 : dtype == MOEI_WDTYPE_BF16 ? 2 : 1; }
 inline int kv_io_bytes(int dtype) { return dtype == MOEI_WDTYPE_FP32 ? 4 : 2; }
 
+// What a sequence shares with others of its group: `prefix` tokens, whose `parts` partial sums lie in rows row + (part * n_kv + head) * rows + h.
+struct KvShared {
+    int prefix, parts;
+    unsigned rows, row;
+};
+
 // What kv_attend and kv_attend_blocks hand to the attention's kernels.
 struct KvAttendArgs {
     const void* q;       // [B][q_stride], Hq heads of k_dim
@@ -41,7 +47,32 @@ struct KvAttendArgs {
     float* stat;             // [workgroups][2][rows][2] their maximum and sum
     unsigned* arrived;       // [workgroups] parts that are there, of the item that begins in a workgroup's stretch; zero between launches
     int32_t* flags;
+    float* logits;           // sums of weights: [B][n_kv][width * page / 16][group][16], unscaled ...
+    float2* tops;            // ... and [B][Hq] maximum (of what exp2 takes) and reciprocal of the sum
+    const KvShared* shared;  // behind shared prefixes: [B] ...
+    const float* pre_part;   // ... and [rows][v_dim] sums of the prefixes' parts
+    const float* pre_stat;   // [rows][2] their maximum and sum
 };
+
+// Sums of weights: what the attention is given, and where they are added up.
+struct KvWeightsArgs {
+    KvAttendArgs a;
+    float* weights;    // [B][n_kv][w_row]
+    long long w_row;
+    int wide;          // four at a time
+};
+
+// The prefixes that groups of sequences share.
+struct KvSharedArgs {
+    KvAttendArgs a;
+    const int32_t *starts, *prefix;  // [n_groups + 1] first sequences, [n_groups] tokens
+    int n_groups;
+    KvShared* told;                  // [B] out
+    float *part, *stat;              // out, KvAttendArgs::pre_part and pre_stat
+};
+
+constexpr int kKvSharedBlock = 128;  // rows of a workgroup of the prefixes' launch, at most ...
+constexpr int kKvSharedResident = 2;  // ... and workgroups of a compute unit
 
 // Chooses the pages: keys of all pages of every (sequence, key/value head), then the list.
 struct KvBlocksArgs {
@@ -75,12 +106,20 @@ struct moei_kv {
     unsigned* d_scored = nullptr;  // [2][max_batch][n_kv_heads]
     int32_t* d_list = nullptr;
     int32_t* d_flags = nullptr;
+    long long weight_tokens = 0;     // moei_kv_set_weights
+    float* d_logits = nullptr;       // [weight_tokens][n_q_heads]
+    float2* d_tops = nullptr;        // [max_batch][n_q_heads]
+    moei::KvShared* d_told = nullptr;  // [max_batch], moei_kv_set_shared
+    float* d_pre_part = nullptr;     // [rows][v_dim]
+    float* d_pre_stat = nullptr;     // [rows][2]
 };
 
 namespace moei {
 
 int launch_kv_attend(const moei_kv& kv, const KvAttendArgs& a, hipStream_t s);
 int launch_kv_blocks(const moei_kv& kv, KvBlocksArgs a, hipStream_t s);
+int launch_kv_attend_weights(const moei_kv& kv, KvWeightsArgs a, hipStream_t s);
+int launch_kv_attend_shared(const moei_kv& kv, KvSharedArgs a, hipStream_t s);
 
 #if defined(__HIPCC__)
 

@@ -32,6 +32,20 @@ struct KvAppendArgs {
     const int32_t* turn;  // positions that queries and keys are turned by; null: pos
 };
 
+// What is kept of sequences, and where it goes.
+struct KvEvictArgs {
+    KvAppendArgs append;  // the pages and their summaries
+    const int32_t *table, *to_table, *lens;
+    int32_t *to_lens, *kept;  // [B], [B][n_kv][keep]
+    const float* weights;     // [B][n_kv][w_row]
+    float* to_weights;        // [B][n_kv][to_w_row] or null
+    long long w_row, to_w_row;
+    int B, n_kv, width, to_width, page_shift, n_pages, keep, first, last;
+    int rows;  // of a workgroup that moves
+    int32_t* flags;
+};
+
+int launch_kv_evict(const moei_kv& kv, KvEvictArgs a, hipStream_t s);
 int launch_kv_append_norm(const moei_kv& kv, const KvAppendArgs& a, bool wide, hipStream_t s);
 int launch_kv_summary(int dtype, const KvAppendArgs& a, hipStream_t s);
 

@@ -1,0 +1,88 @@
+// Attention of one new token per sequence that adds up what each cached token was given:
+//   weights[b][hk][j] += sum over the heads h of the group of exp(scale q_h.k_j - lse_h).
+//
+// A token's weight is known when its sequence's maximum and sum are, behind the last key.  The attention leaves its logits (4 bytes a query head and token,
+// beside (k_dim + v_dim) elements a key/value head), and a second launch turns them into weights: keys are read once.
+#include "kv_attend.hpp"
+
+namespace moei {
+
+namespace {
+
+template <typename T, int KC, int VC, int NS, int NW>
+__global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kResident * NW / 4)) kv_attend_weigh_kernel(KvAttendArgs) {
+    extern __shared__ __align__(16) unsigned char smem[];
+    attend<T, KC, VC, NS, NW, kWeigh>(smem);
+}
+
+struct Weigh {
+    template <typename T, int KC, int VC, int NS, int NW>
+    static constexpr auto kernel = kv_attend_weigh_kernel<T, KC, VC, NS, NW>;
+};
+
+constexpr int kSumThreads = 256, kSumUnit = 4 * kSumThreads;  // tokens: a thread takes four
+
+// The logits of all sequences are one line of units, of which every workgroup takes an equal stretch, as in the attention.  A thread's sums go over the
+// heads of the group in their order: the same bits every run.
+__global__ void __launch_bounds__(kSumThreads) kv_weights_kernel(KvWeightsArgs) {
+    const auto* z = (const __attribute__((address_space(4))) KvWeightsArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+    const Args a = &z->a;
+    const int tid = threadIdx.x, group = a->group, n_kv = a->n_kv;
+    const Stretch mine = my_stretch<kSumUnit, kPlain>(a, tid & (kWave - 1));
+    if (mine.b < 0) return;
+    const long long tiles = (long long)a->width << (a->page_shift - 4);
+    int b = mine.b;
+    unsigned base = mine.base, at = mine.first;
+    while (at < mine.end) {
+        const Span sp = span_of<kPlain>(a, b == mine.b ? mine.len : ((kv_const_ints)(uintptr_t)a->lens)[b], b);
+        const unsigned units = units_of<kSumUnit>(sp), room = (units + mine.step - 1) / mine.step * mine.step;
+        const unsigned hk = (at - base) / room, u = at - base - hk * room;
+        const int j = sp.start + (int)u * kSumUnit + 4 * tid;
+        if (u < units && j < sp.end && j + 4 > sp.begin) {
+            const long long row = (long long)b * n_kv + hk;
+            const f32x4* logits = reinterpret_cast<const f32x4*>(a->logits + ((row * tiles + (j >> 4)) * group) * kRows + (j & 15));
+            const auto* tops = (const __attribute__((address_space(4))) float2*)(uintptr_t)(a->tops + row * group);
+            const float scale2 = a->k_scale ? a->scale2 * ((const __attribute__((address_space(4))) float*)(uintptr_t)a->k_scale)[hk] : a->scale2;
+            float* to = z->weights + row * z->w_row + j;
+            const bool whole = z->wide && j >= sp.begin && j + 4 <= sp.end;
+            f32x4 sum{0.f, 0.f, 0.f, 0.f}, had{0.f, 0.f, 0.f, 0.f};
+            if (whole) had = *reinterpret_cast<const f32x4*>(to);
+#pragma unroll 4
+            for (int h = 0; h < group; ++h) {
+                const f32x4 s = logits[h * (kRows / 4)];
+                const float top = tops[h].x, by = tops[h].y;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) sum[r] += __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], scale2, -top)) * by;
+            }
+            if (whole) {
+                *reinterpret_cast<f32x4*>(to) = had + sum;
+            } else {
+                for (int r = 0; r < 4; ++r)
+                    if (j + r >= sp.begin && j + r < sp.end) to[r] += sum[r];
+            }
+        }
+        if (u + 1 < units) {
+            ++at;
+        } else {
+            at = base + (hk + 1) * room;
+            if ((int)hk + 1 == n_kv) {
+                base = at;
+                ++b;
+            }
+        }
+    }
+}
+
+}  // namespace
+
+int launch_kv_attend_weights(const moei_kv& kv, KvWeightsArgs w, hipStream_t s) {
+    const int rc = launch_attend<Weigh>(kv, w.a, s);
+    if (rc) return rc;
+    w.a.blocks_of_heads = 1;
+    const long long line = (((long long)w.a.width << w.a.page_shift) / kSumUnit + 1) * w.a.B * w.a.n_kv, grid = 8 * kv.cus;
+    launch(K_KV_WEIGHTS, kv_weights_kernel, dim3((unsigned)(line < grid ? line : grid)), dim3(kSumThreads), 0, s, w);
+    MOEI_LAUNCH_CHECK();
+    return MOEI_OK;
+}
+
+}  // namespace moei
