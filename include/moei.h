@@ -390,7 +390,7 @@ int moei_kv_destroy(moei_kv* kv);
 /* Scratch of kv_attend_weights: calls of up to max_tokens tokens (B * table_width * page_size), 4 * n_q_heads bytes each; 0 gives it back.  Allocates; the
  * caller has waited for every call that names the handle, and captures the call in no graph.  What there was stays if there is no memory. */
 int moei_kv_set_weights(moei_kv* kv, int64_t max_tokens);
-/* Scratch of kv_attend_shared, (256 rows a compute unit + max_batch * n_q_heads) * (v_dim + 2) * 4 bytes; on = 0 gives it back.  As moei_kv_set_weights. */
+/* Scratch of kv_attend_shared, (256 rows a compute unit + 2 * max_batch * n_q_heads) * (v_dim + 2) * 4 bytes; on = 0 gives it back.  As moei_kv_set_weights. */
 int moei_kv_set_shared(moei_kv* kv, int32_t on);
 /* Error flags raised since the last call (bit 0: a page id outside the pool, bit 1: a length or position outside the page table, a
  * sequence number outside the batch, or groups of sequences outside it).  Synchronises `stream`. */
@@ -467,7 +467,7 @@ int kv_attend_weights(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_
                       void* d_out, float* d_lse, void* stream);
 
 /* Moves what is kept of every sequence to other pages of the pool: for each key/value head its first keep_first and last keep_last tokens and, of the others, those with the
- * largest weights (equal ones: the lower token; one that is no number comes last), n_keep in all; a sequence of at most n_keep tokens is moved whole.
+ * largest weights (equal ones: the lower token; one that is no number counts as minus infinity), n_keep in all; a sequence of at most n_keep tokens is moved whole.
  * Keys, values and weights of the kept tokens go, in their order, to the first places of d_to_table's pages [B][to_width] and of d_to_weights (rows to_w_stride apart, 0: to_width
  * * page_size; may be NULL); d_to_len[b] = min(length, n_keep); d_kept[B][n_kv_heads][n_keep]: their numbers within the sequence, ascending, -1 behind the last.  Heads keep tokens of their own:
  * a place is no position any longer, and windows and positions (kv_append_norm's d_turn) are the caller's to keep.  With summaries: d_k_min and d_k_max of

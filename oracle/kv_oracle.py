@@ -138,8 +138,8 @@ def attend_weights(q, k, table, lens, lse, scale, window=0, k_scale=None):
 
 
 def keep(w, n, n_keep, first, last):
-    """Which of n tokens are kept, ascending: the first, the last, and of the others those with the largest w (no number: least; ties: the lower)."""
+    """Which of n tokens are kept, ascending: the first, the last, and of the others those with the largest w (no number: -inf; ties: the lower)."""
     if n <= n_keep:
         return list(range(n))
-    inner = sorted(range(first, n - last), key=lambda j: (0, -float(w[j]), j) if w[j] == w[j] else (1, 0.0, j))
+    inner = sorted(range(first, n - last), key=lambda j: (-float(w[j]) if w[j] == w[j] else np.inf, j))
     return sorted([*range(first), *inner[:n_keep - first - last], *range(n - last, n)])

@@ -65,6 +65,7 @@ enum KernelId {
     K_KV_BLOCKS,
     K_KV_APPEND_NORM,
     K_KV_SHARED,
+    K_KV_JOIN,
     K_KV_WEIGHTS,
     K_KV_EVICT,
     K_KV_MOVE,

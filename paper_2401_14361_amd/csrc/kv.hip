@@ -311,7 +311,7 @@ extern "C" int moei_kv_destroy(moei_kv* kv) {
     int dev = -1;
     const bool other = hipGetDevice(&dev) == hipSuccess && dev != kv->device && hipSetDevice(kv->device) == hipSuccess;
     for (void* p : {(void*)kv->d_part, (void*)kv->d_stat, (void*)kv->d_arrived, (void*)kv->d_keys, (void*)kv->d_scores, (void*)kv->d_scored, (void*)kv->d_list, (void*)kv->d_flags,
-                    (void*)kv->d_logits, (void*)kv->d_tops, (void*)kv->d_told, (void*)kv->d_pre_part, (void*)kv->d_pre_stat})
+                    (void*)kv->d_evict, (void*)kv->d_logits, (void*)kv->d_tops, (void*)kv->d_told, (void*)kv->d_pre_part, (void*)kv->d_pre_stat})
         if (p) (void)hipFree(p);
     if (other) (void)hipSetDevice(dev);
     delete kv;
@@ -346,7 +346,8 @@ extern "C" int moei_kv_create(const moei_kv_desc* desc, moei_kv** out) {
     const size_t groups = (size_t)kKvResident * kv->cus, rows = 2 * groups * kv->rows, sel = d.max_sel ? (size_t)d.max_batch * d.n_kv_heads : 0;
     auto room = [&](auto*& p, size_t n) { return n == 0 || (e = hipMalloc(reinterpret_cast<void**>(&p), n * sizeof(*p))) == hipSuccess; };
     if (!room(kv->d_part, rows * d.v_dim) || !room(kv->d_stat, rows * 2) || !room(kv->d_arrived, groups) || !room(kv->d_keys, sel * d.max_pages) || !room(kv->d_scores, sel * d.max_pages) || !room(kv->d_scored, 2 * sel) ||
-        !room(kv->d_list, sel * d.max_sel) || !room(kv->d_flags, 1) || (e = hipMemset(kv->d_flags, 0, 4)) != hipSuccess ||
+        !room(kv->d_list, sel * d.max_sel) || !room(kv->d_flags, 1) || !room(kv->d_evict, kKvEvictWords) || (e = hipMemset(kv->d_flags, 0, 4)) != hipSuccess ||
+        (e = hipMemset(kv->d_evict, 0, kKvEvictWords * sizeof(unsigned))) != hipSuccess ||
         (e = hipMemset(kv->d_arrived, 0, groups * sizeof(unsigned))) != hipSuccess ||
         (sel && (e = hipMemset(kv->d_scored, 0, 2 * sel * sizeof(unsigned))) != hipSuccess) ||
         (e = hipDeviceSynchronize()) != hipSuccess) {
@@ -405,8 +406,8 @@ extern "C" int moei_kv_set_weights(moei_kv* kv, int64_t max_tokens) {
 extern "C" int moei_kv_set_shared(moei_kv* kv, int32_t on) {
     const char* who = "moei_kv_set_shared";
     MOEI_REQUIRE(kv, "%s: null pointer", who);
-    // Parts of prefixes are no longer than the workgroups' shares, but for one of each row: see kv_shared.hip.
-    const size_t rows = on ? (size_t)kKvSharedBlock * kKvSharedResident * kv->cus + (size_t)kv->d.max_batch * kv->d.n_q_heads : 0;
+    // Rows of parts: of every sequence's own tokens, and of prefixes, whose parts are the workgroups' shares, or for each row one that is shorter.
+    const size_t rows = on ? (size_t)kKvSharedBlock * kKvSharedResident * kv->cus + 2 * (size_t)kv->d.max_batch * kv->d.n_q_heads : 0;
     return exchange(who, kv, {{reinterpret_cast<void**>(&kv->d_told), on ? kv->d.max_batch * sizeof(KvShared) : 0}, {reinterpret_cast<void**>(&kv->d_pre_part), rows * kv->d.v_dim * 4},
                               {reinterpret_cast<void**>(&kv->d_pre_stat), rows * 8}});
 }
@@ -586,8 +587,8 @@ extern "C" int kv_attend_shared(moei_kv* kv, const moei_kv_pages* pages, const i
     a.prefix = d_prefix;
     a.n_groups = n_groups;
     a.told = kv->d_told;
-    a.part = kv->d_pre_part;
-    a.stat = kv->d_pre_stat;
+    a.a.pre_part = kv->d_pre_part;
+    a.a.pre_stat = kv->d_pre_stat;
     return launch_kv_attend_shared(*kv, a, as_stream(stream));
 }
 

@@ -18,9 +18,9 @@ constexpr int kKvBadPage = 1, kKvBadLength = 2;
 inline int kv_page_bytes(int dtype) { return dtype == MOEI_WDTYPE_FP32 ? 4 : dtype == MOEI_WDTYPE_BF16 ? 2 : 1; }
 inline int kv_io_bytes(int dtype) { return dtype == MOEI_WDTYPE_FP32 ? 4 : 2; }
 
-// What a sequence shares with others of its group: `prefix` tokens, whose `parts` partial sums lie in rows row + (part * n_kv + head) * rows + h.
+// What a sequence shares with others of its group: the sums of `parts` parts of a prefix lie in rows row + (part * n_kv + head) * rows + h.
 struct KvShared {
-    int prefix, parts;
+    int parts;
     unsigned rows, row;
 };
 
@@ -49,9 +49,8 @@ struct KvAttendArgs {
     int32_t* flags;
     float* logits;           // sums of weights: [B][n_kv][width * page / 16][group][16], unscaled ...
     float2* tops;            // ... and [B][Hq] maximum (of what exp2 takes) and reciprocal of the sum
-    const KvShared* shared;  // behind shared prefixes: [B] ...
-    const float* pre_part;   // ... and [rows][v_dim] sums of the prefixes' parts
-    const float* pre_stat;   // [rows][2] their maximum and sum
+    float* pre_part;         // behind shared prefixes: [B][Hq][v_dim] sums of what is a sequence's own, not yet divided, then those of the prefixes' parts ...
+    float* pre_stat;         // ... and [..][2] their maximum and sum
 };
 
 // Sums of weights: what the attention is given, and where they are added up.
@@ -64,12 +63,15 @@ struct KvWeightsArgs {
 
 // The prefixes that groups of sequences share.
 struct KvSharedArgs {
-    KvAttendArgs a;
+    KvAttendArgs a;                  // (first: what attends to the sequences' own tokens is given these)
     const int32_t *starts, *prefix;  // [n_groups + 1] first sequences, [n_groups] tokens
     int n_groups;
     KvShared* told;                  // [B] out
-    float *part, *stat;              // out, KvAttendArgs::pre_part and pre_stat
 };
+
+constexpr int kKvSplitItems = 128;  // sequences and key/value heads whose tokens several workgroups choose from ...
+constexpr int kKvSplitParts = 256;  // ... and workgroups of one, at most
+constexpr size_t kKvEvictWords = (size_t)kKvSplitItems * (3 * 2048 + 2 * kKvSplitParts);
 
 constexpr int kKvSharedBlock = 128;  // rows of a workgroup of the prefixes' launch, at most ...
 constexpr int kKvSharedResident = 2;  // ... and workgroups of a compute unit
@@ -106,15 +108,19 @@ struct moei_kv {
     unsigned* d_scored = nullptr;  // [2][max_batch][n_kv_heads]
     int32_t* d_list = nullptr;
     int32_t* d_flags = nullptr;
+    unsigned* d_evict = nullptr;     // [kKvEvictWords]
     long long weight_tokens = 0;     // moei_kv_set_weights
     float* d_logits = nullptr;       // [weight_tokens][n_q_heads]
     float2* d_tops = nullptr;        // [max_batch][n_q_heads]
     moei::KvShared* d_told = nullptr;  // [max_batch], moei_kv_set_shared
-    float* d_pre_part = nullptr;     // [rows][v_dim]
-    float* d_pre_stat = nullptr;     // [rows][2]
+    float* d_pre_part = nullptr;     // [max_batch * n_q_heads + rows][v_dim]
+    float* d_pre_stat = nullptr;     // [..][2]
 };
 
 namespace moei {
+
+// Raises what a kernel may ask for of a compute unit's LDS to `bytes`.
+int kv_allow_lds(const moei_kv& kv, const void* kernel, int bytes);
 
 int launch_kv_attend(const moei_kv& kv, const KvAttendArgs& a, hipStream_t s);
 int launch_kv_blocks(const moei_kv& kv, KvBlocksArgs a, hipStream_t s);

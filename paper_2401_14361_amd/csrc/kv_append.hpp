@@ -42,6 +42,9 @@ struct KvEvictArgs {
     long long w_row, to_w_row;
     int B, n_kv, width, to_width, page_shift, n_pages, keep, first, last;
     int rows;  // of a workgroup that moves
+    int ranks;                   // that fit a workgroup's LDS, 0: none are held
+    int step, per, parts;        // of a choice by several workgroups: tokens of one, and workgroups
+    unsigned *hist, *counts;     // [B * n_kv][3][2048], zero between calls (null: one workgroup), and [B * n_kv][parts][2]
     int32_t* flags;
 };
 

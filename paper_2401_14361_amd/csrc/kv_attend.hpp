@@ -5,7 +5,6 @@
 #include <math.h>
 
 #include "kv.hpp"
-#include "lds_limit.hpp"
 
 namespace moei {
 
@@ -25,8 +24,8 @@ __device__ __forceinline__ Args again(Args p) {
 }
 
 // What a launch does besides: nothing; it leaves logits, and every head's maximum and sum, for the sums of weights; it begins behind the prefix that
-// a sequence shares, and adds what is there of that.
-enum { kPlain, kWeigh, kJoin };
+// a sequence shares, and leaves sums instead of outputs.
+enum { kPlain, kWeigh, kOwn };
 
 constexpr int kRows = 16;  // keys of a subtile: the rows of a matrix instruction; a page holds whole ones
 
@@ -39,15 +38,28 @@ struct Span {
     int begin, end, start;  // tokens [begin, end) of the (listed) sequence; units are counted from `start`, a whole subtile
 };
 
-typedef const __attribute__((address_space(4))) KvShared* shared_of;
+typedef const __attribute__((address_space(4))) KvSharedArgs* SharedArgs;
+
+// The prefix that sequence b, `len` tokens long, shares: groups ascend (n_groups 0: there are none).
+__device__ __forceinline__ int prefix_of(SharedArgs z, int n_groups, int b, int len, int room) {
+    int lo = 0, hi = n_groups;  // the last group that begins at b or before lies in [lo, hi)
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (z->starts[mid] <= b) lo = mid;
+        else hi = mid;
+    }
+    if (n_groups == 0 || z->starts[lo] > b || z->starts[lo + 1] <= b) return 0;
+    const int p = z->prefix[lo];
+    return p > 0 && len >= min(p, room) ? min(p, room) : 0;
+}
 
 template <int kMode, typename A>
-__device__ __forceinline__ Span span_of(A a, int len, int b) {
+__device__ __forceinline__ Span span_of(A a, int len, int b, int n_groups) {
     const long long room = (long long)a->width << a->page_shift;
     len = len < 0 ? 0 : len > room ? (int)room : len;
     Span s{0, len, 0};
-    if constexpr (kMode == kJoin) {
-        s.begin = ((shared_of)(uintptr_t)a->shared)[b].prefix;  // (not past len)
+    if constexpr (kMode == kOwn) {
+        s.begin = prefix_of((SharedArgs)a, n_groups, b, len, (int)room);  // (KvSharedArgs begins with these arguments)
         s.start = s.begin & ~(kRows - 1);
     } else if (a->list) {
         const int nb = (len + (1 << a->page_shift) - 1) >> a->page_shift;
@@ -76,13 +88,13 @@ struct Stretch {
 // quarter, or by four units, if then none crosses from an item to the next.  (64 sequences of up to 1,000 tokens, four heads of 128: 19.7 us, with
 // two units 26.5; of up to 2,000 in 8 bits 21.6 and 31.8; with six units as with four.)
 template <int kUnit, int kMode>
-__device__ __forceinline__ Stretch my_stretch(Args a, int lane) {
-    const unsigned items = a->n_kv * a->blocks_of_heads, grid = gridDim.x;
+__device__ __forceinline__ Stretch my_stretch(Args a, int lane, unsigned wg, unsigned grid, int n_groups) {
+    const unsigned items = a->n_kv * a->blocks_of_heads;
     unsigned units = 0;  // of an item of this lane's sequence
     int len = 0;
     auto look = [&](int b0) __attribute__((always_inline)) {
         len = b0 + lane < a->B ? a->lens[b0 + lane] : 0;
-        units = b0 + lane < a->B ? units_of<kUnit>(span_of<kMode>(a, len, b0 + lane)) : 0u;
+        units = b0 + lane < a->B ? units_of<kUnit>(span_of<kMode>(a, len, b0 + lane, n_groups)) : 0u;
     };
     unsigned total = 0;
     for (int b0 = 0; b0 < a->B; b0 += kWave) {
@@ -106,7 +118,7 @@ __device__ __forceinline__ Stretch my_stretch(Args a, int lane) {
             }
         }
     }
-    s.first = blockIdx.x * s.per;
+    s.first = wg * s.per;
     s.end = s.first + s.per;
     s.b = -1;
     s.base = 0;
@@ -212,31 +224,6 @@ __device__ __forceinline__ float2 load_past(const unsigned long long* p) {
     return make_float2(__uint_as_float((unsigned)v), __uint_as_float((unsigned)(v >> 32)));
 }
 
-// Adds what the launch before has left of a shared prefix, part by part in their order.
-__device__ __forceinline__ void join_prefix(Args a, Sums& r, int b, int hk, int h, int d) {
-    const shared_of at = (shared_of)(uintptr_t)a->shared + b;
-    const KvShared s{at->prefix, at->parts, at->rows, at->row};
-    constexpr int kAhead = 8;  // under way
-    for (int p0 = 0; p0 < s.parts; p0 += kAhead) {
-        float2 ps[kAhead];
-        f32x4 po[kAhead];
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) {
-            const unsigned row = s.row + (min(p0 + j, s.parts - 1) * a->n_kv + hk) * s.rows + h;
-            ps[j] = reinterpret_cast<const float2*>(a->pre_stat)[row];
-            po[j] = *reinterpret_cast<const f32x4*>(a->pre_part + (long long)row * a->v_dim + d);
-        }
-        const float before = r.m;
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) r.m = fmaxf(r.m, ps[j].x);
-        const float from = r.m == -INFINITY ? 0.f : r.m, fade = __builtin_amdgcn_exp2f(before - from);
-        r.l *= fade;
-        r.o *= fade;
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j) r.add(p0 + j < s.parts ? __builtin_amdgcn_exp2f(ps[j].x - from) : 0.f, ps[j].y, po[j]);
-    }
-}
-
 // ------------------------------------------------------------------------------------------------ a stretch of units
 // A wavefront brings tiles of sixteen keys and values (8-bit: 32) into a ring of its own in LDS, by loads that pass the registers by, and waits for
 // the oldest only.  Most classes have two stages, 128 KB of rings in a compute unit (192-wide keys 160); fp32 heads of 96 have three, 144 KB;
@@ -275,18 +262,19 @@ __device__ __forceinline__ void wait_stage(int rest) {
 }
 
 template <typename T, int KC, int VC, int NS, int NW, int kMode>
-__device__ __forceinline__ void attend(unsigned char* smem) {
+__device__ __forceinline__ void attend(unsigned char* smem, unsigned wg, unsigned wgs, int n_groups) {
     using S = Shape<T, KC, VC, NS, NW>;
     constexpr int kWaves = NW;
     typedef typename T::io io;
     constexpr int kUnits = KC * T::kBytes / 64;  // of 64 bytes of a key: a 16-byte piece for each of the four lane groups
     constexpr int kOut = VC / 16;                // tiles of sixteen output columns
-    const int lane = threadIdx.x & (kWave - 1);
+    int lane = threadIdx.x & (kWave - 1);
+    if constexpr (kMode == kOwn) asm volatile("" : "+v"(lane));  // (else what depends on it is formed ahead of the other half of the launch, and kept through that)
     const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int col = lane & 15, grp = lane >> 4;
     Args a = (Args)__builtin_amdgcn_kernarg_segment_ptr();
 
-    const Stretch mine_of = my_stretch<S::kUnit, kMode>(a, lane);
+    const Stretch mine_of = my_stretch<S::kUnit, kMode>(a, lane, wg, wgs, n_groups);
     if (mine_of.b < 0) return;
 
     // where a lane's pieces of a tile come from, behind the subtile's first byte
@@ -314,7 +302,7 @@ __device__ __forceinline__ void attend(unsigned char* smem) {
     do {
         a = again(a);
         const int len = b == mine_of.b ? mine_of.len : ((kv_const_ints)(uintptr_t)a->lens)[b];
-        const Span sp = span_of<kMode>(a, len, b);
+        const Span sp = span_of<kMode>(a, len, b, n_groups);
         const unsigned units = units_of<S::kUnit>(sp);
         const unsigned room = mine_of.step == 1 ? units : (units + mine_of.step - 1) / mine_of.step * mine_of.step;  // of an item, in the line
         const unsigned item = (at_unit - base) / room, u0 = at_unit - base - item * room;
@@ -611,8 +599,12 @@ __device__ __forceinline__ void attend(unsigned char* smem) {
                     r.add(__builtin_amdgcn_exp2f(f[w] - from), s_l[h * kWaves + w], *reinterpret_cast<const f32x4*>(out + (w * kKvHeads + h) * S::kOutRow + d));
                 if (write) {
                     const Args z = again(a);
-                    if constexpr (kMode == kJoin) join_prefix(z, r, b, hk, h0 + h, d);
                     const long long head = (long long)b * z->n_kv * z->group + hk * z->group + h0 + h;
+                    if constexpr (kMode == kOwn) {
+                        *reinterpret_cast<f32x4*>(z->pre_part + head * v_dim + d) = r.o;
+                        if (d == 0) reinterpret_cast<float2*>(z->pre_stat)[head] = make_float2(r.m, r.l);
+                        continue;
+                    }
                     // (the reciprocal is good to an ulp of fp32; of no weights it is not taken)
                     const float g = r.m == -INFINITY ? 0.f : __builtin_amdgcn_rcpf(r.l) * (z->v_scale ? z->v_scale[hk] : 1.f);
                     if constexpr (sizeof(io) == 2)
@@ -623,7 +615,7 @@ __device__ __forceinline__ void attend(unsigned char* smem) {
                         if (d == 0) z->tops[head] = r.m == -INFINITY ? make_float2(0.f, 0.f) : make_float2(r.m, 1.f / r.l);  // (no weights: logits of -inf add nothing)
                     if (d == 0 && z->lse) z->lse[head] = (r.m + __builtin_amdgcn_logf(r.l)) * 0.69314718055994531f;  // (no weights: -inf, from both)
                 } else {
-                    const unsigned row = (2 * blockIdx.x + (u0 == 0 ? 1 : 0)) * rows + h;
+                    const unsigned row = (2 * wg + (u0 == 0 ? 1 : 0)) * rows + h;
                     unsigned long long* to = reinterpret_cast<unsigned long long*>(part + (row * v_dim + d));
                     store_past(to, r.o[0], r.o[1]);
                     store_past(to + 1, r.o[2], r.o[3]);
@@ -693,18 +685,6 @@ __device__ __forceinline__ void attend(unsigned char* smem) {
     } while (at_unit < mine_of.end);
 }
 
-LdsLimits<16> g_limits[8];  // of a device
-
-// raises what a kernel may ask for of a compute unit's LDS
-inline int allow_lds(const moei_kv& kv, const void* kernel, int bytes) {
-    if (bytes <= 64 * 1024) return MOEI_OK;
-    const auto raise = [&]() -> int {
-        MOEI_HIP(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
-        return MOEI_OK;
-    };
-    return kv.device < 8 ? g_limits[kv.device].at_least(kernel, bytes, raise) : raise();
-}
-
 // K names the kernel of a shape
 template <typename K, typename T, int KC, int VC, int NW>
 int launch_shape(const moei_kv& kv, const KvAttendArgs& a, hipStream_t s) {
@@ -713,7 +693,7 @@ int launch_shape(const moei_kv& kv, const KvAttendArgs& a, hipStream_t s) {
     using S = Shape<T, KC, VC, NS, NW>;
     static_assert(S::kLds <= kMost, "the rings fit a compute unit");
     const auto kernel = K::template kernel<T, KC, VC, NS, NW>;
-    const int rc = allow_lds(kv, reinterpret_cast<const void*>(kernel), S::kLds);
+    const int rc = kv_allow_lds(kv, reinterpret_cast<const void*>(kernel), S::kLds);
     if (rc) return rc;
     const long long line = (((long long)a.width << a.page_shift) / S::kUnit + 1) * a.B * a.n_kv * a.blocks_of_heads;  // units, at most
     const int grid = kv.cus * S::kResident;

@@ -12,7 +12,7 @@ namespace {
 template <typename T, int KC, int VC, int NS, int NW>
 __global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kResident * NW / 4)) kv_attend_weigh_kernel(KvAttendArgs) {
     extern __shared__ __align__(16) unsigned char smem[];
-    attend<T, KC, VC, NS, NW, kWeigh>(smem);
+    attend<T, KC, VC, NS, NW, kWeigh>(smem, blockIdx.x, gridDim.x, 0);
 }
 
 struct Weigh {
@@ -28,13 +28,13 @@ __global__ void __launch_bounds__(kSumThreads) kv_weights_kernel(KvWeightsArgs) 
     const auto* z = (const __attribute__((address_space(4))) KvWeightsArgs*)__builtin_amdgcn_kernarg_segment_ptr();
     const Args a = &z->a;
     const int tid = threadIdx.x, group = a->group, n_kv = a->n_kv;
-    const Stretch mine = my_stretch<kSumUnit, kPlain>(a, tid & (kWave - 1));
+    const Stretch mine = my_stretch<kSumUnit, kPlain>(a, tid & (kWave - 1), blockIdx.x, gridDim.x, 0);
     if (mine.b < 0) return;
     const long long tiles = (long long)a->width << (a->page_shift - 4);
     int b = mine.b;
     unsigned base = mine.base, at = mine.first;
     while (at < mine.end) {
-        const Span sp = span_of<kPlain>(a, b == mine.b ? mine.len : ((kv_const_ints)(uintptr_t)a->lens)[b], b);
+        const Span sp = span_of<kPlain>(a, b == mine.b ? mine.len : ((kv_const_ints)(uintptr_t)a->lens)[b], b, 0);
         const unsigned units = units_of<kSumUnit>(sp), room = (units + mine.step - 1) / mine.step * mine.step;
         const unsigned hk = (at - base) / room, u = at - base - hk * room;
         const int j = sp.start + (int)u * kSumUnit + 4 * tid;

@@ -21,7 +21,7 @@ const char* const kNames[K_COUNT] = {
     "priority_rank_kernel", "ffn_fused_kernel", "ffn_reduce_kernel", "prefill_group_kernels",
     "prefill_route_kernel", "prefill_gateup_kernel", "prefill_down_kernel", "prefill_reduce_kernel",
     "ffn_grouped_mm_kernel", "kv_append_kernel", "kv_summary_kernel", "kv_attend_kernel", "kv_blocks_kernel",
-    "kv_append_norm_kernel", "kv_shared_kernel", "kv_weights_kernel", "kv_evict_kernel", "kv_move_kernel",
+    "kv_append_norm_kernel", "kv_shared_kernel", "kv_join_kernel", "kv_weights_kernel", "kv_evict_kernel", "kv_move_kernel",
 };
 
 void drop_pool() {

@@ -265,6 +265,19 @@ def test_equal_and_special_weights(m, what):  # noqa: F811
         evict(m, c, w, n_keep, first, last)
 
 
+@pytest.mark.parametrize("B,Hkv,top", [(3, 1, 70000), (3, 43, 20000), (130, 1, 16500), (2, 64, 16385)])
+@pytest.mark.parametrize("what", ["spread", "equal", "few"])
+def test_long_sequences(m, B, Hkv, top, what):  # noqa: F811
+    # more tokens than a workgroup holds: chosen from by several workgroups, or where there are many heads by one that reads the weights again and again
+    rng = np.random.default_rng(B)
+    lens = [top, *(int(x) for x in rng.integers(0, top // 8, B - 1))]
+    c = Case(m, "fp8", Hkv, Hkv, 16, 16, 256, lens, seed=1, nan_tail=False)
+    w = rows_of(c)
+    w = {"spread": w, "equal": torch.full_like(w, 0.5), "few": torch.round(w * 3)}[what]
+    for _ in range(2):  # what the choice keeps in memory is as it was
+        evict(m, c, w, 1999, 3, 130)
+
+
 def test_evict_bad_pages_and_lengths(m):  # noqa: F811
     c = Case(m, "bf16", 2, 2, 64, 64, 16, [100, 90, 80, 70], seed=1, nan_tail=False)
     w = rows_of(c)
