@@ -6,6 +6,8 @@ namespace moei {
 
 namespace {
 
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
 // Sum over groups of `lanes` (a power of two) neighbouring lanes; every lane of a group ends with the same bits.
 __device__ __forceinline__ float group_sum(float v, int lanes) {
     if (lanes > 1) v += MOEI_DPP_F32(v, 0xB1);   // quad_perm [1,0,3,2]
@@ -26,8 +28,6 @@ struct Part {
     int d1[P], d2[P];
     bool there[P], turned[P];
     typename V::raw r1[P], r2[P];
-    float2 cs[P][W];
-    float w[P][2 * W];
 
     static __device__ __forceinline__ int lanes_of(Args a) {
         const int n = (a->k_dim / (2 * W) + P - 1) / P;
@@ -51,28 +51,6 @@ struct Part {
             if (there[p]) r1[p] = V::load(head + d1[p]), r2[p] = V::load(head + d2[p]);
         }
     }
-    __device__ __forceinline__ void turns(Args a, int lane, int lanes, const float2* s_turn) {
-#pragma unroll
-        for (int p = 0; p < P; ++p)
-#pragma unroll
-            for (int k = 0; k < W; ++k) cs[p][k] = turned[p] ? s_turn[(lane + p * lanes) * W + k] : make_float2(1.f, 0.f);
-    }
-    __device__ __forceinline__ void weights(const float* row) {
-#pragma unroll
-        for (int p = 0; p < P; ++p)
-            if (there[p]) {
-                if constexpr (W == 1) {
-                    w[p][0] = row[d1[p]];
-                    w[p][1] = row[d2[p]];
-                } else {
-#pragma unroll
-                    for (int i = 0; i < W; i += 4) {
-                        *reinterpret_cast<float4*>(&w[p][i]) = *reinterpret_cast<const float4*>(row + d1[p] + i);
-                        *reinterpret_cast<float4*>(&w[p][W + i]) = *reinterpret_cast<const float4*>(row + d2[p] + i);
-                    }
-                }
-            }
-    }
     __device__ __forceinline__ void unpack(float (*f)[2 * W]) const {
 #pragma unroll
         for (int p = 0; p < P; ++p) {
@@ -80,8 +58,8 @@ struct Part {
             V::unpack(r2[p], f[p] + W);
         }
     }
-    // norm and turn of a head
-    __device__ __forceinline__ void make(Args a, int lanes, float (*f)[2 * W]) const {
+    // norm and turn of a head (the pairs' turns stay in LDS: in registers they would cost a compute unit two of its wavefronts)
+    __device__ __forceinline__ void make(Args a, int lane, int lanes, const float* row, const float2* s_turn, float (*f)[2 * W]) const {
         float sum = 0.f;
 #pragma unroll
         for (int p = 0; p < P; ++p)
@@ -90,15 +68,26 @@ struct Part {
         const float by = 1.f / sqrtf(group_sum(sum, lanes) / (float)a->k_dim + a->eps);
 #pragma unroll
         for (int p = 0; p < P; ++p) {
+            if (!there[p]) continue;
+            if constexpr (W == 1) {
+                f[p][0] = f[p][0] * by * row[d1[p]];
+                f[p][1] = f[p][1] * by * row[d2[p]];
+            } else {
 #pragma unroll
-            for (int i = 0; i < 2 * W; ++i) f[p][i] = f[p][i] * by * w[p][i];
+                for (int i = 0; i < 2 * W; i += 4) {
+                    const f32x4 w = *reinterpret_cast<const f32x4*>(row + (i < W ? d1[p] : d2[p] - W) + i);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) f[p][i + j] = f[p][i + j] * by * w[j];
+                }
+            }
             if (turned[p]) {
+                const float2* cs = s_turn + (lane + p * lanes) * W;
                 if (a->interleaved) {
 #pragma unroll
-                    for (int k = 0; k < W; ++k) turn_pair(f[p][2 * k], f[p][2 * k + 1], cs[p][k]);
+                    for (int k = 0; k < W; ++k) turn_pair(f[p][2 * k], f[p][2 * k + 1], cs[k]);
                 } else {
 #pragma unroll
-                    for (int k = 0; k < W; ++k) turn_pair(f[p][k], f[p][W + k], cs[p][k]);
+                    for (int k = 0; k < W; ++k) turn_pair(f[p][k], f[p][W + k], cs[k]);
                 }
             }
         }
@@ -113,12 +102,13 @@ __device__ __forceinline__ float as_held(float x, float scale) {
     else return x;
 }
 
-// As in kv_append_kernel a workgroup takes a share of a token's heads, a thread keeps its place in a head and has the next head's part under
-// way.  A head is a power of two of neighbouring lanes, so that its sum of squares takes a few steps in registers; the norm costs no bytes but
-// its weights, which stay in registers until queries are followed by keys (weights of every head are read from cache with the head).
+// As in kv_append_kernel a workgroup takes a share of a token's heads, and a thread keeps its place in a head.  A head is a power of two of neighbouring lanes, so that its
+// sum of squares takes a few steps in registers.  Latency for a token, 4.0 us as without norms; memory for prompts: 8,192 tokens of 32 + 8 + 8 heads of 128 in bf16, 201 MB, with
+// weights of their own for every head, 51 us (without norms 38; 42 if no weights were read: they come from cache with each head, 64 bytes beside a lane's 32).  Weights and turns that stay in
+// registers leave four wavefronts a SIMD instead of six, 60 us; weights asked for before the next head instead of behind it 55, at five.
 // kSums: as there; the row that completes a page is formed a second time by the same steps, so that it has the same bits.
 template <typename IO, typename PG, int W, bool kSums>
-__global__ void __launch_bounds__(kAppThreads, 4) kv_append_norm_kernel(KvAppendArgs) {
+__global__ void __launch_bounds__(kAppThreads, kSums ? 4 : 6) kv_append_norm_kernel(KvAppendArgs) {
     const Args a = (Args)__builtin_amdgcn_kernarg_segment_ptr();
     using V = Vec<IO, W>;
     using L = Part<IO, W>;
@@ -140,11 +130,9 @@ __global__ void __launch_bounds__(kAppThreads, 4) kv_append_norm_kernel(KvAppend
         __syncthreads();
         if (tid < lanes) {
             part.load(static_cast<const IO*>(a->k) + t * a->k_row + h * a->k_dim);
-            part.weights(a->k_weight + (a->per_head ? h * a->k_dim : 0));
-            part.turns(a, lane, lanes, s_turn);
             float f[P][2 * W];
             part.unpack(f);
-            part.make(a, lanes, f);
+            part.make(a, lane, lanes, a->k_weight + (a->per_head ? h * a->k_dim : 0), s_turn, f);
             const float scale = sizeof(PG) == 1 ? a->k_scale[h] : 1.f;
 #pragma unroll
             for (int p = 0; p < P; ++p)
@@ -172,19 +160,14 @@ __global__ void __launch_bounds__(kAppThreads, 4) kv_append_norm_kernel(KvAppend
     for (int j = tid; j < half; j += kAppThreads) s_turn[j] = turn(angle, a->inv_freq[j]);
     __syncthreads();
     const int row = pos & (size - 1);
-    part.turns(a, lane, lanes, s_turn);
     PG* k_page = static_cast<PG*>(a->k_pages) + page * a->k_stride + (long long)row * a->k_dim;
-    int of = -1;  // whose weights there are: of queries, of keys
     while (head < n_heads) {
         const int now = head, kind = now >= a->n_q;
-        if (a->per_head) part.weights(kind ? a->k_weight + (now - a->n_q) * a->k_dim : a->q_weight + now * a->k_dim);
-        else if (kind != of) part.weights(kind ? a->k_weight : a->q_weight);
-        of = kind;
         float f[P][2 * W];
         part.unpack(f);
         head += per_step;
+        part.make(a, lane, lanes, kind ? a->k_weight + (a->per_head ? (now - a->n_q) * a->k_dim : 0) : a->q_weight + (a->per_head ? now * a->k_dim : 0), s_turn, f);
         if (head < n_heads) load();
-        part.make(a, lanes, f);
         if (kind == 0) {
             IO* to = static_cast<IO*>(a->q_out) + ((long long)t * a->n_q + now) * a->k_dim;
 #pragma unroll
