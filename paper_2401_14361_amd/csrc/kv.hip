@@ -611,6 +611,7 @@ extern "C" int kv_evict(moei_kv* kv, const moei_kv_pages* pages, const int32_t* 
     const long long to_room = (long long)to_width * d.page_size, to_w_row = to_w_stride ? to_w_stride : to_room;
     MOEI_REQUIRE((uintptr_t)d_weights % 4 == 0 && (uintptr_t)d_to_weights % 4 == 0 && w_row >= room && to_w_row >= n_keep,
                  "%s: w_stride = %lld or to_w_stride = %lld is shorter than a row, or weights are not aligned", who, (long long)w_stride, (long long)to_w_stride);
+    if (n_keep > 1 << 29) MOEI_FAIL(MOEI_ECAPACITY, "%s: n_keep = %d exceeds 2^29", who, n_keep);  // (a launch counts its threads in 32 bits)
     const long long rows = (long long)B * d.n_kv_heads, from = ((rows - 1) * w_row + room) * 4, to = ((rows - 1) * to_w_row + n_keep) * 4;
     MOEI_REQUIRE(!overlap(d_len, 1, B * 4ll, B * 4ll, d_to_len, B * 4ll), "%s: d_to_len overlaps d_len", who);  // (other workgroups read it still)
     MOEI_REQUIRE(!d_to_weights || !overlap(d_weights, 1, from, from, d_to_weights, to), "%s: d_to_weights overlaps d_weights", who);
