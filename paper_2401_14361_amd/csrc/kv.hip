@@ -556,8 +556,8 @@ extern "C" int kv_attend_weights(moei_kv* kv, const moei_kv_pages* pages, const 
     if (B * room > kv->weight_tokens)
         MOEI_FAIL(MOEI_ECAPACITY, "%s: %d sequences of up to %lld tokens are more than the %lld of moei_kv_set_weights", who, B, room, kv->weight_tokens);
     w.a.window = window;
-    w.a.logits = kv->d_logits;
-    w.a.tops = kv->d_tops;
+    w.logits = kv->d_logits;
+    w.tops = kv->d_tops;
     w.weights = d_weights;
     w.w_row = w_row;
     w.wide = (uintptr_t)d_weights % 16 == 0 && w_row % 4 == 0;
@@ -587,8 +587,8 @@ extern "C" int kv_attend_shared(moei_kv* kv, const moei_kv_pages* pages, const i
     a.prefix = d_prefix;
     a.n_groups = n_groups;
     a.told = kv->d_told;
-    a.a.pre_part = kv->d_pre_part;
-    a.a.pre_stat = kv->d_pre_stat;
+    a.pre_part = kv->d_pre_part;
+    a.pre_stat = kv->d_pre_stat;
     return launch_kv_attend_shared(*kv, a, as_stream(stream));
 }
 

@@ -47,15 +47,13 @@ struct KvAttendArgs {
     float* stat;             // [workgroups][2][rows][2] their maximum and sum
     unsigned* arrived;       // [workgroups] parts that are there, of the item that begins in a workgroup's stretch; zero between launches
     int32_t* flags;
-    float* logits;           // sums of weights: [B][n_kv][width * page / 16][group][16], unscaled ...
-    float2* tops;            // ... and [B][Hq] maximum (of what exp2 takes) and reciprocal of the sum
-    float* pre_part;         // behind shared prefixes: [B][Hq][v_dim] sums of what is a sequence's own, not yet divided, then those of the prefixes' parts ...
-    float* pre_stat;         // ... and [..][2] their maximum and sum
 };
 
 // Sums of weights: what the attention is given, and where they are added up.
 struct KvWeightsArgs {
-    KvAttendArgs a;
+    KvAttendArgs a;    // (first: the attention is given these)
+    float* logits;     // [B][n_kv][width * page / 16][group][16], unscaled ...
+    float2* tops;      // ... and [B][Hq] maximum (of what exp2 takes) and reciprocal of the sum
     float* weights;    // [B][n_kv][w_row]
     long long w_row;
     int wide;          // four at a time
@@ -67,6 +65,8 @@ struct KvSharedArgs {
     const int32_t *starts, *prefix;  // [n_groups + 1] first sequences, [n_groups] tokens
     int n_groups;
     KvShared* told;                  // [B] out
+    float* pre_part;                 // [B][Hq][v_dim] sums of what is a sequence's own, not yet divided, then those of the prefixes' parts ...
+    float* pre_stat;                 // ... and [..][2] their maximum and sum
 };
 
 constexpr int kKvSplitItems = 128;  // sequences and key/value heads whose tokens several workgroups choose from ...

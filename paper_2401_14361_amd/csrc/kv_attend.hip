@@ -18,6 +18,8 @@ __global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kReside
 }
 
 struct Plain {
+    typedef KvAttendArgs Whole;
+    static const KvAttendArgs& args(const Whole& w) { return w; }
     template <typename T, int KC, int VC, int NS, int NW>
     static constexpr auto kernel = kv_attend_kernel<T, KC, VC, NS, NW>;
 };

@@ -18,6 +18,8 @@ typedef int i32x2 __attribute__((ext_vector_type(2)));
 // The arguments are read where they are used: held from the start they would be 60 scalar registers more than there are, moved to lanes and
 // back at every phase.  (A launch runs most of its code once, from memory: 2 KB a microsecond.)
 typedef const __attribute__((address_space(4))) KvAttendArgs* Args;
+typedef const __attribute__((address_space(4))) KvWeightsArgs* WeightsArgs;  // (both begin with the attention's)
+typedef const __attribute__((address_space(4))) KvSharedArgs* SharedArgs;
 __device__ __forceinline__ Args again(Args p) {
     asm volatile("" : "+s"(p));
     return p;
@@ -38,7 +40,6 @@ struct Span {
     int begin, end, start;  // tokens [begin, end) of the (listed) sequence; units are counted from `start`, a whole subtile
 };
 
-typedef const __attribute__((address_space(4))) KvSharedArgs* SharedArgs;
 
 // The prefix that sequence b, `len` tokens long, shares: groups ascend (n_groups 0: there are none).
 __device__ __forceinline__ int prefix_of(SharedArgs z, int n_groups, int b, int len, int room) {
@@ -59,7 +60,7 @@ __device__ __forceinline__ Span span_of(A a, int len, int b, int n_groups) {
     len = len < 0 ? 0 : len > room ? (int)room : len;
     Span s{0, len, 0};
     if constexpr (kMode == kOwn) {
-        s.begin = prefix_of((SharedArgs)a, n_groups, b, len, (int)room);  // (KvSharedArgs begins with these arguments)
+        s.begin = prefix_of((SharedArgs)a, n_groups, b, len, (int)room);
         s.start = s.begin & ~(kRows - 1);
     } else if (a->list) {
         const int nb = (len + (1 << a->page_shift) - 1) >> a->page_shift;
@@ -465,7 +466,7 @@ __device__ __forceinline__ void attend(unsigned char* smem, unsigned wg, unsigne
             if constexpr (kMode == kWeigh) {  // [sequence][key/value head][subtile][head of the group][16 tokens]
                 const Args z = again(a);
                 const long long row = (long long)b * z->n_kv + hk, tiles = (long long)z->width << (page_shift - 4);
-                float* to = z->logits + ((row * tiles + (t0 >> 4)) * z->group + h0 + col) * kRows + 4 * grp;
+                float* to = ((WeightsArgs)z)->logits + ((row * tiles + (t0 >> 4)) * z->group + h0 + col) * kRows + 4 * grp;
                 if (col < heads)
 #pragma unroll
                     for (int st = 0; st < T::kSub; ++st)
@@ -601,8 +602,8 @@ __device__ __forceinline__ void attend(unsigned char* smem, unsigned wg, unsigne
                     const Args z = again(a);
                     const long long head = (long long)b * z->n_kv * z->group + hk * z->group + h0 + h;
                     if constexpr (kMode == kOwn) {
-                        *reinterpret_cast<f32x4*>(z->pre_part + head * v_dim + d) = r.o;
-                        if (d == 0) reinterpret_cast<float2*>(z->pre_stat)[head] = make_float2(r.m, r.l);
+                        *reinterpret_cast<f32x4*>(((SharedArgs)z)->pre_part + head * v_dim + d) = r.o;
+                        if (d == 0) reinterpret_cast<float2*>(((SharedArgs)z)->pre_stat)[head] = make_float2(r.m, r.l);
                         continue;
                     }
                     // (the reciprocal is good to an ulp of fp32; of no weights it is not taken)
@@ -612,7 +613,7 @@ __device__ __forceinline__ void attend(unsigned char* smem, unsigned wg, unsigne
                     else
                         *reinterpret_cast<f32x4*>(static_cast<float*>(z->out) + head * v_dim + d) = r.o * g;
                     if constexpr (kMode == kWeigh)
-                        if (d == 0) z->tops[head] = r.m == -INFINITY ? make_float2(0.f, 0.f) : make_float2(r.m, 1.f / r.l);  // (no weights: logits of -inf add nothing)
+                        if (d == 0) ((WeightsArgs)z)->tops[head] = r.m == -INFINITY ? make_float2(0.f, 0.f) : make_float2(r.m, 1.f / r.l);  // (no weights: logits of -inf add nothing)
                     if (d == 0 && z->lse) z->lse[head] = (r.m + __builtin_amdgcn_logf(r.l)) * 0.69314718055994531f;  // (no weights: -inf, from both)
                 } else {
                     const unsigned row = (2 * wg + (u0 == 0 ? 1 : 0)) * rows + h;
@@ -685,9 +686,10 @@ __device__ __forceinline__ void attend(unsigned char* smem, unsigned wg, unsigne
     } while (at_unit < mine_of.end);
 }
 
-// K names the kernel of a shape
+// K names the kernel of a shape, and what it is given
 template <typename K, typename T, int KC, int VC, int NW>
-int launch_shape(const moei_kv& kv, const KvAttendArgs& a, hipStream_t s) {
+int launch_shape(const moei_kv& kv, const typename K::Whole& all, hipStream_t s) {
+    const KvAttendArgs& a = K::args(all);
     constexpr int kMost = 160 * 1024;
     constexpr int NS = KC == 96 && Shape<T, KC, VC, 3, NW>::kLds <= kMost ? 3 : Shape<T, KC, VC, 2, NW>::kLds <= kMost ? 2 : 1;
     using S = Shape<T, KC, VC, NS, NW>;
@@ -697,7 +699,7 @@ int launch_shape(const moei_kv& kv, const KvAttendArgs& a, hipStream_t s) {
     if (rc) return rc;
     const long long line = (((long long)a.width << a.page_shift) / S::kUnit + 1) * a.B * a.n_kv * a.blocks_of_heads;  // units, at most
     const int grid = kv.cus * S::kResident;
-    launch(K_KV_ATTEND, kernel, dim3((unsigned)(line < grid ? line : grid)), dim3(NW * kWave), S::kLds, s, a);
+    launch(K_KV_ATTEND, kernel, dim3((unsigned)(line < grid ? line : grid)), dim3(NW * kWave), S::kLds, s, all);
     MOEI_LAUNCH_CHECK();
     return MOEI_OK;
 }
@@ -723,27 +725,28 @@ bool many_short_items(const moei_kv& kv, const KvAttendArgs& a) {
 }
 
 template <typename K, typename T>
-int launch_type(const moei_kv& kv, const KvAttendArgs& a, hipStream_t s) {
+int launch_type(const moei_kv& kv, const typename K::Whole& all, hipStream_t s) {
+    const KvAttendArgs& a = K::args(all);
     const bool many = many_short_items<T>(kv, a);
-    if (a.k_dim <= 64 && a.v_dim <= 64) return many ? launch_shape<K, T, 64, 64, 4>(kv, a, s) : launch_shape<K, T, 64, 64, 8>(kv, a, s);
+    if (a.k_dim <= 64 && a.v_dim <= 64) return many ? launch_shape<K, T, 64, 64, 4>(kv, all, s) : launch_shape<K, T, 64, 64, 8>(kv, all, s);
     if constexpr (T::kBytes == 4)
-        if (a.k_dim <= 96 && a.v_dim <= 96) return launch_shape<K, T, 96, 96, 4>(kv, a, s);
+        if (a.k_dim <= 96 && a.v_dim <= 96) return launch_shape<K, T, 96, 96, 4>(kv, all, s);
     if (a.k_dim <= 128 && a.v_dim <= 128) {
-        if (T::kBytes == 4 || many) return launch_shape<K, T, 128, 128, 4>(kv, a, s);
-        if constexpr (T::kBytes != 4) return launch_shape<K, T, 128, 128, 8>(kv, a, s);
+        if (T::kBytes == 4 || many) return launch_shape<K, T, 128, 128, 4>(kv, all, s);
+        if constexpr (T::kBytes != 4) return launch_shape<K, T, 128, 128, 8>(kv, all, s);
     }
-    if (a.k_dim <= 192 && a.v_dim <= 128) return launch_shape<K, T, 192, 128, 4>(kv, a, s);
+    if (a.k_dim <= 192 && a.v_dim <= 128) return launch_shape<K, T, 192, 128, 4>(kv, all, s);
     if constexpr (T::kBytes != 4)
-        if (many) return launch_shape<K, T, 256, 256, 2>(kv, a, s);
-    return launch_shape<K, T, 256, 256, 4>(kv, a, s);
+        if (many) return launch_shape<K, T, 256, 256, 2>(kv, all, s);
+    return launch_shape<K, T, 256, 256, 4>(kv, all, s);
 }
 
 template <typename K>
-int launch_attend(const moei_kv& kv, const KvAttendArgs& a, hipStream_t s) {
+int launch_attend(const moei_kv& kv, const typename K::Whole& all, hipStream_t s) {
     switch (kv.d.dtype) {
-        case MOEI_WDTYPE_FP32: return launch_type<K, Fp32>(kv, a, s);
-        case MOEI_WDTYPE_BF16: return launch_type<K, Bf16>(kv, a, s);
-        default: return launch_type<K, Fp8>(kv, a, s);
+        case MOEI_WDTYPE_FP32: return launch_type<K, Fp32>(kv, all, s);
+        case MOEI_WDTYPE_BF16: return launch_type<K, Bf16>(kv, all, s);
+        default: return launch_type<K, Fp8>(kv, all, s);
     }
 }
 

@@ -546,8 +546,8 @@ __device__ __forceinline__ void attend_prefixes(unsigned char* smem, SharedArgs 
                 const int at_r = v * G::kBlock + r;
                 x.add(G::kKeyWaves == 1 ? 1.f : __builtin_amdgcn_exp2f(s_m[at_r] - from), s_l[at_r], *reinterpret_cast<const f32x4*>(out + at_r * G::kOutRow + d));
             }
-            *reinterpret_cast<f32x4*>(a->pre_part + (long long)(first + r) * a->v_dim + d) = x.o;
-            if (d == 0) reinterpret_cast<float2*>(a->pre_stat)[first + r] = make_float2(x.m, x.l);
+            *reinterpret_cast<f32x4*>(z->pre_part + (long long)(first + r) * a->v_dim + d) = x.o;
+            if (d == 0) reinterpret_cast<float2*>(z->pre_stat)[first + r] = make_float2(x.m, x.l);
         }
         barrier_lds();  // LDS is free for the next part
     }
@@ -598,8 +598,8 @@ __global__ void __launch_bounds__(256) kv_join_kernel(KvSharedArgs) {
             for (int j = 0; j < kAhead; ++j) {
                 const int p = min(p0 + j * slots, parts - 1);
                 const unsigned row = p == 0 ? blockIdx.x : first + (unsigned)(p - 1) * a->n_kv * rows;
-                ps[j] = reinterpret_cast<const float2*>(a->pre_stat)[row];
-                po[j] = *reinterpret_cast<const f32x4*>(a->pre_part + (long long)row * v_dim + d);
+                ps[j] = reinterpret_cast<const float2*>(z->pre_stat)[row];
+                po[j] = *reinterpret_cast<const f32x4*>(z->pre_part + (long long)row * v_dim + d);
                 if (p0 + j * slots >= parts) ps[j].x = -INFINITY;
             }
             const float before = r.m;

@@ -10,12 +10,14 @@ namespace moei {
 namespace {
 
 template <typename T, int KC, int VC, int NS, int NW>
-__global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kResident * NW / 4)) kv_attend_weigh_kernel(KvAttendArgs) {
+__global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kResident * NW / 4)) kv_attend_weigh_kernel(KvWeightsArgs) {
     extern __shared__ __align__(16) unsigned char smem[];
     attend<T, KC, VC, NS, NW, kWeigh>(smem, blockIdx.x, gridDim.x, 0);
 }
 
 struct Weigh {
+    typedef KvWeightsArgs Whole;
+    static const KvAttendArgs& args(const Whole& w) { return w.a; }
     template <typename T, int KC, int VC, int NS, int NW>
     static constexpr auto kernel = kv_attend_weigh_kernel<T, KC, VC, NS, NW>;
 };
@@ -25,7 +27,7 @@ constexpr int kSumThreads = 256, kSumUnit = 4 * kSumThreads;  // tokens: a threa
 // The logits of all sequences are one line of units, of which every workgroup takes an equal stretch, as in the attention.  A thread's sums go over the
 // heads of the group in their order: the same bits every run.
 __global__ void __launch_bounds__(kSumThreads) kv_weights_kernel(KvWeightsArgs) {
-    const auto* z = (const __attribute__((address_space(4))) KvWeightsArgs*)__builtin_amdgcn_kernarg_segment_ptr();
+    const WeightsArgs z = (WeightsArgs)__builtin_amdgcn_kernarg_segment_ptr();
     const Args a = &z->a;
     const int tid = threadIdx.x, group = a->group, n_kv = a->n_kv;
     const Stretch mine = my_stretch<kSumUnit, kPlain>(a, tid & (kWave - 1), blockIdx.x, gridDim.x, 0);
@@ -40,8 +42,8 @@ __global__ void __launch_bounds__(kSumThreads) kv_weights_kernel(KvWeightsArgs) 
         const int j = sp.start + (int)u * kSumUnit + 4 * tid;
         if (u < units && j < sp.end && j + 4 > sp.begin) {
             const long long row = (long long)b * n_kv + hk;
-            const f32x4* logits = reinterpret_cast<const f32x4*>(a->logits + ((row * tiles + (j >> 4)) * group) * kRows + (j & 15));
-            const auto* tops = (const __attribute__((address_space(4))) float2*)(uintptr_t)(a->tops + row * group);
+            const f32x4* logits = reinterpret_cast<const f32x4*>(z->logits + ((row * tiles + (j >> 4)) * group) * kRows + (j & 15));
+            const auto* tops = (const __attribute__((address_space(4))) float2*)(uintptr_t)(z->tops + row * group);
             const float scale2 = a->k_scale ? a->scale2 * ((const __attribute__((address_space(4))) float*)(uintptr_t)a->k_scale)[hk] : a->scale2;
             float* to = z->weights + row * z->w_row + j;
             const bool whole = z->wide && j >= sp.begin && j + 4 <= sp.end;
@@ -76,7 +78,7 @@ __global__ void __launch_bounds__(kSumThreads) kv_weights_kernel(KvWeightsArgs) 
 }  // namespace
 
 int launch_kv_attend_weights(const moei_kv& kv, KvWeightsArgs w, hipStream_t s) {
-    const int rc = launch_attend<Weigh>(kv, w.a, s);
+    const int rc = launch_attend<Weigh>(kv, w, s);
     if (rc) return rc;
     w.a.blocks_of_heads = 1;
     const long long line = (((long long)w.a.width << w.a.page_shift) / kSumUnit + 1) * w.a.B * w.a.n_kv, grid = 8 * kv.cus;
