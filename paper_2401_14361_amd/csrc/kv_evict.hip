@@ -55,10 +55,10 @@ __device__ __forceinline__ uint2 bin_of(Hist hist, unsigned need, unsigned* s_wa
 // Which tokens of a sequence and key/value head are kept: the rank of the least one is found by its bits, eleven at a time (steps 0 - 2), then what is kept is
 // counted (3) and its numbers are written in order (4).  Tokens that are always kept have the highest rank.  Every wavefront has a stretch of the tokens, 64 side by side at a
 // time; their ranks lie in LDS for the later steps where they fit, else the weights are read again.
-// Bound by latency - five steps, of which three end with two scans - and for long rows by its instructions: few heads of long sequences would leave the card idle.  Those take a
-// workgroup for each a->per tokens and a launch for each step (a->step), between which histograms and counts lie in memory: one sequence of 131,072 tokens, eight
-// heads, 100 us by a workgroup a head, 32 in five launches.  Ranks in registers, sixteen a thread, cost more for their code, which a launch runs once, from memory, at 2 KB a
-// microsecond, than they save.
+// Bound by latency: five steps, of which three end with two scans (8 heads of 1,088 tokens 8.1 us, 512 of up to 12,000 20 us).  Long rows are bound by their instructions, and
+// few of them would leave the card idle: these take a workgroup for each a->per tokens and a launch for each step (a->step), between which histograms and counts lie in
+// memory.  Eight heads of 131,072 tokens 100 us by a workgroup a head, 29 in five launches; 33 if the last workgroup of a step looks for its digit, instead of every one of the next
+// step.  Ranks in registers, sixteen a thread, save less than their code costs, which a launch runs once, from memory, at 2 KB a microsecond (1,088 tokens 10.6 us).
 template <int kThreads, bool kSplit>
 __global__ void __launch_bounds__(kThreads) kv_evict_kernel(KvEvictArgs) {
     constexpr int kWaves = kThreads / kWave;
@@ -209,7 +209,8 @@ __global__ void __launch_bounds__(kThreads) kv_evict_kernel(KvEvictArgs) {
     }
 }
 
-// The kept rows of a sequence and key/value head, `rows` of them to a workgroup (whole pages of the destination).
+// The kept rows of a sequence and key/value head, `rows` of them to a workgroup (whole pages of the destination).  Bound by memory: 64 sequences, 2,048 tokens of eight heads of 128
+// in bf16 each, 1.07 GB, 212 us (5.0 TB/s; a copy of 2 GB 4.9).
 constexpr int kMoveThreads = 256;
 
 template <typename IO, typename PG>
@@ -267,13 +268,13 @@ __global__ void __launch_bounds__(kMoveThreads) kv_move_kernel(KvEvictArgs) {
 int launch_kv_evict(const moei_kv& kv, KvEvictArgs a, hipStream_t s) {
     const long long room = (long long)a.width << a.page_shift;
     if (room > 16384 && a.B * a.n_kv <= kKvSplitItems) {
-        constexpr int kAtOnce = 4096;
+        constexpr int kSplitThreads = 512, kAtOnce = 4096;  // (256 threads, or 8,192 tokens: 50 and 62 us for the 131,072 tokens below, 2,048: 45 as here)
         a.per = (int)((room + (long long)kKvSplitParts * kAtOnce - 1) / ((long long)kKvSplitParts * kAtOnce)) * kAtOnce;
         a.parts = (int)((room + a.per - 1) / a.per);
         a.hist = kv.d_evict;
         a.counts = kv.d_evict + (size_t)kKvSplitItems * 3 * kBins;
         for (a.step = 0; a.step < 5; ++a.step) {
-            launch(K_KV_EVICT, kv_evict_kernel<256, true>, dim3((unsigned)a.parts, (unsigned)a.n_kv, (unsigned)a.B), dim3(256), 0, s, a);
+            launch(K_KV_EVICT, kv_evict_kernel<kSplitThreads, true>, dim3((unsigned)a.parts, (unsigned)a.n_kv, (unsigned)a.B), dim3(kSplitThreads), 0, s, a);
             MOEI_LAUNCH_CHECK();
         }
     } else {

@@ -61,6 +61,9 @@ SHARED = [
     ("fp32", 2, 2, 192, 128, 16, [131, 140], [0, 2], [128]),
     ("fp32", 5, 1, 256, 240, 64, [330, 264], [0, 2], [257]),
     ("fp32", 6, 2, 96, 80, 32, [1000, 999, 1010], [0, 3], [990]),
+    ("bf16", 4, 2, 64, 256, 32, [200, 210], [0, 2], [150]),                                       # values wider than keys
+    ("fp8", 4, 2, 16, 208, 16, [200, 210], [0, 2], [150]),
+    ("fp32", 4, 2, 256, 16, 16, [200, 210], [0, 2], [150]),
 ]
 
 
@@ -110,6 +113,28 @@ def test_many_groups(m, dtype):  # noqa: F811
     c = Case(m, dtype, 4, 2, 64, 64, 16, lens, seed=5)
     out, lse = attend(m, c, starts, prefix)
     check(c, out, lse, *oracle(c, starts, prefix))
+    assert c.kv.error_flags() == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8", "fp32"])
+def test_groups_of_unlike_sizes(m, dtype):  # noqa: F811
+    # one of 300 query heads a key/value head beside many of three: what is planned for small groups takes several blocks of rows for the large one
+    sizes, rng = [1] * 20 + [100] + [1] * 15, np.random.default_rng(2)
+    starts = [0, *np.cumsum(sizes).tolist()]
+    prefix = [int(x) for x in rng.integers(1, 200, len(sizes))]
+    lens = [prefix[g] + int(rng.integers(0, 30)) for g, n in enumerate(sizes) for _ in range(n)]
+    c = Case(m, dtype, 6, 2, 64, 64, 16, lens, seed=6)
+    check(c, *attend(m, c, starts, prefix), *oracle(c, starts, prefix))
+
+
+def test_the_largest_batch(m):  # noqa: F811
+    rng = np.random.default_rng(4)
+    B, prefix = 4096, 40
+    lens = [prefix + int(x) for x in rng.integers(-1, 20, B)]
+    c = Case(m, "bf16", 2, 1, 16, 16, 16, lens, seed=4)
+    check(c, *attend(m, c, [0, B], [prefix]), *oracle(c, [0, B], [prefix]))
+    one = list(range(B + 1))  # a group for every sequence
+    check(c, *attend(m, c, one, [prefix] * B), *oracle(c, [0], []))
     assert c.kv.error_flags() == 0
 
 

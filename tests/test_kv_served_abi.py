@@ -5,6 +5,7 @@ import numpy as np
 import pytest
 
 from oracle import kv_oracle as O
+from tests.test_kernel_resources import kernels  # noqa: F401 (a fixture)
 from tests.test_kv_abi import m  # noqa: F401 (a fixture)
 
 
@@ -64,3 +65,12 @@ def test_oracle_shared_is_attention_where_rows_name_the_same_pages():
 ])
 def test_oracle_keep(w, n, keep, first, last, want):
     assert O.keep(w, n, keep, first, last) == want
+
+
+def test_kernels_keep_to_their_registers(kernels):  # noqa: F811
+    """As few registers as the wavefronts that a compute unit is to hold at once allow (those of the products' sums among them)."""
+    for start, waves_a_simd in (("kv_append_norm_kernel<unsigned short, unsigned short, 8, false>", 6), ("kv_shared_kernel<moei::Bf16, 128, 128, 4>", 2),
+                                ("kv_shared_kernel<moei::Fp8, 128, 128, 4>", 2), ("kv_attend_weigh_kernel<moei::Bf16, 128, 128, 2, 8>", 2), ("kv_evict_kernel<1024, false>", 8)):
+        got, = [k for n, k in kernels.items() if n.startswith(start)]
+        assert got[".private_segment_fixed_size"] == 0
+        assert waves_a_simd * (got[".vgpr_count"] + 7 & ~7) <= 512, (start, got[".vgpr_count"])
