@@ -639,15 +639,17 @@ int launch_group(const moei_kv& kv, const KvSharedArgs& a, hipStream_t s) {
     return MOEI_OK;
 }
 
+// The wavefronts of a workgroup have different rows where there are many, else different keys, whose stages are larger and whose sums are joined in LDS at the end.  With 1, 2 and 4
+// wavefronts of rows (32,768 tokens behind 8 key/value heads of 128 in bf16) 32 rows take 34.5, 33.0 and 37.9 us, 64 rows 51.4, 39.3 and 43.6, 128 rows 85.2, 52.6 and 45.5; eight prefixes of
+// 4,000 - 8,192 tokens and 32 rows each 87.3, 53.3 and 62.5: with one a compute unit holds half as many workgroups of that type and width.  Where it does not, one is right for 32 rows (fp32 heads of 64:
+// 43.9, 60.1 and 98.8), in 8 bits for 64 (32 rows 26.0, 28.4 and 38.0, 64 rows 33.9, 36.0 and 44.1, 128 rows 51.7, 48.3 and 45.1).
 template <typename T, int KC, int VC>
 int launch_rows(const moei_kv& kv, const KvSharedArgs& a, hipStream_t s) {
     const int rows = (a.a.B * a.a.group + a.n_groups - 1) / a.n_groups;  // of a group, if they are alike
+    if constexpr (Group<T, KC, VC, 1>::kLds <= kMostLds && Group<T, KC, VC, 1>::kResident == Group<T, KC, VC, 2>::kResident)
+        if (rows <= (T::kBytes == 1 ? 2 : 1) * kWide) return launch_group<T, KC, VC, 1>(kv, a, s);
     if constexpr (Group<T, KC, VC, 2>::kLds <= kMostLds)
-        if (rows <= 2 * kWide) {
-            if constexpr (Group<T, KC, VC, 1>::kLds <= kMostLds)
-                if (rows <= kWide) return launch_group<T, KC, VC, 1>(kv, a, s);
-            return launch_group<T, KC, VC, 2>(kv, a, s);
-        }
+        if (rows <= 2 * kWide) return launch_group<T, KC, VC, 2>(kv, a, s);
     return launch_group<T, KC, VC, 4>(kv, a, s);
 }
 

@@ -265,7 +265,7 @@ def test_equal_and_special_weights(m, what):  # noqa: F811
         evict(m, c, w, n_keep, first, last)
 
 
-@pytest.mark.parametrize("B,Hkv,top", [(3, 1, 70000), (3, 43, 20000), (130, 1, 16500), (2, 64, 16385)])
+@pytest.mark.parametrize("B,Hkv,top", [(3, 1, 70000), (3, 43, 20000), (2, 16, 30000), (130, 1, 16500), (2, 64, 16385)])
 @pytest.mark.parametrize("what", ["spread", "equal", "few"])
 def test_long_sequences(m, B, Hkv, top, what):  # noqa: F811
     # more tokens than a workgroup holds: chosen from by several workgroups, or where there are many heads by one that reads the weights again and again
