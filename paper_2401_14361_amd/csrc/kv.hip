@@ -616,6 +616,10 @@ extern "C" int kv_evict(moei_kv* kv, const moei_kv_pages* pages, const int32_t* 
     MOEI_REQUIRE(!overlap(d_len, 1, B * 4ll, B * 4ll, d_to_len, B * 4ll), "%s: d_to_len overlaps d_len", who);  // (other workgroups read it still)
     MOEI_REQUIRE(!d_to_weights || !overlap(d_weights, 1, from, from, d_to_weights, to), "%s: d_to_weights overlaps d_weights", who);
     MOEI_REQUIRE(!overlap(d_table, 1, (long long)B * table_width * 4, (long long)B * table_width * 4, d_to_table, (long long)B * to_width * 4), "%s: d_to_table overlaps d_table", who);
+    const long long kept = rows * n_keep * 4, tables = (long long)B * table_width * 4, to_tables = (long long)B * to_width * 4;
+    MOEI_REQUIRE(!overlap(d_weights, 1, from, from, d_kept, kept) && !overlap(d_table, 1, tables, tables, d_kept, kept) && !overlap(d_to_table, 1, to_tables, to_tables, d_kept, kept) &&
+                     !overlap(d_len, 1, B * 4ll, B * 4ll, d_kept, kept) && !(d_to_weights && overlap(d_to_weights, 1, to, to, d_kept, kept)) && !overlap(d_to_len, 1, B * 4ll, B * 4ll, d_kept, kept),
+                 "%s: d_kept overlaps another tensor", who);
     KvEvictArgs a{};
     a.append.k_pages = pages->d_k; a.append.v_pages = pages->d_v;
     strides_of(kv, pages, &a.append.k_stride, &a.append.v_stride);

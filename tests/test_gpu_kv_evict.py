@@ -333,6 +333,14 @@ def test_evict_refusals(m):  # noqa: F811
     refused("d_to_len", to_lens=c.len_t)
     refused("d_to_weights", to_weights=w)
     refused("d_to_table", to=c.table, n_keep=33)
+    for other in (w, c.table, to_table, c.len_t):  # (a buffer that begins with the other's last element)
+        room = torch.zeros(2 ** 16, dtype=torch.int32, device="cuda")
+        moved = room[:other.numel()].view(other.dtype).view(other.shape).copy_(other)
+        kept = room[other.numel() - 1:other.numel() - 1 + 2 * 2 * 33].view(2, 2, 33)
+        refused("d_kept", kept=kept, **{"weights" if other is w else "table" if other is c.table else "to" if other is to_table else "lens": moved})
+    both = torch.zeros(2 * 2 * 33 + 1, dtype=torch.int32, device="cuda")
+    refused("d_kept", kept=both[1:].view(2, 2, 33), to_lens=both[:2])
+    refused("d_kept", kept=both[:-1].view(2, 2, 33), to_weights=both[1:].view(torch.float32).view(2, 2, 33))
     refused("", AssertionError, weights=w[..., :-1].contiguous())
     refused("", AssertionError, to_weights=w[..., :32].contiguous())
     refused("", AssertionError, to=to_table[:1])
