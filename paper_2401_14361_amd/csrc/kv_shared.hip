@@ -55,7 +55,7 @@ struct Group {
 template <typename T>
 __device__ __forceinline__ int wide_v_key(int row, int pieces) {
     if (T::kBytes == 4) return (row & 4) << 1;
-    if (T::kBytes == 2) return (row & 3) << 1;
+    if (T::kBytes == 2) return pieces == 8 ? (row & 2) << 1 : (row & 3) << 2;
     return ((row & 3) | (row >> 3 & 1) << 2) & key_bits(pieces);
 }
 
@@ -281,6 +281,7 @@ __device__ __forceinline__ void attend_prefixes(unsigned char* smem, SharedArgs 
                 g.rows = __builtin_amdgcn_readlane(r.rows, l);
                 g.prefix = __builtin_amdgcn_readlane(r.prefix, l);
                 g.stages = __builtin_amdgcn_readlane((int)r.stages, l);
+                g.blocks = __builtin_amdgcn_readlane((int)r.blocks, l);
                 g_parts = __builtin_amdgcn_readlane((int)parts, l);
                 local = at - (unsigned)__builtin_amdgcn_readlane((int)(upto - mine), l);
                 row_base = (unsigned)__builtin_amdgcn_readlane((int)(rows_upto - rows), l);
@@ -289,8 +290,9 @@ __device__ __forceinline__ void attend_prefixes(unsigned char* smem, SharedArgs 
             before = (unsigned)__builtin_amdgcn_readlane((int)upto, kWave - 1);
             row_base = (unsigned)__builtin_amdgcn_readlane((int)rows_upto, kWave - 1);
         }
-        // blocks of the same keys lie n_kv * parts workgroups apart: with eight heads on the same die
-        const unsigned line = g_parts * a->n_kv, block = local / line, rest = local - block * line;
+        // blocks of the same keys lie side by side, eight workgroups apart: on the same die, whose cache they read the keys through, at the same time
+        const unsigned line = g_parts * a->n_kv, chunk = 8 * g.blocks, from = local / chunk * 8, in = local - from * g.blocks, wide = min(8u, line - from);
+        const unsigned block = in / wide, rest = from + in - block * wide;
         const int part = rest / a->n_kv, hk = rest - part * a->n_kv;
         const unsigned each = (g.stages + g_parts - 1) / g_parts;  // equal parts
         const int c0 = part * each * G::kKeys, c1 = min(g.prefix, c0 + (int)each * G::kKeys);
