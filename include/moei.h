@@ -460,7 +460,7 @@ int kv_attend_shared(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_t
 /* kv_attend that adds up what every token was given: for every sequence b, key/value head hk and token j that it attends to,
  *   d_weights[b][hk][j] += sum over the group's query heads h of exp(scale * q_h.k_j - d_lse[b][h]),
  * in fp32, the heads in their order.  d_weights: [B][n_kv_heads] rows that lie w_stride elements apart (0: table_width * page_size, which none is shorter than); j counts within the
- * sequence, and nothing else of a row is touched.  Out and lse have kv_attend's bits.  A token of a page outside the pool is given nothing.
+ * sequence, and nothing else of a row is touched.  Out and lse are kv_attend's (for a few long sequences by sums in another order).  A token of a page outside the pool is given nothing.
  * Needs moei_kv_set_weights (MOEI_ECAPACITY).  d_weights overlaps neither d_q, d_out nor d_lse. */
 int kv_attend_weights(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, int32_t table_width, const int32_t* d_len, int32_t B,
                       const void* d_q, int64_t q_stride, float scale, int32_t window, float* d_weights, int64_t w_stride,

@@ -20,6 +20,10 @@ __global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kReside
 struct Plain {
     typedef KvAttendArgs Whole;
     static const KvAttendArgs& args(const Whole& w) { return w; }
+    template <typename T>
+    static int grid(const KvAttendArgs&, int all) {
+        return all;
+    }
     template <typename T, int KC, int VC, int NS, int NW>
     static constexpr auto kernel = kv_attend_kernel<T, KC, VC, NS, NW>;
 };

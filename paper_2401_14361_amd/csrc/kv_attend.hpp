@@ -686,7 +686,7 @@ __device__ __forceinline__ void attend(unsigned char* smem, unsigned wg, unsigne
     } while (at_unit < mine_of.end);
 }
 
-// K names the kernel of a shape, and what it is given
+// K names the kernel of a shape, what it is given, and how many workgroups of those that fit the card
 template <typename K, typename T, int KC, int VC, int NW>
 int launch_shape(const moei_kv& kv, const typename K::Whole& all, hipStream_t s) {
     const KvAttendArgs& a = K::args(all);
@@ -698,7 +698,7 @@ int launch_shape(const moei_kv& kv, const typename K::Whole& all, hipStream_t s)
     const int rc = kv_allow_lds(kv, reinterpret_cast<const void*>(kernel), S::kLds);
     if (rc) return rc;
     const long long line = (((long long)a.width << a.page_shift) / S::kUnit + 1) * a.B * a.n_kv * a.blocks_of_heads;  // units, at most
-    const int grid = kv.cus * S::kResident;
+    const int grid = K::template grid<T>(a, kv.cus * S::kResident);
     launch(K_KV_ATTEND, kernel, dim3((unsigned)(line < grid ? line : grid)), dim3(NW * kWave), S::kLds, s, all);
     MOEI_LAUNCH_CHECK();
     return MOEI_OK;

@@ -555,8 +555,8 @@ __device__ __forceinline__ void attend_prefixes(unsigned char* smem, SharedArgs 
     }
 }
 
-// 64 sequences of 1 - 1,024 tokens behind 32,768 shared ones, 32 query and 8 key/value heads of 128 in bf16 (266 MB, 34.9 GFLOP: 38 us of reading or 28 of products): 115 us.
-// The prefix alone takes 81 - 30 % of the matrix cores' time, with the weights in two parts of eight bits half as much again for the values; logits, maxima and weights are
+// 64 sequences of 1 - 1,024 tokens behind 32,768 shared ones, 32 query and 8 key/value heads of 128 in bf16 (266 MB, 34.9 GFLOP: 38 us of reading or 28 of products): 114 us.
+// The prefix alone takes 81 - 31 % of the matrix cores' time, with the weights in two parts of eight bits half as much again for the values; logits, maxima and weights are
 // vector work between the products - and the sequences alone 51, of which 43 are the attention's.  5 us go to the queries and the first stage, 11 to 34 MB of partial sums.  Two
 // launches, one after the other, 142 us; workgroups of eight wavefronts whose halves take turns at products and weights 123; own tokens joined at an item's end 75 us more.
 // 48 sequences behind three prefixes of up to 20,000 tokens, 8 bits, 8 query heads to a key/value head (171 MB): 69 us.

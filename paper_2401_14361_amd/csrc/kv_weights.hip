@@ -6,6 +6,9 @@
 // Bound by memory: 64 sequences of up to 16,384 tokens, 32 / 8 heads of 128 in bf16 (2.42 GB) 455 + 20 us, two of up to 131,072 with 64 / 8 in 8 bits (496 MB) 104 + 14; without
 // weights 367 and 83.  What the attention loses is the writing of logits amid its reads: 75 MB cost 87 us of 455, and nothing if they all go to one small buffer that stays in
 // cache.  Wait counts, the non-temporal hint, the order of rows and of lanes in a store change none of it; an attention that ran again for the weights would read the keys again, 1.2 GB.
+#include <algorithm>
+#include <cmath>
+
 #include "kv_attend.hpp"
 
 namespace moei {
@@ -21,6 +24,15 @@ __global__ void __launch_bounds__(NW * kWave, (Shape<T, KC, VC, NS, NW>::kReside
 struct Weigh {
     typedef KvWeightsArgs Whole;
     static const KvAttendArgs& args(const Whole& w) { return w.a; }
+    // What one workgroup joins of an item takes 0.0095 us a head of 128 values and part, and a workgroup streams 62 KB a microsecond: of few items neither is to outweigh the other.
+    // One sequence of 60,000 tokens, a key/value head of 128, bf16, with 256 / 128 / 64 / 32 parts at most: 16 query heads 55.1 / 36.5 / 31.7 / 34.2 us, 8 34.4 / 25.0 / 24.8 / 30.7, 4 23.9 / 20.4 / 22.0 / 28.6,
+    // one 16.7 / 16.5 / 19.9 / 27.6; 200,000 tokens with 4 heads 32.5 / 32.6 / 43.4 / 71.8.  Not below 32 parts: eight items have a workgroup a compute unit with those.
+    template <typename T>
+    static int grid(const KvAttendArgs& a, int all) {
+        const long long room = (long long)a.width << a.page_shift, tokens = a.window > 0 && a.window < room ? a.window : room;
+        const double streams = (double)tokens * (a.k_dim + a.v_dim) * T::kBytes / 62e3, joins = 0.0095 / 128 * std::min(a.group, kKvHeads) * a.v_dim;
+        return (int)std::min((double)all, std::max(32.0, std::sqrt(streams / joins)) * a.B * a.n_kv * a.blocks_of_heads);
+    }
     template <typename T, int KC, int VC, int NS, int NW>
     static constexpr auto kernel = kv_attend_weigh_kernel<T, KC, VC, NS, NW>;
 };

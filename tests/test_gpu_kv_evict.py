@@ -112,6 +112,28 @@ def test_weights_of_batches_of_any_size(m, B, top):  # noqa: F811
     check_weights(c, weights, before)
 
 
+@pytest.mark.parametrize("dtype,Hq,Hkv,Dk,Dv,page,lens,window", [
+    ("bf16", 16, 1, 128, 128, 32, [40000], 0),
+    ("bf16", 40, 1, 64, 64, 64, [30001, 17], 0),
+    ("fp8", 12, 1, 192, 128, 32, [50000], 0),
+    ("fp8", 16, 2, 128, 128, 16, [40000], 33333),
+    ("fp32", 16, 1, 256, 256, 32, [9000, 8875, 611], 0),
+])
+def test_weights_of_few_long_sequences(m, dtype, Hq, Hkv, Dk, Dv, page, lens, window):  # noqa: F811
+    # fewer workgroups than fit the card, whose parts one of them joins
+    c = Case(m, dtype, Hq, Hkv, Dk, Dv, page, lens, seed=Hq)
+    c.kv.set_weights(len(lens) * c.width * page)
+    weights = rows_of(c)
+    before = weights.clone()
+    out, lse = m.kv_attend_weights(c.kv, c.pages, c.table, c.len_t, c.q, c.scale, weights, window=window, want_lse=True)
+    c.check(out, lse, *c.oracle(window=window))
+    check_weights(c, weights, before, window=window)
+    first = weights.clone()
+    weights.copy_(before)
+    assert torch.equal(m.kv_attend_weights(c.kv, c.pages, c.table, c.len_t, c.q, c.scale, weights, window=window), out)
+    assert torch.equal(weights, first)
+
+
 def test_weights_of_bad_pages_and_lengths(m):  # noqa: F811
     for dtype in ("bf16", "fp8", "fp32"):
         c = Case(m, dtype, 4, 2, 64, 64, 16, [200, 210, 16, 60], seed=2)
