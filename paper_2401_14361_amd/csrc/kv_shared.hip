@@ -38,6 +38,7 @@ struct Group {
     static constexpr int kLoadsK = kBring * kPiecesK / kWave, kLoadsV = kBring * kPiecesV / kWave;
     static constexpr int kFrom = kBring > kRows ? kBring / kRows : 1;               // subtiles of a page that a wavefront brings
     static constexpr int kStageK = kKeys * KC * T::kBytes, kStage = kStageK + kKeys * VC * T::kBytes;
+    static constexpr float kPartByStage = 0.16f / (1024 * 128) / ((T::kBytes == 4 ? 5.f : 1.2f) * (KC + VC) / 256);  // what a sum of a part takes, by what a stage does
     static constexpr int kOutRow = VC + 4;                                          // floats of a row of sums in LDS
     static constexpr int kSums = kWaves * kWide * (kOutRow + 2) * 4;
     static constexpr int kNS = Shape<T, KC, VC, 2, kWaves>::kLds + 2048 <= kMostLds ? 2 : 1;
@@ -115,7 +116,10 @@ struct Groups {
     __device__ __forceinline__ GroupOf at(int g0) const { return g0 == 0 ? held[lane] : group_of<kKeys, kBlock>(z, g0, lane); }
 };
 
-template <typename Gs>
+// A longer part takes 1.2 us a stage with heads of 128 in 16 or 8 bits (fp32 5), one more part of every row 0.16 us for 1,024 rows of 128 sums that are written and joined: no part is
+// shorter than what makes these equal.  Without / so, and by half as much again: 8,192 tokens behind 8 key/value heads in bf16 with 128 rows each 36.9 / 33.1 / 33.2 us, 16,384 tokens 42.8 / 42.8 / 44.5,
+// three prefixes of up to 20,000 tokens in 8 bits 75 / 75 / 79.
+template <typename G, typename Gs>
 __device__ __forceinline__ Plan plan_of(const Gs& groups, SharedArgs z, unsigned grid) {
     unsigned total = 0;
     const unsigned n_kv = z->a.n_kv;
@@ -125,7 +129,8 @@ __device__ __forceinline__ Plan plan_of(const Gs& groups, SharedArgs z, unsigned
     }
     Plan p{(total + grid - 1) / grid, 0};
     if (p.per == 0) return p;
-    const unsigned least = p.per, most = least + max(2u, least / 2);
+    const int rows = min(G::kBlock, z->a.B * z->a.group / z->n_groups + 1);  // of a block, if groups are alike
+    const unsigned least = max(p.per, (unsigned)__builtin_amdgcn_sqrtf((float)total * (float)(rows * z->a.v_dim) * G::kPartByStage)), most = least + max(2u, least / 2);
     for (unsigned per = least; per <= most; per += max(1u, least / 16)) {  // no workgroup has two parts if parts that are a little longer allow it
         unsigned parts = 0;
         for (int g0 = 0; g0 < groups.n; g0 += kWave) {
@@ -574,7 +579,7 @@ __global__ void __launch_bounds__(256, (Group<T, KC, VC, WR>::kResident)) kv_sha
     }
     const Groups<G::kKeys, G::kBlock> groups(z, lane, good, reinterpret_cast<GroupOf*>(smem + G::kHeld));
     const unsigned grid = gridDim.x - 1, wg = blockIdx.x - 1;  // (the first workgroup tells the second launch)
-    const Plan plan = plan_of(groups, z, grid);
+    const Plan plan = plan_of<G>(groups, z, grid);
     if (blockIdx.x == 0) return tell(groups, z, plan, lane);
 #pragma nounroll
     for (int turn = 0; turn < 2; ++turn) {
