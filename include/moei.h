@@ -451,8 +451,8 @@ int kv_attend_blocks(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_t
  * tokens or more, these first tokens are read by way of the table's row of the first such sequence, the others by way of each one's own; the prefix may end inside a page.
  * A shorter sequence shares nothing and is read by its own row, and so is one that lies in no group.
  * Starts that do not ascend within [0, B] count as no groups, a prefix outside [0, table_width * page_size] as the nearest one inside; both raise an error
- * flag.  The rest is as for kv_attend, but for MOEI_ECAPACITY from 2^31 blocks of 16 query heads and 32 tokens on; sums are in another order, and weights of prefixes enter the
- * products of 16- and 8-bit pages with 17 bits.  Needs moei_kv_set_shared (MOEI_ESTATE). */
+ * flag.  The rest is as for kv_attend, but for MOEI_ECAPACITY from 2^31 blocks of 16 query heads and 32 tokens on; sums are in another order.
+ * Needs moei_kv_set_shared (MOEI_ESTATE). */
 int kv_attend_shared(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, int32_t table_width, const int32_t* d_len, int32_t B,
                      const int32_t* d_start, const int32_t* d_prefix, int32_t n_groups,
                      const void* d_q, int64_t q_stride, float scale, void* d_out, float* d_lse, void* stream);

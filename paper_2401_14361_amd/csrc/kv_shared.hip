@@ -480,8 +480,8 @@ __device__ __forceinline__ void attend_prefixes(unsigned char* smem, SharedArgs 
                     x = __builtin_amdgcn_exp2f(__builtin_fmaf(x, scale2, -from));
                     sum += x;
                 }
-            // Weights enter the bf16 products in two parts, 17 bits: what is left out is 2^-17 of a weight.
-            constexpr int kParts = 2;
+            // Weights enter the bf16 products whole, in three parts of eight bits, as those of the sequences' own tokens do.
+            constexpr int kParts = 3;
             [[maybe_unused]] bf16x8 w[kParts];
 #pragma unroll
             for (int i = 0; i < kSteps * kChunks; ++i) {
@@ -560,11 +560,12 @@ __device__ __forceinline__ void attend_prefixes(unsigned char* smem, SharedArgs 
     }
 }
 
-// 64 sequences of 1 - 1,024 tokens behind 32,768 shared ones, 32 query and 8 key/value heads of 128 in bf16 (266 MB, 34.9 GFLOP: 38 us of reading or 28 of products): 114 us.
-// The prefix alone takes 81 - 31 % of the matrix cores' time, with the weights in two parts of eight bits half as much again for the values; logits, maxima and weights are
-// vector work between the products - and the sequences alone 51, of which 43 are the attention's.  5 us go to the queries and the first stage, 11 to 34 MB of partial sums.  Two
-// launches, one after the other, 142 us; workgroups of eight wavefronts whose halves take turns at products and weights 123; own tokens joined at an item's end 75 us more.
-// 48 sequences behind three prefixes of up to 20,000 tokens, 8 bits, 8 query heads to a key/value head (171 MB): 69 us.
+// 64 sequences of 1 - 1,024 tokens behind 32,768 shared ones, 32 query and 8 key/value heads of 128 in bf16 (266 MB, 34.9 GFLOP: 38 us of reading or 28 of products): 125 us.
+// The prefix alone takes 86 - with the weights in three parts of eight bits the values' products are three times those of the keys; logits, maxima and weights are
+// vector work between the products - and the sequences alone 51, of which 43 are the attention's.  Weights in two parts, 17 bits, would take 72 and in all 111.  5 us go to the queries and the
+// first stage, 11 to 38 MB of partial sums.  With two parts: two launches, one after the other, 142 us; workgroups of eight wavefronts whose halves take turns at products and weights 123 (four: 114);
+// own tokens joined at an item's end 75 us more.
+// 48 sequences behind three prefixes of up to 20,000 tokens, 8 bits, 8 query heads to a key/value head (171 MB): 73 us (two parts 69).
 template <typename T, int KC, int VC, int WR>
 __global__ void __launch_bounds__(256, (Group<T, KC, VC, WR>::kResident)) kv_shared_kernel(KvSharedArgs) {
     using G = Group<T, KC, VC, WR>;

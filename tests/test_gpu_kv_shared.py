@@ -10,6 +10,7 @@ import torch
 
 from oracle import kv_oracle as O
 from tests.test_gpu_kv import E, Case, bits, host, m  # noqa: F401 (a fixture)
+from tests.test_gpu_kv_exact import bf16, e4m3, logits_whose_weights_need_24_bits
 
 pytestmark = pytest.mark.gpu
 
@@ -280,3 +281,38 @@ def test_refusals(m):  # noqa: F811
     c.kv.set_shared(False)
     with pytest.raises(m.MoeiError):
         m.kv_attend_shared(*args)
+
+
+@pytest.mark.parametrize("D,Dv", [(64, 64), (128, 128), (192, 128), (256, 256)])
+@pytest.mark.parametrize("B", [1, 40, 70])
+@pytest.mark.parametrize("dtype", ["bf16", "fp8", "fp32"])
+def test_weights_of_prefixes_keep_24_bits(m, dtype, B, D, Dv):  # noqa: F811
+    # The inputs and the bound of tests/test_gpu_kv_exact.py, where two bf16 numbers for a weight would give 0: five tokens, one of weight p = exp(-x) and value 256, four of
+    # weight 1 whose values take away 256 times the nearest two.  All five are a prefix, met by 1, 40 and 70 query heads: one, two and four wavefronts of rows.  What is
+    # joined with it are sums of nothing, times 0, and itself, times 1: no rounding more.  Allowed: the weight is off by 2^-22.5, seven additions of magnitudes up to 512 p by
+    # 2^-23 each, and half a step of the output.
+    Hkv, page = 8, 16
+    x = logits_whose_weights_need_24_bits(Hkv, dtype, np.random.default_rng(D))
+    p = np.exp(-x)
+    hi = bf16(p)
+    lo = bf16(p - hi)
+    take = []
+    for part in (256 * hi, 256 * lo):  # four bits each, so that 8-bit pages hold them
+        a = e4m3(part)
+        take += [a, part - a]
+        assert (e4m3(part - a) == part - a).all()
+    kv = m.Kv(Hkv, Hkv, D, Dv, page, dtype, max_batch=B, max_pages=1, shared=True)
+    k, v = torch.zeros((1, Hkv, page, D), dtype=torch.float64), torch.zeros((1, Hkv, page, Dv), dtype=torch.float64)
+    k[0, :, 4, 0] = torch.from_numpy(-np.ones(Hkv) if dtype == "fp8" else -x)
+    for t, a in enumerate(take):
+        v[0, :, t] = torch.from_numpy(-a)[:, None]
+    v[0, :, 4] = 256
+    k, v = k.to(kv.page_dtype).cuda(), v.to(kv.page_dtype).cuda()
+    scales = dict(k_scale=torch.from_numpy(x).float().cuda(), v_scale=torch.ones(Hkv, device="cuda")) if dtype == "fp8" else {}
+    q = torch.zeros((B, Hkv, D), dtype=kv.dtype, device="cuda")
+    q[:, :, 0] = 1
+    out = m.kv_attend_shared(kv, m.KvPages(kv, k, v, **scales), torch.zeros((B, 1), dtype=torch.int32, device="cuda"), ints([5] * B), ints([0, B]), ints([5]), q, 1.0)
+    ref = 256 * (p - hi - lo) / (4 + p)
+    tol = (256 * 2.0 ** -22.5 + 7 * 2.0 ** -23 * 512 * p) / (4 + p) + 2.0 ** -8 * np.abs(ref)
+    assert (np.abs(ref) > 1.5 * tol).all()
+    assert (np.abs(host(out) - ref[None, :, None]) <= tol[None, :, None]).all()
