@@ -61,7 +61,7 @@ __device__ __forceinline__ Span span_of(A a, int len, int b, int n_groups) {
     Span s{0, len, 0};
     if constexpr (kMode == kOwn) {
         s.begin = prefix_of((SharedArgs)a, n_groups, b, len, (int)room);
-        s.start = s.begin & ~(kRows - 1);
+        s.start = s.begin == len ? len : s.begin & ~(kRows - 1);  // (nothing of its own: not even the page in which the prefix ends)
     } else if (a->list) {
         const int nb = (len + (1 << a->page_shift) - 1) >> a->page_shift;
         if (nb > a->n_sel) s.end = len - ((nb - a->n_sel) << a->page_shift);  // the last page, whole or not, is always listed

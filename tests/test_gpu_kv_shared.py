@@ -316,3 +316,14 @@ def test_weights_of_prefixes_keep_24_bits(m, dtype, B, D, Dv):  # noqa: F811
     tol = (256 * 2.0 ** -22.5 + 7 * 2.0 ** -23 * 512 * p) / (4 + p) + 2.0 ** -8 * np.abs(ref)
     assert (np.abs(ref) > 1.5 * tol).all()
     assert (np.abs(host(out) - ref[None, :, None]) <= tol[None, :, None]).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8", "fp32"])
+@pytest.mark.parametrize("prefix", [135, 128, 3])
+def test_a_sequence_without_tokens_of_its_own_needs_no_pages(m, dtype, prefix):  # noqa: F811
+    # as long as the prefix, which ends inside a page or with one, behind the first sequence that has as many: its own row of the table names nothing
+    c = Case(m, dtype, 8, 2, 128, 128, 32, [prefix, prefix, 170, prefix], seed=4)
+    c.table[1], c.table[3] = -1, c.n_pages
+    out, lse = attend(m, c, [0, 4], [prefix])
+    check(c, out, lse, *oracle(c, [0, 4], [prefix]))
+    assert c.kv.error_flags() == 0
