@@ -226,10 +226,10 @@ __global__ void __launch_bounds__(kMoveThreads) kv_move_kernel(KvEvictArgs) {
     if (tid < rows) {
         const int j = a->kept[row * a->keep + i0 + tid], i = i0 + tid;
         const int from = a->table[(long long)b * a->width + (j >> page_shift)], to = a->to_table[(long long)b * a->to_width + (i >> page_shift)];
-        const bool good = from >= 0 && from < a->n_pages && to >= 0 && to < a->n_pages;
-        if (!good) atomicOr(a->flags, kKvBadPage);
-        s_from[tid] = good ? ((long long)from << page_shift) + (j & (page - 1)) : -1;
-        s_to[tid] = good ? ((long long)to << page_shift) + (i & (page - 1)) : -1;
+        const bool old = from >= 0 && from < a->n_pages, there = to >= 0 && to < a->n_pages;
+        if (!old || !there) atomicOr(a->flags, kKvBadPage);
+        s_from[tid] = old && there ? ((long long)from << page_shift) + (j & (page - 1)) : -1;
+        s_to[tid] = there ? ((long long)to << page_shift) + (i & (page - 1)) : -1;
         if (a->to_weights) a->to_weights[row * a->to_w_row + i] = a->weights[row * a->w_row + j];
     }
     __syncthreads();
@@ -259,7 +259,7 @@ __global__ void __launch_bounds__(kMoveThreads) kv_move_kernel(KvEvictArgs) {
     copy(static_cast<unsigned char*>(a->append.v_pages), a->append.v_stride * sizeof(PG), a->append.v_dim * sizeof(PG));
     if (!a->append.k_min) return;
     __syncthreads();
-    for (int r = page - 1; r < rows; r += page)  // pages that are whole
+    for (int r = page - 1; r < rows; r += page)  // pages that are whole, as they are: also one whose last row had no old page
         if (s_to[r] >= 0) summarise<IO, PG>(&a->append, (int)(s_to[r] >> page_shift), hk, nullptr, -1);
 }
 

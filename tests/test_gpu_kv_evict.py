@@ -411,3 +411,14 @@ def test_captured_replayed_and_on_another_stream(m):  # noqa: F811
     got = m.kv_evict(c.kv, c.pages, c.table, c.len_t, w, 120, to_table, to_w, keep_first=2, keep_last=8, stream=side)
     torch.cuda.synchronize()
     assert torch.equal(got[0], to_lens) and torch.equal(got[1], kept)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8", "fp32"])
+def test_summaries_of_full_pages_whose_last_row_was_not_moved(m, dtype):  # noqa: F811
+    # a full page's summary is that of all it holds, moved or not: the first one's first 16 have no old page, the second one's second 16, of the third one's first page the last
+    c = Case(m, dtype, 2, 2, 64, 64, 16, [100, 100, 100, 40], seed=1, nan_tail=False)
+    c.table[0, 0], c.table[1, 1], c.table[2, 2] = -1, 2 ** 31 - 1, 10 ** 6
+    w = torch.zeros_like(rows_of(c))
+    w[2, :, :15] = w[2, 0, 40] = w[2, 1, 45] = w[2, :, 48:72] = 1.0
+    evict(m, c, w, 40, 0, 0, summaries=True)
+    assert c.kv.error_flags() == 1
