@@ -388,9 +388,11 @@ int moei_kv_create(const moei_kv_desc* desc, moei_kv** out);
 /* The caller has waited for every call that names it. */
 int moei_kv_destroy(moei_kv* kv);
 /* Scratch of kv_attend_weights: calls of up to max_tokens tokens (B * table_width * page_size), 4 * n_q_heads bytes each; 0 gives it back.  Allocates; the
- * caller has waited for every call that names the handle, and captures the call in no graph.  What there was stays if there is no memory. */
+ * caller has waited for every call that names the handle, and captures the call in no graph.  What there was stays if there is no memory, and if it has the
+ * size that is asked for; else it is freed, and a graph that holds a kv_attend_weights of this handle is replayed no more. */
 int moei_kv_set_weights(moei_kv* kv, int64_t max_tokens);
-/* Scratch of kv_attend_shared, (256 rows a compute unit + 2 * max_batch * n_q_heads) * (v_dim + 2) * 4 bytes; on = 0 gives it back.  As moei_kv_set_weights. */
+/* Scratch of kv_attend_shared, (256 rows a compute unit + 2 * max_batch * n_q_heads) * (v_dim + 2) * 4 bytes; on = 0 gives it back, and a
+ * graph that holds a kv_attend_shared of this handle is replayed no more.  Where it is on already, nothing is done.  The rest is as for moei_kv_set_weights. */
 int moei_kv_set_shared(moei_kv* kv, int32_t on);
 /* Error flags raised since the last call (bit 0: a page id outside the pool, bit 1: a length or position outside the page table, a
  * sequence number outside the batch, or groups of sequences outside it).  Synchronises `stream`. */

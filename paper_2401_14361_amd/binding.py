@@ -502,7 +502,7 @@ class Kv:
     max_sel, the largest n_sel of kv_attend_blocks (None: 256 or max_pages), costs scratch: 12 bytes for each of max_pages pages of each
     key/value head of each of max_batch sequences, 25 MB for the defaults and eight heads.  0 where pages are never selected: none.
     shared: there is scratch for kv_attend_shared; max_weight_tokens, tokens (sequences times the table's) of a kv_attend_weights call, costs 4 bytes for each
-    query head of each of them.  set_shared and set_weights change these later."""
+    query head of each of them.  set_shared and set_weights change these later: graphs that hold such calls are replayed no more, unless nothing changes."""
 
     DTYPES = {"fp32": WDTYPE_FP32, "bf16": WDTYPE_BF16, "fp8": KVDTYPE_FP8}
     _PAGE = {"fp32": torch.float32, "bf16": torch.bfloat16, "fp8": torch.float8_e4m3fn}

@@ -398,6 +398,10 @@ extern "C" int moei_kv_set_weights(moei_kv* kv, int64_t max_tokens) {
     MOEI_REQUIRE(kv, "%s: null pointer", who);
     MOEI_REQUIRE(max_tokens >= 0 && max_tokens <= (1ll << 40), "%s: max_tokens = %lld outside [0, 2^40]", who, (long long)max_tokens);
     const size_t heads = kv->d.n_q_heads, tokens = ((size_t)max_tokens + 15) / 16 * 16;
+    if (tokens == ((size_t)kv->weight_tokens + 15) / 16 * 16) {  // (what a captured graph points to stays where it is)
+        kv->weight_tokens = max_tokens;
+        return MOEI_OK;
+    }
     const int rc = exchange(who, kv, {{reinterpret_cast<void**>(&kv->d_logits), tokens * heads * 4}, {reinterpret_cast<void**>(&kv->d_tops), max_tokens ? (size_t)kv->d.max_batch * heads * 8 : 0}});
     if (rc == MOEI_OK) kv->weight_tokens = max_tokens;
     return rc;
@@ -406,6 +410,7 @@ extern "C" int moei_kv_set_weights(moei_kv* kv, int64_t max_tokens) {
 extern "C" int moei_kv_set_shared(moei_kv* kv, int32_t on) {
     const char* who = "moei_kv_set_shared";
     MOEI_REQUIRE(kv, "%s: null pointer", who);
+    if (!on == !kv->d_told) return MOEI_OK;  // (as above)
     // Rows of parts: of every sequence's own tokens, and of prefixes, whose parts are the workgroups' shares, or for each row one that is shorter.
     const size_t rows = on ? (size_t)kKvSharedBlock * kKvSharedResident * kv->cus + 2 * (size_t)kv->d.max_batch * kv->d.n_q_heads : 0;
     return exchange(who, kv, {{reinterpret_cast<void**>(&kv->d_told), on ? kv->d.max_batch * sizeof(KvShared) : 0}, {reinterpret_cast<void**>(&kv->d_pre_part), rows * kv->d.v_dim * 4},

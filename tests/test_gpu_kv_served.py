@@ -207,3 +207,34 @@ def test_pages_beyond_32_bits(m, dtype):  # noqa: F811
     want = O.norm(host(x), np.ones(256), float(np.float32(1e-6)))
     assert (np.abs(host(k[rows[0][7], 0, 15]) - want[0, 0]) <= HALF[dtype] * np.abs(want[0, 0]) + 2.0 ** -19 * np.abs(want).max()).all()
     assert kv.error_flags() == 0
+
+
+def test_scratch_that_is_there_stays_where_a_captured_graph_finds_it(m):  # noqa: F811
+    s = Server(m, "bf16", 3, 20, seed=5)
+    s.k.copy_(torch.randn(s.k.shape, generator=s.g, device="cuda"))
+    s.v.copy_(torch.randn(s.v.shape, generator=s.g, device="cuda"))
+    table, lens = ints(s.take(3 * 20)).view(3, 20), ints([300, 310, 290])
+    q, starts, prefix = torch.randn((3, HQ, D), generator=s.g, device="cuda").bfloat16(), ints([0, 3]), ints([250])
+    w = torch.zeros((3, HKV, 20 * PAGE), device="cuda")
+    outs = [torch.empty_like(q) for _ in range(2)]
+
+    def steps(outs):
+        s.m.kv_attend_shared(s.kv, s.pages, table, lens, starts, prefix, q, s.scale, out=outs[0])
+        s.m.kv_attend_weights(s.kv, s.pages, table, lens, q, s.scale, w, out=outs[1])
+
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        steps(outs)
+    for i in range(4):
+        torch.cuda.synchronize()
+        s.kv.set_shared(True)
+        s.kv.set_weights(3 * 20 * PAGE)
+        other = torch.full((64 << 20,), 7, dtype=torch.uint8, device="cuda")  # what would lie where scratch had been
+        q.copy_(torch.randn(q.shape, generator=s.g, device="cuda"))
+        w.zero_()
+        graph.replay()
+        got, got_w = [x.clone() for x in outs], w.clone()
+        w.zero_()
+        want = [torch.empty_like(q) for _ in range(2)]
+        steps(want)
+        assert all(torch.equal(x, y) for x, y in zip(got, want)) and torch.equal(got_w, w) and (other == 7).all()
