@@ -475,7 +475,7 @@ int kv_attend_weights(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_
  * a place is no position any longer, and windows and positions (kv_append_norm's d_turn) are the caller's to keep.  With summaries: d_k_min and d_k_max of
  * the pages that are full.  Rows behind the last are left as they are, and so are the old pages, which other sequences may share.
  * No page of d_to_table is one of d_table's, or stands in it twice.  A token whose old or new page lies outside the pool is not moved (its weight is), and raises a flag,
- * as a length outside the table does, which counts as the nearest one inside.  d_to_len overlaps not d_len, d_to_table not d_table, d_to_weights not d_weights, d_kept nothing else.  n_keep <= 2^29 (MOEI_ECAPACITY). */
+ * as a length outside the table does, which counts as the nearest one inside.  d_to_len, d_to_weights and d_kept overlap neither each other nor what is read, d_to_table not d_table.  n_keep <= 2^29 (MOEI_ECAPACITY). */
 int kv_evict(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_table, int32_t table_width, const int32_t* d_len, int32_t B,
              const float* d_weights, int64_t w_stride, int32_t n_keep, int32_t keep_first, int32_t keep_last,
              const int32_t* d_to_table, int32_t to_width, int32_t* d_to_len, float* d_to_weights, int64_t to_w_stride, int32_t* d_kept, void* stream);

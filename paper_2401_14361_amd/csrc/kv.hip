@@ -625,6 +625,12 @@ extern "C" int kv_evict(moei_kv* kv, const moei_kv_pages* pages, const int32_t* 
     MOEI_REQUIRE(!overlap(d_weights, 1, from, from, d_kept, kept) && !overlap(d_table, 1, tables, tables, d_kept, kept) && !overlap(d_to_table, 1, to_tables, to_tables, d_kept, kept) &&
                      !overlap(d_len, 1, B * 4ll, B * 4ll, d_kept, kept) && !(d_to_weights && overlap(d_to_weights, 1, to, to, d_kept, kept)) && !overlap(d_to_len, 1, B * 4ll, B * 4ll, d_kept, kept),
                  "%s: d_kept overlaps another tensor", who);
+    // (the move reads lengths, tables and weights while other workgroups of it write: a length that grew meanwhile would name places that d_kept has not)
+    auto apart = [&](const void* p, long long n) {  // from all that is read
+        return !overlap(d_len, 1, B * 4ll, B * 4ll, p, n) && !overlap(d_table, 1, tables, tables, p, n) && !overlap(d_to_table, 1, to_tables, to_tables, p, n) && !overlap(d_weights, 1, from, from, p, n);
+    };
+    MOEI_REQUIRE(apart(d_to_len, B * 4ll) && !(d_to_weights && overlap(d_to_weights, 1, to, to, d_to_len, B * 4ll)), "%s: d_to_len overlaps another tensor", who);
+    MOEI_REQUIRE(!d_to_weights || apart(d_to_weights, to), "%s: d_to_weights overlaps another tensor", who);
     KvEvictArgs a{};
     a.append.k_pages = pages->d_k; a.append.v_pages = pages->d_v;
     strides_of(kv, pages, &a.append.k_stride, &a.append.v_stride);

@@ -422,3 +422,28 @@ def test_summaries_of_full_pages_whose_last_row_was_not_moved(m, dtype):  # noqa
     w[2, :, :15] = w[2, 0, 40] = w[2, 1, 45] = w[2, :, 48:72] = 1.0
     evict(m, c, w, 40, 0, 0, summaries=True)
     assert c.kv.error_flags() == 1
+
+
+def test_evict_refuses_outputs_over_what_it_reads(m):  # noqa: F811
+    c = Case(m, "bf16", 2, 2, 64, 64, 16, [100, 90], seed=1, nan_tail=False, spare=9)
+    given = dict(weights=rows_of(c), table=c.table, to=c.spare[:6].view(2, 3).contiguous(), lens=c.len_t)
+    before = bits(c.k), bits(c.v)
+
+    def refused(text, weights, table, to, lens, **more):
+        with pytest.raises(m.MoeiError) as e:
+            m.kv_evict(c.kv, c.pages, table, lens, weights, 33, to, **more)
+        assert text in str(e.value)
+
+    for name, other in given.items():  # (an output that begins with the other's last element, or ends with its first)
+        for at_end in (True, False):
+            for text, n, dtype, shape in (("d_to_len", 2, torch.int32, (2,)), ("d_to_weights", 2 * 2 * 33, torch.float32, (2, 2, 33))):
+                room = torch.zeros(n + other.numel() - 1, dtype=torch.int32, device="cuda")
+                at, to = (0, other.numel() - 1) if at_end else (n - 1, 0)
+                moved = room[at:at + other.numel()].view(other.dtype).view(other.shape).copy_(other)
+                output = room[to:to + n].view(dtype).view(shape)
+                refused(text, **{**given, name: moved}, **{"to_lens" if text == "d_to_len" else "to_weights": output})
+    room = torch.zeros(2 * 2 * 33 + 1, device="cuda")
+    refused("d_to_len", **given, to_weights=room[:-1].view(2, 2, 33), to_lens=room[-2:].view(torch.int32))
+    refused("d_to_len", **given, to_weights=room[1:].view(2, 2, 33), to_lens=room[:2].view(torch.int32))
+    torch.cuda.synchronize()
+    assert (bits(c.k) == before[0]).all() and (bits(c.v) == before[1]).all()
