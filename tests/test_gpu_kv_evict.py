@@ -447,3 +447,17 @@ def test_evict_refuses_outputs_over_what_it_reads(m):  # noqa: F811
     refused("d_to_len", **given, to_weights=room[1:].view(2, 2, 33), to_lens=room[:2].view(torch.int32))
     torch.cuda.synchronize()
     assert (bits(c.k) == before[0]).all() and (bits(c.v) == before[1]).all()
+
+
+@pytest.mark.parametrize("B,Hkv,width,lens,n_keep", [
+    (1, 1, 5100, [1_305_000], 1999),                                                   # more tokens than so many workgroups take in the smallest stretches
+    (16, 8, 430, [110_080, 3, 0, 2000, 9_999, *range(400, 1500, 100)], 333),     # as many rows as several workgroups choose from, most of them short
+])
+@pytest.mark.parametrize("what", ["spread", "few"])
+def test_the_widest_choices_by_several_workgroups(m, B, Hkv, width, lens, n_keep, what):  # noqa: F811
+    c = Case(m, "fp8", Hkv, Hkv, 16, 16, 256, lens, seed=1, nan_tail=False, width=width, max_sel=0)
+    w = rows_of(c)
+    w = w if what == "spread" else torch.round(w * 3)
+    for _ in range(2):  # what the choice keeps in memory is as it was
+        evict(m, c, w, n_keep, 3, 130)
+    assert c.kv.error_flags() == 0

@@ -74,3 +74,11 @@ def test_kernels_keep_to_their_registers(kernels):  # noqa: F811
         got, = [k for n, k in kernels.items() if n.startswith(start)]
         assert got[".private_segment_fixed_size"] == 0
         assert waves_a_simd * (got[".vgpr_count"] + 7 & ~7) <= 512, (start, got[".vgpr_count"])
+
+
+def test_no_served_kernel_has_private_memory(kernels):  # noqa: F811
+    """Every instance, those at the limit of 512 registers too: vectors never leave registers (scalars may stand in lanes of one)."""
+    found = {n: k for n, k in kernels.items() if n.startswith(("kv_append_norm_kernel<", "kv_shared_kernel<", "kv_join_kernel<", "kv_attend_weigh_kernel<", "kv_weights_kernel", "kv_evict_kernel<", "kv_move_kernel<"))}
+    assert len(found) == 12 + 28 + 2 + 20 + 1 + 2 + 3, sorted(found)
+    for n, k in found.items():
+        assert k[".private_segment_fixed_size"] == 0 and k[".vgpr_spill_count"] == 0 and k[".vgpr_count"] <= 512, n
