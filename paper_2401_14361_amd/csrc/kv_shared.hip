@@ -391,15 +391,22 @@ __device__ __forceinline__ void attend_prefixes(unsigned char* smem, SharedArgs 
 #pragma unroll
             for (int w = 0; w < G::kWaves; ++w) any |= lost[w] = __builtin_amdgcn_readfirstlane(s_gone[stage * G::kWaves + w]);
 
+            int here = lane;  // (places in LDS are formed for each stage where there are no registers for them)
+            if constexpr (kLate) asm volatile("" : "+v"(here));
+
             // logits: lane (col, half) holds those of row col with keys 8 i + 4 half + r of every product
             f32x4 s[kSubs][4];
             constexpr int kAtK = KC > 192 ? (T::kBytes == 4 ? 1 : 2) : kUnits <= 4 ? kUnits : kUnits % 4 ? 3 : 4, kChunksK = kUnits / kAtK;  // units that are read from LDS ahead
-            static_assert(kUnits % kAtK == 0);
+            // fp32: sums of 32 products, which are added up.  One chain over all of a head rounds as often as that has dimensions, at the size of the whole sum: of outputs behind 20,000 tokens
+            // with heads of 256 it leaves an error of 1.8e-6, sums of 32 5.2e-7 (kv_attend, whose four sums are a quarter as long each, 6.2e-7), for 2 % of the time (117.6 -> 121.2 us of 8,192
+            // tokens, 64 rows; heads of 128 45.3 -> 45.8).
+            constexpr int kChain = T::kBytes == 4 ? 4 : kUnits;  // units of a sum
+            static_assert(kUnits % kAtK == 0 && kUnits % kChain == 0 && kChain % kAtK == 0);
             u32x4 kk[2][kAtK];
             auto read_k = [&](int i) __attribute__((always_inline)) {
-                const uint32_t row = at_k + ((wk * kSubs + i / kChunksK) * kWide + col) * (KC * T::kBytes);
+                const uint32_t row = at_k + ((wk * kSubs + i / kChunksK) * kWide + (here & 31)) * (KC * T::kBytes);
 #pragma unroll
-                for (int u = 0; u < kAtK; ++u) kk[i & 1][u] = lds_16(row + (((2 * (i % kChunksK * kAtK + u) + half) ^ k_key(col & 15, G::kPiecesK)) << 4));
+                for (int u = 0; u < kAtK; ++u) kk[i & 1][u] = lds_16(row + (((2 * (i % kChunksK * kAtK + u) + (here >> 5)) ^ k_key(here & 15, G::kPiecesK)) << 4));
             };
             read_k(0);
             in_order_from_here();
@@ -409,7 +416,7 @@ __device__ __forceinline__ void attend_prefixes(unsigned char* smem, SharedArgs 
             for (int i = 0; i < kSubs * kChunksK; ++i) {
                 if (i + 1 < kSubs * kChunksK) read_k(i + 1);
                 in_order_from_here();
-                if (i % kChunksK == 0) z16 = f32x16{};
+                if (i % kChunksK * kAtK % kChain == 0) z16 = f32x16{};
 #pragma unroll
                 for (int v = 0; v < kAtK; ++v) {
                     const u32x4 x = kk[i & 1][v];
@@ -425,9 +432,12 @@ __device__ __forceinline__ void attend_prefixes(unsigned char* smem, SharedArgs 
                         for (int j = 0; j < 4; ++j) z16 = __builtin_amdgcn_mfma_f32_32x32x2f32(x4[j], y4[j], z16, 0, 0, 0);
                     }
                 }
-                if (i % kChunksK == kChunksK - 1)
+                if ((i % kChunksK + 1) * kAtK % kChain == 0)
 #pragma unroll
-                    for (int j = 0; j < 16; ++j) s[i / kChunksK][j / 4][j % 4] = z16[j];
+                    for (int j = 0; j < 16; ++j) {
+                        float& x = reinterpret_cast<float*>(&s[i / kChunksK][j / 4])[j % 4];
+                        x = (i % kChunksK + 1) * kAtK == kChain ? z16[j] : x + z16[j];
+                    }
                 in_order_from_here();
             }
 
@@ -438,7 +448,7 @@ __device__ __forceinline__ void attend_prefixes(unsigned char* smem, SharedArgs 
             auto read_v = [&](int i) __attribute__((always_inline)) {  // chunk i % kChunks of step i / kChunks
                 const uint32_t from = at_v + (wk * kSubs * kWide + i / kChunks * (kWide / V::kSteps)) * (VC * T::kBytes);
 #pragma unroll
-                for (int j = 0; j < kAtOnce; ++j) vt[i & 1][j] = V::template read<VC>(from, i % kChunks * kAtOnce + j, lane);
+                for (int j = 0; j < kAtOnce; ++j) vt[i & 1][j] = V::template read<VC>(from, i % kChunks * kAtOnce + j, here);
             };
             read_v(0);
             in_order_from_here();

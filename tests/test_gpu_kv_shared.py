@@ -327,3 +327,19 @@ def test_a_sequence_without_tokens_of_its_own_needs_no_pages(m, dtype, prefix): 
     out, lse = attend(m, c, [0, 4], [prefix])
     check(c, out, lse, *oracle(c, [0, 4], [prefix]))
     assert c.kv.error_flags() == 0
+
+
+@pytest.mark.parametrize("D,Dv", [(128, 128), (192, 128), (256, 256)])
+@pytest.mark.parametrize("B", [1, 40, 70])
+def test_logits_of_prefixes_in_fp32_are_sums_of_short_sums(m, B, D, Dv):  # noqa: F811
+    # Two tokens of equal logits, D (1 + 2^-19): one in a single dimension, one in all of them.  Up to 32 of the latter add up exactly (32 + 2^-14: 20 bits), and so do such
+    # sums up to 256 (multiples of 2^-14); one chain loses 2^-18 with every two from 64 on, and would be off by (D - 64) / 2 times that, 2^-13 at least.  Values of 1 and -1 show half
+    # of that.  Weights that are equal but for exp2 and its argument, 2^-21, cancel but for that.
+    kv = m.Kv(8, 8, D, Dv, 16, "fp32", max_batch=B, max_pages=1, shared=True)
+    k, v = torch.zeros((1, 8, 16, D), device="cuda"), torch.zeros((1, 8, 16, Dv), device="cuda")
+    k[0, :, 0, 0] = D * (1 + 2.0 ** -19)
+    k[0, :, 1] = 1 + 2.0 ** -19
+    v[0, :, 0], v[0, :, 1] = 1, -1
+    q, table, lens = torch.ones((B, 8, D), device="cuda"), torch.zeros((B, 1), dtype=torch.int32, device="cuda"), ints([2] * B)
+    pages = m.KvPages(kv, k, v)
+    assert (m.kv_attend_shared(kv, pages, table, lens, ints([0, B]), ints([2]), q, 1.0).abs() <= 2.0 ** -20).all()
