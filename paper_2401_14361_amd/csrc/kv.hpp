@@ -113,7 +113,7 @@ struct moei_kv {
     float* d_logits = nullptr;       // [weight_tokens][n_q_heads]
     float2* d_tops = nullptr;        // [max_batch][n_q_heads]
     moei::KvShared* d_told = nullptr;  // [max_batch], moei_kv_set_shared
-    float* d_pre_part = nullptr;     // [max_batch * n_q_heads + rows][v_dim]
+    float* d_pre_part = nullptr;     // [2 * max_batch * n_q_heads + 256 a compute unit][v_dim]: sums of own tokens, and of the prefixes' parts
     float* d_pre_stat = nullptr;     // [..][2]
 };
 

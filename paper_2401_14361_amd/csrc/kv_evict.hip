@@ -269,7 +269,8 @@ int launch_kv_evict(const moei_kv& kv, KvEvictArgs a, hipStream_t s) {
     const long long room = (long long)a.width << a.page_shift;
     // Times of the choice, in us: by a workgroup a row 6.5 and 0.77 for every 1,024 tokens of one (a sixth less where their ranks fit), in five launches 24 and 5 for a million tokens of all rows.
     // 8 rows of 16,384 / 16,448 / 32,768 / 131,072 tokens 16.0 / 21.2 / 31.6 / 106.7 and 24.7 / 25.6 / 24.4 / 27.5; 32 rows of 32,768 tokens 32.0 and 25.7; 128 rows of 65,536 / 131,072 tokens
-    // 62.2 / 131.9 and 67.0 / 111.4.  The lengths lie on the device: what decides is the room that the table's width gives them.
+    // 62.2 / 131.9 and 67.0 / 111.4.  The lengths lie on the device: what decides is the room that the table's width gives them: 8 rows of 1,000 tokens take
+    // 13 us with their move in tables of up to 16,384 tokens and 32 in one of 131,072; 512 rows of 700 - 2,000 tokens 61, with one of 16,000 among them 68, of 16,400 or 20,000 74, when no row's ranks are held.
     const long long items = (long long)a.B * a.n_kv;
     if (items <= kKvSplitItems && room * (160 - items) > 3500000) {
         constexpr int kSplitThreads = 512, kAtOnce = 4096;  // (256 threads, or 8,192 tokens: 50 and 62 us for the 131,072 tokens below, 2,048: 45 as here)

@@ -103,7 +103,9 @@ __device__ __forceinline__ bool in_order(SharedArgs z, int lane) {
     return __ballot(bad) == 0;
 }
 
-// The groups, 64 at a time: the first ones, mostly all, are looked up once (three trips to memory one after the other) and kept in LDS.
+// The groups, 64 at a time: the first ones, mostly all, are looked up once (three trips to memory one after the other) and kept in LDS.  Those behind are looked up again by every
+// wavefront for every plan and part: with two sequences to a group and prefixes of 512 tokens (8 / 2 heads of 128 in bf16) 16 groups take 18 us, 64 38, 65 37, 128 68, 256 107, 512 259 and 1,024 549, where
+// kv_attend takes 11, 18, 25, 28, 53, 102 and 201: small groups in such numbers are better left out.
 template <int kKeys, int kBlock>
 struct Groups {
     SharedArgs z;
@@ -116,9 +118,9 @@ struct Groups {
     __device__ __forceinline__ GroupOf at(int g0) const { return g0 == 0 ? held[lane] : group_of<kKeys, kBlock>(z, g0, lane); }
 };
 
-// A longer part takes 1.2 us a stage with heads of 128 in 16 or 8 bits (fp32 5), one more part of every row 0.16 us for 1,024 rows of 128 sums that are written and joined: no part is
-// shorter than what makes these equal.  Without / so, and by half as much again: 8,192 tokens behind 8 key/value heads in bf16 with 128 rows each 36.9 / 33.1 / 33.2 us, 16,384 tokens 42.8 / 42.8 / 44.5,
-// three prefixes of up to 20,000 tokens in 8 bits 75 / 75 / 79.
+// A longer part takes 1.2 us a stage with heads of 128 in 16 or 8 bits (fp32 5; a sixth more since weights have three parts), one more part of every row 0.16 us for 1,024 rows of 128 sums that are
+// written and joined: no part is shorter than what makes these equal.  Without / so, and by half as much again: 8,192 tokens behind 8 key/value heads in bf16 with 128 rows each 39.1 / 35.3 / 37.2 us,
+// 16,384 tokens 45.6 / 45.1 / 45.0, three prefixes of up to 20,000 tokens in 8 bits 79 / 79 / 88.
 template <typename G, typename Gs>
 __device__ __forceinline__ Plan plan_of(const Gs& groups, SharedArgs z, unsigned grid) {
     unsigned total = 0;
@@ -571,11 +573,15 @@ __device__ __forceinline__ void attend_prefixes(unsigned char* smem, SharedArgs 
 }
 
 // 64 sequences of 1 - 1,024 tokens behind 32,768 shared ones, 32 query and 8 key/value heads of 128 in bf16 (266 MB, 34.9 GFLOP: 38 us of reading or 28 of products): 125 us.
-// The prefix alone takes 86 - with the weights in three parts of eight bits the values' products are three times those of the keys; logits, maxima and weights are
-// vector work between the products - and the sequences alone 51, of which 43 are the attention's.  Weights in two parts, 17 bits, would take 72 and in all 111.  5 us go to the queries and the
-// first stage, 11 to 38 MB of partial sums.  With two parts: two launches, one after the other, 142 us; workgroups of eight wavefronts whose halves take turns at products and weights 123 (four: 114);
-// own tokens joined at an item's end 75 us more.
-// 48 sequences behind three prefixes of up to 20,000 tokens, 8 bits, 8 query heads to a key/value head (171 MB): 73 us (two parts 69).
+// The prefix alone takes 86: with the weights in three parts of eight bits the values' products are three times those of the keys, and logits, maxima and weights are
+// vector work between the products, which keep the matrix cores busy for 37 % of the whole; the sequences alone take 50 (kv_attend 36).  Weights in two parts, 17 bits, would take 72 and in all 111.  5 us go
+// to the queries and the first stage, 11 to 35 MB of partial sums.  With two parts: two launches, one after the other, 142 us; workgroups of eight wavefronts whose halves take turns at products and weights
+// 123 (four: 114); own tokens joined at an item's end 75 us more.
+// 48 sequences behind three prefixes of up to 20,000 tokens, 8 bits, 8 query heads to a key/value head (171 MB): 72 us (two parts 69).
+// Where there is little to share the second launch and the larger kernel cost more than they save.  32 / 8 heads of 128, one group, kv_attend / this, us a call: in bf16 4 sequences behind 1,024 tokens
+// 10.8 / 18.1, behind 16,384 28.9 / 26.9, 16 behind 4,096 29.3 / 25.6, 64 behind 1,024 24.8 / 28.6 and behind 32,768 581 / 93; in 8 bits 16 behind 4,096 23.4 / 24.1, 8 behind 16,384 35.7 / 27.5; in fp32
+// 16 behind 1,024 29.4 / 28.8, 8 behind 4,096 47 / 33, two behind 32,768 84 / 110: it pays from about 65,000 tokens on that the sequences would read of the prefix in all (8 bits 100,000; fp32 30,000).
+// Both halves and the plan are one kernel: 33 - 65 scalar registers stand in lanes of vector ones, in every instance.
 template <typename T, int KC, int VC, int WR>
 __global__ void __launch_bounds__(256, (Group<T, KC, VC, WR>::kResident)) kv_shared_kernel(KvSharedArgs) {
     using G = Group<T, KC, VC, WR>;
@@ -664,9 +670,11 @@ int launch_group(const moei_kv& kv, const KvSharedArgs& a, hipStream_t s) {
 }
 
 // The wavefronts of a workgroup have different rows where there are many, else different keys, whose stages are larger and whose sums are joined in LDS at the end.  With 1, 2 and 4
-// wavefronts of rows (32,768 tokens behind 8 key/value heads of 128 in bf16) 32 rows take 34.5, 33.0 and 37.9 us, 64 rows 51.4, 39.3 and 43.6, 128 rows 85.2, 52.6 and 45.5; eight prefixes of
-// 4,000 - 8,192 tokens and 32 rows each 87.3, 53.3 and 62.5: with one a compute unit holds half as many workgroups of that type and width.  Where it does not, one is right for 32 rows (fp32 heads of 64:
-// 43.9, 60.1 and 98.8), in 8 bits for 64 (32 rows 26.0, 28.4 and 38.0, 64 rows 33.9, 36.0 and 44.1, 128 rows 51.7, 48.3 and 45.1).
+// wavefronts of rows (32,768 tokens behind 8 key/value heads of 128 in bf16) 32 rows take 39.8, 38.5 and 47.2 us, 64 rows 57.8, 44.8 and 54.9, 128 rows 96.4, 59.7 and 59.8; eight prefixes of
+// 4,000 - 8,192 tokens and 32 rows each 98.6, 63.5 and 78.0: with one a compute unit holds half as many workgroups of that type and width.  Where it does not, one is right for 32 rows (fp32 heads of 64:
+// 47.2, 65.0 and 105.2), in 8 bits for 64 (32 rows 31.1, 35.1 and 47.3, 64 rows 40.3, 42.6 and 53.2, 128 rows 60.8, 57.6 and 58.7).
+// Groups that are not alike go by their mean, and one of a single sequence costs what its prefix takes by this kernel, with nothing to share: 128 sequences behind 4,096 tokens beside 200 of 600 tokens each
+// (32 / 8 heads of 128), with a group of 512 for every one of these / in no group: bf16 194 / 194 us, 8 bits 171 / 132, fp32 792 / 519.
 template <typename T, int KC, int VC>
 int launch_rows(const moei_kv& kv, const KvSharedArgs& a, hipStream_t s) {
     const int rows = (a.a.B * a.a.group + a.n_groups - 1) / a.n_groups;  // of a group, if they are alike

@@ -1,8 +1,8 @@
 """Attention of a batch whose sequences share prefixes, against the definition in 64 bits (oracle/kv_oracle.py).
 
 Tolerances are those of tests/test_gpu_kv.py, with twice the roundings of sums: a part of a prefix is a sum of its tokens, and joining it costs three
-roundings more, for 32 tokens at least, or for the whole prefix: (2 n + 64) e of the largest value.  Weights of prefixes enter the products of bf16 values in two
-parts of eight bits each: what is left out is below 2^-17 of a weight, and 2^-16 is allowed for as there.
+roundings more, for 32 tokens at least, or for the whole prefix: (2 n + 64) e of the largest value.  2^-16 of a weight is allowed for products of bf16 values as there,
+though weights of prefixes enter them whole: test_weights_of_prefixes_keep_24_bits does without.
 """
 import numpy as np
 import pytest
