@@ -461,3 +461,39 @@ def test_the_widest_choices_by_several_workgroups(m, B, Hkv, width, lens, n_keep
     for _ in range(2):  # what the choice keeps in memory is as it was
         evict(m, c, w, n_keep, 3, 130)
     assert c.kv.error_flags() == 0
+
+
+def test_weights_that_are_no_numbers_of_either_kind_and_sign(m):  # noqa: F811
+    # quiet and signalling ones with every sign, and the numbers beside them
+    c = Case(m, "bf16", 2, 2, 16, 16, 16, [3000, 20_000], seed=1, nan_tail=False)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(3)
+    odd = torch.tensor([0x7f800001, 0x7fbfffff, 0x7fc00000, 0x7fffffff, 0x7f800000, 0x7f7fffff, 1, 0, 0x007fffff, 0x00800000], dtype=torch.int64, device="cuda")
+    odd = torch.cat([odd, odd - 2 ** 31]).to(torch.int32)
+    w = rows_of(c)
+    w = torch.where(torch.rand(w.shape, generator=g, device="cuda") < 0.7, odd[torch.randint(0, 20, w.shape, generator=g, device="cuda")], w.view(torch.int32)).view(torch.float32)
+    for n_keep in (1, 500, 1700, 2900):
+        evict(m, c, w.contiguous(), n_keep, 0, 0)
+
+
+def test_weights_and_eviction_of_the_largest_batch(m):  # noqa: F811
+    rng = np.random.default_rng(6)
+    c = Case(m, "bf16", 2, 1, 16, 16, 16, [int(x) for x in rng.integers(0, 60, 4096)], seed=6, nan_tail=False, max_sel=0)
+    c.kv.set_weights(4096 * c.width * 16)
+    w = rows_of(c)
+    before = w.clone()
+    m.kv_attend_weights(c.kv, c.pages, c.table, c.len_t, c.q, c.scale, w)
+    check_weights(c, w, before)
+    evict(m, c, w, 20, 2, 3)
+    assert c.kv.error_flags() == 0
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv", [("bf16", 1024, 1), ("fp32", 1024, 2), ("fp8", 1024, 1024)])
+def test_weights_and_eviction_of_1024_heads(m, dtype, Hq, Hkv):  # noqa: F811
+    c = Case(m, dtype, Hq, Hkv, 16, 16, 16, [100, 33], seed=6, nan_tail=False, max_sel=0)
+    c.kv.set_weights(2 * c.width * 16)
+    w = rows_of(c)
+    before = w.clone()
+    m.kv_attend_weights(c.kv, c.pages, c.table, c.len_t, c.q, c.scale, w)
+    check_weights(c, w, before)
+    evict(m, c, w, 35, 2, 3)

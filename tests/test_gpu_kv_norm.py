@@ -213,3 +213,22 @@ def test_captured_and_replayed(m):  # noqa: F811
         q_out.zero_()
         want = m.kv_append_norm(c.kv, c.pages, c.table, pos, q, k, v, qw, kw, freq, turn=turn)
         assert (bits(want) == got).all() and (bits(c.k) == pages).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp8", "fp32"])
+def test_a_token_to_each_of_many_sequences_with_summaries(m, dtype):  # noqa: F811
+    # so many that a workgroup takes all heads of a token, beside those that form the summaries
+    rng = np.random.default_rng(7)
+    pos = [int(x) for x in rng.choice([0, 14, 15, 31, 30, -1], 2100)]
+    c = Case(m, dtype, 4, 2, 32, 48, 16, [max(p, 0) + 1 for p in pos], seed=7, summaries=True, nan_tail=False)
+    q, k, v = _append_inputs(c, len(pos), seed=7)
+    qw, kw = weights(c, True)
+    before = [t.clone() for t in (c.k, c.v, c.lo, c.hi)]
+    q_out = torch.zeros_like(q)
+    q_before = q_out.clone()
+    m.kv_append_norm(c.kv, c.pages, c.table, ints(pos), q, k, v, qw, kw, _freq(32), q_out=q_out)
+    place = check(c, q, k, v, qw, kw, float(np.float32(1e-6)), q_out, q_before, before[0], before[1], range(len(pos)), pos, _freq(32), False)
+    lo, hi = before[2], before[3]
+    for i in {at[0] for at in place if at is not None and at[1] == 15}:
+        lo[i], hi[i] = c.k[i].to(c.kv.dtype).amin(1), c.k[i].to(c.kv.dtype).amax(1)
+    assert (bits(c.lo) == bits(lo)).all() and (bits(c.hi) == bits(hi)).all()

@@ -343,3 +343,10 @@ def test_logits_of_prefixes_in_fp32_are_sums_of_short_sums(m, B, D, Dv):  # noqa
     q, table, lens = torch.ones((B, 8, D), device="cuda"), torch.zeros((B, 1), dtype=torch.int32, device="cuda"), ints([2] * B)
     pages = m.KvPages(kv, k, v)
     assert (m.kv_attend_shared(kv, pages, table, lens, ints([0, B]), ints([2]), q, 1.0).abs() <= 2.0 ** -20).all()
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv", [("bf16", 1024, 1), ("fp32", 1024, 2), ("fp8", 1024, 1024)])
+def test_1024_heads_behind_a_prefix(m, dtype, Hq, Hkv):  # noqa: F811
+    c = Case(m, dtype, Hq, Hkv, 16, 32, 16, [100, 90, 133, 45], seed=6, max_sel=0)
+    check(c, *attend(m, c, [0, 3, 4], [90, 45]), *oracle(c, [0, 3, 4], [90, 45]))
+    assert c.kv.error_flags() == 0
