@@ -452,8 +452,8 @@ int kv_attend_blocks(moei_kv* kv, const moei_kv_pages* pages, const int32_t* d_t
  * sequences d_start[g] <= b < d_start[g + 1] (d_start[n_groups + 1], d_prefix[n_groups] int32, device).  Of those that have d_prefix[g]
  * tokens or more, these first tokens are read by way of the table's row of the first such sequence, the others by way of each one's own; the prefix may end inside a page.
  * A shorter sequence shares nothing and is read by its own row, and so is one that lies in no group.
- * It pays from about 65,000 tokens on that a group's sequences would read of the prefix in all (sequences times its length; 8-bit pages 100,000, fp32 30,000); below that kv_attend takes
- * as little as half the time, also for part of a batch: groups of one sequence are better left out, and so are small ones by the hundred.
+ * It pays for four sequences and more that would read about 65,000 tokens of the prefix in all (sequences times its length; 8-bit pages 100,000, fp32 30,000); below that kv_attend takes
+ * as little as half the time.  In a larger batch too groups of one sequence are better left out, and so are small ones by the hundred.
  * Starts that do not ascend within [0, B] count as no groups, a prefix outside [0, table_width * page_size] as the nearest one inside; both raise an error
  * flag.  The rest is as for kv_attend, but for MOEI_ECAPACITY from 2^31 blocks of 16 query heads and 32 tokens on; sums are in another order.
  * Needs moei_kv_set_shared (MOEI_ESTATE). */

@@ -580,7 +580,8 @@ __device__ __forceinline__ void attend_prefixes(unsigned char* smem, SharedArgs 
 // 48 sequences behind three prefixes of up to 20,000 tokens, 8 bits, 8 query heads to a key/value head (171 MB): 72 us (two parts 69).
 // Where there is little to share the second launch and the larger kernel cost more than they save.  32 / 8 heads of 128, one group, kv_attend / this, us a call: in bf16 4 sequences behind 1,024 tokens
 // 10.8 / 18.1, behind 16,384 28.9 / 26.9, 16 behind 4,096 29.3 / 25.6, 64 behind 1,024 24.8 / 28.6 and behind 32,768 581 / 93; in 8 bits 16 behind 4,096 23.4 / 24.1, 8 behind 16,384 35.7 / 27.5; in fp32
-// 16 behind 1,024 29.4 / 28.8, 8 behind 4,096 47 / 33, two behind 32,768 84 / 110: it pays from about 65,000 tokens on that the sequences would read of the prefix in all (8 bits 100,000; fp32 30,000).
+// 16 behind 1,024 29.4 / 28.8, 8 behind 4,096 47 / 33, two behind 32,768 84 / 110: it pays for four sequences and more that would read about 65,000 tokens of
+// the prefix in all (8 bits 100,000; fp32 30,000).
 // Both halves and the plan are one kernel: 33 - 65 scalar registers stand in lanes of vector ones, in every instance.
 template <typename T, int KC, int VC, int WR>
 __global__ void __launch_bounds__(256, (Group<T, KC, VC, WR>::kResident)) kv_shared_kernel(KvSharedArgs) {
